@@ -140,11 +140,12 @@ def _page_bytes(dim, page):
 
 def _encode(x, dtype):
     """x (float32 values of `dtype`, last axis the channels) -> codes uint8, scale bytes uint8 [..., dim / 32]: the least
-    power of two with |x| <= 7 of it, and to it the nearest 4-bit float, ties to the even code."""
+    power of two with |x| <= 7 of it (of those whose values `dtype` holds), and to it the nearest 4-bit float, ties to
+    the even code."""
     g = x.view(*x.shape[:-1], -1, GROUP)
     m, ex = torch.frexp(g.abs().amax(-1))
-    low = 104 if dtype == torch.float16 else 2
-    byte = (ex - 3 + (m > 0.875).int() + 127).clamp(min=low)
+    low, high = (104, 140) if dtype == torch.float16 else (2, 252)
+    byte = (ex - 3 + (m > 0.875).int() + 127).clamp(low, high)
     byte = torch.where(m == 0, low, byte)
     a = (g * ((254 - byte) << 23).view(torch.float32)[..., None])
     t = a.abs()
