@@ -526,6 +526,174 @@ spl_status spl_sparse_linear_int8_group_scratch(const spl_int8_task* tasks, int3
 spl_status spl_dense_linear_int8_group(const spl_dense_int8_task* tasks, int32_t count, int64_t M,
                                        hipStream_t stream);
 
+/* The attention half of a decoder layer, between the q, k, v projections and o
+ * (the Llama layer whose linears the paper sparsifies; not a method of the
+ * paper).  One step of a serving loop on a batch of requests is
+ *   spl_block_tables          pages and slots for the new tokens,
+ *   (q, k, v projections)
+ *   spl_qk_norm_rope_append   norms, rotation, keys and values into the cache,
+ *   spl_attention_fp4         attention over the cache,
+ *   (o projection)
+ * and spl_qk_norm_rope with spl_qk_norm_rope_grad are the norms and the rotation
+ * of a training step.
+ *
+ * Heads: a view of [tokens][heads][dim] payloads of 16 bits, the dim channels
+ * of a head contiguous, with strides in elements.  data is 16-byte aligned, the
+ * strides are multiples of 8 (a slice of a fused q|k|v product is such a view).
+ * Outputs are contiguous [tokens][heads][dim], 16-byte aligned. */
+typedef struct {
+  const void* data;
+  int64_t token_stride;
+  int64_t head_stride;
+  int32_t heads;
+} spl_heads;
+
+/* A cache of keys and values in 4 bits, in pages of `page` tokens.  A slot is a
+ * token's place in the cache: page number * page + place in the page.
+ *
+ * Format: per token and head, groups of 32 channels share a scale 2^e and hold
+ * 4-bit floats (1 sign, 2 exponent, 1 fraction bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6
+ * times the scale).  e is the least with |x| <= 7 * 2^e over the group (7 rounds
+ * to 6; on Gaussian groups the error is 0.112 of the standard deviation, with
+ * a limit of 6 0.116, of 8 0.115), within [-23, 13] for fp16 and [-125, 125] for
+ * bf16, so that every value is one of the type's (larger ones are held as the
+ * largest).  Codes round to nearest, ties to the even code.  The scale byte is
+ * e + 127; 255 stands for a group that held an infinity or a NaN, and all of it
+ * reads back as NaN.
+ *
+ * Layout: data is [pages][heads] regions of spl_kv_page_bytes(head_dim, page)
+ * bytes.  With D = head_dim, G = D / 32, S = G rounded up to a power of two (at
+ * least 2), U = 4 (D 64), 8 (D 96 and 128) or 16 (D 256), code e of a run at
+ * nibble e (low nibble first), a region holds
+ *   key codes     token b, channel 32g + 8j + e: byte b D/2 + 4 (j G + g), nibble e
+ *   value codes   at page D/2: token b, channel U u + e: byte
+ *                 U/2 (8 (b/8 (D/U) + u) + b%8), nibble e
+ *   key scales    at page D: token b, group g: byte b S + g
+ *   value scales  at page (D + S): token b, group g: byte 8 (b/8 S + g) + b%8
+ * so that a lane of a matrix instruction loads its operands in one piece: of a
+ * key 8 channels of every group, of the values 8 tokens of a run of channels.
+ *   head_dim 64, 96, 128 or 256; page a power of two from 16 to 256; data
+ *   16-byte aligned; pages * page < 2^31. */
+typedef struct {
+  void* data;
+  int64_t pages;
+  int64_t data_bytes;            /* bytes allocated at `data` */
+  int32_t page;                  /* tokens of a page */
+  int32_t heads;                 /* key / value heads */
+  int32_t head_dim;
+  int32_t dtype;                 /* SPL_F16 or SPL_BF16: the type of what is stored and read back */
+} spl_kv_cache;
+
+/* Bytes of one head's region of one page; 0 for sizes the cache does not have. */
+int64_t spl_kv_page_bytes(int32_t head_dim, int32_t page);
+
+/* Pages and slots of a batch's new tokens, from the lengths alone (all arrays
+ * on the device, int32).  Request r holds cached[r] tokens and gets fresh[r]
+ * (negative: taken as 0); its pages are table[r][0 .. width).
+ *   table       [requests][width] in / out.  With have = ceil(cached / page) and
+ *               want = ceil((cached + fresh) / page), entries [have, want) are
+ *               written with the next pages of the free list, request by
+ *               request; other entries stay (ones past the width are not
+ *               asked for).  -1 where the list has run out.
+ *   free_pages  [free_count] page numbers; free_head [1]: how many are taken.
+ *   row_start   out [requests + 1]: a request's first row among the new tokens.
+ *   lens        out [requests]: cached + fresh.
+ *   positions   out [tokens]: the row's position in its request.
+ *   slots       out [tokens]: its slot, or -1 where it has no page.
+ *   state       out [2]: the free list's new head; 0 if every new token has a
+ *               row and a slot, else how many lack one.
+ * tokens is the rows of the step's tensors: rows past the requests' get
+ * position 0 and slot -1 (a batch padded for a captured graph), tokens past the
+ * rows are counted in state[1].  The same arguments give the same results, so a
+ * call can be repeated.  requests >= 1, 0 <= tokens < 2^31, page a power of two
+ * from 16 to 256, 1 <= width, requests * width < 2^40; free_head may not be state. */
+spl_status spl_block_tables(const int32_t* cached, const int32_t* fresh, int64_t requests, int64_t tokens,
+                            int32_t page, int32_t* table, int64_t width, const int32_t* free_pages,
+                            int64_t free_count, const int32_t* free_head, int32_t* row_start, int32_t* lens,
+                            int32_t* positions, int32_t* slots, int32_t* state, hipStream_t stream);
+
+/* Norm of each query and key head, then the rotation by position, in one pass:
+ *   n = x / sqrt(mean(x^2) + eps) * weight          (weight NULL: n = x)
+ *   (n[i], n[j]) -> (n[i] c - n[j] s, n[j] c + n[i] s),  (c, s) = rope[position][p]
+ * for the rot / 2 pairs p of the first rot channels: (p, p + rot / 2), or with
+ * interleaved (2p, 2p + 1).  fp32, every product and sum rounded on its own, the
+ * mean's squares added in pairs of neighbours, one rounding to dtype: the result
+ * for a head does not depend on what else is in the call.
+ *   q, k        views of `tokens` rows of dtype (fp16 / bf16).
+ *   q_weight, k_weight   [dim] of dtype, 16-byte aligned, or NULL.
+ *   positions   [tokens] int32; a position outside [0, rope_rows) gives NaN in
+ *               the rotated channels.  rope: [rope_rows][rot / 2][2] float32
+ *               (cosine, sine).  rot == 0: no rotation (both may be NULL).
+ *   q_out, k_out  contiguous; each may be its input itself where that is contiguous.
+ * dim % 8 == 0, 8 <= dim <= 256; rot % 16 == 0, 0 <= rot <= dim
+ * (SPL_ERR_UNSUPPORTED otherwise).  tokens == 0 is a no-op. */
+spl_status spl_qk_norm_rope(const spl_heads* q, const spl_heads* k, int64_t tokens, int32_t dim, int32_t dtype,
+                            const void* q_weight, const void* k_weight, float eps, const int32_t* positions,
+                            const float* rope, int64_t rope_rows, int32_t rot, int32_t interleaved, void* q_out,
+                            void* k_out, hipStream_t stream);
+
+/* Its gradients: from dq, dk (of q_out, k_out) those of q, k and of the weights.
+ *   dq_out, dk_out  contiguous, of dtype.  dq_weight, dk_weight  [dim] float32, or
+ *   NULL (they must be NULL without the weight).
+ *   workspace   spl_qk_norm_rope_grad_workspace_bytes(...) bytes (-1 for sizes
+ *               that the call rejects), 16-byte aligned, caller-owned.
+ * Sums in fp32 in a fixed order: the same call gives the same bits.  q and k are
+ * not read without weights.  tokens == 0: the weights' gradients are 0. */
+int64_t spl_qk_norm_rope_grad_workspace_bytes(int64_t tokens, int32_t q_heads, int32_t k_heads, int32_t dim);
+spl_status spl_qk_norm_rope_grad(const spl_heads* dq, const spl_heads* dk, const spl_heads* q, const spl_heads* k,
+                                 int64_t tokens, int32_t dim, int32_t dtype, const void* q_weight,
+                                 const void* k_weight, float eps, const int32_t* positions, const float* rope,
+                                 int64_t rope_rows, int32_t rot, int32_t interleaved, void* dq_out, void* dk_out,
+                                 float* dq_weight, float* dk_weight, void* workspace, hipStream_t stream);
+
+/* spl_qk_norm_rope with the keys, rounded to dtype, and the values v (as they
+ * are) stored at slots[token] of the cache in the same launch.  k_out may be
+ * NULL; q_out and k_out are those of spl_qk_norm_rope bit for bit.  A slot
+ * outside the cache is not stored.  k and v have cache->heads heads of
+ * cache->head_dim channels.  Two tokens of one call must not share a slot. */
+spl_status spl_qk_norm_rope_append(const spl_heads* q, const spl_heads* k, const spl_heads* v, int64_t tokens,
+                                   const void* q_weight, const void* k_weight, float eps, const int32_t* positions,
+                                   const float* rope, int64_t rope_rows, int32_t rot, int32_t interleaved,
+                                   const int32_t* slots, const spl_kv_cache* cache, void* q_out, void* k_out,
+                                   hipStream_t stream);
+
+/* What the cache holds at slots[0 .. tokens): k, v out [tokens][heads][head_dim]
+ * of the cache's type, either may be NULL; zeros for a slot outside the cache. */
+spl_status spl_cache_read(const spl_kv_cache* cache, const int32_t* slots, int64_t tokens, void* k, void* v,
+                          hipStream_t stream);
+
+/* Causal attention of a batch's rows over the 4-bit cache:
+ *   out[t][h] = sum_u softmax_u(scale q[t][h] . key_u) value_u
+ * over the tokens u <= p (with window > 0: u > p - window) of the row's request,
+ * the keys and values of head h / (q heads / cache heads).
+ *   q           view of `tokens` rows of the cache's type; heads a multiple of
+ *               the cache's.
+ *   table       [requests][width] page numbers; a page outside the cache holds no keys.
+ *   lens        [requests]: tokens of the request, the new ones among them (in
+ *               the cache before the call).
+ *   row_start   [requests + 1]: request r's rows are row_start[r] ..
+ *               row_start[r + 1] - 1, at the last positions of the request:
+ *               p = lens[r] - row_start[r + 1] + t.
+ *   max_new     the most rows of a request, 0 if not known: rows past it may be
+ *               left out.  max_len  about the most tokens of a request, 0 if not
+ *               known (a hint: it sets how far the work is split).
+ *   out         [tokens][heads][head_dim]; rows that no request owns are not written.
+ *   lse         optional out [tokens][heads] float32: the natural logarithm of the
+ *               softmax's sum, -inf for a row that sees no key.
+ *   workspace   spl_attention_fp4_workspace_bytes(...) bytes for the same
+ *               arguments (-1 if they are rejected), 256-byte aligned, caller-owned.
+ * Scores, softmax statistics and sums in fp32; a weight of the softmax is
+ * rounded to the cache's type before it meets the values, out once.  A row that
+ * sees no key gives 0.  Keys and values of masked tokens have no influence,
+ * whatever they hold.  The result of a row depends on the split, and so on the
+ * sizes of the call, in the order of its sums only. */
+int64_t spl_attention_fp4_workspace_bytes(const spl_kv_cache* cache, int64_t tokens, int32_t heads, int64_t requests,
+                                          int64_t width, int64_t max_new, int64_t max_len);
+spl_status spl_attention_fp4(const spl_heads* q, int64_t tokens, const spl_kv_cache* cache, const int32_t* table,
+                             int64_t requests, int64_t width, const int32_t* lens, const int32_t* row_start,
+                             int64_t max_new, int64_t max_len, float scale, int32_t window, void* out, float* lse,
+                             void* workspace, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -15,7 +15,10 @@ Names follow the C ABI without its ``spl_`` prefix:
   linears (e.g. q, k, v) of one batch size in one launch;
 * ``unpack``, ``dense_linear``, ``dense_linear_int8``: decoder and dense comparators;
 * ``sparse_weight_grad[_group]``, ``sparse_input_grad``, ``sparse_sgd_update``:
-  the training step with the mask held fixed (Algorithm 1).
+  the training step with the mask held fixed (Algorithm 1);
+* ``block_tables``, ``qk_norm_rope[_grad|_append]``, ``cache_read``,
+  ``attention_fp4`` over a :class:`KVCache`: the attention half of a layer,
+  between the q, k, v projections and o.
 """
 from __future__ import annotations
 
@@ -75,6 +78,17 @@ class _Int8Task(ctypes.Structure):
 class _WeightGradTask(ctypes.Structure):
     _fields_ = [("dY", ctypes.c_void_p), ("X", ctypes.c_void_p), ("W", ctypes.POINTER(_Matrix)),
                 ("grad_values", ctypes.c_void_p)]
+
+
+class _Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("heads", ctypes.c_int32)]
+
+
+class _KVCache(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("pages", ctypes.c_int64), ("data_bytes", ctypes.c_int64),
+                ("page", ctypes.c_int32), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
 
 
 class _DenseInt8Task(ctypes.Structure):
@@ -150,6 +164,19 @@ def lib() -> ctypes.CDLL:
         "spl_sparse_linear_int8_group": (ctypes.c_int, [ctypes.POINTER(_Int8Task), I32, I64, P]),
         "spl_dense_linear_int8_group": (ctypes.c_int, [ctypes.POINTER(_DenseInt8Task), I32, I64, P]),
     }
+    HP, CP, F32 = ctypes.POINTER(_Heads), ctypes.POINTER(_KVCache), ctypes.c_float
+    sigs.update({
+        "spl_kv_page_bytes": (I64, [I32, I32]),
+        "spl_block_tables": (ctypes.c_int, [P, P, I64, I64, I32, P, I64, P, I64, P, P, P, P, P, P, P]),
+        "spl_qk_norm_rope": (ctypes.c_int, [HP, HP, I64, I32, I32, P, P, F32, P, P, I64, I32, I32, P, P, P]),
+        "spl_qk_norm_rope_grad_workspace_bytes": (I64, [I64, I32, I32, I32]),
+        "spl_qk_norm_rope_grad": (ctypes.c_int, [HP, HP, HP, HP, I64, I32, I32, P, P, F32, P, P, I64, I32, I32, P, P, P,
+                                                 P, P, P]),
+        "spl_qk_norm_rope_append": (ctypes.c_int, [HP, HP, HP, I64, P, P, F32, P, P, I64, I32, I32, P, CP, P, P, P]),
+        "spl_cache_read": (ctypes.c_int, [CP, P, I64, P, P, P]),
+        "spl_attention_fp4_workspace_bytes": (I64, [CP, I64, I32, I64, I64, I64, I64]),
+        "spl_attention_fp4": (ctypes.c_int, [HP, I64, CP, P, I64, I64, P, P, I64, I64, F32, I32, P, P, P, P]),
+    })
     for name, (res, args) in sigs.items():
         fn = getattr(L, name)
         fn.restype = res
@@ -918,3 +945,275 @@ def dense_linear_int8_group(Xqs, x_scales, Wqs, w_scales, outs=None, acc_outs=No
         tasks[i].acc_out = None if accs[i] is None else accs[i].data_ptr()
     _check("spl_dense_linear_int8_group", L.spl_dense_linear_int8_group(tasks, n, M, _stream(stream)))
     return outs
+
+
+# ------------------------------------------------------------------------------ the attention half of a layer
+
+
+class KVCache:
+    """Keys and values in 4 bits (format and layout: spl_kv_cache), in pages of `page` tokens.
+
+    data: uint8 [pages, heads, kv_page_bytes(head_dim, page)]; dtype: the type (fp16 or bf16) of what is stored and read
+    back.  ``KVCache.empty`` allocates one."""
+
+    __slots__ = ("data", "page", "head_dim", "dtype", "_view")
+
+    def __init__(self, data: torch.Tensor, page: int, head_dim: int, dtype: torch.dtype):
+        if dtype not in (torch.float16, torch.bfloat16):
+            raise ValueError("a cache holds fp16 or bf16 keys and values")
+        size = kv_page_bytes(head_dim, page)
+        if not isinstance(data, torch.Tensor) or data.dim() != 3 or data.shape[2] != size:
+            raise ValueError(f"data must be [pages, heads, {size}]")
+        _arg(data, "data", dtype=torch.uint8, device=False)
+        self.data, self.page, self.head_dim, self.dtype = data, page, head_dim, dtype
+        self._view = _KVCache(data.data_ptr(), data.shape[0], data.numel(), page, data.shape[1], head_dim,
+                              _TORCH_DTYPE[dtype])
+
+    @classmethod
+    def empty(cls, pages: int, heads: int, head_dim: int, page: int, dtype: torch.dtype, device="cuda") -> "KVCache":
+        return cls(torch.zeros((pages, heads, kv_page_bytes(head_dim, page)), dtype=torch.uint8, device=device), page,
+                   head_dim, dtype)
+
+    @property
+    def pages(self) -> int:
+        return self.data.shape[0]
+
+    @property
+    def heads(self) -> int:
+        return self.data.shape[1]
+
+
+def kv_page_bytes(head_dim: int, page: int) -> int:
+    """Bytes of one head's region of a page (see spl_kv_page_bytes)."""
+    size = lib().spl_kv_page_bytes(head_dim, page)
+    if size == 0:
+        raise ValueError(f"no cache of {head_dim} channels in pages of {page} tokens: 64, 96, 128 or 256 channels, a "
+                         "power of two from 16 to 256 tokens")
+    return size
+
+
+@dataclass
+class BlockPlan:
+    """A step's rows and slots (see spl_block_tables)."""
+
+    row_start: torch.Tensor            # int32 [requests + 1]
+    lens: torch.Tensor                 # int32 [requests]
+    positions: torch.Tensor            # int32 [tokens]
+    slots: torch.Tensor                # int32 [tokens]
+    free_head: torch.Tensor            # int32 [1]: free_head of the next step
+    missing: torch.Tensor              # int32 [1]: new tokens without a row or a slot
+
+
+def block_tables(cached: torch.Tensor, new: torch.Tensor, table: torch.Tensor, free_pages: torch.Tensor,
+                 free_head: torch.Tensor, page: int, tokens: int, stream=None) -> BlockPlan:
+    """Pages from the free list for each request's `new` tokens after its `cached` ones, written into `table`
+    [requests, width], and the row, position and slot of every new token (see spl_block_tables).  `tokens` is the rows
+    of the step's tensors; nothing waits for the GPU."""
+    L = lib()
+    i32 = torch.int32
+    _arg(cached, "cached", dtype=i32, min_numel=1, device=False)
+    R = cached.shape[0]
+    _arg(new, "new", shape=(R,), dtype=i32, device=False)
+    if not isinstance(table, torch.Tensor) or table.dim() != 2 or table.shape[0] != R:
+        raise ValueError("table must be [requests, width]")
+    _arg(table, "table", dtype=i32, device=False)
+    _arg(free_pages, "free_pages", dtype=i32, min_numel=0, device=False)
+    _arg(free_head, "free_head", shape=(1,), dtype=i32, device=False)
+    if tokens < 0:
+        raise ValueError("tokens must not be negative")
+    for t, nm in ((cached, "cached"), (new, "new"), (table, "table"), (free_pages, "free_pages"),
+                  (free_head, "free_head")):
+        _dev_tensor(t, nm)
+    # one allocation for all results, each part 16-byte aligned
+    sizes = (R + 1, R, tokens, tokens, 2)
+    at, n = [], 0
+    for m in sizes:
+        at.append(n)
+        n += (m + 3) // 4 * 4
+    buf = torch.empty((n,), dtype=i32, device=cached.device)
+    p = buf.data_ptr()
+    _check("spl_block_tables",
+           L.spl_block_tables(_ptr(cached), _ptr(new), R, tokens, page, _ptr(table), table.shape[1], _ptr(free_pages),
+                              free_pages.shape[0], _ptr(free_head), *(p + 4 * a for a in at), _stream(stream)))
+    row_start, lens, positions, slots, state = (buf.narrow(0, a, m) for a, m in zip(at, sizes))
+    return BlockPlan(row_start, lens, positions, slots, state.narrow(0, 0, 1), state.narrow(0, 1, 1))
+
+
+def _heads(x: torch.Tensor, name: str, tokens: int | None = None, dim: int | None = None, dtype=None) -> _Heads:
+    """A [tokens, heads, dim] view with contiguous channels and other strides that are multiples of 8."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 3:
+        raise ValueError(f"{name} must be [tokens, heads, dim]")
+    T, H, D = x.shape
+    if (tokens is not None and T != tokens) or (dim is not None and D != dim):
+        raise ValueError(f"{name} has shape {tuple(x.shape)}, expected [{tokens}, heads, {dim}]")
+    if x.dtype not in (torch.float16, torch.bfloat16) or (dtype is not None and x.dtype != dtype):
+        raise ValueError(f"{name} has dtype {x.dtype}, expected {dtype or 'fp16 or bf16'}")
+    st, sh, sd = x.stride()
+    if T <= 1:
+        st = 0
+    if H == 1:
+        sh = 0
+    if sd != 1 or st % 8 or sh % 8 or x.data_ptr() % 16:
+        raise ValueError(f"{name}: channels must be contiguous, the other strides multiples of 8, the start 16-byte "
+                         "aligned")
+    return _Heads(x.data_ptr(), st, sh, H)
+
+
+def _turn_args(tokens: int, dim: int, dtype, positions, rope, q_weight, k_weight):
+    """The rotation's and the norms' arguments: checked, as (rope rows, rot)."""
+    for w, nm in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None:
+            _arg(w, nm, shape=(dim,), dtype=dtype)
+    if rope is None:
+        return 0, 0
+    _arg(positions, "positions", shape=(tokens,), dtype=torch.int32)
+    if not isinstance(rope, torch.Tensor) or rope.dim() != 3 or rope.shape[2] != 2:
+        raise ValueError("rope must be float32 [positions, rot / 2, 2] (cosine, sine)")
+    _arg(rope, "rope", dtype=torch.float32)
+    return rope.shape[0], 2 * rope.shape[1]
+
+
+def _heads_out(out, like: torch.Tensor, name: str) -> torch.Tensor:
+    if out is None:
+        return torch.empty(like.shape, dtype=like.dtype, device=like.device)
+    return _arg(out, name, shape=like.shape, dtype=like.dtype)
+
+
+def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor | None, rope: torch.Tensor | None,
+                 q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None, eps: float = 1e-6,
+                 interleaved: bool = False, q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None,
+                 stream=None):
+    """(q_out, k_out): the RMS norm of every head of q [tokens, heads, dim] and k, with the weights given, then the
+    rotation by rope[position] (see spl_qk_norm_rope).  rope: float32 [positions, rot / 2, 2], or None for none.  q and
+    k may be slices of one fused product."""
+    L = lib()
+    hq = _heads(q, "q")
+    T, _, D = q.shape
+    hk = _heads(k, "k", T, D, q.dtype)
+    rows, rot = _turn_args(T, D, q.dtype, positions, rope, q_weight, k_weight)
+    _on_device(q, "q")
+    _on_device(k, "k")
+    q_out, k_out = _heads_out(q_out, q, "q_out"), _heads_out(k_out, k, "k_out")
+    _check("spl_qk_norm_rope",
+           L.spl_qk_norm_rope(ctypes.byref(hq), ctypes.byref(hk), T, D, _TORCH_DTYPE[q.dtype], _ptr(q_weight),
+                              _ptr(k_weight), eps, _ptr(positions) if rot else None, _ptr(rope), rows, rot,
+                              int(interleaved), _ptr(q_out), _ptr(k_out), _stream(stream)))
+    return q_out, k_out
+
+
+def _on_device(t: torch.Tensor, name: str) -> None:
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+
+
+def qk_norm_rope_grad(dq: torch.Tensor, dk: torch.Tensor, q: torch.Tensor, k: torch.Tensor,
+                      positions: torch.Tensor | None, rope: torch.Tensor | None,
+                      q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None, eps: float = 1e-6,
+                      interleaved: bool = False, dq_out: torch.Tensor | None = None,
+                      dk_out: torch.Tensor | None = None, stream=None):
+    """(dq, dk, dq_weight, dk_weight) of the inputs of qk_norm_rope from the gradients dq, dk of its results; the
+    weights' are float32, None without a weight (see spl_qk_norm_rope_grad)."""
+    L = lib()
+    hq = _heads(q, "q")
+    T, _, D = q.shape
+    hk = _heads(k, "k", T, D, q.dtype)
+    hdq, hdk = _heads(dq, "dq", T, D, q.dtype), _heads(dk, "dk", T, D, q.dtype)
+    if hdq.heads != hq.heads or hdk.heads != hk.heads:
+        raise ValueError("a gradient has its input's heads")
+    rows, rot = _turn_args(T, D, q.dtype, positions, rope, q_weight, k_weight)
+    for t, nm in ((q, "q"), (k, "k"), (dq, "dq"), (dk, "dk")):
+        _on_device(t, nm)
+    need = L.spl_qk_norm_rope_grad_workspace_bytes(T, hq.heads, hk.heads, D)
+    if need < 0:
+        raise ValueError("the workspace-size function rejected the shape")
+    dq_out, dk_out = _heads_out(dq_out, q, "dq_out"), _heads_out(dk_out, k, "dk_out")
+    dwq, dwk = (None if w is None else torch.empty((D,), dtype=torch.float32, device=q.device)
+                for w in (q_weight, k_weight))
+    ws = _workspace_on(need, q.device, stream) if need else None
+    _check("spl_qk_norm_rope_grad",
+           L.spl_qk_norm_rope_grad(ctypes.byref(hdq), ctypes.byref(hdk), ctypes.byref(hq), ctypes.byref(hk), T, D,
+                                   _TORCH_DTYPE[q.dtype], _ptr(q_weight), _ptr(k_weight), eps,
+                                   _ptr(positions) if rot else None, _ptr(rope), rows, rot, int(interleaved),
+                                   _ptr(dq_out), _ptr(dk_out), _ptr(dwq), _ptr(dwk), _ptr(ws), _stream(stream)))
+    return dq_out, dk_out, dwq, dwk
+
+
+def qk_norm_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor | None,
+                        rope: torch.Tensor | None, slots: torch.Tensor, cache: KVCache,
+                        q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None,
+                        eps: float = 1e-6, interleaved: bool = False, q_out: torch.Tensor | None = None,
+                        k_out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """q_out of qk_norm_rope; its keys and the values v go to `slots` of the cache in the same launch (and the keys to
+    k_out, where given; see spl_qk_norm_rope_append)."""
+    L = lib()
+    hq = _heads(q, "q", None, cache.head_dim, cache.dtype)
+    T, _, D = q.shape
+    hk, hv = _heads(k, "k", T, D, q.dtype), _heads(v, "v", T, D, q.dtype)
+    if hk.heads != cache.heads or hv.heads != cache.heads:
+        raise ValueError(f"k and v have {hk.heads} and {hv.heads} heads, the cache has {cache.heads}")
+    _arg(slots, "slots", shape=(T,), dtype=torch.int32, device=False)
+    rows, rot = _turn_args(T, D, q.dtype, positions, rope, q_weight, k_weight)
+    for t, nm in ((q, "q"), (k, "k"), (v, "v"), (slots, "slots"), (cache.data, "the cache")):
+        _on_device(t, nm)
+    q_out = _heads_out(q_out, q, "q_out")
+    if k_out is not None:
+        k_out = _heads_out(k_out, k, "k_out")
+    _check("spl_qk_norm_rope_append",
+           L.spl_qk_norm_rope_append(ctypes.byref(hq), ctypes.byref(hk), ctypes.byref(hv), T, _ptr(q_weight),
+                                     _ptr(k_weight), eps, _ptr(positions) if rot else None, _ptr(rope), rows, rot,
+                                     int(interleaved), _ptr(slots), ctypes.byref(cache._view), _ptr(q_out),
+                                     _ptr(k_out), _stream(stream)))
+    return q_out
+
+
+def cache_read(cache: KVCache, slots: torch.Tensor, stream=None):
+    """(keys, values) [tokens, heads, head_dim] that the cache holds at `slots` (see spl_cache_read)."""
+    _arg(slots, "slots", dtype=torch.int32, min_numel=0)
+    _on_device(cache.data, "the cache")
+    out = torch.empty((2, slots.shape[0], cache.heads, cache.head_dim), dtype=cache.dtype, device=slots.device)
+    _check("spl_cache_read", lib().spl_cache_read(ctypes.byref(cache._view), _ptr(slots), slots.shape[0],
+                                                  _ptr(out[0]), _ptr(out[1]), _stream(stream)))
+    return out[0], out[1]
+
+
+def attention_fp4(q: torch.Tensor, cache: KVCache, table: torch.Tensor, lens: torch.Tensor, row_start: torch.Tensor,
+                  scale: float | None = None, window: int = 0, max_new: int = 0, max_len: int = 0,
+                  out: torch.Tensor | None = None, lse: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Causal attention of the rows q [tokens, heads, head_dim] over the 4-bit cache, whose pages `table` [requests,
+    width] lists (see spl_attention_fp4).  `row_start` [requests + 1] and `lens` [requests] are those of block_tables;
+    scale is 1 / sqrt(head_dim) unless given.  max_new (the most rows of a request) and max_len (about the most tokens)
+    let the call choose its launch without asking the GPU.  lse: float32 [tokens, heads], written if given."""
+    L = lib()
+    hq = _heads(q, "q", None, cache.head_dim, cache.dtype)
+    T, H, D = q.shape
+    if H % cache.heads:
+        raise ValueError(f"q has {H} heads, not a multiple of the cache's {cache.heads}")
+    if not isinstance(table, torch.Tensor) or table.dim() != 2:
+        raise ValueError("table must be [requests, width]")
+    R, width = table.shape
+    _arg(table, "table", dtype=torch.int32, device=False)
+    _arg(lens, "lens", shape=(R,), dtype=torch.int32, device=False)
+    _arg(row_start, "row_start", shape=(R + 1,), dtype=torch.int32, device=False)
+    if lse is not None:
+        _arg(lse, "lse", shape=(T, H), dtype=torch.float32, device=False)
+    for t, nm in ((q, "q"), (cache.data, "the cache"), (table, "table"), (lens, "lens"), (row_start, "row_start")):
+        _on_device(t, nm)
+    out = _heads_out(out, q, "out")
+    view = ctypes.byref(cache._view)
+    need = L.spl_attention_fp4_workspace_bytes(view, T, H, R, width, max_new, max_len)
+    if need < 0:
+        raise ValueError("spl_attention_fp4_workspace_bytes rejected the arguments")
+    ws = _workspace_on(need, q.device, stream) if need else None
+    _check("spl_attention_fp4",
+           L.spl_attention_fp4(ctypes.byref(hq), T, view, _ptr(table), R, width, _ptr(lens), _ptr(row_start), max_new,
+                               max_len, D ** -0.5 if scale is None else scale, window, _ptr(out), _ptr(lse), _ptr(ws),
+                               _stream(stream)))
+    return out
+
+
+def _workspace_on(need: int, device, stream) -> torch.Tensor:
+    """As _scratch, for a call that cannot do without."""
+    ws = _scratch(need, device, stream)
+    if ws is None:
+        raise torch.OutOfMemoryError(f"no {need} bytes of workspace")
+    return ws

@@ -1,0 +1,108 @@
+// Device code shared by the attention kernels: operands out of the 4-bit
+// cache, the requests' rows in tiles, the masks.
+#pragma once
+
+#include "spl_attn.h"
+
+namespace spl {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ uint32_t cvt_pair(Bf16, uint32_t code, float scale, int sel) {
+  switch (sel) {
+    case 0: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 0));
+    case 1: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 1));
+    case 2: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 2));
+    default: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 3));
+  }
+}
+__device__ __forceinline__ uint32_t cvt_pair(F16, uint32_t code, float scale, int sel) {
+  switch (sel) {
+    case 0: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(code, scale, 0));
+    case 1: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(code, scale, 1));
+    case 2: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(code, scale, 2));
+    default: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(code, scale, 3));
+  }
+}
+// The eight values of a dword of codes under scale byte `b` of the word `s`
+// (the conversion reads the scale's exponent alone: what the shift leaves in
+// the sign and the fraction has no effect).
+template <class T>
+__device__ __forceinline__ u32x4 cvt8(uint32_t code, float scale) {
+  u32x4 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = cvt_pair(T{}, code, scale, i);
+  return v;
+}
+__device__ __forceinline__ float scale_of(uint32_t s, int b) {
+  return __uint_as_float(b == 0 ? s << 23 : b == 1 ? s << 15 : b == 2 ? s << 7 : s >> 1);
+}
+
+__device__ __forceinline__ f32x4 mfma16(Bf16, const u32x4& a, const u32x4& b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0,
+                                                 0);
+}
+__device__ __forceinline__ f32x4 mfma16(F16, const u32x4& a, const u32x4& b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0,
+                                                0);
+}
+
+// Two floats rounded to nearest even, the first in the low half.
+__device__ __forceinline__ uint32_t pack2(Bf16, float a, float b) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const bf16x2 v = {(__bf16)a, (__bf16)b};
+  return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ uint32_t pack2(F16, float a, float b) {
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+  const f16x2 v = {(_Float16)a, (_Float16)b};
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Row indexes of a request, clamped to the call's rows, and its length.
+struct Rows {
+  int64_t first;
+  int32_t count, len;
+};
+__device__ __forceinline__ Rows rows_of(const AttnArgs& a, int64_t r) {
+  const int64_t t = a.tokens;
+  int64_t s = a.row_start[r], e = a.row_start[r + 1];
+  s = s < 0 ? 0 : (s > t ? t : s);
+  e = e < s ? s : (e > t ? t : e);
+  const int64_t most = a.width * (int64_t)a.cache.page;
+  int64_t len = a.lens[r];
+  len = len < 0 ? 0 : (len > most ? most : len);
+  return {s, (int32_t)(e - s), (int32_t)len};
+}
+
+// The request that owns tile `tile` when each has ceil(rows * group / size)
+// tiles, and the tile's number in it; request -1 past the last.  Every lane
+// of the wave calls it with the same tile.
+struct Tile {
+  int64_t request;
+  int64_t index;
+};
+__device__ __forceinline__ Tile find_tile(const AttnArgs& a, int group, int size, int64_t tile) {
+  const int lane = lane_id();
+  int64_t before = 0;
+  for (int64_t base = 0; base < a.requests; base += 64) {
+    int64_t n = 0;
+    if (base + lane < a.requests) n = ((int64_t)rows_of(a, base + lane).count * group + size - 1) / size;
+    int64_t sum = n;
+    for (int d = 1; d < 64; d <<= 1) {
+      const int64_t y = __shfl_up(sum, d);
+      if (lane >= d) sum += y;
+    }
+    const uint64_t past = __ballot(before + sum > tile);
+    if (past) {
+      const int k = __builtin_ctzll(past);
+      return {base + k, tile - before - __shfl(sum - n, k)};
+    }
+    before += __shfl(sum, 63);
+  }
+  return {-1, 0};
+}
+
+}  // namespace spl

@@ -1,0 +1,490 @@
+// Norms of query and key heads with the rotation by position in the same pass,
+// storing keys and values in the 4-bit cache, and the gradients.
+//
+// A head's D channels are read by LPH = 8, 16 or 32 lanes (D / 8 rounded up to
+// a power of two), eight channels (16 bytes) a lane, so that a wave holds
+// 64 / LPH heads and everything stays in registers: one read and one write of
+// each element.  A wave takes up to kHeads heads of one token, so the angles
+// and norm weights of its channels are loaded once for all of them.
+//
+// The mean of squares adds neighbours in pairs (channels 2i and 2i + 1, then
+// pairs of pairs, ...), by lane exchanges whose sums do not depend on the side:
+// together with products and sums that are rounded one by one this makes every
+// bit of a key, and so its 4-bit codes, a function of the key alone.
+//
+// Bound: HBM at large sizes (2 + 2 bytes an element forward, 4 + 2 backward),
+// the launch at small ones.
+#include "spl_attn.h"
+
+#pragma clang fp contract(off)
+
+namespace {
+
+using spl::Bf16;
+using spl::F16;
+using spl::u32x2;
+using spl::u32x4;
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+
+template <int C>
+__device__ __forceinline__ float dpp(float x) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), C, 0xf, 0xf, true));
+}
+
+// Sum over the LPH lanes of a head, added in pairs of neighbours.  Past the
+// quad a mirrored lane stands for the exchanged one: its group has the same sum.
+template <int LPH>
+__device__ __forceinline__ float head_sum(float x) {
+  x += dpp<0xB1>(x);                            // lane ^ 1
+  x += dpp<0x4E>(x);                            // lane ^ 2
+  x += dpp<0x141>(x);                           // half row mirrored: the other quad
+  if (LPH >= 16) x += dpp<0x140>(x);            // row mirrored: the other half row
+  if (LPH >= 32) x += __shfl_xor(x, 16);
+  return x;
+}
+
+__device__ __forceinline__ float pair_tree(const float* p) {
+  return ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+}
+
+template <class T>
+__device__ __forceinline__ void widen(const u32x4& v, float* x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = T::to_f32(v[i] & 0xffffu);
+    x[2 * i + 1] = T::to_f32(v[i] >> 16);
+  }
+}
+template <class T>
+__device__ __forceinline__ u32x4 narrow(const float* x) {
+  u32x4 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = (uint32_t)T::from_f32(x[2 * i]) | ((uint32_t)T::from_f32(x[2 * i + 1]) << 16);
+  return v;
+}
+
+// The rotation's part of a lane: for each of its channels the cosine and the
+// signed sine, and the lane that holds the other channel of each pair (halves).
+template <bool kInter>
+struct Turn {
+  float c[8], s[8];
+  int partner;
+  bool on;
+};
+
+template <bool kInter>
+__device__ __forceinline__ Turn<kInter> load_turn(const float* rope, int64_t rows, int64_t pos, int rot, int chunk,
+                                                  int lane) {
+  Turn<kInter> t;
+  const int half = rot >> 4;                    // chunks of one half of the rotated channels
+  t.on = chunk < 2 * half;
+  t.partner = lane;
+  const bool known = pos >= 0 && pos < rows;
+  if (!t.on) return t;
+  const float* row = rope + (known ? pos : 0) * rot;
+  if (kInter) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float c = known ? row[8 * chunk + 2 * i] : NAN, s = known ? row[8 * chunk + 2 * i + 1] : NAN;
+      t.c[2 * i] = t.c[2 * i + 1] = c;
+      t.s[2 * i] = -s;
+      t.s[2 * i + 1] = s;
+    }
+  } else {
+    const bool low = chunk < half;
+    t.partner = low ? lane + half : lane - half;
+    const float* at = row + 16 * (low ? chunk : chunk - half);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float c = known ? at[2 * i] : NAN, s = known ? at[2 * i + 1] : NAN;
+      t.c[i] = c;
+      t.s[i] = low ? -s : s;
+    }
+  }
+  return t;
+}
+
+// x turned by the angle (kBack: by its negative): x c + other s, each product
+// and the sum rounded.  Every lane of the wave takes part.
+template <bool kInter, bool kBack>
+__device__ __forceinline__ void turn(const Turn<kInter>& t, float* x) {
+  float y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] = kInter ? x[i ^ 1] : __shfl(x[i], t.partner);
+  if (!t.on) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float p = y[i] * t.s[i];
+    x[i] = kBack ? x[i] * t.c[i] - p : x[i] * t.c[i] + p;
+  }
+}
+
+template <int LPH>
+__device__ __forceinline__ float inverse_rms(const float* x, float inv_dim, float eps) {
+  float sq[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) sq[i] = x[i] * x[i];
+  const float ms = head_sum<LPH>(pair_tree(sq)) * inv_dim;
+  return 1.0f / __fsqrt_rn(ms + eps);
+}
+
+// ---- the 4-bit cache
+
+// Scale byte and eight 4-bit codes of a lane's channels; the four lanes of a
+// quad hold one group of 32.  A group that holds an infinity or a NaN gets
+// scale 255, which reads back as NaN.
+template <class T>
+__device__ __forceinline__ uint32_t encode8(const u32x4& bits, uint32_t* code) {
+  constexpr uint32_t kInf = T::code == SPL_F16 ? 0x7c00u : 0x7f80u;
+  constexpr int kLow = T::code == SPL_F16 ? 104 : 2, kHigh = T::code == SPL_F16 ? 140 : 252;
+  uint32_t top = 0;                             // magnitudes are ordered as their bits
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t lo = bits[i] & 0x7fffu, hi = (bits[i] >> 16) & 0x7fffu;
+    top = top > lo ? top : lo;
+    top = top > hi ? top : hi;
+  }
+  uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xf, 0xf, true);
+  top = top > o ? top : o;
+  o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xf, 0xf, true);
+  top = top > o ? top : o;
+  // amax = f 2^x with 1 <= f < 2: the least e with amax <= 7 * 2^e is x - 2, or x - 1 for f > 1.75
+  const uint32_t u = __float_as_uint(T::to_f32(top));
+  int byte = (int)(u >> 23) - 2 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
+  byte = byte < kLow ? kLow : (byte > kHigh ? kHigh : byte);
+  const float scale = __uint_as_float((uint32_t)byte << 23);
+  float x[8];
+  widen<T>(bits, x);
+  uint32_t c = 0;
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[0], x[1], scale, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2], x[3], scale, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4], x[5], scale, 2);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6], x[7], scale, 3);
+  *code = c;
+  return top >= kInf ? 255u : (uint32_t)byte;
+}
+
+// Where a lane's eight channels (chunk c of the head) of token b go.
+__device__ __forceinline__ void store_codes(uint8_t* region, const spl::PageGeom& g, bool value, int b, int c,
+                                            uint32_t code, uint32_t scale) {
+  if (!value) {
+    const int grp = c >> 2, j = c & 3;
+    *reinterpret_cast<uint32_t*>(region + b * (g.dim >> 1) + (j * g.groups + grp) * 4) = code;
+    if (j == 0) region[g.page * g.dim + b * g.scale_bytes + grp] = (uint8_t)scale;
+    return;
+  }
+  uint8_t* at = region + g.page * (g.dim >> 1);
+  if (g.unit == 8) {
+    *reinterpret_cast<uint32_t*>(at + ((b >> 3) * (g.dim >> 3) + c) * 32 + (b & 7) * 4) = code;
+  } else if (g.unit == 16) {
+    *reinterpret_cast<uint32_t*>(at + ((b >> 3) * 16 + (c >> 1)) * 64 + (b & 7) * 8 + (c & 1) * 4) = code;
+  } else {
+    uint16_t* p = reinterpret_cast<uint16_t*>(at + ((b >> 3) * 16 + 2 * c) * 16 + (b & 7) * 2);
+    p[0] = (uint16_t)code;
+    p[8] = (uint16_t)(code >> 16);
+  }
+  if ((c & 3) == 0)
+    region[g.page * (g.dim + g.scale_bytes) + ((b >> 3) * g.scale_bytes + (c >> 2)) * 8 + (b & 7)] = (uint8_t)scale;
+}
+
+// A wave's heads: kIter slots of 64 / LPH heads.
+constexpr int kIter = 4;
+
+// Waves of one token: first q's, then k's, then (with a cache) v's.
+template <class T, int LPH, bool kInter>
+__global__ __launch_bounds__(kThreads) void k_norm_rope(spl::NormRopeArgs a, int q_waves, int k_waves, int all_waves,
+                                                        float inv_dim) {
+  constexpr int kSlots = 64 / LPH;
+  const int64_t task = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+  const int64_t t = task / all_waves;
+  if (t >= a.tokens) return;
+  const int part = (int)(task - t * all_waves);
+  const int lane = threadIdx.x & 63, chunk = lane & (LPH - 1);
+  const bool is_q = part < q_waves, is_v = part >= q_waves + k_waves;
+  const spl_heads& src = is_q ? a.q : (is_v ? a.v : a.k);
+  const int first = (is_q ? part : (is_v ? part - q_waves - k_waves : part - q_waves)) * kIter * kSlots + lane / LPH;
+  const bool live = 8 * chunk < a.dim;
+  const uint16_t* in = static_cast<const uint16_t*>(src.data) + t * src.token_stride + 8 * chunk;
+
+  u32x4 x[kIter];
+#pragma unroll
+  for (int i = 0; i < kIter; ++i) {
+    const int h = first + i * kSlots;
+    x[i] = u32x4{0, 0, 0, 0};
+    if (live && h < src.heads) x[i] = *reinterpret_cast<const u32x4*>(in + h * src.head_stride);
+  }
+  const uint16_t* w16 = static_cast<const uint16_t*>(is_q ? a.wq : a.wk);
+  if (!is_v) {
+    float w[8];
+    if (w16 && live) widen<T>(*reinterpret_cast<const u32x4*>(w16 + 8 * chunk), w);
+    const Turn<kInter> tr = load_turn<kInter>(a.rope, a.rope_rows, a.rot ? a.positions[t] : 0, a.rot, chunk, lane);
+    uint16_t* out = static_cast<uint16_t*>(is_q ? a.q_out : a.k_out);
+    if (out) out += t * src.heads * (int64_t)a.dim + 8 * chunk;
+#pragma unroll
+    for (int i = 0; i < kIter; ++i) {
+      float f[8];
+      widen<T>(x[i], f);
+      if (w16) {
+        const float r = inverse_rms<LPH>(f, inv_dim, a.eps);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = f[e] * r * w[e];
+      }
+      turn<kInter, false>(tr, f);
+      x[i] = narrow<T>(f);
+      const int h = first + i * kSlots;
+      if (out && live && h < src.heads) *reinterpret_cast<u32x4*>(out + (int64_t)h * a.dim) = x[i];
+    }
+  }
+  if (is_q || !a.cache.data) return;
+  const int64_t slot = a.slots[t];
+  const int shift = __builtin_ctz((unsigned)a.cache.page);
+  if (slot < 0 || (slot >> shift) >= a.cache.pages) return;
+  const spl::PageGeom g = spl::page_geom(a.dim, a.cache.page);
+  const int b = (int)(slot & (a.cache.page - 1));
+  uint8_t* page = static_cast<uint8_t*>(a.cache.data) + (slot >> shift) * (int64_t)a.cache.heads * g.bytes;
+#pragma unroll
+  for (int i = 0; i < kIter; ++i) {
+    uint32_t code;
+    const uint32_t scale = encode8<T>(x[i], &code);
+    const int h = first + i * kSlots;
+    if (live && h < src.heads) store_codes(page + (int64_t)h * g.bytes, g, is_v, b, chunk, code, scale);
+  }
+}
+
+// The cache's values of given slots: eight channels of one key and value a thread.
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_cache_read(spl_kv_cache c, const int32_t* slots, int64_t tokens,
+                                                         uint16_t* k, uint16_t* v) {
+  const spl::PageGeom g = spl::page_geom(c.head_dim, c.page);
+  const int chunks = g.dim >> 3, shift = __builtin_ctz((unsigned)c.page);
+  const int64_t n = tokens * c.heads * chunks;
+  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (i >= n) return;
+  const int64_t th = i / chunks, t = th / c.heads;
+  const int ch = (int)(i - th * chunks), h = (int)(th - t * c.heads);
+  const int64_t slot = slots[t];
+  u32x4 ko = {0, 0, 0, 0}, vo = {0, 0, 0, 0};
+  if (slot >= 0 && (slot >> shift) < c.pages) {
+    const int b = (int)(slot & (c.page - 1));
+    const uint8_t* r = static_cast<const uint8_t*>(c.data) + ((slot >> shift) * c.heads + h) * (int64_t)g.bytes;
+    const int grp = ch >> 2;
+    const uint32_t kc = *reinterpret_cast<const uint32_t*>(r + b * (g.dim >> 1) + ((ch & 3) * g.groups + grp) * 4);
+    const uint32_t ks = r[g.page * g.dim + b * g.scale_bytes + grp];
+    const uint8_t* at = r + g.page * (g.dim >> 1);
+    uint32_t vc;
+    if (g.unit == 8) {
+      vc = *reinterpret_cast<const uint32_t*>(at + ((b >> 3) * (g.dim >> 3) + ch) * 32 + (b & 7) * 4);
+    } else if (g.unit == 16) {
+      vc = *reinterpret_cast<const uint32_t*>(at + ((b >> 3) * 16 + (ch >> 1)) * 64 + (b & 7) * 8 + (ch & 1) * 4);
+    } else {
+      const uint16_t* p = reinterpret_cast<const uint16_t*>(at + ((b >> 3) * 16 + 2 * ch) * 16 + (b & 7) * 2);
+      vc = (uint32_t)p[0] | ((uint32_t)p[8] << 16);
+    }
+    const uint32_t vs = r[g.page * (g.dim + g.scale_bytes) + ((b >> 3) * g.scale_bytes + grp) * 8 + (b & 7)];
+    const float fk = __uint_as_float(ks << 23), fv = __uint_as_float(vs << 23);
+#define SPL_READ2(i)                                                                                       \
+  if (T::code == SPL_F16) {                                                                                \
+    ko[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(kc, fk, i));             \
+    vo[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(vc, fv, i));             \
+  } else {                                                                                                 \
+    ko[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(kc, fk, i));            \
+    vo[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(vc, fv, i));            \
+  }
+    SPL_READ2(0) SPL_READ2(1) SPL_READ2(2) SPL_READ2(3)
+#undef SPL_READ2
+  }
+  if (k) *reinterpret_cast<u32x4*>(k + th * g.dim + 8 * ch) = ko;
+  if (v) *reinterpret_cast<u32x4*>(v + th * g.dim + 8 * ch) = vo;
+}
+
+// ---- gradients
+//
+// With xh = x r, r = 1 / rms(x), y = turn(xh w) and g = turn back(dy):
+//   dw = sum over tokens and heads of g xh,   dx = r (g w - xh mean(g w xh)).
+// A workgroup walks tokens in a fixed stride, its lanes keeping the same
+// channels, so dw's terms stay in registers; its sums go to one row of
+// `partial`, which k_norm_rope_dw adds up in order: the result does not change
+// from run to run.
+template <class T, int LPH, bool kInter>
+__global__ __launch_bounds__(kThreads) void k_norm_rope_grad(spl::NormRopeGradArgs a, int q_groups, int groups,
+                                                             float inv_dim) {
+  constexpr int kSlots = 64 / LPH;
+  __shared__ float sum_s[kWaves][LPH * 8];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, chunk = lane & (LPH - 1);
+  const bool is_q = (int)blockIdx.x < q_groups, live = 8 * chunk < a.dim;
+  const int group = is_q ? blockIdx.x : blockIdx.x - q_groups, count = is_q ? q_groups : groups - q_groups;
+  const spl_heads& src = is_q ? a.q : a.k;
+  const spl_heads& grad = is_q ? a.dq : a.dk;
+  uint16_t* out = static_cast<uint16_t*>(is_q ? a.dq_out : a.dk_out) + 8 * chunk;
+  const uint16_t* in = static_cast<const uint16_t*>(src.data) + 8 * chunk;
+  const uint16_t* up = static_cast<const uint16_t*>(grad.data) + 8 * chunk;
+  const uint16_t* w16 = static_cast<const uint16_t*>(is_q ? a.wq : a.wk);
+  float w[8], dw[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) dw[e] = 0.0f, w[e] = 1.0f;
+  if (w16 && live) widen<T>(*reinterpret_cast<const u32x4*>(w16 + 8 * chunk), w);
+  const int per = (src.heads + kIter * kSlots - 1) / (kIter * kSlots);       // waves of one token
+  const int64_t tasks = a.tokens * per;
+  for (int64_t task = (int64_t)group * kWaves + wave; task < tasks; task += (int64_t)count * kWaves) {
+    const int64_t t = task / per;
+    const int first = (int)(task - t * per) * kIter * kSlots + lane / LPH;
+    u32x4 x[kIter], g[kIter];
+#pragma unroll
+    for (int i = 0; i < kIter; ++i) {
+      const int h = first + i * kSlots;
+      x[i] = g[i] = u32x4{0, 0, 0, 0};
+      if (live && h < src.heads) {
+        g[i] = *reinterpret_cast<const u32x4*>(up + t * grad.token_stride + h * grad.head_stride);
+        if (w16) x[i] = *reinterpret_cast<const u32x4*>(in + t * src.token_stride + h * src.head_stride);
+      }
+    }
+    const Turn<kInter> tr = load_turn<kInter>(a.rope, a.rope_rows, a.rot ? a.positions[t] : 0, a.rot, chunk, lane);
+#pragma unroll
+    for (int i = 0; i < kIter; ++i) {
+      float f[8], d[8];
+      widen<T>(g[i], d);
+      turn<kInter, true>(tr, d);
+      if (w16) {
+        widen<T>(x[i], f);
+        const float r = inverse_rms<LPH>(f, inv_dim, a.eps);
+        float p[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          f[e] *= r;
+          dw[e] += d[e] * f[e];
+          d[e] *= w[e];
+          p[e] = d[e] * f[e];
+        }
+        const float m = head_sum<LPH>(pair_tree(p)) * inv_dim;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[e] = r * (d[e] - f[e] * m);
+      }
+      const int h = first + i * kSlots;
+      if (live && h < src.heads) *reinterpret_cast<u32x4*>(out + (t * src.heads + h) * a.dim) = narrow<T>(d);
+    }
+  }
+  if (!w16) return;                                             // the same for the whole workgroup
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    for (int o = LPH; o < 64; o <<= 1) dw[e] += __shfl_xor(dw[e], o);
+  if (lane < LPH) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum_s[wave][8 * chunk + e] = dw[e];
+  }
+  __syncthreads();
+  for (int c = threadIdx.x; c < a.dim; c += kThreads) {
+    float s = 0.0f;
+    for (int v = 0; v < kWaves; ++v) s += sum_s[v][c];
+    a.partial[(int64_t)blockIdx.x * a.dim + c] = s;
+  }
+}
+
+// dw[c] = the sum of a column of `partial`: 32 columns a workgroup, its eight
+// row groups added in order.
+__global__ __launch_bounds__(kThreads) void k_norm_rope_dw(const float* partial, int q_groups, int groups, int dim,
+                                                           float* dwq, float* dwk) {
+  __shared__ float sum_s[8][32];
+  const bool is_q = blockIdx.y == 0;
+  float* dw = is_q ? dwq : dwk;
+  if (!dw) return;
+  const int c = blockIdx.x * 32 + (threadIdx.x & 31), row = threadIdx.x >> 5;
+  const int r0 = is_q ? 0 : q_groups, r1 = is_q ? q_groups : groups;
+  float s = 0.0f;
+  if (c < dim)
+    for (int r = r0 + row; r < r1; r += 8) s += partial[(int64_t)r * dim + c];
+  sum_s[row][threadIdx.x & 31] = s;
+  __syncthreads();
+  if (row == 0 && c < dim) {
+    float total = 0.0f;
+    for (int r = 0; r < 8; ++r) total += sum_s[r][threadIdx.x & 31];
+    dw[c] = total;
+  }
+}
+
+// Workgroups of the gradient for q and for k: shared out by heads, at most
+// four a CU, so that few rows of partial sums are left.
+void grad_groups(int64_t tokens, int32_t q_heads, int32_t k_heads, int32_t dim, int* q, int* k) {
+  const int lph = dim <= 64 ? 8 : (dim <= 128 ? 16 : 32), heads = kIter * (64 / lph);
+  const int64_t most = 4 * (int64_t)spl::device_cus();
+  const auto waves = [&](int64_t h) { return (tokens * ((h + heads - 1) / heads) + kWaves - 1) / kWaves; };
+  const int64_t wq = waves(q_heads), wk = waves(k_heads);
+  int64_t nq = wq, nk = wk;
+  if (wq + wk > most) {
+    nq = most * wq / (wq + wk);
+    nq = nq < 1 ? 1 : nq;
+    nk = most - nq < 1 ? 1 : most - nq;
+  }
+  *q = (int)nq;
+  *k = (int)nk;
+}
+
+#define SPL_LPH(dim, call)                   \
+  do {                                       \
+    if ((dim) <= 64) { call(8); }            \
+    else if ((dim) <= 128) { call(16); }     \
+    else { call(32); }                       \
+  } while (0)
+
+template <class T>
+hipError_t norm_rope(const spl::NormRopeArgs& a, hipStream_t s) {
+  const int lph = a.dim <= 64 ? 8 : (a.dim <= 128 ? 16 : 32), heads = kIter * (64 / lph);
+  const int qw = (a.q.heads + heads - 1) / heads, kw = (a.k.heads + heads - 1) / heads;
+  const int all = qw + kw + (a.cache.data ? kw : 0);
+  const dim3 grid((unsigned)((a.tokens * all + kWaves - 1) / kWaves));
+  const float inv = (float)(1.0 / a.dim);
+#define SPL_CALL(L)                                                                                          \
+  if (a.interleaved) k_norm_rope<T, L, true><<<grid, kThreads, 0, s>>>(a, qw, kw, all, inv);                 \
+  else k_norm_rope<T, L, false><<<grid, kThreads, 0, s>>>(a, qw, kw, all, inv)
+  SPL_LPH(a.dim, SPL_CALL);
+#undef SPL_CALL
+  return hipGetLastError();
+}
+
+template <class T>
+hipError_t norm_rope_grad(const spl::NormRopeGradArgs& a, hipStream_t s) {
+  int nq, nk;
+  grad_groups(a.tokens, a.q.heads, a.k.heads, a.dim, &nq, &nk);
+  const float inv = (float)(1.0 / a.dim);
+#define SPL_CALL(L)                                                                                          \
+  if (a.interleaved) k_norm_rope_grad<T, L, true><<<nq + nk, kThreads, 0, s>>>(a, nq, nq + nk, inv);         \
+  else k_norm_rope_grad<T, L, false><<<nq + nk, kThreads, 0, s>>>(a, nq, nq + nk, inv)
+  SPL_LPH(a.dim, SPL_CALL);
+#undef SPL_CALL
+  if (a.dwq || a.dwk)
+    k_norm_rope_dw<<<dim3((unsigned)((a.dim + 31) / 32), 2), kThreads, 0, s>>>(a.partial, nq, nq + nk, a.dim, a.dwq,
+                                                                            a.dwk);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+namespace spl {
+
+hipError_t launch_norm_rope(const NormRopeArgs& a, int32_t dtype, hipStream_t s) {
+  return dtype == SPL_F16 ? norm_rope<F16>(a, s) : norm_rope<Bf16>(a, s);
+}
+
+hipError_t launch_cache_read(const spl_kv_cache& c, const int32_t* slots, int64_t tokens, void* k, void* v,
+                             hipStream_t s) {
+  const int64_t n = tokens * c.heads * (c.head_dim / 8);
+  const dim3 grid((unsigned)((n + kThreads - 1) / kThreads));
+  if (c.dtype == SPL_F16)
+    k_cache_read<F16><<<grid, kThreads, 0, s>>>(c, slots, tokens, (uint16_t*)k, (uint16_t*)v);
+  else
+    k_cache_read<Bf16><<<grid, kThreads, 0, s>>>(c, slots, tokens, (uint16_t*)k, (uint16_t*)v);
+  return hipGetLastError();
+}
+
+int64_t norm_rope_grad_bytes(int64_t tokens, int32_t q_heads, int32_t k_heads, int32_t dim) {
+  int nq, nk;
+  grad_groups(tokens, q_heads, k_heads, dim, &nq, &nk);
+  return (int64_t)(nq + nk) * dim * 4;
+}
+
+hipError_t launch_norm_rope_grad(const NormRopeGradArgs& a, int32_t dtype, hipStream_t s) {
+  return dtype == SPL_F16 ? norm_rope_grad<F16>(a, s) : norm_rope_grad<Bf16>(a, s);
+}
+
+}  // namespace spl
