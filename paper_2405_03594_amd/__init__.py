@@ -956,7 +956,7 @@ class KVCache:
     data: uint8 [pages, heads, kv_page_bytes(head_dim, page)]; dtype: the type (fp16 or bf16) of what is stored and read
     back.  ``KVCache.empty`` allocates one."""
 
-    __slots__ = ("data", "page", "head_dim", "dtype", "_view")
+    __slots__ = ("data", "pages", "heads", "page", "head_dim", "dtype", "_view")
 
     def __init__(self, data: torch.Tensor, page: int, head_dim: int, dtype: torch.dtype):
         if dtype not in (torch.float16, torch.bfloat16):
@@ -966,6 +966,7 @@ class KVCache:
             raise ValueError(f"data must be [pages, heads, {size}]")
         _arg(data, "data", dtype=torch.uint8, device=False)
         self.data, self.page, self.head_dim, self.dtype = data, page, head_dim, dtype
+        self.pages, self.heads, _ = data.shape
         self._view = _KVCache(data.data_ptr(), data.shape[0], data.numel(), page, data.shape[1], head_dim,
                               _TORCH_DTYPE[dtype])
 
@@ -973,14 +974,6 @@ class KVCache:
     def empty(cls, pages: int, heads: int, head_dim: int, page: int, dtype: torch.dtype, device="cuda") -> "KVCache":
         return cls(torch.zeros((pages, heads, kv_page_bytes(head_dim, page)), dtype=torch.uint8, device=device), page,
                    head_dim, dtype)
-
-    @property
-    def pages(self) -> int:
-        return self.data.shape[0]
-
-    @property
-    def heads(self) -> int:
-        return self.data.shape[1]
 
 
 def kv_page_bytes(head_dim: int, page: int) -> int:
@@ -1004,39 +997,66 @@ class BlockPlan:
     missing: torch.Tensor              # int32 [1]: new tokens without a row or a slot
 
 
+def _on(stream) -> int:
+    """_stream for the calls of this section, whose smallest take a few microseconds: the handle of the current
+    stream without the stream object."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return stream.cuda_stream
+
+
+def _all_on_device(**tensors) -> None:
+    for name, t in tensors.items():
+        if t is not None and not t.is_cuda:
+            raise ValueError(f"{name} must be a device tensor")
+
+
+def _ints(t, name: str, n: int) -> int:
+    """The address of an int32 vector of n entries."""
+    if not isinstance(t, torch.Tensor) or t.shape != (n,) or t.dtype != torch.int32 or not t.is_contiguous():
+        _arg(t, name, shape=(n,), dtype=torch.int32, device=False)
+    return t.data_ptr()
+
+
+def _table(table) -> tuple[int, int]:
+    """(requests, width) of a page table."""
+    if not isinstance(table, torch.Tensor) or table.dim() != 2:
+        raise ValueError("table must be [requests, width]")
+    if table.dtype != torch.int32 or not table.is_contiguous():
+        _arg(table, "table", dtype=torch.int32, device=False)
+    return table.shape
+
+
+def _workspace_on(need: int, device, stream) -> torch.Tensor:
+    """As _scratch, for a call that cannot do without."""
+    ws = _scratch(need, device, stream)
+    if ws is None:
+        raise torch.OutOfMemoryError(f"no {need} bytes of workspace")
+    return ws
+
+
 def block_tables(cached: torch.Tensor, new: torch.Tensor, table: torch.Tensor, free_pages: torch.Tensor,
                  free_head: torch.Tensor, page: int, tokens: int, stream=None) -> BlockPlan:
     """Pages from the free list for each request's `new` tokens after its `cached` ones, written into `table`
     [requests, width], and the row, position and slot of every new token (see spl_block_tables).  `tokens` is the rows
     of the step's tensors; nothing waits for the GPU."""
-    L = lib()
-    i32 = torch.int32
-    _arg(cached, "cached", dtype=i32, min_numel=1, device=False)
-    R = cached.shape[0]
-    _arg(new, "new", shape=(R,), dtype=i32, device=False)
-    if not isinstance(table, torch.Tensor) or table.dim() != 2 or table.shape[0] != R:
-        raise ValueError("table must be [requests, width]")
-    _arg(table, "table", dtype=i32, device=False)
-    _arg(free_pages, "free_pages", dtype=i32, min_numel=0, device=False)
-    _arg(free_head, "free_head", shape=(1,), dtype=i32, device=False)
+    R, width = _table(table)
+    args = (_ints(cached, "cached", R), _ints(new, "new", R))
+    if not isinstance(free_pages, torch.Tensor) or free_pages.dim() != 1:
+        raise ValueError("free_pages must be 1-D")
+    free = _ints(free_pages, "free_pages", free_pages.shape[0])
+    head = _ints(free_head, "free_head", 1)
     if tokens < 0:
         raise ValueError("tokens must not be negative")
-    for t, nm in ((cached, "cached"), (new, "new"), (table, "table"), (free_pages, "free_pages"),
-                  (free_head, "free_head")):
-        _dev_tensor(t, nm)
-    # one allocation for all results, each part 16-byte aligned
-    sizes = (R + 1, R, tokens, tokens, 2)
-    at, n = [], 0
-    for m in sizes:
-        at.append(n)
-        n += (m + 3) // 4 * 4
-    buf = torch.empty((n,), dtype=i32, device=cached.device)
+    _all_on_device(cached=cached, new=new, table=table, free_pages=free_pages, free_head=free_head)
+    # one allocation for all results
+    buf = torch.empty((2 * R + 2 * tokens + 3,), dtype=torch.int32, device=table.device)
     p = buf.data_ptr()
     _check("spl_block_tables",
-           L.spl_block_tables(_ptr(cached), _ptr(new), R, tokens, page, _ptr(table), table.shape[1], _ptr(free_pages),
-                              free_pages.shape[0], _ptr(free_head), *(p + 4 * a for a in at), _stream(stream)))
-    row_start, lens, positions, slots, state = (buf.narrow(0, a, m) for a, m in zip(at, sizes))
-    return BlockPlan(row_start, lens, positions, slots, state.narrow(0, 0, 1), state.narrow(0, 1, 1))
+           lib().spl_block_tables(*args, R, tokens, page, table.data_ptr(), width, free, free_pages.shape[0], head, p,
+                                  p + 4 * (R + 1), p + 4 * (2 * R + 1), p + 4 * (2 * R + 1 + tokens),
+                                  p + 4 * (2 * R + 1 + 2 * tokens), _on(stream)))
+    return BlockPlan(*buf.split_with_sizes((R + 1, R, tokens, tokens, 1, 1)))
 
 
 def _heads(x: torch.Tensor, name: str, tokens: int | None = None, dim: int | None = None, dtype=None) -> _Heads:
@@ -1046,36 +1066,41 @@ def _heads(x: torch.Tensor, name: str, tokens: int | None = None, dim: int | Non
     T, H, D = x.shape
     if (tokens is not None and T != tokens) or (dim is not None and D != dim):
         raise ValueError(f"{name} has shape {tuple(x.shape)}, expected [{tokens}, heads, {dim}]")
-    if x.dtype not in (torch.float16, torch.bfloat16) or (dtype is not None and x.dtype != dtype):
+    if (x.dtype != dtype) if dtype is not None else (x.dtype not in (torch.float16, torch.bfloat16)):
         raise ValueError(f"{name} has dtype {x.dtype}, expected {dtype or 'fp16 or bf16'}")
     st, sh, sd = x.stride()
-    if T <= 1:
-        st = 0
-    if H == 1:
-        sh = 0
-    if sd != 1 or st % 8 or sh % 8 or x.data_ptr() % 16:
-        raise ValueError(f"{name}: channels must be contiguous, the other strides multiples of 8, the start 16-byte "
-                         "aligned")
-    return _Heads(x.data_ptr(), st, sh, H)
+    at = x.data_ptr()
+    if sd != 1 or (st | sh) & 7 or at & 15:
+        st, sh = 0 if T <= 1 else st, 0 if H == 1 else sh
+        if (sd != 1 and D != 1) or (st | sh) & 7 or at & 15:
+            raise ValueError(f"{name}: channels must be contiguous, the other strides multiples of 8, the start "
+                             "16-byte aligned")
+    return _Heads(at, st, sh, H)
 
 
-def _turn_args(tokens: int, dim: int, dtype, positions, rope, q_weight, k_weight):
-    """The rotation's and the norms' arguments: checked, as (rope rows, rot)."""
-    for w, nm in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        if w is not None:
-            _arg(w, nm, shape=(dim,), dtype=dtype)
+def _weight(w, name: str, dim: int, dtype) -> int | None:
+    if w is None:
+        return None
+    if not isinstance(w, torch.Tensor) or w.shape != (dim,) or w.dtype != dtype or not w.is_contiguous():
+        _arg(w, name, shape=(dim,), dtype=dtype, device=False)
+    return w.data_ptr()
+
+
+def _turn_args(tokens: int, positions, rope):
+    """The rotation's arguments: (positions, angles, rows of angles, rotated channels)."""
     if rope is None:
-        return 0, 0
-    _arg(positions, "positions", shape=(tokens,), dtype=torch.int32)
+        return None, None, 0, 0
     if not isinstance(rope, torch.Tensor) or rope.dim() != 3 or rope.shape[2] != 2:
         raise ValueError("rope must be float32 [positions, rot / 2, 2] (cosine, sine)")
-    _arg(rope, "rope", dtype=torch.float32)
-    return rope.shape[0], 2 * rope.shape[1]
+    if rope.dtype != torch.float32 or not rope.is_contiguous():
+        _arg(rope, "rope", dtype=torch.float32, device=False)
+    rows, half, _ = rope.shape
+    return _ints(positions, "positions", tokens), rope.data_ptr(), rows, 2 * half
 
 
 def _heads_out(out, like: torch.Tensor, name: str) -> torch.Tensor:
     if out is None:
-        return torch.empty(like.shape, dtype=like.dtype, device=like.device)
+        return torch.empty_like(like, memory_format=torch.contiguous_format)
     return _arg(out, name, shape=like.shape, dtype=like.dtype)
 
 
@@ -1086,24 +1111,17 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor | Non
     """(q_out, k_out): the RMS norm of every head of q [tokens, heads, dim] and k, with the weights given, then the
     rotation by rope[position] (see spl_qk_norm_rope).  rope: float32 [positions, rot / 2, 2], or None for none.  q and
     k may be slices of one fused product."""
-    L = lib()
     hq = _heads(q, "q")
     T, _, D = q.shape
     hk = _heads(k, "k", T, D, q.dtype)
-    rows, rot = _turn_args(T, D, q.dtype, positions, rope, q_weight, k_weight)
-    _on_device(q, "q")
-    _on_device(k, "k")
+    wq, wk = _weight(q_weight, "q_weight", D, q.dtype), _weight(k_weight, "k_weight", D, q.dtype)
+    at, angles, rows, rot = _turn_args(T, positions, rope)
+    _all_on_device(q=q, k=k, q_weight=q_weight, k_weight=k_weight, positions=positions, rope=rope)
     q_out, k_out = _heads_out(q_out, q, "q_out"), _heads_out(k_out, k, "k_out")
     _check("spl_qk_norm_rope",
-           L.spl_qk_norm_rope(ctypes.byref(hq), ctypes.byref(hk), T, D, _TORCH_DTYPE[q.dtype], _ptr(q_weight),
-                              _ptr(k_weight), eps, _ptr(positions) if rot else None, _ptr(rope), rows, rot,
-                              int(interleaved), _ptr(q_out), _ptr(k_out), _stream(stream)))
+           lib().spl_qk_norm_rope(hq, hk, T, D, _TORCH_DTYPE[q.dtype], wq, wk, eps, at, angles, rows, rot, interleaved,
+                                  q_out.data_ptr(), k_out.data_ptr(), _on(stream)))
     return q_out, k_out
-
-
-def _on_device(t: torch.Tensor, name: str) -> None:
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a device tensor")
 
 
 def qk_norm_rope_grad(dq: torch.Tensor, dk: torch.Tensor, q: torch.Tensor, k: torch.Tensor,
@@ -1115,15 +1133,15 @@ def qk_norm_rope_grad(dq: torch.Tensor, dk: torch.Tensor, q: torch.Tensor, k: to
     weights' are float32, None without a weight (see spl_qk_norm_rope_grad)."""
     L = lib()
     hq = _heads(q, "q")
-    T, _, D = q.shape
+    T, H, D = q.shape
     hk = _heads(k, "k", T, D, q.dtype)
     hdq, hdk = _heads(dq, "dq", T, D, q.dtype), _heads(dk, "dk", T, D, q.dtype)
-    if hdq.heads != hq.heads or hdk.heads != hk.heads:
+    if hdq.heads != H or hdk.heads != hk.heads:
         raise ValueError("a gradient has its input's heads")
-    rows, rot = _turn_args(T, D, q.dtype, positions, rope, q_weight, k_weight)
-    for t, nm in ((q, "q"), (k, "k"), (dq, "dq"), (dk, "dk")):
-        _on_device(t, nm)
-    need = L.spl_qk_norm_rope_grad_workspace_bytes(T, hq.heads, hk.heads, D)
+    wq, wk = _weight(q_weight, "q_weight", D, q.dtype), _weight(k_weight, "k_weight", D, q.dtype)
+    at, angles, rows, rot = _turn_args(T, positions, rope)
+    _all_on_device(q=q, k=k, dq=dq, dk=dk, q_weight=q_weight, k_weight=k_weight, positions=positions, rope=rope)
+    need = L.spl_qk_norm_rope_grad_workspace_bytes(T, H, hk.heads, D)
     if need < 0:
         raise ValueError("the workspace-size function rejected the shape")
     dq_out, dk_out = _heads_out(dq_out, q, "dq_out"), _heads_out(dk_out, k, "dk_out")
@@ -1131,10 +1149,9 @@ def qk_norm_rope_grad(dq: torch.Tensor, dk: torch.Tensor, q: torch.Tensor, k: to
                 for w in (q_weight, k_weight))
     ws = _workspace_on(need, q.device, stream) if need else None
     _check("spl_qk_norm_rope_grad",
-           L.spl_qk_norm_rope_grad(ctypes.byref(hdq), ctypes.byref(hdk), ctypes.byref(hq), ctypes.byref(hk), T, D,
-                                   _TORCH_DTYPE[q.dtype], _ptr(q_weight), _ptr(k_weight), eps,
-                                   _ptr(positions) if rot else None, _ptr(rope), rows, rot, int(interleaved),
-                                   _ptr(dq_out), _ptr(dk_out), _ptr(dwq), _ptr(dwk), _ptr(ws), _stream(stream)))
+           L.spl_qk_norm_rope_grad(hdq, hdk, hq, hk, T, D, _TORCH_DTYPE[q.dtype], wq, wk, eps, at, angles, rows, rot,
+                                   interleaved, dq_out.data_ptr(), dk_out.data_ptr(), _ptr(dwq), _ptr(dwk), _ptr(ws),
+                                   _on(stream)))
     return dq_out, dk_out, dwq, dwk
 
 
@@ -1145,35 +1162,37 @@ def qk_norm_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, posit
                         k_out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """q_out of qk_norm_rope; its keys and the values v go to `slots` of the cache in the same launch (and the keys to
     k_out, where given; see spl_qk_norm_rope_append)."""
-    L = lib()
-    hq = _heads(q, "q", None, cache.head_dim, cache.dtype)
-    T, _, D = q.shape
-    hk, hv = _heads(k, "k", T, D, q.dtype), _heads(v, "v", T, D, q.dtype)
-    if hk.heads != cache.heads or hv.heads != cache.heads:
-        raise ValueError(f"k and v have {hk.heads} and {hv.heads} heads, the cache has {cache.heads}")
-    _arg(slots, "slots", shape=(T,), dtype=torch.int32, device=False)
-    rows, rot = _turn_args(T, D, q.dtype, positions, rope, q_weight, k_weight)
-    for t, nm in ((q, "q"), (k, "k"), (v, "v"), (slots, "slots"), (cache.data, "the cache")):
-        _on_device(t, nm)
+    D, dtype, heads = cache.head_dim, cache.dtype, cache.heads
+    hq = _heads(q, "q", None, D, dtype)
+    T = q.shape[0]
+    hk, hv = _heads(k, "k", T, D, dtype), _heads(v, "v", T, D, dtype)
+    if hk.heads != heads or hv.heads != heads:
+        raise ValueError(f"k and v have {hk.heads} and {hv.heads} heads, the cache has {heads}")
+    to = _ints(slots, "slots", T)
+    wq, wk = _weight(q_weight, "q_weight", D, dtype), _weight(k_weight, "k_weight", D, dtype)
+    at, angles, rows, rot = _turn_args(T, positions, rope)
+    _all_on_device(q=q, k=k, v=v, slots=slots, cache=cache.data, q_weight=q_weight, k_weight=k_weight,
+                   positions=positions, rope=rope)
     q_out = _heads_out(q_out, q, "q_out")
     if k_out is not None:
         k_out = _heads_out(k_out, k, "k_out")
     _check("spl_qk_norm_rope_append",
-           L.spl_qk_norm_rope_append(ctypes.byref(hq), ctypes.byref(hk), ctypes.byref(hv), T, _ptr(q_weight),
-                                     _ptr(k_weight), eps, _ptr(positions) if rot else None, _ptr(rope), rows, rot,
-                                     int(interleaved), _ptr(slots), ctypes.byref(cache._view), _ptr(q_out),
-                                     _ptr(k_out), _stream(stream)))
+           lib().spl_qk_norm_rope_append(hq, hk, hv, T, wq, wk, eps, at, angles, rows, rot, interleaved, to,
+                                         cache._view, q_out.data_ptr(), _ptr(k_out), _on(stream)))
     return q_out
 
 
 def cache_read(cache: KVCache, slots: torch.Tensor, stream=None):
     """(keys, values) [tokens, heads, head_dim] that the cache holds at `slots` (see spl_cache_read)."""
-    _arg(slots, "slots", dtype=torch.int32, min_numel=0)
-    _on_device(cache.data, "the cache")
-    out = torch.empty((2, slots.shape[0], cache.heads, cache.head_dim), dtype=cache.dtype, device=slots.device)
-    _check("spl_cache_read", lib().spl_cache_read(ctypes.byref(cache._view), _ptr(slots), slots.shape[0],
-                                                  _ptr(out[0]), _ptr(out[1]), _stream(stream)))
-    return out[0], out[1]
+    if not isinstance(slots, torch.Tensor) or slots.dim() != 1:
+        raise ValueError("slots must be 1-D")
+    T = slots.shape[0]
+    at = _ints(slots, "slots", T)
+    _all_on_device(slots=slots, cache=cache.data)
+    k = torch.empty((T, cache.heads, cache.head_dim), dtype=cache.dtype, device=slots.device)
+    v = torch.empty_like(k)
+    _check("spl_cache_read", lib().spl_cache_read(cache._view, at, T, k.data_ptr(), v.data_ptr(), _on(stream)))
+    return k, v
 
 
 def attention_fp4(q: torch.Tensor, cache: KVCache, table: torch.Tensor, lens: torch.Tensor, row_start: torch.Tensor,
@@ -1183,37 +1202,23 @@ def attention_fp4(q: torch.Tensor, cache: KVCache, table: torch.Tensor, lens: to
     width] lists (see spl_attention_fp4).  `row_start` [requests + 1] and `lens` [requests] are those of block_tables;
     scale is 1 / sqrt(head_dim) unless given.  max_new (the most rows of a request) and max_len (about the most tokens)
     let the call choose its launch without asking the GPU.  lse: float32 [tokens, heads], written if given."""
-    L = lib()
-    hq = _heads(q, "q", None, cache.head_dim, cache.dtype)
-    T, H, D = q.shape
+    L, D, view = lib(), cache.head_dim, cache._view
+    hq = _heads(q, "q", None, D, cache.dtype)
+    T, H, _ = q.shape
     if H % cache.heads:
         raise ValueError(f"q has {H} heads, not a multiple of the cache's {cache.heads}")
-    if not isinstance(table, torch.Tensor) or table.dim() != 2:
-        raise ValueError("table must be [requests, width]")
-    R, width = table.shape
-    _arg(table, "table", dtype=torch.int32, device=False)
-    _arg(lens, "lens", shape=(R,), dtype=torch.int32, device=False)
-    _arg(row_start, "row_start", shape=(R + 1,), dtype=torch.int32, device=False)
+    R, width = _table(table)
+    ends, starts = _ints(lens, "lens", R), _ints(row_start, "row_start", R + 1)
     if lse is not None:
         _arg(lse, "lse", shape=(T, H), dtype=torch.float32, device=False)
-    for t, nm in ((q, "q"), (cache.data, "the cache"), (table, "table"), (lens, "lens"), (row_start, "row_start")):
-        _on_device(t, nm)
+    _all_on_device(q=q, cache=cache.data, table=table, lens=lens, row_start=row_start, lse=lse)
     out = _heads_out(out, q, "out")
-    view = ctypes.byref(cache._view)
     need = L.spl_attention_fp4_workspace_bytes(view, T, H, R, width, max_new, max_len)
     if need < 0:
         raise ValueError("spl_attention_fp4_workspace_bytes rejected the arguments")
     ws = _workspace_on(need, q.device, stream) if need else None
     _check("spl_attention_fp4",
-           L.spl_attention_fp4(ctypes.byref(hq), T, view, _ptr(table), R, width, _ptr(lens), _ptr(row_start), max_new,
-                               max_len, D ** -0.5 if scale is None else scale, window, _ptr(out), _ptr(lse), _ptr(ws),
-                               _stream(stream)))
+           L.spl_attention_fp4(hq, T, view, table.data_ptr(), R, width, ends, starts, max_new, max_len,
+                               D ** -0.5 if scale is None else scale, window, out.data_ptr(), _ptr(lse), _ptr(ws),
+                               _on(stream)))
     return out
-
-
-def _workspace_on(need: int, device, stream) -> torch.Tensor:
-    """As _scratch, for a call that cannot do without."""
-    ws = _scratch(need, device, stream)
-    if ws is None:
-        raise torch.OutOfMemoryError(f"no {need} bytes of workspace")
-    return ws

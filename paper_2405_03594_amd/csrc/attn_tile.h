@@ -61,6 +61,22 @@ __device__ __forceinline__ uint32_t pack2(F16, float a, float b) {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// A wave-uniform load through the scalar cache (the memory is not written by
+// the kernel).
+__device__ __forceinline__ int32_t uniform_load(const int32_t* p) {
+  return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>((uintptr_t)p);
+}
+
+// Maximum over the four lanes that share lane % 16.
+__device__ __forceinline__ float quad_max(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const uint32_t v = __float_as_uint(x);
+  const auto b = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
 // Row indexes of a request, clamped to the call's rows, and its length.
 struct Rows {
   int64_t first;
@@ -68,7 +84,7 @@ struct Rows {
 };
 __device__ __forceinline__ Rows rows_of(const AttnArgs& a, int64_t r) {
   const int64_t t = a.tokens;
-  int64_t s = a.row_start[r], e = a.row_start[r + 1];
+  int64_t s = a.row_start[r], e = a.row_start[r + 1];    // lane by lane: requests may differ
   s = s < 0 ? 0 : (s > t ? t : s);
   e = e < s ? s : (e > t ? t : e);
   const int64_t most = a.width * (int64_t)a.cache.page;

@@ -30,6 +30,9 @@ using spl::u32x4;
 constexpr int kRows = 16;
 constexpr int kStep = 32;
 constexpr int kWaves = 4;
+constexpr int kGroupsPerCu = 2;
+constexpr int kMaxSplits = 64;
+constexpr int kMinChunk = 16;
 
 template <int D>
 struct Geom {
@@ -49,17 +52,17 @@ struct Raw {
   uint32_t vs[2];
 };
 
+// Page numbers of the step's two halves of 16 tokens; -1: none there.
 struct Where {
-  int64_t page[2];                               // of the step's two halves; -1: none
+  int32_t page[2];
 };
 
-template <int D>
 __device__ __forceinline__ Where where(const AttnArgs& a, const int32_t* table, int32_t t0, int32_t len, int shift) {
   Where w;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int32_t t = t0 + 16 * h;
-    const int64_t p = t < len ? table[t >> shift] : -1;
+    const int32_t p = t < len ? spl::uniform_load(table + (t >> shift)) : -1;
     w.page[h] = p >= 0 && p < a.cache.pages ? p : -1;
   }
   return w;
@@ -86,45 +89,102 @@ __device__ __forceinline__ void load_words(uint32_t* d, const uint8_t* p) {
   }
 }
 
-// The lane's data of the step at t0: the key of token 8 (m / 4) + m % 4 and of
-// the one four further (m = lane % 16), of every group the 8 channels j = lane
-// / 16; the values of tokens 8 j .. 8 j + 7, unit lane % 16.  A page that does
-// not exist reads page 0 instead (its tokens are masked).
+// The tokens of a step that lane / 16 = j holds, i = 0 .. 7 in the order of the
+// matrix instruction's depth.  They are chosen so that each load instruction of
+// a wave covers whole lines: 16 bytes a lane, 1 KB in a row.
+template <int D>
+__device__ __forceinline__ int token_of(int j, int i) {
+  constexpr int U = Geom<D>::U;
+  if (U == 4) return 8 * j + i;
+  if (U == 8) return (i & 3) + 4 * j + 16 * (i >> 2);
+  return (i & 1) + 2 * j + 8 * (i >> 1);
+}
+
+// Where a lane's data lie in a region, for half a step at the region's start:
+// the key of the half's row m = lane % 16 (token_of(m / 4, m % 4), and 16
+// further in the second half), of every group the 8 channels j = lane / 16; the
+// values of unit m.  With 64 channels the halves' rows lie 8 j apart instead,
+// so that a lane's 8 values are one piece of 16 bytes, and a step is loaded as
+// one.
+struct LaneOff {
+  uint32_t k, ks, v, vs;
+};
+template <int D>
+__device__ __forceinline__ LaneOff lane_off(int page, int lane) {
+  using Gm = Geom<D>;
+  const int m = lane & 15, j = lane >> 4, u = m < Gm::kUnits ? m : Gm::kUnits - 1;
+  LaneOff o;
+  const int b = token_of<D>(m >> 2, m & 3) & (page - 1);
+  o.k = b * (D / 2) + 4 * Gm::G * j;
+  o.ks = page * D + b * Gm::S;
+  o.v = page * (D / 2);
+  o.vs = page * (D + Gm::S) + u * Gm::U / 32 * 8;
+  if (Gm::U == 4) {
+    const int b8 = ((8 * j) & (page - 1)) >> 3;
+    o.v += (b8 * Gm::kUnits + u) * 16;
+    o.vs += b8 * Gm::S * 8;
+  } else if (Gm::U == 8) {
+    o.v += ((j >> 1) * Gm::kUnits + u) * 32 + (j & 1) * 16;
+    o.vs += (j >> 1) * Gm::S * 8 + (j & 1) * 4;
+  } else {
+    o.v += u * 64 + j * 16;
+    o.vs += 2 * j;
+  }
+  return o;
+}
+
+template <int D>
+__device__ __forceinline__ void load_scales(uint32_t* d, const uint8_t* p) {
+  if constexpr (Geom<D>::S == 2) d[0] = *reinterpret_cast<const uint16_t*>(p);
+  else load_words<Geom<D>::S / 4>(d, p);
+}
+
+// The step at t0 (a multiple of 32).  A page that does not exist reads page 0
+// instead (its tokens are masked).
 template <int D>
 __device__ __forceinline__ void load_step(Raw<D>& r, const AttnArgs& a, int head, int32_t t0, const Where& w,
-                                          int lane) {
+                                          const LaneOff& o, int lane) {
   using Gm = Geom<D>;
   const int page = a.cache.page, bytes = page * (D + 2 * Gm::S);
-  const int m = lane & 15, j = lane >> 4;
   const uint8_t* base = static_cast<const uint8_t*>(a.cache.data);
-  const auto region = [&](int64_t p) { return base + ((p < 0 ? 0 : p) * a.cache.heads + head) * (int64_t)bytes; };
-  const uint8_t* r0 = region(w.page[0]);
-  const uint8_t* r1 = region(w.page[1]);
-  const int off = (t0 & (page - 1));
-  {
-    const uint8_t* rk = m < 8 ? r0 : r1;
-    const int b = ((off + 8 * (m >> 2)) & (page - 1)) + (m & 3);
-    const uint8_t* p = rk + b * (D / 2) + 4 * Gm::G * j;
-    const uint8_t* s = rk + page * D + b * Gm::S;
-    load_words<Gm::G>(r.k[0], p);
-    load_words<Gm::G>(r.k[1], p + 4 * (D / 2));
-    if constexpr (Gm::S == 2) {
-      r.ks[0][0] = *reinterpret_cast<const uint16_t*>(s);
-      r.ks[1][0] = *reinterpret_cast<const uint16_t*>(s + 4 * Gm::S);
-    } else {
-      load_words<Gm::S / 4>(r.ks[0], s);
-      load_words<Gm::S / 4>(r.ks[1], s + 4 * Gm::S);
+  const auto region = [&](int32_t p) {
+    return base + ((int64_t)(p < 0 ? 0 : p) * a.cache.heads + head) * (int64_t)bytes;
+  };
+  if constexpr (Gm::U == 4) {
+    const int off = t0 & (page - 1);
+    const uint8_t *c = region(w.page[0]) + off * (D / 2), *s = region(w.page[0]) + off * Gm::S, *cv = c, *sv = s;
+    if (page == 16) {                            // the second half is in another page
+      const uint8_t* r1 = region(w.page[1]);
+      cv = lane >= 32 ? r1 : c, sv = lane >= 32 ? r1 : s;
+      if (lane & 8) c = s = r1;
     }
-  }
-  {
-    const uint8_t* rv = j < 2 ? r0 : r1;
-    const int b8 = ((off + 8 * j) & (page - 1)) >> 3, u = m < Gm::kUnits ? m : Gm::kUnits - 1;
-    load_words<Gm::VD>(r.v, rv + page * (D / 2) + (b8 * Gm::kUnits + u) * (4 * Gm::U));
-    load_words<2>(r.vs, rv + page * (D + Gm::S) + (b8 * Gm::S + u * Gm::U / 32) * 8);
+    load_words<Gm::G>(r.k[0], c + o.k);
+    load_words<Gm::G>(r.k[1], c + (o.k + 2 * D));
+    load_scales<D>(r.ks[0], s + o.ks);
+    load_scales<D>(r.ks[1], s + (o.ks + 4 * Gm::S));
+    load_words<Gm::VD>(r.v, cv + o.v);
+    load_words<2>(r.vs, sv + o.vs);
+  } else {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int off = (t0 + 16 * h) & (page - 1);
+      const uint8_t *c = region(w.page[h]) + off * (D / 2), *s = region(w.page[h]) + off * Gm::S;
+      load_words<Gm::G>(r.k[h], c + o.k);
+      load_scales<D>(r.ks[h], s + o.ks);
+      if constexpr (Gm::U == 8) {
+        load_words<4>(r.v + 4 * h, c + o.v);
+        load_words<1>(r.vs + h, s + o.vs);
+      } else {
+        load_words<4>(r.v + 8 * h, c + o.v);
+        load_words<4>(r.v + 8 * h + 4, c + (o.v + 1024));
+        r.vs[h] = *reinterpret_cast<const uint16_t*>(s + o.vs) |
+                  ((uint32_t)*reinterpret_cast<const uint16_t*>(s + (o.vs + 8 * Gm::S)) << 16);
+      }
+    }
   }
 }
 
-// S^T of the step: s[i] is token 8 j + i against the lane's query row.
+// S^T of the step: s[i] is token token_of(j, i) against the lane's query row.
 template <class T, int D>
 __device__ __forceinline__ void scores(const Raw<D>& r, const u32x4* q, float* s) {
 #pragma unroll
@@ -160,11 +220,18 @@ __device__ __forceinline__ void value_pair(const Raw<D>& r, int c, u32x4& even, 
   }
 }
 
-// The state of a tile's softmax: per lane the row's maximum (times log2 e) and
-// the sum over the lane's tokens; o[n] channels U (4 j + i) + n of the row.
+// The state of a tile's softmax: per lane the row's reference m, with mc = c m;
+// l (four times the same) the sum of the weights 2^(c (s - m)) as they meet the
+// values, rounded, so that what a rounding adds to a weight it adds to the sum
+// too; o[n] channels U (4 j + i) + n of the row.  l is a row of ones among the
+// values: a matrix instruction adds it up.  m is a maximum of the scores so far,
+// but moves only when one passes it by kSlack: until then the weights are at
+// most 2^kSlack, and keep their 8 or 11 bits at any size.
+constexpr float kSlack = 8.0f;
 template <int D>
 struct State {
-  float m, l;
+  float m, mc;
+  f32x4 l;
   f32x4 o[Geom<D>::U];
 };
 
@@ -183,16 +250,15 @@ __device__ __forceinline__ void step(State<D>& st, Raw<D>& r, const u32x4* q, co
                      (v.window == 0 || t0 > v.high - v.window);
   float s[8];
   scores<T, D>(r, q, s);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) s[i] *= c;
   uint32_t poison = 0;                           // groups of 32 channels in which the row sees a NaN (rare)
   if (!whole) {
-    const bool held = (j < 2 ? w.page[0] : w.page[1]) >= 0;
-    const int32_t t = t0 + 8 * j;
     uint32_t seen = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const bool see = held && t + i < len && t + i <= v.pos && (v.window == 0 || t + i > v.pos - v.window);
+      const int at = token_of<D>(j, i);
+      const int32_t t = t0 + at;
+      const bool see = (at < 16 ? w.page[0] : w.page[1]) >= 0 && t < len && t <= v.pos &&
+                       (v.window == 0 || t > v.pos - v.window);
       seen |= see ? 1u << i : 0u;
       s[i] = see ? s[i] : -INFINITY;
     }
@@ -207,7 +273,7 @@ __device__ __forceinline__ void step(State<D>& st, Raw<D>& r, const u32x4* q, co
       for (int i = 0; i < 8; ++i)
         if (bad >> i & 1) r.vs[i / 4] = (r.vs[i / 4] & ~(0xffu << (8 * (i % 4)))) | (127u << (8 * (i % 4)));
       for (int g = 0; g < Gm::G; ++g) {
-        const int from = (lane & 48) + g * 32 / Gm::U;           // a lane of this block of tokens that holds group g
+        const int from = (lane & 48) + g * 32 / Gm::U;           // a lane of the same tokens that holds group g
         const uint32_t b = __shfl(bad, from);
         if (b & seen) poison |= 1u << g;
       }
@@ -215,29 +281,26 @@ __device__ __forceinline__ void step(State<D>& st, Raw<D>& r, const u32x4* q, co
       poison |= __shfl_xor(poison, 32);
     }
   }
-  float top = s[0];
-#pragma unroll
-  for (int i = 1; i < 8; ++i) top = fmaxf(top, s[i]);
-  top = fmaxf(top, __shfl_xor(top, 16));
-  top = fmaxf(top, __shfl_xor(top, 32));
-  const float m = fmaxf(st.m, top);
-  if (__ballot(m != st.m)) {
-    const float alpha = m == -INFINITY ? 1.0f : spl::exp2_fast(st.m - m);
+  const float top = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+  if (__ballot(top * c > st.mc + kSlack)) {
+    const float m = fmaxf(st.m, spl::quad_max(top));
+    const float mc = m == -INFINITY ? -INFINITY : m * c;
+    const float alpha = m == -INFINITY ? 1.0f : spl::exp2_fast(st.mc - mc);
     st.l *= alpha;
 #pragma unroll
     for (int n = 0; n < Gm::U; ++n) st.o[n] *= alpha;
     st.m = m;
+    st.mc = mc;
   }
-  const float base = m == -INFINITY ? 0.0f : m;
+  const float base = st.m == -INFINITY ? 0.0f : -st.mc;
   float p[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    p[i] = spl::exp2_fast(s[i] - base);
-    st.l += p[i];
-  }
+  for (int i = 0; i < 8; ++i) p[i] = spl::exp2_fast(__builtin_fmaf(s[i], c, base));
   u32x4 pf;
 #pragma unroll
   for (int i = 0; i < 4; ++i) pf[i] = spl::pack2(T{}, p[2 * i], p[2 * i + 1]);
+  constexpr uint32_t kOne = T::code == SPL_F16 ? 0x3c003c00u : 0x3f803f80u;
+  st.l = spl::mfma16(T{}, u32x4{kOne, kOne, kOne, kOne}, pf, st.l);
 #pragma unroll
   for (int n = 0; n < Gm::U; n += 2) {
     u32x4 even, odd;
@@ -254,39 +317,98 @@ __device__ __forceinline__ void step(State<D>& st, Raw<D>& r, const u32x4* q, co
   }
 }
 
+// The steps that any row of the tile at row0 sees, and a split's share of them:
+// chunk of them, more where the splits would not reach the end.
+struct TileSteps {
+  int32_t low, high;                             // positions of the tile's first and last row
+  int32_t s0, steps, share;
+};
+__device__ __forceinline__ TileSteps tile_steps(const AttnArgs& a, const spl::Rows& rows, int32_t row0, int32_t all,
+                                                int group, int splits, int chunk) {
+  TileSteps t;
+  const int32_t last = (all - row0 < kRows ? all : row0 + kRows) - 1;
+  const int32_t first_pos = rows.len - rows.count;
+  t.low = first_pos + row0 / group;
+  t.high = first_pos + last / group;
+  const int32_t end = t.high + 1 < rows.len ? t.high + 1 : rows.len;
+  const int32_t begin = a.window > 0 && t.low - a.window + 1 > 0 ? t.low - a.window + 1 : 0;
+  t.s0 = begin / kStep;
+  t.steps = end > begin ? (end + kStep - 1) / kStep - t.s0 : 0;
+  const int32_t least = (t.steps + splits - 1) / splits;
+  t.share = chunk > least ? chunk : least;
+  return t;
+}
+
+// The request that place `at` of the launch serves when the workgroups of
+// `round` requests go to the chip's CUs in each round: the longest first, every
+// other round backwards, so that what a CU gets in two rounds is alike.
+// Requests up to 32: each lane ranks one.
+__device__ __forceinline__ int64_t ranked_request(const AttnArgs& a, int at, int round) {
+  const int lane = spl::lane_id(), n = (int)a.requests;
+  const int32_t len = lane < n ? a.lens[lane] : 0;
+  int rank = 0;
+  for (int i = 0; i < n; ++i) {
+    const int32_t other = __builtin_amdgcn_readlane(len, i);
+    rank += other > len || (other == len && i < lane) ? 1 : 0;
+  }
+  const int first = at / round * round, size = n - first < round ? n - first : round;
+  const int want = at / round & 1 ? 2 * first + size - 1 - at : at;
+  const uint64_t who = __ballot(lane < n && rank == want);
+  return who ? __builtin_ctzll(who) : -1;
+}
+
+// The workspace of split calls: per row and split the sums and (reference times
+// log2 e, weight), per row the splits that hold any of it.
+struct Parts {
+  float* sums;
+  float* stats;
+  int32_t* counts;
+};
+template <int D>
+__device__ __forceinline__ Parts parts_of(const AttnArgs& a, int splits) {
+  const int64_t n = a.tokens * a.q.heads * splits;
+  float* w = static_cast<float*>(a.workspace);
+  return {w, w + n * D, reinterpret_cast<int32_t*>(w + n * (D + 2))};
+}
+
 // One workgroup: a tile of rows, a key head, one of the splits of its tokens.
 // The four waves take every fourth step and are joined through LDS.
 template <class T, int D>
-__global__ __launch_bounds__(kWaves * 64) void k_attn_rows(AttnArgs a, int group, int direct, int splits) {
+__global__ __launch_bounds__(kWaves * 64, D == 256 ? 2 : 3) void k_attn_rows(AttnArgs a, int group, int direct,
+                                                                            int splits, int chunk, int snake) {
   using Gm = Geom<D>;
   __shared__ float o_s[2][Gm::U * 4][64];
   __shared__ float m_s[kWaves][kRows], l_s[kWaves][kRows];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int head = blockIdx.y, split = blockIdx.z;
-  spl::Tile tile{(int64_t)blockIdx.x, 0};
-  if (!direct) tile = spl::find_tile(a, group, kRows, blockIdx.x);
+  // heads fastest: consecutive workgroups go to different XCDs, so each has a
+  // share of every request, however their lengths differ
+  const int head = blockIdx.x, split = blockIdx.z;
+  spl::Tile tile{(int64_t)blockIdx.y, 0};
+  if (!direct) tile = spl::find_tile(a, group, kRows, blockIdx.y);
+  else if (snake > 0) tile.request = ranked_request(a, blockIdx.y, snake);
   const int64_t req = __builtin_amdgcn_readfirstlane((int)tile.request);
   if (req < 0) return;
-  const spl::Rows rows = spl::rows_of(a, req);
-  const int64_t row0 = tile.index * kRows, all = (int64_t)rows.count * group;
+  spl::Rows rows = spl::rows_of(a, req);
+  rows.first = __builtin_amdgcn_readfirstlane((int)rows.first);
+  rows.count = __builtin_amdgcn_readfirstlane(rows.count);
+  rows.len = __builtin_amdgcn_readfirstlane(rows.len);
+  const int32_t row0 = __builtin_amdgcn_readfirstlane((int)tile.index) * kRows, all = rows.count * group;
   if (row0 >= all) return;
-  const int n = (int)(all - row0 < kRows ? all - row0 : kRows);            // rows of this tile
+  const int n = all - row0 < kRows ? all - row0 : kRows;                   // rows of this tile
   const int m16 = lane & 15, j = lane >> 4;
   const int32_t first_pos = rows.len - rows.count;
-  const int64_t row = row0 + (m16 < n ? m16 : n - 1);
-  const int32_t tok = (int32_t)(row / group);
-  const int64_t t_row = rows.first + tok, h_row = head * group + (row - (int64_t)tok * group);
+  const int32_t row = row0 + (m16 < n ? m16 : n - 1), tok = row / group;
+  const int64_t t_row = rows.first + tok, h_row = head * group + (row - tok * group);
+  const TileSteps ts = tile_steps(a, rows, row0, all, group, splits, chunk);
+  const int32_t s0 = ts.s0, from = split * ts.share;
+  const int32_t to = from + ts.share < ts.steps ? from + ts.share : ts.steps;
+  const bool only = ts.steps <= ts.share;        // the tile is one split's
+  if (split > 0 && from >= ts.steps) return;
   RowView view;
   view.pos = m16 < n ? first_pos + tok : -1;
-  view.low = first_pos + (int32_t)(row0 / group);
-  view.high = first_pos + (int32_t)((row0 + n - 1) / group);
+  view.low = ts.low;
+  view.high = ts.high;
   view.window = a.window;
-  // the steps that any row of the tile sees, and this split's share of them
-  const int32_t end = view.high + 1 < rows.len ? view.high + 1 : rows.len;
-  const int32_t begin = a.window > 0 && view.low - a.window + 1 > 0 ? view.low - a.window + 1 : 0;
-  const int32_t s0 = begin / kStep, steps = end > begin ? (end + kStep - 1) / kStep - s0 : 0;
-  const int32_t share = (steps + splits - 1) / splits;
-  const int32_t from = split * share, to = from + share < steps ? from + share : steps;
   const int32_t* table = a.table + req * a.width;
   const int shift = __builtin_ctz((unsigned)a.cache.page);
 
@@ -296,33 +418,45 @@ __global__ __launch_bounds__(kWaves * 64) void k_attn_rows(AttnArgs a, int group
 #pragma unroll
     for (int g = 0; g < Gm::G; ++g) q[g] = *reinterpret_cast<const u32x4*>(at + 32 * g + 8 * j);
   }
+  // the scores' factor is taken positive: its sign goes to q, and 0 makes all scores 0
+  float c = fabsf(a.scale) * spl::kLog2e;
+  const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u, keep = c > 0.0f ? 0xffffffffu : 0u;
+#pragma unroll
+  for (int g = 0; g < Gm::G; ++g) q[g] = (q[g] ^ flip) & keep;
+  c = c > 0.0f ? c : 1.0f;
   State<D> st;
-  st.m = -INFINITY;
-  st.l = 0;
+  st.m = st.mc = -INFINITY;
+  st.l = f32x4{0, 0, 0, 0};
 #pragma unroll
   for (int i = 0; i < Gm::U; ++i) st.o[i] = f32x4{0, 0, 0, 0};
-  const float c = a.scale * spl::kLog2e;
+  const LaneOff off = lane_off<D>(a.cache.page, lane);
 
   int32_t i = from + wave;
   if (i < to) {
-    Raw<D> cur;
-    Where w = where<D>(a, table, (s0 + i) * kStep, rows.len, shift);
-    load_step<D>(cur, a, head, (s0 + i) * kStep, w, lane);
-    for (; i < to; i += kWaves) {
-      const int32_t next = i + kWaves < to ? i + kWaves : i;
-      const Where wn = where<D>(a, table, (s0 + next) * kStep, rows.len, shift);
-      Raw<D> ahead;
-      load_step<D>(ahead, a, head, (s0 + next) * kStep, wn, lane);
-      step<T, D>(st, cur, q, view, (s0 + i) * kStep, w, rows.len, c, lane);
-      cur = ahead;
-      w = wn;
+    // the next step's data are requested before this one's are used (two steps ahead gained nothing)
+    Raw<D> r0, r1;
+    Where w0, w1;
+    const auto fetch = [&](Raw<D>& r, Where& w, int32_t k) {
+      k = k < to ? k : i;
+      w = where(a, table, (s0 + k) * kStep, rows.len, shift);
+      load_step<D>(r, a, head, (s0 + k) * kStep, w, off, lane);
+    };
+    fetch(r0, w0, i);
+    const auto turn = [&](Raw<D>& now, Where& wn, Raw<D>& ahead, Where& wa) {
+      fetch(ahead, wa, i + kWaves);
+      step<T, D>(st, now, q, view, (s0 + i) * kStep, wn, rows.len, c, lane);
+      i += kWaves;
+    };
+    while (true) {
+      turn(r0, w0, r1, w1);
+      if (i >= to) break;
+      turn(r1, w1, r0, w0);
+      if (i >= to) break;
     }
   }
 
   // join the waves
-  st.l += __shfl_xor(st.l, 16);
-  st.l += __shfl_xor(st.l, 32);
-  if (lane < kRows) m_s[wave][lane] = st.m, l_s[wave][lane] = st.l;
+  if (lane < kRows) m_s[wave][lane] = st.mc, l_s[wave][lane] = st.l[0];
   __syncthreads();
   float top = m_s[0][m16];
 #pragma unroll
@@ -331,7 +465,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_attn_rows(AttnArgs a, int group
   float total = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) total += l_s[w][m16] * weight(m_s[w][m16]);
-  const float mine = weight(st.m);
+  const float mine = weight(st.mc);
 #pragma unroll
   for (int k = 0; k < Gm::U; ++k) st.o[k] *= mine;
   const auto give = [&](int buf) {
@@ -357,12 +491,12 @@ __global__ __launch_bounds__(kWaves * 64) void k_attn_rows(AttnArgs a, int group
   if (m16 >= n) return;
 
   const int64_t out_row = t_row * a.q.heads + h_row;
-  if (splits > 1) {
-    float* part = static_cast<float*>(a.workspace);
-    const int64_t all_rows = a.tokens * a.q.heads;
+  const Parts w = parts_of<D>(a, splits);
+  if (splits > 1 && split == 0 && j == 1) w.counts[out_row] = only ? 1 : (ts.steps + ts.share - 1) / ts.share;
+  if (!only) {
     const int64_t at = out_row * splits + split;
-    float* stats = part + all_rows * splits * D;
-    if (j == 0) stats[2 * at] = top, stats[2 * at + 1] = total;
+    float* part = w.sums;
+    if (j == 0) w.stats[2 * at] = top, w.stats[2 * at + 1] = total;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int ch = Gm::U * (4 * j + e);
@@ -391,48 +525,66 @@ __global__ __launch_bounds__(kWaves * 64) void k_attn_rows(AttnArgs a, int group
   if (a.lse && j == 0) a.lse[out_row] = total == 0.0f ? -INFINITY : (top + log2f(total)) * 0.6931471805599453f;
 }
 
-// The splits of a row joined: one wave a row, D / 64 channels a lane.
+// The splits of a row joined: a workgroup a row, its eight waves sharing the
+// splits, D / 64 channels a lane.  A lane knows the statistics of one split.
+// Loads go out in two rounds: the counts and statistics, then all sums.
+constexpr int kJoinWaves = 8;
 template <class T, int D>
-__global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, int splits) {
+__global__ __launch_bounds__(kJoinWaves * 64) void k_attn_join(AttnArgs a, int splits) {
   constexpr int C = D == 256 ? 4 : 2;                            // channels of a lane; D 64 and 96 leave lanes idle
-  const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), rows = a.tokens * a.q.heads;
-  if (row >= rows) return;
-  // rows that no request owns have no partial results
-  const int64_t t = row / a.q.heads;
-  const int64_t t0 = a.row_start[0], t1 = a.row_start[a.requests];
-  if (t < t0 || t >= t1) return;
-  const float* part = static_cast<const float*>(a.workspace);
-  const float* stats = part + rows * splits * D + 2 * row * splits;
-  float top = -INFINITY;
-  for (int s = lane; s < splits; s += 64) top = fmaxf(top, stats[2 * s]);
-  for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-  float total = 0, o[C];
-#pragma unroll
-  for (int k = 0; k < C; ++k) o[k] = 0;
+  typedef float vec __attribute__((ext_vector_type(C)));
+  __shared__ vec o_s[kJoinWaves - 1][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t row = blockIdx.x;
+  const Parts p = parts_of<D>(a, splits);
+  const int32_t t = (int32_t)blockIdx.x / a.q.heads;             // tokens * heads < 2^31
+  const int32_t t0 = a.row_start[0], t1 = a.row_start[a.requests];
+  int n = __builtin_amdgcn_readfirstlane(p.counts[row]);
+  const float* st = p.stats + 2 * (row * splits + (lane < splits ? lane : 0));
+  float m = st[0], l = st[1];
+  if (t < t0 || t >= t1 || n <= 1) return;                       // no request's, or written by its one split
+  n = n < splits ? n : splits;
+  m = lane < n ? m : -INFINITY;
+  l = lane < n ? l : 0.0f;
   const int ch = lane * C;
-  for (int s = 0; s < splits; ++s) {
-    const float m = stats[2 * s], l = stats[2 * s + 1];
-    if (m == -INFINITY && l == 0.0f) continue;                   // saw no key
-    const float w = spl::exp2_fast(m - top);
-    total += l * w;
-    if (ch < D) {
+  const float* part = p.sums + row * splits * D + (ch < D ? ch : 0);
+  vec x[kMaxSplits / kJoinWaves];
 #pragma unroll
-      for (int k = 0; k < C; ++k) o[k] += w * part[(row * splits + s) * D + ch + k];
+  for (int i = 0; i < kMaxSplits / kJoinWaves; ++i) {
+    const int s = wave + i * kJoinWaves;
+    if (i * kJoinWaves < n) x[i] = *reinterpret_cast<const vec*>(part + (int64_t)(s < n ? s : 0) * D);
+  }
+  float top = m;
+  for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+  const float w = m == -INFINITY && l == 0.0f ? 0.0f : spl::exp2_fast(m - top);          // saw no key: 0
+  float total = l * w;
+  for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d);
+  vec o = 0;
+#pragma unroll
+  for (int i = 0; i < kMaxSplits / kJoinWaves; ++i) {
+    const int s = wave + i * kJoinWaves;
+    if (s < n) {
+      const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s));
+      if (ws != 0.0f) o += ws * x[i];                            // the sums of a split that saw no key are 0
     }
   }
-  const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+  if (wave > 0) o_s[wave - 1][lane] = o;
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int k = 0; k < kJoinWaves - 1; ++k) o += o_s[k][lane];
+  o *= total == 0.0f ? 0.0f : 1.0f / total;
   if (ch < D) {
     uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + row * D + ch);
 #pragma unroll
-    for (int k = 0; k < C; k += 2) out[k / 2] = spl::pack2(T{}, o[k] * inv, o[k + 1] * inv);
+    for (int k = 0; k < C; k += 2) out[k / 2] = spl::pack2(T{}, o[k], o[k + 1]);
   }
   if (a.lse && lane == 0) a.lse[row] = total == 0.0f ? -INFINITY : (top + log2f(total)) * 0.6931471805599453f;
 }
 
 struct Plan {
   int64_t tiles;
-  int group, direct, splits;
+  int group, direct, splits, chunk, snake;
 };
 
 Plan plan_of(const AttnArgs& a) {
@@ -441,31 +593,34 @@ Plan plan_of(const AttnArgs& a) {
   p.direct = a.max_new > 0 && a.max_new * p.group <= kRows;
   const int64_t most = a.tokens * (int64_t)p.group / kRows + a.requests;
   p.tiles = p.direct ? a.requests : (most < a.tokens * p.group ? most : a.tokens * p.group);
-  // split the tokens while the launch has fewer workgroups than the chip takes
+  // split the tokens into chunks while the launch has fewer workgroups than the chip takes
   int64_t len = a.width * (int64_t)a.cache.page;
   if (a.max_len > 0 && a.max_len < len) len = a.max_len;
   if (a.window > 0) {
     const int64_t seen = a.window + (a.max_new > 0 && a.max_new < kRows ? a.max_new : kRows);
     len = len < seen ? len : seen;
   }
-  const int64_t groups = p.tiles * a.cache.heads, want = 4 * (int64_t)spl::device_cus();
+  const int64_t groups = p.tiles * a.cache.heads, want = kGroupsPerCu * (int64_t)spl::device_cus();
   const int64_t steps = (len + kStep - 1) / kStep;
   int64_t s = (want + groups - 1) / groups;
-  const int64_t most_s = (steps + 2 * kWaves - 1) / (2 * kWaves);
-  s = s < most_s ? s : most_s;
-  s = s < 1 ? 1 : (s > 256 ? 256 : s);
-  p.splits = (int)s;
+  s = s < 1 ? 1 : (s > kMaxSplits ? kMaxSplits : s);
+  int64_t chunk = (steps + s - 1) / s;
+  chunk = chunk < kMinChunk ? kMinChunk : chunk;
+  chunk = (chunk + kWaves - 1) / kWaves * kWaves;
+  p.chunk = (int)chunk;
+  p.splits = (int)((steps + chunk - 1) / chunk);
+  // several requests of unknown lengths, and more workgroups than CUs
+  const int64_t round = spl::device_cus() / a.cache.heads;
+  p.snake = p.direct && a.requests <= 32 && round >= 1 && a.requests > round ? (int)round : 0;
   return p;
 }
 
 template <class T, int D>
 hipError_t run(const AttnArgs& a, const Plan& p, hipStream_t s) {
-  const dim3 grid((unsigned)p.tiles, (unsigned)a.cache.heads, (unsigned)p.splits);
-  k_attn_rows<T, D><<<grid, kWaves * 64, 0, s>>>(a, p.group, p.direct, p.splits);
-  if (p.splits > 1) {
-    const int64_t rows = a.tokens * a.q.heads;
-    k_attn_join<T, D><<<dim3((unsigned)((rows + 3) / 4)), 256, 0, s>>>(a, p.splits);
-  }
+  const dim3 grid((unsigned)a.cache.heads, (unsigned)p.tiles, (unsigned)p.splits);
+  k_attn_rows<T, D><<<grid, kWaves * 64, 0, s>>>(a, p.group, p.direct, p.splits, p.chunk, p.snake);
+  if (p.splits > 1)
+    k_attn_join<T, D><<<dim3((unsigned)(a.tokens * a.q.heads)), kJoinWaves * 64, 0, s>>>(a, p.splits);
   return hipGetLastError();
 }
 
@@ -486,7 +641,7 @@ namespace spl {
 int64_t attn_workspace_bytes(const AttnArgs& a) {
   const Plan p = plan_of(a);
   if (p.splits == 1) return 0;
-  return a.tokens * a.q.heads * (int64_t)p.splits * (a.cache.head_dim + 2) * 4;
+  return a.tokens * a.q.heads * ((int64_t)p.splits * (a.cache.head_dim + 2) + 1) * 4;
 }
 
 hipError_t launch_attn(const AttnArgs& a, hipStream_t s) {

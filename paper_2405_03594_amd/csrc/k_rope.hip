@@ -4,8 +4,8 @@
 // A head's D channels are read by LPH = 8, 16 or 32 lanes (D / 8 rounded up to
 // a power of two), eight channels (16 bytes) a lane, so that a wave holds
 // 64 / LPH heads and everything stays in registers: one read and one write of
-// each element.  A wave takes up to kHeads heads of one token, so the angles
-// and norm weights of its channels are loaded once for all of them.
+// each element.  A wave takes several slots of heads of one token, so the
+// angles and norm weights of its channels are loaded once for all of them.
 //
 // The mean of squares adds neighbours in pairs (channels 2i and 2i + 1, then
 // pairs of pairs, ...), by lane exchanges whose sums do not depend on the side:
@@ -57,11 +57,20 @@ __device__ __forceinline__ void widen(const u32x4& v, float* x) {
     x[2 * i + 1] = T::to_f32(v[i] >> 16);
   }
 }
+// Round to nearest even: bf16 two an instruction (v_cvt_pk_bf16_f32).
 template <class T>
 __device__ __forceinline__ u32x4 narrow(const float* x) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
   u32x4 v;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = (uint32_t)T::from_f32(x[2 * i]) | ((uint32_t)T::from_f32(x[2 * i + 1]) << 16);
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (T::code == SPL_BF16) {
+      const bf16x2 p = {(__bf16)x[2 * i], (__bf16)x[2 * i + 1]};
+      v[i] = __builtin_bit_cast(uint32_t, p);
+    } else {
+      v[i] = (uint32_t)T::from_f32(x[2 * i]) | ((uint32_t)T::from_f32(x[2 * i + 1]) << 16);
+    }
+  }
   return v;
 }
 
@@ -71,15 +80,15 @@ template <bool kInter>
 struct Turn {
   float c[8], s[8];
   int partner;
-  bool on;
+  bool on;                                      // the lane's channels are rotated
 };
 
-template <bool kInter>
+template <int LPH, bool kInter, bool kWhole>
 __device__ __forceinline__ Turn<kInter> load_turn(const float* rope, int64_t rows, int64_t pos, int rot, int chunk,
                                                   int lane) {
   Turn<kInter> t;
-  const int half = rot >> 4;                    // chunks of one half of the rotated channels
-  t.on = chunk < 2 * half;
+  const int half = kWhole ? LPH / 2 : rot >> 4; // chunks of one half of the rotated channels
+  t.on = kWhole || chunk < 2 * half;
   t.partner = lane;
   const bool known = pos >= 0 && pos < rows;
   if (!t.on) return t;
@@ -108,26 +117,43 @@ __device__ __forceinline__ Turn<kInter> load_turn(const float* rope, int64_t row
 
 // x turned by the angle (kBack: by its negative): x c + other s, each product
 // and the sum rounded.  Every lane of the wave takes part.
-template <bool kInter, bool kBack>
+template <int LPH, bool kInter, bool kWhole, bool kBack>
 __device__ __forceinline__ void turn(const Turn<kInter>& t, float* x) {
   float y[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = kInter ? x[i ^ 1] : __shfl(x[i], t.partner);
-  if (!t.on) return;
+  for (int i = 0; i < 8; ++i) {
+    if (kInter) y[i] = x[i ^ 1];
+    else if (kWhole && LPH == 16) y[i] = dpp<0x128>(x[i]);      // the other half row: a rotation by 8 lanes
+    else y[i] = __shfl(x[i], t.partner);
+  }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float p = y[i] * t.s[i];
-    x[i] = kBack ? x[i] * t.c[i] - p : x[i] * t.c[i] + p;
+    const float p = y[i] * t.s[i], z = kBack ? x[i] * t.c[i] - p : x[i] * t.c[i] + p;
+    x[i] = kWhole || t.on ? z : x[i];
   }
 }
 
-template <int LPH>
-__device__ __forceinline__ float inverse_rms(const float* x, float inv_dim, float eps) {
-  float sq[8];
+// 1 / rms of the heads of N payloads a lane.  The root and the division are
+// some thirty instructions: each lane of a group of N does them for one of its
+// heads, and the others take the result from it.
+template <class T, int LPH, int N>
+__device__ __forceinline__ void inverse_rms(const u32x4* x, float inv_dim, float eps, bool zero, int lane, float* r) {
+  float ms[N];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) sq[i] = x[i] * x[i];
-  const float ms = head_sum<LPH>(pair_tree(sq)) * inv_dim;
-  return 1.0f / __fsqrt_rn(ms + eps);
+  for (int i = 0; i < N; ++i) {
+    float f[8];
+    widen<T>(x[i], f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = f[e] * f[e];
+    ms[i] = head_sum<LPH>(zero ? 0.0f : pair_tree(f)) * inv_dim;
+  }
+  float mine = ms[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) mine = (lane & (N - 1)) == i ? ms[i] : mine;
+  mine = 1.0f / sqrtf(mine + eps);
+  if (N == 1) r[0] = mine;
+  if (N == 2) r[0] = dpp<0xA0>(mine), r[1] = dpp<0xF5>(mine);                // the even, the odd lane of each pair
+  if (N == 4) r[0] = dpp<0x00>(mine), r[1] = dpp<0x55>(mine), r[2] = dpp<0xAA>(mine), r[3] = dpp<0xFF>(mine);
 }
 
 // ---- the 4-bit cache
@@ -189,56 +215,57 @@ __device__ __forceinline__ void store_codes(uint8_t* region, const spl::PageGeom
     region[g.page * (g.dim + g.scale_bytes) + ((b >> 3) * g.scale_bytes + (c >> 2)) * 8 + (b & 7)] = (uint8_t)scale;
 }
 
-// A wave's heads: kIter slots of 64 / LPH heads.
-constexpr int kIter = 4;
-
-// Waves of one token: first q's, then k's, then (with a cache) v's.
-template <class T, int LPH, bool kInter>
+// Waves of one token: first q's, then k's, then (with a cache) v's, each of
+// kIter slots of 64 / LPH heads.  A slot past the last head repeats it, and
+// writes nothing.
+template <class T, int LPH, bool kInter, int kIter, bool kWhole>
 __global__ __launch_bounds__(kThreads) void k_norm_rope(spl::NormRopeArgs a, int q_waves, int k_waves, int all_waves,
                                                         float inv_dim) {
   constexpr int kSlots = 64 / LPH;
-  const int64_t task = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
-  const int64_t t = task / all_waves;
+  const int task = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * kWaves + (threadIdx.x >> 6)));    // < 2^31
+  const int t32 = task / all_waves, part = task - t32 * all_waves;
+  const int64_t t = t32;
   if (t >= a.tokens) return;
-  const int part = (int)(task - t * all_waves);
   const int lane = threadIdx.x & 63, chunk = lane & (LPH - 1);
   const bool is_q = part < q_waves, is_v = part >= q_waves + k_waves;
   const spl_heads& src = is_q ? a.q : (is_v ? a.v : a.k);
-  const int first = (is_q ? part : (is_v ? part - q_waves - k_waves : part - q_waves)) * kIter * kSlots + lane / LPH;
-  const bool live = 8 * chunk < a.dim;
-  const uint16_t* in = static_cast<const uint16_t*>(src.data) + t * src.token_stride + 8 * chunk;
+  const int first = (is_q ? part : (is_v ? part - q_waves - k_waves : part - q_waves)) * kIter * kSlots;
+  const int mine = first + lane / LPH, last = src.heads - 1;
+  const bool live = kWhole || 8 * chunk < a.dim, full = kWhole && first + kIter * kSlots <= src.heads;
+  const int at = live ? 8 * chunk : 0;
+  const uint16_t* in = static_cast<const uint16_t*>(src.data) + t * src.token_stride + at;
 
   u32x4 x[kIter];
 #pragma unroll
   for (int i = 0; i < kIter; ++i) {
-    const int h = first + i * kSlots;
-    x[i] = u32x4{0, 0, 0, 0};
-    if (live && h < src.heads) x[i] = *reinterpret_cast<const u32x4*>(in + h * src.head_stride);
+    const int h = mine + i * kSlots;
+    x[i] = *reinterpret_cast<const u32x4*>(in + (h < last ? h : last) * src.head_stride);
   }
+  const int64_t slot = is_q || !a.cache.data ? -1 : a.slots[t];
   const uint16_t* w16 = static_cast<const uint16_t*>(is_q ? a.wq : a.wk);
   if (!is_v) {
-    float w[8];
-    if (w16 && live) widen<T>(*reinterpret_cast<const u32x4*>(w16 + 8 * chunk), w);
-    const Turn<kInter> tr = load_turn<kInter>(a.rope, a.rope_rows, a.rot ? a.positions[t] : 0, a.rot, chunk, lane);
+    float w[8], r[kIter];
+    if (w16) widen<T>(*reinterpret_cast<const u32x4*>(w16 + at), w);
+    const Turn<kInter> tr =
+        load_turn<LPH, kInter, kWhole>(a.rope, a.rope_rows, kWhole || a.rot ? a.positions[t] : 0, a.rot, chunk, lane);
     uint16_t* out = static_cast<uint16_t*>(is_q ? a.q_out : a.k_out);
-    if (out) out += t * src.heads * (int64_t)a.dim + 8 * chunk;
+    if (out) out += t * src.heads * (int64_t)a.dim + at;
+    if (w16) inverse_rms<T, LPH, kIter>(x, inv_dim, a.eps, !live, lane, r);
 #pragma unroll
     for (int i = 0; i < kIter; ++i) {
       float f[8];
       widen<T>(x[i], f);
       if (w16) {
-        const float r = inverse_rms<LPH>(f, inv_dim, a.eps);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = f[e] * r * w[e];
+        for (int e = 0; e < 8; ++e) f[e] = f[e] * r[i] * w[e];
       }
-      turn<kInter, false>(tr, f);
+      if (kWhole || a.rot) turn<LPH, kInter, kWhole, false>(tr, f);
       x[i] = narrow<T>(f);
-      const int h = first + i * kSlots;
-      if (out && live && h < src.heads) *reinterpret_cast<u32x4*>(out + (int64_t)h * a.dim) = x[i];
+      const int h = mine + i * kSlots;
+      if (out && (full || (live && h <= last))) *reinterpret_cast<u32x4*>(out + (int64_t)h * a.dim) = x[i];
     }
   }
   if (is_q || !a.cache.data) return;
-  const int64_t slot = a.slots[t];
   const int shift = __builtin_ctz((unsigned)a.cache.page);
   if (slot < 0 || (slot >> shift) >= a.cache.pages) return;
   const spl::PageGeom g = spl::page_geom(a.dim, a.cache.page);
@@ -248,8 +275,8 @@ __global__ __launch_bounds__(kThreads) void k_norm_rope(spl::NormRopeArgs a, int
   for (int i = 0; i < kIter; ++i) {
     uint32_t code;
     const uint32_t scale = encode8<T>(x[i], &code);
-    const int h = first + i * kSlots;
-    if (live && h < src.heads) store_codes(page + (int64_t)h * g.bytes, g, is_v, b, chunk, code, scale);
+    const int h = mine + i * kSlots;
+    if (live && h <= last) store_codes(page + (int64_t)h * g.bytes, g, is_v, b, chunk, code, scale);
   }
 }
 
@@ -307,62 +334,65 @@ __global__ __launch_bounds__(kThreads) void k_cache_read(spl_kv_cache c, const i
 // channels, so dw's terms stay in registers; its sums go to one row of
 // `partial`, which k_norm_rope_dw adds up in order: the result does not change
 // from run to run.
-template <class T, int LPH, bool kInter>
+template <class T, int LPH, bool kInter, int kIter, bool kWhole>
 __global__ __launch_bounds__(kThreads) void k_norm_rope_grad(spl::NormRopeGradArgs a, int q_groups, int groups,
                                                              float inv_dim) {
   constexpr int kSlots = 64 / LPH;
   __shared__ float sum_s[kWaves][LPH * 8];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, chunk = lane & (LPH - 1);
-  const bool is_q = (int)blockIdx.x < q_groups, live = 8 * chunk < a.dim;
+  const bool is_q = (int)blockIdx.x < q_groups, live = kWhole || 8 * chunk < a.dim;
   const int group = is_q ? blockIdx.x : blockIdx.x - q_groups, count = is_q ? q_groups : groups - q_groups;
   const spl_heads& src = is_q ? a.q : a.k;
   const spl_heads& grad = is_q ? a.dq : a.dk;
-  uint16_t* out = static_cast<uint16_t*>(is_q ? a.dq_out : a.dk_out) + 8 * chunk;
-  const uint16_t* in = static_cast<const uint16_t*>(src.data) + 8 * chunk;
-  const uint16_t* up = static_cast<const uint16_t*>(grad.data) + 8 * chunk;
+  const int at = live ? 8 * chunk : 0, last = src.heads - 1;
+  uint16_t* out = static_cast<uint16_t*>(is_q ? a.dq_out : a.dk_out) + at;
+  const uint16_t* in = static_cast<const uint16_t*>(src.data) + at;
+  const uint16_t* up = static_cast<const uint16_t*>(grad.data) + at;
   const uint16_t* w16 = static_cast<const uint16_t*>(is_q ? a.wq : a.wk);
   float w[8], dw[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) dw[e] = 0.0f, w[e] = 1.0f;
-  if (w16 && live) widen<T>(*reinterpret_cast<const u32x4*>(w16 + 8 * chunk), w);
+  if (w16) widen<T>(*reinterpret_cast<const u32x4*>(w16 + at), w);
   const int per = (src.heads + kIter * kSlots - 1) / (kIter * kSlots);       // waves of one token
-  const int64_t tasks = a.tokens * per;
+  const int64_t tasks = a.tokens * per;                         // < 2^31
   for (int64_t task = (int64_t)group * kWaves + wave; task < tasks; task += (int64_t)count * kWaves) {
-    const int64_t t = task / per;
-    const int first = (int)(task - t * per) * kIter * kSlots + lane / LPH;
+    const int task32 = __builtin_amdgcn_readfirstlane((int)task), t32 = task32 / per;
+    const int64_t t = t32;
+    const int first = (task32 - t32 * per) * kIter * kSlots, mine = first + lane / LPH;
+    const bool full = kWhole && first + kIter * kSlots <= src.heads;
     u32x4 x[kIter], g[kIter];
 #pragma unroll
     for (int i = 0; i < kIter; ++i) {
-      const int h = first + i * kSlots;
-      x[i] = g[i] = u32x4{0, 0, 0, 0};
-      if (live && h < src.heads) {
-        g[i] = *reinterpret_cast<const u32x4*>(up + t * grad.token_stride + h * grad.head_stride);
-        if (w16) x[i] = *reinterpret_cast<const u32x4*>(in + t * src.token_stride + h * src.head_stride);
-      }
+      const int h = mine + i * kSlots < last ? mine + i * kSlots : last;
+      g[i] = *reinterpret_cast<const u32x4*>(up + t * grad.token_stride + h * grad.head_stride);
+      if (w16) x[i] = *reinterpret_cast<const u32x4*>(in + t * src.token_stride + h * src.head_stride);
     }
-    const Turn<kInter> tr = load_turn<kInter>(a.rope, a.rope_rows, a.rot ? a.positions[t] : 0, a.rot, chunk, lane);
+    const Turn<kInter> tr =
+        load_turn<LPH, kInter, kWhole>(a.rope, a.rope_rows, kWhole || a.rot ? a.positions[t] : 0, a.rot, chunk, lane);
+    float r[kIter];
+    if (w16) inverse_rms<T, LPH, kIter>(x, inv_dim, a.eps, !live, lane, r);
 #pragma unroll
     for (int i = 0; i < kIter; ++i) {
+      const int h = mine + i * kSlots;
+      const bool counts = full || (live && h <= last);          // a repeated head adds nothing to dw
       float f[8], d[8];
       widen<T>(g[i], d);
-      turn<kInter, true>(tr, d);
+      if (kWhole || a.rot) turn<LPH, kInter, kWhole, true>(tr, d);
       if (w16) {
         widen<T>(x[i], f);
-        const float r = inverse_rms<LPH>(f, inv_dim, a.eps);
         float p[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          f[e] *= r;
-          dw[e] += d[e] * f[e];
+          f[e] *= r[i];
+          dw[e] = __builtin_fmaf(full || counts ? d[e] : 0.0f, f[e], dw[e]);
           d[e] *= w[e];
           p[e] = d[e] * f[e];
         }
-        const float m = head_sum<LPH>(pair_tree(p)) * inv_dim;
+        const float m = head_sum<LPH>(live ? pair_tree(p) : 0.0f) * -inv_dim;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) d[e] = r * (d[e] - f[e] * m);
+        for (int e = 0; e < 8; ++e) d[e] = r[i] * __builtin_fmaf(f[e], m, d[e]);
       }
-      const int h = first + i * kSlots;
-      if (live && h < src.heads) *reinterpret_cast<u32x4*>(out + (t * src.heads + h) * a.dim) = narrow<T>(d);
+      if (counts) *reinterpret_cast<u32x4*>(out + (t * src.heads + h) * a.dim) = narrow<T>(d);
     }
   }
   if (!w16) return;                                             // the same for the whole workgroup
@@ -381,38 +411,53 @@ __global__ __launch_bounds__(kThreads) void k_norm_rope_grad(spl::NormRopeGradAr
   }
 }
 
-// dw[c] = the sum of a column of `partial`: 32 columns a workgroup, its eight
-// row groups added in order.
-__global__ __launch_bounds__(kThreads) void k_norm_rope_dw(const float* partial, int q_groups, int groups, int dim,
-                                                           float* dwq, float* dwk) {
-  __shared__ float sum_s[8][32];
+// dw[c] = the sum of a column of `partial`: 32 columns a workgroup, its 32 row
+// groups added in order.
+constexpr int kSumThreads = 1024;
+__global__ __launch_bounds__(kSumThreads) void k_norm_rope_dw(const float* partial, int q_groups, int groups, int dim,
+                                                              float* dwq, float* dwk) {
+  constexpr int kRowGroups = kSumThreads / 32;
+  __shared__ float sum_s[kRowGroups][32];
   const bool is_q = blockIdx.y == 0;
   float* dw = is_q ? dwq : dwk;
   if (!dw) return;
   const int c = blockIdx.x * 32 + (threadIdx.x & 31), row = threadIdx.x >> 5;
   const int r0 = is_q ? 0 : q_groups, r1 = is_q ? q_groups : groups;
   float s = 0.0f;
-  if (c < dim)
-    for (int r = r0 + row; r < r1; r += 8) s += partial[(int64_t)r * dim + c];
+  if (c < dim) {
+#pragma unroll 8
+    for (int r = r0 + row; r < r1; r += kRowGroups) s += partial[(int64_t)r * dim + c];
+  }
   sum_s[row][threadIdx.x & 31] = s;
   __syncthreads();
   if (row == 0 && c < dim) {
     float total = 0.0f;
-    for (int r = 0; r < 8; ++r) total += sum_s[r][threadIdx.x & 31];
+#pragma unroll
+    for (int r = 0; r < kRowGroups; ++r) total += sum_s[r][threadIdx.x & 31];
     dw[c] = total;
   }
 }
 
+// Slots of a wave: four, but two where four would leave the chip without enough
+// waves to hide the loads (forward and backward of 397 tokens of 24 + 8 heads of
+// 96 channels: 15.7 us with four, 12.4 with two; 2048 of 32 + 32 of 128: 49.3 and
+// 54.5).
+constexpr int kFewWaves = 16;                   // a CU
+int slots_of(int64_t tokens, int64_t heads, int lph) {
+  return tokens * heads * lph >= (int64_t)kFewWaves * spl::device_cus() * 64 * 4 ? 4 : 2;
+}
+int lanes_of(int dim) { return dim <= 64 ? 8 : (dim <= 128 ? 16 : 32); }
+
 // Workgroups of the gradient for q and for k: shared out by heads, at most
 // four a CU, so that few rows of partial sums are left.
 void grad_groups(int64_t tokens, int32_t q_heads, int32_t k_heads, int32_t dim, int* q, int* k) {
-  const int lph = dim <= 64 ? 8 : (dim <= 128 ? 16 : 32), heads = kIter * (64 / lph);
+  const int lph = lanes_of(dim), heads = slots_of(tokens, (int64_t)q_heads + k_heads, lph) * (64 / lph);
   const int64_t most = 4 * (int64_t)spl::device_cus();
-  const auto waves = [&](int64_t h) { return (tokens * ((h + heads - 1) / heads) + kWaves - 1) / kWaves; };
-  const int64_t wq = waves(q_heads), wk = waves(k_heads);
-  int64_t nq = wq, nk = wk;
-  if (wq + wk > most) {
-    nq = most * wq / (wq + wk);
+  const auto groups = [&](int64_t h) { return (tokens * ((h + heads - 1) / heads) + kWaves - 1) / kWaves; };
+  const int64_t gq = groups(q_heads), gk = groups(k_heads);
+  int64_t nq = gq, nk = gk;
+  if (gq + gk > most) {
+    nq = most * gq / (gq + gk);
     nq = nq < 1 ? 1 : nq;
     nk = most - nq < 1 ? 1 : most - nq;
   }
@@ -420,25 +465,41 @@ void grad_groups(int64_t tokens, int32_t q_heads, int32_t k_heads, int32_t dim, 
   *k = (int)nk;
 }
 
-#define SPL_LPH(dim, call)                   \
-  do {                                       \
-    if ((dim) <= 64) { call(8); }            \
-    else if ((dim) <= 128) { call(16); }     \
-    else { call(32); }                       \
+// The instance for a head's lanes, the pairs, the slots, and whether all of its
+// lanes hold rotated channels (then nothing is masked).
+#define SPL_PICK(kernel, lph, inter, iter, whole, ...)                                                   \
+  do {                                                                                                   \
+    if ((lph) == 8) SPL_PICK_I(kernel, 8, inter, iter, whole, __VA_ARGS__);                              \
+    else if ((lph) == 16) SPL_PICK_I(kernel, 16, inter, iter, whole, __VA_ARGS__);                       \
+    else SPL_PICK_I(kernel, 32, inter, iter, whole, __VA_ARGS__);                                        \
+  } while (0)
+#define SPL_PICK_I(kernel, L, inter, iter, whole, ...)                                                   \
+  do {                                                                                                   \
+    if (inter) SPL_PICK_N(kernel, L, true, iter, whole, __VA_ARGS__);                                    \
+    else SPL_PICK_N(kernel, L, false, iter, whole, __VA_ARGS__);                                         \
+  } while (0)
+#define SPL_PICK_N(kernel, L, I, iter, whole, ...)                                                       \
+  do {                                                                                                   \
+    if ((iter) == 4) SPL_PICK_W(kernel, L, I, 4, whole, __VA_ARGS__);                                    \
+    else SPL_PICK_W(kernel, L, I, 2, whole, __VA_ARGS__);                                                \
+  } while (0)
+#define SPL_PICK_W(kernel, L, I, N, whole, ...)                                                          \
+  do {                                                                                                   \
+    if (whole) kernel<T, L, I, N, true> __VA_ARGS__;                                                     \
+    else kernel<T, L, I, N, false> __VA_ARGS__;                                                          \
   } while (0)
 
 template <class T>
 hipError_t norm_rope(const spl::NormRopeArgs& a, hipStream_t s) {
-  const int lph = a.dim <= 64 ? 8 : (a.dim <= 128 ? 16 : 32), heads = kIter * (64 / lph);
+  const int lph = lanes_of(a.dim);
+  const int iter = slots_of(a.tokens, (int64_t)a.q.heads + (a.cache.data ? 2 : 1) * (int64_t)a.k.heads, lph);
+  const int heads = iter * (64 / lph);
   const int qw = (a.q.heads + heads - 1) / heads, kw = (a.k.heads + heads - 1) / heads;
   const int all = qw + kw + (a.cache.data ? kw : 0);
   const dim3 grid((unsigned)((a.tokens * all + kWaves - 1) / kWaves));
   const float inv = (float)(1.0 / a.dim);
-#define SPL_CALL(L)                                                                                          \
-  if (a.interleaved) k_norm_rope<T, L, true><<<grid, kThreads, 0, s>>>(a, qw, kw, all, inv);                 \
-  else k_norm_rope<T, L, false><<<grid, kThreads, 0, s>>>(a, qw, kw, all, inv)
-  SPL_LPH(a.dim, SPL_CALL);
-#undef SPL_CALL
+  SPL_PICK(k_norm_rope, lph, a.interleaved, iter, a.rot == 8 * lph,
+           <<<grid, kThreads, 0, s>>>(a, qw, kw, all, inv));
   return hipGetLastError();
 }
 
@@ -446,15 +507,13 @@ template <class T>
 hipError_t norm_rope_grad(const spl::NormRopeGradArgs& a, hipStream_t s) {
   int nq, nk;
   grad_groups(a.tokens, a.q.heads, a.k.heads, a.dim, &nq, &nk);
+  const int lph = lanes_of(a.dim), iter = slots_of(a.tokens, (int64_t)a.q.heads + a.k.heads, lph);
   const float inv = (float)(1.0 / a.dim);
-#define SPL_CALL(L)                                                                                          \
-  if (a.interleaved) k_norm_rope_grad<T, L, true><<<nq + nk, kThreads, 0, s>>>(a, nq, nq + nk, inv);         \
-  else k_norm_rope_grad<T, L, false><<<nq + nk, kThreads, 0, s>>>(a, nq, nq + nk, inv)
-  SPL_LPH(a.dim, SPL_CALL);
-#undef SPL_CALL
+  SPL_PICK(k_norm_rope_grad, lph, a.interleaved, iter, a.rot == 8 * lph,
+           <<<nq + nk, kThreads, 0, s>>>(a, nq, nq + nk, inv));
   if (a.dwq || a.dwk)
-    k_norm_rope_dw<<<dim3((unsigned)((a.dim + 31) / 32), 2), kThreads, 0, s>>>(a.partial, nq, nq + nk, a.dim, a.dwq,
-                                                                            a.dwk);
+    k_norm_rope_dw<<<dim3((unsigned)((a.dim + 31) / 32), 2), kSumThreads, 0, s>>>(a.partial, nq, nq + nk, a.dim,
+                                                                                a.dwq, a.dwk);
   return hipGetLastError();
 }
 
