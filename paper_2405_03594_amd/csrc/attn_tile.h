@@ -38,12 +38,25 @@ __device__ __forceinline__ float scale_of(uint32_t s, int b) {
   return __uint_as_float(b == 0 ? s << 23 : b == 1 ? s << 15 : b == 2 ? s << 7 : s >> 1);
 }
 
+// The largest scale byte whose values the type holds.
+__device__ constexpr uint32_t max_scale(Bf16) { return 252; }
+__device__ constexpr uint32_t max_scale(F16) { return 140; }
+
 __device__ __forceinline__ f32x4 mfma16(Bf16, const u32x4& a, const u32x4& b, const f32x4& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0,
                                                  0);
 }
 __device__ __forceinline__ f32x4 mfma16(F16, const u32x4& a, const u32x4& b, const f32x4& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0,
+                                                0);
+}
+
+__device__ __forceinline__ f32x16 mfma32(Bf16, const u32x4& a, const u32x4& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0,
+                                                 0);
+}
+__device__ __forceinline__ f32x16 mfma32(F16, const u32x4& a, const u32x4& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0,
                                                 0);
 }
 
@@ -93,19 +106,20 @@ __device__ __forceinline__ Rows rows_of(const AttnArgs& a, int64_t r) {
   return {s, (int32_t)(e - s), (int32_t)len};
 }
 
-// The request that owns tile `tile` when each has ceil(rows * group / size)
-// tiles, and the tile's number in it; request -1 past the last.  Every lane
-// of the wave calls it with the same tile.
+// The request that owns tile `tile` when each of more than `few` rows (rows *
+// group) has ceil(rows * group / size) tiles, and the tile's number in it;
+// request -1 past the last.  Every lane of the wave calls it with the same tile.
 struct Tile {
   int64_t request;
   int64_t index;
 };
-__device__ __forceinline__ Tile find_tile(const AttnArgs& a, int group, int size, int64_t tile) {
+__device__ __forceinline__ Tile find_tile(const AttnArgs& a, int group, int size, int few, int64_t tile) {
   const int lane = lane_id();
   int64_t before = 0;
   for (int64_t base = 0; base < a.requests; base += 64) {
     int64_t n = 0;
-    if (base + lane < a.requests) n = ((int64_t)rows_of(a, base + lane).count * group + size - 1) / size;
+    if (base + lane < a.requests) n = (int64_t)rows_of(a, base + lane).count * group;
+    n = n > few ? (n + size - 1) / size : 0;
     int64_t sum = n;
     for (int d = 1; d < 64; d <<= 1) {
       const int64_t y = __shfl_up(sum, d);
@@ -119,6 +133,41 @@ __device__ __forceinline__ Tile find_tile(const AttnArgs& a, int group, int size
     before += __shfl(sum, 63);
   }
   return {-1, 0};
+}
+
+// The steps of `unit` tokens that any of the rows [row0, end_row) of a request
+// sees, and a split's share of them: chunk of them, more where the splits would
+// not reach the end.
+struct Span {
+  int32_t low, high;                             // positions of the first and the last row
+  int32_t s0, steps, share;
+};
+__device__ __forceinline__ Span tile_span(const Rows& rows, int32_t row0, int32_t end_row, int group, int32_t window,
+                                          int unit, int splits, int chunk) {
+  Span t;
+  const int32_t first_pos = rows.len - rows.count;
+  t.low = first_pos + row0 / group;
+  t.high = first_pos + (end_row - 1) / group;
+  const int32_t end = t.high + 1 < rows.len ? t.high + 1 : rows.len;
+  const int32_t begin = window > 0 && t.low - window + 1 > 0 ? t.low - window + 1 : 0;
+  t.s0 = begin / unit;
+  t.steps = end > begin ? (end + unit - 1) / unit - t.s0 : 0;
+  const int32_t least = (t.steps + splits - 1) / splits;
+  t.share = chunk > least ? chunk : least;
+  return t;
+}
+
+// The workspace of split calls: per row and split the sums and (reference times
+// log2 e, weight), per row the splits that hold any of it.
+struct Parts {
+  float* sums;
+  float* stats;
+  int32_t* counts;
+};
+__device__ __forceinline__ Parts parts_of(const AttnArgs& a, int dim, int splits) {
+  const int64_t n = a.tokens * a.q.heads * splits;
+  float* w = static_cast<float*>(a.workspace);
+  return {w, w + n * dim, reinterpret_cast<int32_t*>(w + n * (dim + 2))};
 }
 
 }  // namespace spl

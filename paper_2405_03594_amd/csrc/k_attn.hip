@@ -27,7 +27,7 @@ using spl::f32x4;
 using spl::u32x2;
 using spl::u32x4;
 
-constexpr int kRows = 16;
+constexpr int kRows = spl::kFewRows;
 constexpr int kStep = 32;
 constexpr int kWaves = 4;
 constexpr int kGroupsPerCu = 2;
@@ -262,12 +262,12 @@ __device__ __forceinline__ void step(State<D>& st, Raw<D>& r, const u32x4* q, co
       seen |= see ? 1u << i : 0u;
       s[i] = see ? s[i] : -INFINITY;
     }
-    // values that some row does not see must not reach it as 0 * NaN: take the
-    // NaNs out of the product and put them where they are seen
+    // values that some row does not see must not reach it as 0 * NaN: take what
+    // is not finite out of the product and put NaNs where it is seen
     uint32_t bad = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (((r.vs[i / 4] >> (8 * (i % 4))) & 0xffu) == 255u) bad |= 1u << i;
+      if (((r.vs[i / 4] >> (8 * (i % 4))) & 0xffu) > spl::max_scale(T{})) bad |= 1u << i;
     if (__ballot(bad != 0)) {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
@@ -317,28 +317,6 @@ __device__ __forceinline__ void step(State<D>& st, Raw<D>& r, const u32x4* q, co
   }
 }
 
-// The steps that any row of the tile at row0 sees, and a split's share of them:
-// chunk of them, more where the splits would not reach the end.
-struct TileSteps {
-  int32_t low, high;                             // positions of the tile's first and last row
-  int32_t s0, steps, share;
-};
-__device__ __forceinline__ TileSteps tile_steps(const AttnArgs& a, const spl::Rows& rows, int32_t row0, int32_t all,
-                                                int group, int splits, int chunk) {
-  TileSteps t;
-  const int32_t last = (all - row0 < kRows ? all : row0 + kRows) - 1;
-  const int32_t first_pos = rows.len - rows.count;
-  t.low = first_pos + row0 / group;
-  t.high = first_pos + last / group;
-  const int32_t end = t.high + 1 < rows.len ? t.high + 1 : rows.len;
-  const int32_t begin = a.window > 0 && t.low - a.window + 1 > 0 ? t.low - a.window + 1 : 0;
-  t.s0 = begin / kStep;
-  t.steps = end > begin ? (end + kStep - 1) / kStep - t.s0 : 0;
-  const int32_t least = (t.steps + splits - 1) / splits;
-  t.share = chunk > least ? chunk : least;
-  return t;
-}
-
 // The request that place `at` of the launch serves when the workgroups of
 // `round` requests go to the chip's CUs in each round: the longest first, every
 // other round backwards, so that what a CU gets in two rounds is alike.
@@ -357,35 +335,21 @@ __device__ __forceinline__ int64_t ranked_request(const AttnArgs& a, int at, int
   return who ? __builtin_ctzll(who) : -1;
 }
 
-// The workspace of split calls: per row and split the sums and (reference times
-// log2 e, weight), per row the splits that hold any of it.
-struct Parts {
-  float* sums;
-  float* stats;
-  int32_t* counts;
-};
-template <int D>
-__device__ __forceinline__ Parts parts_of(const AttnArgs& a, int splits) {
-  const int64_t n = a.tokens * a.q.heads * splits;
-  float* w = static_cast<float*>(a.workspace);
-  return {w, w + n * D, reinterpret_cast<int32_t*>(w + n * (D + 2))};
-}
-
 // One workgroup: a tile of rows, a key head, one of the splits of its tokens.
 // The four waves take every fourth step and are joined through LDS.
 template <class T, int D>
-__global__ __launch_bounds__(kWaves * 64, D == 256 ? 2 : 3) void k_attn_rows(AttnArgs a, int group, int direct,
-                                                                            int splits, int chunk, int snake) {
+__global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 3) void k_attn_rows(AttnArgs a, int group, int direct,
+                                                                            int splits, int chunk, int snake, int most) {
   using Gm = Geom<D>;
   __shared__ float o_s[2][Gm::U * 4][64];
   __shared__ float m_s[kWaves][kRows], l_s[kWaves][kRows];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // heads fastest: consecutive workgroups go to different XCDs, so each has a
   // share of every request, however their lengths differ
-  const int head = blockIdx.x, split = blockIdx.z;
-  spl::Tile tile{(int64_t)blockIdx.y, 0};
-  if (!direct) tile = spl::find_tile(a, group, kRows, blockIdx.y);
-  else if (snake > 0) tile.request = ranked_request(a, blockIdx.y, snake);
+  const int place = blockIdx.x / a.cache.heads, head = blockIdx.x - place * a.cache.heads, split = blockIdx.y;
+  spl::Tile tile{place, 0};
+  if (!direct) tile = spl::find_tile(a, group, kRows, 0, place);
+  else if (snake > 0) tile.request = ranked_request(a, place, snake);
   const int64_t req = __builtin_amdgcn_readfirstlane((int)tile.request);
   if (req < 0) return;
   spl::Rows rows = spl::rows_of(a, req);
@@ -393,13 +357,13 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 2 : 3) void k_attn_rows(Att
   rows.count = __builtin_amdgcn_readfirstlane(rows.count);
   rows.len = __builtin_amdgcn_readfirstlane(rows.len);
   const int32_t row0 = __builtin_amdgcn_readfirstlane((int)tile.index) * kRows, all = rows.count * group;
-  if (row0 >= all) return;
+  if (row0 >= all || all > most) return;         // more rows than most: another kernel's
   const int n = all - row0 < kRows ? all - row0 : kRows;                   // rows of this tile
   const int m16 = lane & 15, j = lane >> 4;
   const int32_t first_pos = rows.len - rows.count;
   const int32_t row = row0 + (m16 < n ? m16 : n - 1), tok = row / group;
   const int64_t t_row = rows.first + tok, h_row = head * group + (row - tok * group);
-  const TileSteps ts = tile_steps(a, rows, row0, all, group, splits, chunk);
+  const spl::Span ts = spl::tile_span(rows, row0, row0 + n, group, a.window, kStep, splits, chunk);
   const int32_t s0 = ts.s0, from = split * ts.share;
   const int32_t to = from + ts.share < ts.steps ? from + ts.share : ts.steps;
   const bool only = ts.steps <= ts.share;        // the tile is one split's
@@ -491,7 +455,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 2 : 3) void k_attn_rows(Att
   if (m16 >= n) return;
 
   const int64_t out_row = t_row * a.q.heads + h_row;
-  const Parts w = parts_of<D>(a, splits);
+  const spl::Parts w = spl::parts_of(a, D, splits);
   if (splits > 1 && split == 0 && j == 1) w.counts[out_row] = only ? 1 : (ts.steps + ts.share - 1) / ts.share;
   if (!only) {
     const int64_t at = out_row * splits + split;
@@ -536,7 +500,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_attn_join(AttnArgs a, int s
   __shared__ vec o_s[kJoinWaves - 1][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t row = blockIdx.x;
-  const Parts p = parts_of<D>(a, splits);
+  const spl::Parts p = spl::parts_of(a, D, splits);
   const int32_t t = (int32_t)blockIdx.x / a.q.heads;             // tokens * heads < 2^31
   const int32_t t0 = a.row_start[0], t1 = a.row_start[a.requests];
   int n = __builtin_amdgcn_readfirstlane(p.counts[row]);
@@ -582,17 +546,28 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_attn_join(AttnArgs a, int s
   if (a.lse && lane == 0) a.lse[row] = total == 0.0f ? -INFINITY : (top + log2f(total)) * 0.6931471805599453f;
 }
 
-struct Plan {
-  int64_t tiles;
-  int group, direct, splits, chunk, snake;
-};
-
-Plan plan_of(const AttnArgs& a) {
-  Plan p;
+// k_attn_prefill takes over where its tiles give every CU a workgroup.  us of
+// k_attn_rows / k_attn_prefill, bf16, 128 channels, prompts of one request: 512
+// tokens of 32 heads 13.7 / 17.9, of 32 over 8 13.9 / 18.0, after 8192 tokens 134 /
+// 160; 1024 tokens 31.9 / 28.5, 31.4 / 28.0; 2048 of 32 83.1 / 58.4.  With 256
+// channels its registers do not hold a step (1024 tokens of 16 heads 51.6 / 85.4).
+// Splits: twice as many workgroups as CUs are enough (16 requests of up to 4096
+// tokens, 32 heads: 512 workgroups 43.5 us, 1024 with the join 49; 64 requests of
+// up to 2000, 8 heads: 22.7 and 31), and a wave wants four steps.
+spl::AttnPlan plan_of(const AttnArgs& a) {
+  const int64_t cus = spl::device_cus();
+  spl::AttnPlan p{};
   p.group = a.q.heads / a.cache.heads;
+  const int64_t rows = a.tokens * (int64_t)p.group;
   p.direct = a.max_new > 0 && a.max_new * p.group <= kRows;
-  const int64_t most = a.tokens * (int64_t)p.group / kRows + a.requests;
-  p.tiles = p.direct ? a.requests : (most < a.tokens * p.group ? most : a.tokens * p.group);
+  if (!p.direct && a.cache.head_dim < 256 && rows * a.cache.heads >= spl::kPrefillRows * cus) {
+    const int64_t most = rows / spl::kPrefillRows + a.requests;
+    p.prefill_tiles = a.requests == 1 ? (rows + spl::kPrefillRows - 1) / spl::kPrefillRows : (most < rows ? most : rows);
+    p.direct = 1;                                // what is left
+  }
+  const int64_t most = rows / kRows + a.requests;
+  p.tiles = p.direct ? a.requests : (most < rows ? most : rows);
+  if (p.prefill_tiles > 0 && a.requests == 1) p.tiles = rows > kRows ? 0 : 1;
   // split the tokens into chunks while the launch has fewer workgroups than the chip takes
   int64_t len = a.width * (int64_t)a.cache.page;
   if (a.max_len > 0 && a.max_len < len) len = a.max_len;
@@ -600,32 +575,38 @@ Plan plan_of(const AttnArgs& a) {
     const int64_t seen = a.window + (a.max_new > 0 && a.max_new < kRows ? a.max_new : kRows);
     len = len < seen ? len : seen;
   }
-  const int64_t groups = p.tiles * a.cache.heads, want = kGroupsPerCu * (int64_t)spl::device_cus();
-  const int64_t steps = (len + kStep - 1) / kStep;
-  int64_t s = (want + groups - 1) / groups;
+  const int64_t groups = p.tiles * a.cache.heads, steps = (len + kStep - 1) / kStep;
+  int64_t s = groups > 0 ? (kGroupsPerCu * cus + groups - 1) / groups : 1;
   s = s < 1 ? 1 : (s > kMaxSplits ? kMaxSplits : s);
   int64_t chunk = (steps + s - 1) / s;
   chunk = chunk < kMinChunk ? kMinChunk : chunk;
   chunk = (chunk + kWaves - 1) / kWaves * kWaves;
   p.chunk = (int)chunk;
-  p.splits = (int)((steps + chunk - 1) / chunk);
+  p.splits = p.tiles > 0 ? (int)((steps + chunk - 1) / chunk) : 1;
   // several requests of unknown lengths, and more workgroups than CUs
-  const int64_t round = spl::device_cus() / a.cache.heads;
+  const int64_t round = cus / a.cache.heads;
   p.snake = p.direct && a.requests <= 32 && round >= 1 && a.requests > round ? (int)round : 0;
   return p;
 }
 
 template <class T, int D>
-hipError_t run(const AttnArgs& a, const Plan& p, hipStream_t s) {
-  const dim3 grid((unsigned)a.cache.heads, (unsigned)p.tiles, (unsigned)p.splits);
-  k_attn_rows<T, D><<<grid, kWaves * 64, 0, s>>>(a, p.group, p.direct, p.splits, p.chunk, p.snake);
+hipError_t run(const AttnArgs& a, const spl::AttnPlan& p, hipStream_t s) {
+  if (p.tiles > 0) {
+    const dim3 grid((unsigned)(p.tiles * a.cache.heads), (unsigned)p.splits);
+    k_attn_rows<T, D><<<grid, kWaves * 64, 0, s>>>(a, p.group, p.direct, p.splits, p.chunk, p.snake,
+                                                   p.prefill_tiles > 0 ? kRows : INT32_MAX);
+  }
+  if (p.prefill_tiles > 0) {
+    const hipError_t e = spl::launch_attn_prefill(a, p, s);
+    if (e != hipSuccess) return e;
+  }
   if (p.splits > 1)
     k_attn_join<T, D><<<dim3((unsigned)(a.tokens * a.q.heads)), kJoinWaves * 64, 0, s>>>(a, p.splits);
   return hipGetLastError();
 }
 
 template <class T>
-hipError_t run_dim(const AttnArgs& a, const Plan& p, hipStream_t s) {
+hipError_t run_dim(const AttnArgs& a, const spl::AttnPlan& p, hipStream_t s) {
   switch (a.cache.head_dim) {
     case 64: return run<T, 64>(a, p, s);
     case 96: return run<T, 96>(a, p, s);
@@ -639,13 +620,13 @@ hipError_t run_dim(const AttnArgs& a, const Plan& p, hipStream_t s) {
 namespace spl {
 
 int64_t attn_workspace_bytes(const AttnArgs& a) {
-  const Plan p = plan_of(a);
+  const AttnPlan p = plan_of(a);
   if (p.splits == 1) return 0;
   return a.tokens * a.q.heads * ((int64_t)p.splits * (a.cache.head_dim + 2) + 1) * 4;
 }
 
 hipError_t launch_attn(const AttnArgs& a, hipStream_t s) {
-  const Plan p = plan_of(a);
+  const AttnPlan p = plan_of(a);
   return a.cache.dtype == SPL_F16 ? run_dim<F16>(a, p, s) : run_dim<Bf16>(a, p, s);
 }
 

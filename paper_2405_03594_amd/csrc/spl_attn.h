@@ -90,6 +90,19 @@ struct AttnArgs {
   int32_t window;                               // 0: none
   void* workspace;
 };
+// How a call is launched: k_attn_rows for all requests (prefill_tiles 0), or
+// k_attn_prefill for those of more than kFewRows rows and k_attn_rows for the
+// others, a tile each (tiles 0: there are none).
+constexpr int kFewRows = 16;                    // of a tile of k_attn_rows
+constexpr int kPrefillRows = 128;               // of a tile of k_attn_prefill
+struct AttnPlan {
+  int64_t tiles, prefill_tiles;
+  int group;                                    // query heads of a key head
+  int direct;                                   // a tile is a request
+  int splits, chunk;                            // of the tokens in k_attn_rows; chunk in its steps
+  int snake;                                    // requests of a round of the chip, 0: in their order
+};
+hipError_t launch_attn_prefill(const AttnArgs& a, const AttnPlan& p, hipStream_t s);
 int64_t attn_workspace_bytes(const AttnArgs& a);
 hipError_t launch_attn(const AttnArgs& a, hipStream_t s);
 
