@@ -60,6 +60,17 @@ __device__ __forceinline__ f32x16 mfma32(F16, const u32x4& a, const u32x4& b, co
                                                 0);
 }
 
+// How the softmax's weights 2^(c s - reference) are kept in the type: they are at
+// most 2^lift when the reference is set, to a maximum of the scores, and it moves
+// only when they would pass 2^(lift + slack).  bf16 has fp32's range, so its
+// weights keep 8 bits at any size.  fp16 ends at 2^16 and loses bits below 2^-14:
+// lifted, a weight is whole down to 2^-24 of the largest.
+struct Reference {
+  float lift, slack;
+};
+__device__ constexpr Reference reference_of(Bf16) { return {0.0f, 8.0f}; }
+__device__ constexpr Reference reference_of(F16) { return {10.0f, 5.0f}; }
+
 // Two floats rounded to nearest even, the first in the low half.
 __device__ __forceinline__ uint32_t pack2(Bf16, float a, float b) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));

@@ -220,14 +220,12 @@ __device__ __forceinline__ void value_pair(const Raw<D>& r, int c, u32x4& even, 
   }
 }
 
-// The state of a tile's softmax: per lane the row's reference m, with mc = c m;
-// l (four times the same) the sum of the weights 2^(c (s - m)) as they meet the
+// The state of a tile's softmax: per lane the row's m, with mc = c m - lift; l
+// (four times the same) the sum of the weights 2^(c s - mc) as they meet the
 // values, rounded, so that what a rounding adds to a weight it adds to the sum
 // too; o[n] channels U (4 j + i) + n of the row.  l is a row of ones among the
 // values: a matrix instruction adds it up.  m is a maximum of the scores so far,
-// but moves only when one passes it by kSlack: until then the weights are at
-// most 2^kSlack, and keep their 8 or 11 bits at any size.
-constexpr float kSlack = 8.0f;
+// but moves only when one passes it by the slack of reference_of.
 template <int D>
 struct State {
   float m, mc;
@@ -282,9 +280,10 @@ __device__ __forceinline__ void step(State<D>& st, Raw<D>& r, const u32x4* q, co
     }
   }
   const float top = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
-  if (__ballot(top * c > st.mc + kSlack)) {
+  constexpr spl::Reference ref = spl::reference_of(T{});
+  if (__ballot(top * c > st.mc + (ref.lift + ref.slack))) {
     const float m = fmaxf(st.m, spl::quad_max(top));
-    const float mc = m == -INFINITY ? -INFINITY : m * c;
+    const float mc = m == -INFINITY ? -INFINITY : m * c - ref.lift;
     const float alpha = m == -INFINITY ? 1.0f : spl::exp2_fast(st.mc - mc);
     st.l *= alpha;
 #pragma unroll

@@ -31,7 +31,6 @@ using spl::u32x4;
 constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * 64;
 constexpr int kRows = spl::kPrefillRows;         // of a workgroup
-constexpr float kSlack = 8.0f;                   // as for few rows: the reference moves by more than this only
 
 template <int D>
 struct Geom {
@@ -230,6 +229,8 @@ __device__ __forceinline__ void widen(uint8_t* lds, uint8_t* flags, Raw<D>& r, c
   }
 }
 
+// Per lane the row's m with mc = c m - lift (reference_of), the sum of the lane's
+// weights 2^(c s - mc), and the row's products with the values.
 template <int D>
 struct State {
   float m, mc, l;
@@ -286,8 +287,9 @@ __device__ __forceinline__ void multiply(State<D>& st, const uint8_t* lds, const
   for (int t = 0; t < kTiles; ++t)
 #pragma unroll
     for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
-  if (__ballot(top * c > st.mc + kSlack)) {
-    const float m = fmaxf(st.m, pair_max(top)), mc = m == -INFINITY ? -INFINITY : m * c;
+  constexpr spl::Reference ref = spl::reference_of(T{});
+  if (__ballot(top * c > st.mc + (ref.lift + ref.slack))) {
+    const float m = fmaxf(st.m, pair_max(top)), mc = m == -INFINITY ? -INFINITY : m * c - ref.lift;
     const float alpha = m == -INFINITY ? 1.0f : spl::exp2_fast(st.mc - mc);
     st.l *= alpha;
 #pragma unroll

@@ -1,0 +1,330 @@
+"""attention_fp4 on the GPU against the definition in 64 bits, over what the cache holds.
+
+Tolerance, element by element: a softmax weight is rounded once to the 16-bit type (u of it), and so is the result (u,
+or half the type's smallest step); where the sum of weights is taken before their rounding the same u enters once more: 3 u of sum p |v|.  A score is a sum
+of D fp32 products, off by at most 2^-20 of the sum of their sizes (its partial sums' roundings) for D <= 256, and an
+exponent's error is the weight's relative error, twice with the normalisation: 2^-18 (1 + that sum) more."""
+import pytest
+import torch
+
+import _attn_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+BF, HF = torch.bfloat16, torch.float16
+
+
+def _spl():
+    import paper_2405_03594_amd as spl
+
+    return spl
+
+
+class Batch:
+    """A filled cache and a batch over it; keys and values as the cache reads them back."""
+
+    def __init__(self, new, lens, H, Hk, D, page, dt, seed=0, fill=0xFF, scale_keys=1.0, extra=0):
+        spl = _spl()
+        g = torch.Generator().manual_seed(seed)
+        self.new, self.lens, self.dt = new, lens, dt
+        held = [-(-n // page) for n in lens]
+        pages = sum(held) + 2
+        self.cache = spl.KVCache.empty(pages, Hk, D, page, dt)
+        self.cache.data.fill_(fill)                              # what no token was stored in
+        ids = torch.randperm(pages, generator=g)
+        width = max(held + [1]) + extra
+        self.table = torch.full((len(lens), width), -1)
+        self.keys, self.values = [], []
+        n = 0
+        for r, m in enumerate(held):
+            self.table[r, :m] = ids[n:n + m]
+            n += m
+            L = lens[r]
+            k = (torch.randn(L, Hk, D, generator=g) * torch.exp(0.5 * torch.randn(1, Hk, D, generator=g)) * scale_keys)
+            v = torch.randn(L, Hk, D, generator=g) * torch.exp(torch.randn(L, Hk, 1, generator=g))
+            k, v = k.to(dt), v.to(dt)
+            if L:
+                at = torch.arange(L)
+                slots = (self.table[r, at // page] * page + at % page).int().cuda()
+                k, v = k.cuda(), v.cuda()
+                spl.qk_norm_rope_append(k, k, v, None, None, slots, self.cache)
+                k, v = (x.cpu().double() for x in spl.cache_read(self.cache, slots))
+            self.keys.append(k.double())
+            self.values.append(v.double())
+        self.table = self.table.int().cuda()
+        self.row_start = torch.tensor([sum(new[:i]) for i in range(len(new) + 1)])
+        self.q = torch.randn(sum(new), H, D, generator=g).to(dt)
+        self.D = D
+
+    def run(self, **kw):
+        args = dict(max_new=max(self.new), max_len=max(self.lens))
+        args.update(kw)
+        q = args.pop("q", None)
+        q = self.q.cuda() if q is None else q
+        lse = torch.full(q.shape[:2], 7.0, device="cuda")
+        out = torch.full(q.shape, 9.0, dtype=self.dt, device="cuda")
+        _spl().attention_fp4(q, self.cache, self.table, torch.tensor(self.lens).int().cuda(),
+                             self.row_start.int().cuda(), lse=lse, out=out, **args)
+        torch.cuda.synchronize()
+        return out.cpu().double(), lse.cpu().double()
+
+    def check(self, scale=None, window=0, **kw):
+        got, lse = self.run(scale=scale, window=window, **kw)
+        s = self.D ** -0.5 if scale is None else scale
+        want, want_lse, mag, top = ref.attention(self.q.double(), self.keys, self.values, self.row_start, self.lens, s,
+                                                 window)
+        loose = 2.0 ** -18 * (1 + top)
+        assert torch.equal(torch.isnan(got), torch.isnan(want))
+        bad = (got - want).abs().nan_to_num() > ((3 * ref.UNIT[self.dt] + loose) * mag).nan_to_num() + ref.STEP[self.dt]
+        assert not bad.any(), f"{int(bad.sum())} of {bad.numel()}, worst {float((got - want).abs().nan_to_num().max())}"
+        seen = torch.isfinite(want_lse)
+        assert torch.equal(torch.isneginf(lse), torch.isneginf(want_lse))
+        assert ((lse - want_lse)[seen].abs() <= 3 * ref.UNIT[self.dt] + loose).all()
+        return got
+
+
+@pytest.mark.parametrize("dt", [BF, HF])
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+@pytest.mark.parametrize("page", [16, 32, 64, 256])
+def test_decode(D, page, dt):
+    lens = [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 129, 300]
+    Batch([1] * len(lens), lens, 6, 2, D, page, dt).check()
+
+
+@pytest.mark.parametrize("H,Hk", [(1, 1), (8, 8), (8, 1), (16, 1), (15, 3), (32, 2), (17, 1), (40, 1), (64, 2)])
+def test_head_layouts(H, Hk):
+    Batch([1, 1, 1], [40, 7, 129], H, Hk, 64, 16, BF, seed=1).check()
+
+
+@pytest.mark.parametrize("dt", [BF, HF])
+def test_requests_that_see_nothing(dt):
+    """No tokens yet, no rows, fewer tokens than rows (the first rows stand before the request): zeros and -inf."""
+    b = Batch([1, 0, 3, 1, 5, 2], [0, 40, 3, 1, 2, 50], 4, 2, 64, 16, dt, seed=2)
+    got = b.check()
+    assert (got[0] == 0).all() and (got[5:8] == 0).all()          # 5 rows of a request of 2 tokens: the first 3
+    Batch([1], [0], 4, 2, 128, 16, dt).check()
+
+
+@pytest.mark.parametrize("window", [1, 5, 16, 33, 64, 100, 1000])
+@pytest.mark.parametrize("new", [[1, 1, 1], [9, 1, 40]])
+def test_windows(new, window):
+    Batch(new, [200, 70, 90], 4, 2, 64, 16, BF, seed=3).check(window=window)
+
+
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+@pytest.mark.parametrize("dt", [BF, HF])
+def test_chunks_of_prompts(D, dt):
+    Batch([5, 1, 17, 33, 1, 2], [5, 40, 100, 33, 1, 260], 6, 2, D, 32, dt, seed=4).check()
+
+
+@pytest.mark.parametrize("D,dt,H,Hk", [(64, HF, 8, 8), (96, BF, 24, 8), (128, BF, 16, 16), (128, HF, 12, 3)])
+@pytest.mark.parametrize("window", [0, 150])
+def test_the_kernel_for_many_rows(D, dt, H, Hk, window):
+    """Enough rows for a workgroup on every CU; prompts of odd lengths, one after other tokens, beside single rows."""
+    rows = 128 * torch.cuda.get_device_properties(0).multi_processor_count // H + 40
+    b = Batch([rows - 70, 1, 67, 1, 0, 2], [rows + 61, 300, 67, 1, 5, 2], H, Hk, D, 64, dt, seed=5)
+    big = b.run(window=window)
+    few = [r for r in range(6) if r != 0]
+    # the long prompt's rows are checked at places, the others all
+    pick = sorted({0, 1, 31, 32, 127, 128, rows - 72, rows - 71, *range(0, rows - 70, 97)})
+    at = torch.tensor(pick)
+    first = b.row_start[1]
+    want, want_lse, mag, top = ref.attention(b.q.double()[first:], [b.keys[r] for r in few], [b.values[r] for r in few],
+                                             b.row_start[1:] - first, [b.lens[r] for r in few], D ** -0.5, window)
+    loose = 2.0 ** -18 * (1 + top)
+    assert ((big[0][first:] - want).abs() <= (3 * ref.UNIT[dt] + loose) * mag + ref.STEP[dt]).all()
+    fin = torch.isfinite(want_lse)
+    assert ((big[1][first:] - want_lse)[fin].abs() <= 3 * ref.UNIT[dt] + loose).all()
+    for t in pick:
+        p = b.lens[0] - b.new[0] + t
+        w, l, m, top = ref.attention(b.q.double()[t:t + 1], b.keys[:1], b.values[:1], [0, 1], [p + 1], D ** -0.5, window)
+        tol = (3 * ref.UNIT[dt] + 2.0 ** -18 * (1 + top))
+        assert ((big[0][t] - w[0]).abs() <= tol * m[0] + ref.STEP[dt]).all(), t
+        assert ((big[1][t] - l[0]).abs() <= tol).all(), t
+
+
+def test_long_requests_are_split_and_joined():
+    b = Batch([1, 1, 1], [9000, 1, 700], 4, 2, 128, 128, BF, seed=6)
+    b.check()
+    b.check(max_len=0)                                           # not known: by the table's width
+    b.check(max_len=100)                                         # far too low a hint
+    b = Batch([3, 2], [5000, 2500], 8, 2, 64, 64, HF, seed=7, extra=30)
+    b.check()
+    b.check(max_new=0)                                           # not known: tiles are looked up
+    b.check(max_new=0, window=3000)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.2, 1.0, 3e-3])
+def test_scales(scale):
+    Batch([1, 20], [70, 45], 4, 4, 64, 16, BF, seed=8).check(scale=scale)
+
+
+def test_peaked_scores():
+    """Scores of some hundred: weights of 0 and 1, the reference moving at every step."""
+    Batch([1, 12], [400, 300], 4, 2, 128, 16, BF, seed=9, scale_keys=25.0).check()
+    Batch([1, 12], [400, 300], 4, 2, 128, 16, HF, seed=10, scale_keys=25.0).check()
+
+
+def _poison(b, r, t, head, keys, values):
+    """Stores NaN keys and/or infinite values for one token and head of request r (first 32 channels only)."""
+    spl = _spl()
+    page = b.cache.page
+    slot = (b.table[r, t // page].cpu() * page + t % page).int().view(1).cuda()
+    k, v = b.keys[r][t:t + 1].to(b.dt), b.values[r][t:t + 1].to(b.dt)
+    if keys:
+        k[0, head, 3] = float("nan")
+        b.keys[r][t, head, :32] = float("nan")
+    if values:
+        v[0, head, 5] = float("inf")
+        b.values[r][t, head, :32] = float("nan")
+    spl.qk_norm_rope_append(k.cuda(), k.cuda(), v.cuda(), None, None, slot, b.cache)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("keys,values", [(True, False), (False, True), (True, True)])
+def test_values_that_are_not_finite_reach_the_rows_that_see_them(D, keys, values):
+    b = Batch([1, 1, 8], [50, 60, 70], 4, 2, D, 16, BF, seed=11)
+    _poison(b, 1, 13, 1, keys, values)                           # seen by the one row, by the second pair of heads
+    _poison(b, 2, 66, 0, keys, values)                           # seen by the last 4 of 8 rows, by the first pair
+    got = b.check()
+    assert torch.isfinite(got[0]).all() and torch.isnan(got[1, 2:]).any() and torch.isfinite(got[1, :2]).all()
+    assert torch.isfinite(got[2:6]).all() and torch.isnan(got[6:, :2]).any() and torch.isfinite(got[6:, 2:]).all()
+    b.check(window=4)                                            # outside the window of the first
+
+
+@pytest.mark.parametrize("keys,values", [(True, False), (False, True)])
+def test_values_that_are_not_finite_among_many_rows(keys, values):
+    H, D = 16, 128
+    rows = 128 * torch.cuda.get_device_properties(0).multi_processor_count // H + 5
+    b = Batch([rows], [rows], H, H, D, 64, HF, seed=12)
+    clean = b.run()[0]
+    bad = rows - 150
+    _poison(b, 0, bad, 3, keys, values)
+    got = b.run()[0]
+    assert torch.equal(got[:bad], clean[:bad])                   # earlier rows and other heads do not change by a bit
+    others = [h for h in range(H) if h != 3]
+    assert torch.equal(got[:, others], clean[:, others])
+    part = got[bad:, 3]
+    assert torch.isnan(part[:, :32]).all()
+    assert torch.isnan(part[:, 32:]).all() if keys else torch.equal(part[:, 32:], clean[bad:, 3, 32:])
+
+
+@pytest.mark.parametrize("fill", [0x00, 0x7F, 0x8E, 0xFD, 0xFE])
+@pytest.mark.parametrize("dt", [BF, HF])
+def test_what_no_token_was_stored_in_does_not_matter(dt, fill):
+    Batch([1, 1, 9], [33, 17, 45], 4, 2, 128, 32, dt, seed=13, fill=fill).check()
+
+
+def test_pages_that_are_not_there_hold_no_keys():
+    b = Batch([1, 6, 1], [70, 90, 64], 4, 2, 64, 16, BF, seed=14)
+    b.table[0, 1], b.table[1, 2], b.table[1, 5], b.table[2, :] = -1, 10 ** 6, -5, -1
+    for r, gone in ((0, [1]), (1, [2, 5]), (2, [0, 1, 2, 3])):
+        for p in gone:
+            b.keys[r][16 * p:16 * p + 16] = float("nan")
+    got, lse = b.run()
+    for r in range(3):
+        for t in range(int(b.row_start[r]), int(b.row_start[r + 1])):
+            p = b.lens[r] - int(b.row_start[r + 1]) + t
+            seen = torch.isfinite(b.keys[r][:p + 1, 0, 0])
+            if not seen.any():
+                assert (got[t] == 0).all() and torch.isneginf(lse[t]).all()
+                continue
+            w, l, m, top = ref.attention(b.q.double()[t:t + 1], [b.keys[r][:p + 1][seen]], [b.values[r][:p + 1][seen]],
+                                         [0, 1], [int(seen.sum())], 0.125, 0)
+            assert ((got[t] - w[0]).abs() <= (3 * ref.UNIT[BF] + 2.0 ** -18 * (1 + top)) * m[0]).all()
+
+
+def test_strided_queries_and_rows_of_no_request():
+    b = Batch([2, 3], [40, 50], 4, 2, 64, 16, BF, seed=15)
+    want = b.run()[0]
+    wide = torch.zeros(5, 4 + 3, 64 + 8, dtype=BF, device="cuda")
+    wide[:, :4, :64] = b.q.cuda()
+    assert torch.equal(b.run(q=wide[:, :4, :64])[0], want)
+    flip = b.q.cuda().transpose(0, 1).contiguous().transpose(0, 1)
+    assert torch.equal(b.run(q=flip)[0], want)
+    padded = torch.cat((b.q, torch.zeros(9, 4, 64, dtype=BF))).cuda()
+    got, lse = b.run(q=padded)
+    assert torch.equal(got[:5], want) and (got[5:] == 9).all() and (lse[5:] == 7).all()
+    long = Batch([1, 1], [9000, 4], 4, 2, 64, 64, BF, seed=16)    # the same where the tokens are split
+    one = long.run()[0]
+    got, lse = long.run(q=torch.cat((long.q, torch.zeros(7, 4, 64, dtype=BF))).cuda())
+    assert torch.equal(got[:2], one) and (got[2:] == 9).all() and (lse[2:] == 7).all()
+
+
+def test_no_tokens():
+    spl = _spl()
+    cache = spl.KVCache.empty(1, 2, 64, 16, BF)
+    z = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out = spl.attention_fp4(torch.zeros(0, 4, 64, dtype=BF, device="cuda"), cache, z.view(1, 1), z, torch.cat((z, z)))
+    assert out.shape == (0, 4, 64)
+
+
+def test_the_same_call_gives_the_same_bits_on_any_stream():
+    b = Batch([1] * 9, [4000, 10, 999, 2500, 1, 64, 3000, 2000, 77], 8, 8, 128, 64, HF, seed=17)
+    first = b.run()
+    side = torch.cuda.Stream()
+    q, lens, rows = b.q.cuda(), torch.tensor(b.lens).int().cuda(), b.row_start.int().cuda()
+    torch.cuda.synchronize()
+    for stream in (None, side, side):
+        out = _spl().attention_fp4(q, b.cache, b.table, lens, rows, max_new=1, max_len=4000, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(out.cpu().double(), first[0])
+
+
+def test_a_serving_step_in_a_graph():
+    """Tables, append and attention of one token step captured once and replayed as the requests grow: every replay
+    against the eager calls, with other work between."""
+    spl = _spl()
+    R, H, Hk, D, page, dt = 5, 8, 2, 128, 16, BF
+    g = torch.Generator().manual_seed(18)
+    lens0 = [30, 1, 16, 47, 0]
+    width, pages = 8, 40
+    free = torch.randperm(pages, generator=g).int().cuda()
+    a = torch.arange(256, dtype=torch.float64)[:, None] * 10000.0 ** (-torch.arange(0, D, 2, dtype=torch.float64) / D)
+    rope = torch.stack((a.cos(), a.sin()), -1).float().cuda()
+    q = torch.randn(R, H, D, generator=g).to(dt).cuda()
+    kv = torch.randn(2, R, Hk, D, generator=g).to(dt).cuda()
+    w = torch.ones(D, dtype=dt, device="cuda")
+
+    def fresh():
+        cached, head = torch.tensor(lens0).int().cuda(), torch.zeros(1, dtype=torch.int32, device="cuda")
+        table = torch.full((R, width), -1, dtype=torch.int32, device="cuda")
+        cache = spl.KVCache.empty(pages, Hk, D, page, dt)
+        # the tokens before: zeros in pages of their own
+        p = spl.block_tables(torch.zeros_like(cached), cached, table, free, head, page, sum(lens0))
+        z = torch.zeros(sum(lens0), Hk, D, dtype=dt, device="cuda")
+        spl.qk_norm_rope_append(z, z, z, None, None, p.slots, cache)
+        return cached, p.free_head.clone(), table, cache
+
+    def step(cached, head, table, cache, new):
+        plan = spl.block_tables(cached, new, table, free, head, page, R)
+        qo = spl.qk_norm_rope_append(q, kv[0], kv[1], plan.positions, rope, plan.slots, cache, w, w)
+        out = spl.attention_fp4(qo, cache, table, plan.lens, plan.row_start, max_new=1, max_len=width * page)
+        cached.copy_(plan.lens)
+        head.copy_(plan.free_head)
+        return out, plan.missing
+
+    new = torch.ones(R, dtype=torch.int32, device="cuda")
+    state = fresh()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(*fresh(), new)
+    torch.cuda.current_stream().wait_stream(side)
+    eager = fresh()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, missing = step(*state, new)
+    for i in range(6):
+        q.normal_()
+        kv.normal_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        want, lost = step(*eager, new)
+        torch.cuda.synchronize()
+        assert int(missing) == 0 and int(lost) == 0
+        assert torch.equal(got, want), i
+        assert torch.equal(state[2], eager[2]) and torch.equal(state[3].data, eager[3].data)
+    assert eager[0].tolist() == [n + 6 for n in lens0]
