@@ -23,6 +23,7 @@ Names follow the C ABI without its ``spl_`` prefix:
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 
@@ -950,6 +951,9 @@ def dense_linear_int8_group(Xqs, x_scales, Wqs, w_scales, outs=None, acc_outs=No
 # ------------------------------------------------------------------------------ the attention half of a layer
 
 
+_HEAD_TYPES = (torch.float16, torch.bfloat16)
+
+
 class KVCache:
     """Keys and values in 4 bits (format and layout: spl_kv_cache), in pages of `page` tokens.
 
@@ -959,15 +963,16 @@ class KVCache:
     __slots__ = ("data", "pages", "heads", "page", "head_dim", "dtype", "_view")
 
     def __init__(self, data: torch.Tensor, page: int, head_dim: int, dtype: torch.dtype):
-        if dtype not in (torch.float16, torch.bfloat16):
+        if dtype not in _HEAD_TYPES:
             raise ValueError("a cache holds fp16 or bf16 keys and values")
         size = kv_page_bytes(head_dim, page)
         if not isinstance(data, torch.Tensor) or data.dim() != 3 or data.shape[2] != size:
             raise ValueError(f"data must be [pages, heads, {size}]")
-        _arg(data, "data", dtype=torch.uint8, device=False)
+        if data.dtype != torch.uint8 or not data.is_contiguous():
+            _arg(data, "data", dtype=torch.uint8, device=False)
         self.data, self.page, self.head_dim, self.dtype = data, page, head_dim, dtype
         self.pages, self.heads, _ = data.shape
-        self._view = _KVCache(data.data_ptr(), data.shape[0], data.numel(), page, data.shape[1], head_dim,
+        self._view = _KVCache(data.data_ptr(), self.pages, data.numel(), page, self.heads, head_dim,
                               _TORCH_DTYPE[dtype])
 
     @classmethod
@@ -976,6 +981,7 @@ class KVCache:
                    head_dim, dtype)
 
 
+@functools.lru_cache(maxsize=None)
 def kv_page_bytes(head_dim: int, page: int) -> int:
     """Bytes of one head's region of a page (see spl_kv_page_bytes)."""
     size = lib().spl_kv_page_bytes(head_dim, page)
@@ -983,6 +989,16 @@ def kv_page_bytes(head_dim: int, page: int) -> int:
         raise ValueError(f"no cache of {head_dim} channels in pages of {page} tokens: 64, 96, 128 or 256 channels, a "
                          "power of two from 16 to 256 tokens")
     return size
+
+
+@functools.lru_cache(maxsize=1024)
+def _attention_workspace(page, cache_heads, head_dim, tokens, heads, requests, width, max_new, max_len) -> int:
+    """spl_attention_fp4_workspace_bytes, a function of these sizes (and of the device, whose CUs are the same for all)."""
+    view = _KVCache(16, 1, 1 << 62, page, cache_heads, head_dim, F16)
+    need = lib().spl_attention_fp4_workspace_bytes(view, tokens, heads, requests, width, max_new, max_len)
+    if need < 0:
+        raise ValueError("spl_attention_fp4_workspace_bytes rejected the arguments")
+    return need
 
 
 @dataclass
@@ -1005,10 +1021,10 @@ def _on(stream) -> int:
     return stream.cuda_stream
 
 
-def _all_on_device(**tensors) -> None:
-    for name, t in tensors.items():
+def _on_device(names: str, *tensors) -> None:
+    for t in tensors:
         if t is not None and not t.is_cuda:
-            raise ValueError(f"{name} must be a device tensor")
+            raise ValueError(f"{names}: device tensors only")
 
 
 def _ints(t, name: str, n: int) -> int:
@@ -1048,7 +1064,7 @@ def block_tables(cached: torch.Tensor, new: torch.Tensor, table: torch.Tensor, f
     head = _ints(free_head, "free_head", 1)
     if tokens < 0:
         raise ValueError("tokens must not be negative")
-    _all_on_device(cached=cached, new=new, table=table, free_pages=free_pages, free_head=free_head)
+    _on_device("cached, new, table, free_pages, free_head", cached, new, table, free_pages, free_head)
     # one allocation for all results
     buf = torch.empty((2 * R + 2 * tokens + 3,), dtype=torch.int32, device=table.device)
     p = buf.data_ptr()
@@ -1064,18 +1080,18 @@ def _heads(x: torch.Tensor, name: str, tokens: int | None = None, dim: int | Non
     if not isinstance(x, torch.Tensor) or x.dim() != 3:
         raise ValueError(f"{name} must be [tokens, heads, dim]")
     T, H, D = x.shape
-    if (tokens is not None and T != tokens) or (dim is not None and D != dim):
-        raise ValueError(f"{name} has shape {tuple(x.shape)}, expected [{tokens}, heads, {dim}]")
-    if (x.dtype != dtype) if dtype is not None else (x.dtype not in (torch.float16, torch.bfloat16)):
-        raise ValueError(f"{name} has dtype {x.dtype}, expected {dtype or 'fp16 or bf16'}")
     st, sh, sd = x.stride()
     at = x.data_ptr()
-    if sd != 1 or (st | sh) & 7 or at & 15:
+    if (T == tokens or tokens is None) and (D == dim or dim is None) and (
+            x.dtype == dtype or (dtype is None and x.dtype in _HEAD_TYPES)):
+        if sd == 1 and not (st | sh) & 7 and not at & 15:
+            return _Heads(at, st, sh, H)
         st, sh = 0 if T <= 1 else st, 0 if H == 1 else sh
-        if (sd != 1 and D != 1) or (st | sh) & 7 or at & 15:
-            raise ValueError(f"{name}: channels must be contiguous, the other strides multiples of 8, the start "
-                             "16-byte aligned")
-    return _Heads(at, st, sh, H)
+        if (sd == 1 or D == 1) and not (st | sh) & 7 and not at & 15:
+            return _Heads(at, st, sh, H)
+        raise ValueError(f"{name}: channels must be contiguous, the other strides multiples of 8, the start 16-byte "
+                         "aligned")
+    raise ValueError(f"{name} is {x.dtype} {tuple(x.shape)}, expected {dtype or 'fp16 or bf16'} [{tokens}, heads, {dim}]")
 
 
 def _weight(w, name: str, dim: int, dtype) -> int | None:
@@ -1116,7 +1132,7 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor | Non
     hk = _heads(k, "k", T, D, q.dtype)
     wq, wk = _weight(q_weight, "q_weight", D, q.dtype), _weight(k_weight, "k_weight", D, q.dtype)
     at, angles, rows, rot = _turn_args(T, positions, rope)
-    _all_on_device(q=q, k=k, q_weight=q_weight, k_weight=k_weight, positions=positions, rope=rope)
+    _on_device("q, k, weights, positions, rope", q, k, q_weight, k_weight, positions, rope)
     q_out, k_out = _heads_out(q_out, q, "q_out"), _heads_out(k_out, k, "k_out")
     _check("spl_qk_norm_rope",
            lib().spl_qk_norm_rope(hq, hk, T, D, _TORCH_DTYPE[q.dtype], wq, wk, eps, at, angles, rows, rot, interleaved,
@@ -1140,7 +1156,7 @@ def qk_norm_rope_grad(dq: torch.Tensor, dk: torch.Tensor, q: torch.Tensor, k: to
         raise ValueError("a gradient has its input's heads")
     wq, wk = _weight(q_weight, "q_weight", D, q.dtype), _weight(k_weight, "k_weight", D, q.dtype)
     at, angles, rows, rot = _turn_args(T, positions, rope)
-    _all_on_device(q=q, k=k, dq=dq, dk=dk, q_weight=q_weight, k_weight=k_weight, positions=positions, rope=rope)
+    _on_device("q, k, dq, dk, weights, positions, rope", q, k, dq, dk, q_weight, k_weight, positions, rope)
     need = L.spl_qk_norm_rope_grad_workspace_bytes(T, H, hk.heads, D)
     if need < 0:
         raise ValueError("the workspace-size function rejected the shape")
@@ -1171,8 +1187,8 @@ def qk_norm_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, posit
     to = _ints(slots, "slots", T)
     wq, wk = _weight(q_weight, "q_weight", D, dtype), _weight(k_weight, "k_weight", D, dtype)
     at, angles, rows, rot = _turn_args(T, positions, rope)
-    _all_on_device(q=q, k=k, v=v, slots=slots, cache=cache.data, q_weight=q_weight, k_weight=k_weight,
-                   positions=positions, rope=rope)
+    _on_device("q, k, v, slots, the cache, weights, positions, rope", q, k, v, slots, cache.data, q_weight, k_weight,
+               positions, rope)
     q_out = _heads_out(q_out, q, "q_out")
     if k_out is not None:
         k_out = _heads_out(k_out, k, "k_out")
@@ -1188,7 +1204,7 @@ def cache_read(cache: KVCache, slots: torch.Tensor, stream=None):
         raise ValueError("slots must be 1-D")
     T = slots.shape[0]
     at = _ints(slots, "slots", T)
-    _all_on_device(slots=slots, cache=cache.data)
+    _on_device("slots, the cache", slots, cache.data)
     k = torch.empty((T, cache.heads, cache.head_dim), dtype=cache.dtype, device=slots.device)
     v = torch.empty_like(k)
     _check("spl_cache_read", lib().spl_cache_read(cache._view, at, T, k.data_ptr(), v.data_ptr(), _on(stream)))
@@ -1211,11 +1227,9 @@ def attention_fp4(q: torch.Tensor, cache: KVCache, table: torch.Tensor, lens: to
     ends, starts = _ints(lens, "lens", R), _ints(row_start, "row_start", R + 1)
     if lse is not None:
         _arg(lse, "lse", shape=(T, H), dtype=torch.float32, device=False)
-    _all_on_device(q=q, cache=cache.data, table=table, lens=lens, row_start=row_start, lse=lse)
+    _on_device("q, the cache, table, lens, row_start, lse", q, cache.data, table, lens, row_start, lse)
     out = _heads_out(out, q, "out")
-    need = L.spl_attention_fp4_workspace_bytes(view, T, H, R, width, max_new, max_len)
-    if need < 0:
-        raise ValueError("spl_attention_fp4_workspace_bytes rejected the arguments")
+    need = _attention_workspace(cache.page, cache.heads, D, T, H, R, width, max_new, max_len)
     ws = _workspace_on(need, q.device, stream) if need else None
     _check("spl_attention_fp4",
            L.spl_attention_fp4(hq, T, view, table.data_ptr(), R, width, ends, starts, max_new, max_len,
