@@ -117,6 +117,16 @@ __device__ __forceinline__ Rows rows_of(const AttnArgs& a, int64_t r) {
   return {s, (int32_t)(e - s), (int32_t)len};
 }
 
+// The same for a request that is the wave's: scalar loads, all at once.
+__device__ __forceinline__ Rows wave_rows_of(const AttnArgs& a, int32_t r) {
+  const int32_t t = (int32_t)a.tokens, most = (int32_t)(a.width * a.cache.page);          // < 2^31
+  int32_t s = uniform_load(a.row_start + r), e = uniform_load(a.row_start + r + 1), len = uniform_load(a.lens + r);
+  s = s < 0 ? 0 : (s > t ? t : s);
+  e = e < s ? s : (e > t ? t : e);
+  len = len < 0 ? 0 : (len > most ? most : len);
+  return {s, e - s, len};
+}
+
 // The request that owns tile `tile` when each of more than `few` rows (rows *
 // group) has ceil(rows * group / size) tiles, and the tile's number in it;
 // request -1 past the last.  Every lane of the wave calls it with the same tile.

@@ -52,17 +52,19 @@ struct Raw {
   uint32_t vs[2];
 };
 
-// Page numbers of the step's two halves of 16 tokens; -1: none there.
+// Page numbers of the step's two halves of 16 tokens; -1: none there.  What the
+// table holds past the request's pages may be anything: tokens are masked by the
+// length.
 struct Where {
   int32_t page[2];
 };
 
-__device__ __forceinline__ Where where(const AttnArgs& a, const int32_t* table, int32_t t0, int32_t len, int shift) {
+__device__ __forceinline__ Where where(const AttnArgs& a, const int32_t* table, int32_t t0, int shift) {
   Where w;
+  const int32_t last = (int32_t)a.width - 1;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const int32_t t = t0 + 16 * h;
-    const int32_t p = t < len ? spl::uniform_load(table + (t >> shift)) : -1;
+    const int32_t at = (t0 + 16 * h) >> shift, p = spl::uniform_load(table + (at < last ? at : last));
     w.page[h] = p >= 0 && p < a.cache.pages ? p : -1;
   }
   return w;
@@ -349,12 +351,20 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 3) void k_attn_rows(Att
   spl::Tile tile{place, 0};
   if (!direct) tile = spl::find_tile(a, group, kRows, 0, place);
   else if (snake > 0) tile.request = ranked_request(a, place, snake);
-  const int64_t req = __builtin_amdgcn_readfirstlane((int)tile.request);
+  const int32_t req = __builtin_amdgcn_readfirstlane((int)tile.request);
   if (req < 0) return;
-  spl::Rows rows = spl::rows_of(a, req);
-  rows.first = __builtin_amdgcn_readfirstlane((int)rows.first);
-  rows.count = __builtin_amdgcn_readfirstlane(rows.count);
-  rows.len = __builtin_amdgcn_readfirstlane(rows.len);
+  const int32_t* table = a.table + req * a.width;
+  const int shift = __builtin_ctz((unsigned)a.cache.page);
+  const LaneOff off = lane_off<D>(a.cache.page, lane);
+  // where the first step is known without the lengths, its data are requested before they are
+  Raw<D> r0, r1;
+  Where w0, w1;
+  const bool early = direct && splits == 1 && a.window == 0;
+  if (early) {
+    w0 = where(a, table, wave * kStep, shift);
+    load_step<D>(r0, a, head, wave * kStep, w0, off, lane);
+  }
+  const spl::Rows rows = spl::wave_rows_of(a, req);
   const int32_t row0 = __builtin_amdgcn_readfirstlane((int)tile.index) * kRows, all = rows.count * group;
   if (row0 >= all || all > most) return;         // more rows than most: another kernel's
   const int n = all - row0 < kRows ? all - row0 : kRows;                   // rows of this tile
@@ -372,8 +382,6 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 3) void k_attn_rows(Att
   view.low = ts.low;
   view.high = ts.high;
   view.window = a.window;
-  const int32_t* table = a.table + req * a.width;
-  const int shift = __builtin_ctz((unsigned)a.cache.page);
 
   u32x4 q[Gm::G];
   {
@@ -392,19 +400,16 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 3) void k_attn_rows(Att
   st.l = f32x4{0, 0, 0, 0};
 #pragma unroll
   for (int i = 0; i < Gm::U; ++i) st.o[i] = f32x4{0, 0, 0, 0};
-  const LaneOff off = lane_off<D>(a.cache.page, lane);
 
   int32_t i = from + wave;
   if (i < to) {
     // the next step's data are requested before this one's are used (two steps ahead gained nothing)
-    Raw<D> r0, r1;
-    Where w0, w1;
     const auto fetch = [&](Raw<D>& r, Where& w, int32_t k) {
       k = k < to ? k : i;
-      w = where(a, table, (s0 + k) * kStep, rows.len, shift);
+      w = where(a, table, (s0 + k) * kStep, shift);
       load_step<D>(r, a, head, (s0 + k) * kStep, w, off, lane);
     };
-    fetch(r0, w0, i);
+    if (!early) fetch(r0, w0, i);
     const auto turn = [&](Raw<D>& now, Where& wn, Raw<D>& ahead, Where& wa) {
       fetch(ahead, wa, i + kWaves);
       step<T, D>(st, now, q, view, (s0 + i) * kStep, wn, rows.len, c, lane);

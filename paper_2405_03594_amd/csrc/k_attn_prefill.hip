@@ -345,12 +345,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_prefill(AttnArgs a, int gr
   // the tiles that see the most first
   const spl::Tile tile = a.requests == 1 ? spl::Tile{0, tiles - 1 - place}
                                          : spl::find_tile(a, group, kRows, spl::kFewRows, tiles - 1 - place);
-  const int64_t req = __builtin_amdgcn_readfirstlane((int)tile.request);
+  const int32_t req = __builtin_amdgcn_readfirstlane((int)tile.request);
   if (req < 0) return;
-  spl::Rows rows = spl::rows_of(a, req);
-  rows.first = __builtin_amdgcn_readfirstlane((int)rows.first);
-  rows.count = __builtin_amdgcn_readfirstlane(rows.count);
-  rows.len = __builtin_amdgcn_readfirstlane(rows.len);
+  const spl::Rows rows = spl::wave_rows_of(a, req);
   const int32_t row0 = __builtin_amdgcn_readfirstlane((int)tile.index) * kRows, all = rows.count * group;
   if (row0 >= all) return;
   const int32_t end_row = all - row0 < kRows ? all : row0 + kRows;
