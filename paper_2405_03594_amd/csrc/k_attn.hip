@@ -33,6 +33,7 @@ constexpr int kWaves = 4;
 constexpr int kGroupsPerCu = 2;
 constexpr int kMaxSplits = 64;
 constexpr int kMinChunk = 16;
+constexpr int kWideSteps = 64;
 
 template <int D>
 struct Geom {
@@ -186,17 +187,25 @@ __device__ __forceinline__ void load_step(Raw<D>& r, const AttnArgs& a, int head
   }
 }
 
-// S^T of the step: s[i] is token token_of(j, i) against the lane's query row.
-template <class T, int D>
-__device__ __forceinline__ void scores(const Raw<D>& r, const u32x4* q, float* s) {
+// S^T of the step: s[r][i] is token token_of(j, i) against the lane's query row
+// of tile r.
+template <class T, int D, int R>
+__device__ __forceinline__ void scores(const Raw<D>& r, const u32x4 (&q)[R][Geom<D>::G], float (&s)[R][8]) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    f32x4 acc = {0, 0, 0, 0};
+    f32x4 acc[R];
 #pragma unroll
-    for (int g = 0; g < Geom<D>::G; ++g)
-      acc = spl::mfma16(T{}, spl::cvt8<T>(r.k[h][g], spl::scale_of(r.ks[h][g / 4], g % 4)), q[g], acc);
+    for (int t = 0; t < R; ++t) acc[t] = f32x4{0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s[4 * h + i] = acc[i];
+    for (int g = 0; g < Geom<D>::G; ++g) {
+      const u32x4 k = spl::cvt8<T>(r.k[h][g], spl::scale_of(r.ks[h][g / 4], g % 4));
+#pragma unroll
+      for (int t = 0; t < R; ++t) acc[t] = spl::mfma16(T{}, k, q[t][g], acc[t]);
+    }
+#pragma unroll
+    for (int t = 0; t < R; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[t][4 * h + i] = acc[t][i];
   }
 }
 
@@ -235,32 +244,36 @@ struct State {
   f32x4 o[Geom<D>::U];
 };
 
+template <int R>
 struct RowView {
-  int32_t pos;                                   // of the lane's row; -1: sees nothing
+  int32_t pos[R], first[R];                      // what the lane's rows see: [first, pos]
   int32_t low, high;                             // the least and the most of the tile's
   int32_t window;
 };
 
-template <class T, int D>
-__device__ __forceinline__ void step(State<D>& st, Raw<D>& r, const u32x4* q, const RowView& v, int32_t t0,
-                                     const Where& w, int32_t len, float c, int lane) {
+template <class T, int D, int R>
+__device__ __forceinline__ void step(State<D> (&st)[R], Raw<D>& r, const u32x4 (&q)[R][Geom<D>::G],
+                                     const RowView<R>& v, int32_t t0, const Where& w, int32_t len, float c, int lane) {
   using Gm = Geom<D>;
   const int j = lane >> 4;
   const bool whole = w.page[0] >= 0 && w.page[1] >= 0 && t0 + kStep - 1 <= v.low && t0 + kStep <= len &&
                      (v.window == 0 || t0 > v.high - v.window);
-  float s[8];
-  scores<T, D>(r, q, s);
-  uint32_t poison = 0;                           // groups of 32 channels in which the row sees a NaN (rare)
+  float s[R][8];
+  scores<T, D, R>(r, q, s);
+  uint32_t poison[R] = {};                       // groups of 32 channels in which the row sees a NaN (rare)
   if (!whole) {
-    uint32_t seen = 0;
+    uint32_t seen[R] = {};
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int at = token_of<D>(j, i);
       const int32_t t = t0 + at;
-      const bool see = (at < 16 ? w.page[0] : w.page[1]) >= 0 && t < len && t <= v.pos &&
-                       (v.window == 0 || t > v.pos - v.window);
-      seen |= see ? 1u << i : 0u;
-      s[i] = see ? s[i] : -INFINITY;
+      const bool here = ((at < 16 ? w.page[0] : w.page[1]) >= 0) & (t < len);
+#pragma unroll
+      for (int k = 0; k < R; ++k) {
+        const bool see = here & (t <= v.pos[k]) & (t >= v.first[k]);
+        seen[k] |= see ? 1u << i : 0u;
+        s[k][i] = see ? s[k][i] : -INFINITY;
+      }
     }
     // values that some row does not see must not reach it as 0 * NaN: take what
     // is not finite out of the product and put NaNs where it is seen
@@ -275,47 +288,62 @@ __device__ __forceinline__ void step(State<D>& st, Raw<D>& r, const u32x4* q, co
       for (int g = 0; g < Gm::G; ++g) {
         const int from = (lane & 48) + g * 32 / Gm::U;           // a lane of the same tokens that holds group g
         const uint32_t b = __shfl(bad, from);
-        if (b & seen) poison |= 1u << g;
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+          if (b & seen[k]) poison[k] |= 1u << g;
       }
-      poison |= __shfl_xor(poison, 16);
-      poison |= __shfl_xor(poison, 32);
+#pragma unroll
+      for (int k = 0; k < R; ++k) {
+        poison[k] |= __shfl_xor(poison[k], 16);
+        poison[k] |= __shfl_xor(poison[k], 32);
+      }
     }
   }
-  const float top = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
   constexpr spl::Reference ref = spl::reference_of(T{});
-  if (__ballot(top * c > st.mc + (ref.lift + ref.slack))) {
-    const float m = fmaxf(st.m, spl::quad_max(top));
-    const float mc = m == -INFINITY ? -INFINITY : m * c - ref.lift;
-    const float alpha = m == -INFINITY ? 1.0f : spl::exp2_fast(st.mc - mc);
-    st.l *= alpha;
-#pragma unroll
-    for (int n = 0; n < Gm::U; ++n) st.o[n] *= alpha;
-    st.m = m;
-    st.mc = mc;
-  }
-  const float base = st.m == -INFINITY ? 0.0f : -st.mc;
-  float p[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) p[i] = spl::exp2_fast(__builtin_fmaf(s[i], c, base));
-  u32x4 pf;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) pf[i] = spl::pack2(T{}, p[2 * i], p[2 * i + 1]);
   constexpr uint32_t kOne = T::code == SPL_F16 ? 0x3c003c00u : 0x3f803f80u;
-  st.l = spl::mfma16(T{}, u32x4{kOne, kOne, kOne, kOne}, pf, st.l);
+  u32x4 pf[R];
+#pragma unroll
+  for (int k = 0; k < R; ++k) {
+    const float* x = s[k];
+    const float top =
+        fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+    if (__ballot(top * c > st[k].mc + (ref.lift + ref.slack))) {
+      const float m = fmaxf(st[k].m, spl::quad_max(top));
+      const float mc = m == -INFINITY ? -INFINITY : m * c - ref.lift;
+      const float alpha = m == -INFINITY ? 1.0f : spl::exp2_fast(st[k].mc - mc);
+      st[k].l *= alpha;
+#pragma unroll
+      for (int n = 0; n < Gm::U; ++n) st[k].o[n] *= alpha;
+      st[k].m = m;
+      st[k].mc = mc;
+    }
+    const float base = st[k].m == -INFINITY ? 0.0f : -st[k].mc;
+    float p[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = spl::exp2_fast(__builtin_fmaf(x[i], c, base));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) pf[k][i] = spl::pack2(T{}, p[2 * i], p[2 * i + 1]);
+    st[k].l = spl::mfma16(T{}, u32x4{kOne, kOne, kOne, kOne}, pf[k], st[k].l);
+  }
 #pragma unroll
   for (int n = 0; n < Gm::U; n += 2) {
     u32x4 even, odd;
     value_pair<T, D>(r, n / 2, even, odd);
-    st.o[n] = spl::mfma16(T{}, even, pf, st.o[n]);
-    st.o[n + 1] = spl::mfma16(T{}, odd, pf, st.o[n + 1]);
-  }
-  if (poison) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (poison >> (Gm::U * (4 * j + i) / 32) & 1)
-#pragma unroll
-        for (int n = 0; n < Gm::U; ++n) st.o[n][i] = NAN;
+    for (int k = 0; k < R; ++k) {
+      st[k].o[n] = spl::mfma16(T{}, even, pf[k], st[k].o[n]);
+      st[k].o[n + 1] = spl::mfma16(T{}, odd, pf[k], st[k].o[n + 1]);
+    }
   }
+#pragma unroll
+  for (int k = 0; k < R; ++k)
+    if (poison[k]) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (poison[k] >> (Gm::U * (4 * j + i) / 32) & 1)
+#pragma unroll
+          for (int n = 0; n < Gm::U; ++n) st[k].o[n][i] = NAN;
+    }
 }
 
 // The request that place `at` of the launch serves when the workgroups of
@@ -336,70 +364,60 @@ __device__ __forceinline__ int64_t ranked_request(const AttnArgs& a, int at, int
   return who ? __builtin_ctzll(who) : -1;
 }
 
-// One workgroup: a tile of rows, a key head, one of the splits of its tokens.
-// The four waves take every fourth step and are joined through LDS.
-template <class T, int D>
-__global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 3) void k_attn_rows(AttnArgs a, int group, int direct,
-                                                                            int splits, int chunk, int snake, int most) {
+// What the waves of a workgroup pass to each other at the end.
+template <int D>
+struct Shared {
+  float o[2][Geom<D>::U * 4][64];
+  float m[kWaves][kRows], l[kWaves][kRows];
+};
+
+// One workgroup's work: R tiles of 16 rows of a request from row0 on, a key
+// head, one of the splits of their tokens.  The four waves take every fourth
+// step and are joined through LDS.  early: r0 holds the first step already.
+template <class T, int D, int R>
+__device__ __forceinline__ void rows_of_tile(const AttnArgs& a, Shared<D>& lds, int group, int head, int split,
+                                             int splits, int chunk, int32_t req, const spl::Rows& rows, int32_t row0,
+                                             bool early, Raw<D>& r0, Where& w0, const LaneOff& off, int lane,
+                                             int wave) {
   using Gm = Geom<D>;
-  __shared__ float o_s[2][Gm::U * 4][64];
-  __shared__ float m_s[kWaves][kRows], l_s[kWaves][kRows];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // heads fastest: consecutive workgroups go to different XCDs, so each has a
-  // share of every request, however their lengths differ
-  const int place = blockIdx.x / a.cache.heads, head = blockIdx.x - place * a.cache.heads, split = blockIdx.y;
-  spl::Tile tile{place, 0};
-  if (!direct) tile = spl::find_tile(a, group, kRows, 0, place);
-  else if (snake > 0) tile.request = ranked_request(a, place, snake);
-  const int32_t req = __builtin_amdgcn_readfirstlane((int)tile.request);
-  if (req < 0) return;
-  const int32_t* table = a.table + req * a.width;
-  const int shift = __builtin_ctz((unsigned)a.cache.page);
-  const LaneOff off = lane_off<D>(a.cache.page, lane);
-  // where the first step is known without the lengths, its data are requested before they are
-  Raw<D> r0, r1;
-  Where w0, w1;
-  const bool early = direct && splits == 1 && a.window == 0;
-  if (early) {
-    w0 = where(a, table, wave * kStep, shift);
-    load_step<D>(r0, a, head, wave * kStep, w0, off, lane);
-  }
-  const spl::Rows rows = spl::wave_rows_of(a, req);
-  const int32_t row0 = __builtin_amdgcn_readfirstlane((int)tile.index) * kRows, all = rows.count * group;
-  if (row0 >= all || all > most) return;         // more rows than most: another kernel's
-  const int n = all - row0 < kRows ? all - row0 : kRows;                   // rows of this tile
+  const int32_t all = rows.count * group;
+  const int n = all - row0 < R * kRows ? all - row0 : R * kRows;
   const int m16 = lane & 15, j = lane >> 4;
   const int32_t first_pos = rows.len - rows.count;
-  const int32_t row = row0 + (m16 < n ? m16 : n - 1), tok = row / group;
-  const int64_t t_row = rows.first + tok, h_row = head * group + (row - tok * group);
+  const int32_t* table = a.table + req * a.width;
+  const int shift = __builtin_ctz((unsigned)a.cache.page);
   const spl::Span ts = spl::tile_span(rows, row0, row0 + n, group, a.window, kStep, splits, chunk);
   const int32_t s0 = ts.s0, from = split * ts.share;
   const int32_t to = from + ts.share < ts.steps ? from + ts.share : ts.steps;
   const bool only = ts.steps <= ts.share;        // the tile is one split's
   if (split > 0 && from >= ts.steps) return;
-  RowView view;
-  view.pos = m16 < n ? first_pos + tok : -1;
+  RowView<R> view;
   view.low = ts.low;
   view.high = ts.high;
   view.window = a.window;
-
-  u32x4 q[Gm::G];
-  {
-    const uint16_t* at = static_cast<const uint16_t*>(a.q.data) + t_row * a.q.token_stride + h_row * a.q.head_stride;
-#pragma unroll
-    for (int g = 0; g < Gm::G; ++g) q[g] = *reinterpret_cast<const u32x4*>(at + 32 * g + 8 * j);
-  }
   // the scores' factor is taken positive: its sign goes to q, and 0 makes all scores 0
   float c = fabsf(a.scale) * spl::kLog2e;
   const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u, keep = c > 0.0f ? 0xffffffffu : 0u;
-#pragma unroll
-  for (int g = 0; g < Gm::G; ++g) q[g] = (q[g] ^ flip) & keep;
   c = c > 0.0f ? c : 1.0f;
-  State<D> st;
-  st.m = st.mc = -INFINITY;
-  st.l = f32x4{0, 0, 0, 0};
+  u32x4 q[R][Gm::G];
+  State<D> st[R];
 #pragma unroll
-  for (int i = 0; i < Gm::U; ++i) st.o[i] = f32x4{0, 0, 0, 0};
+  for (int k = 0; k < R; ++k) {
+    const int at = 16 * k + m16;
+    const int32_t row = row0 + (at < n ? at : n - 1), tok = row / group;
+    view.pos[k] = at < n ? first_pos + tok : -1;
+    view.first[k] = a.window > 0 ? view.pos[k] - a.window + 1 : 0;
+    const uint16_t* x = static_cast<const uint16_t*>(a.q.data) + (rows.first + tok) * a.q.token_stride +
+                        (int64_t)(head * group + (row - tok * group)) * a.q.head_stride;
+#pragma unroll
+    for (int g = 0; g < Gm::G; ++g) q[k][g] = *reinterpret_cast<const u32x4*>(x + 32 * g + 8 * j);
+#pragma unroll
+    for (int g = 0; g < Gm::G; ++g) q[k][g] = (q[k][g] ^ flip) & keep;
+    st[k].m = st[k].mc = -INFINITY;
+    st[k].l = f32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < Gm::U; ++i) st[k].o[i] = f32x4{0, 0, 0, 0};
+  }
 
   int32_t i = from + wave;
   if (i < to) {
@@ -409,10 +427,12 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 3) void k_attn_rows(Att
       w = where(a, table, (s0 + k) * kStep, shift);
       load_step<D>(r, a, head, (s0 + k) * kStep, w, off, lane);
     };
+    Raw<D> r1;
+    Where w1;
     if (!early) fetch(r0, w0, i);
     const auto turn = [&](Raw<D>& now, Where& wn, Raw<D>& ahead, Where& wa) {
       fetch(ahead, wa, i + kWaves);
-      step<T, D>(st, now, q, view, (s0 + i) * kStep, wn, rows.len, c, lane);
+      step<T, D, R>(st, now, q, view, (s0 + i) * kStep, wn, rows.len, c, lane);
       i += kWaves;
     };
     while (true) {
@@ -423,94 +443,143 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 3) void k_attn_rows(Att
     }
   }
 
-  // join the waves
-  if (lane < kRows) m_s[wave][lane] = st.mc, l_s[wave][lane] = st.l[0];
-  __syncthreads();
-  float top = m_s[0][m16];
+  const spl::Parts part = spl::parts_of(a, D, splits);
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) top = fmaxf(top, m_s[w][m16]);
-  const auto weight = [&](float m) { return m == -INFINITY ? 0.0f : spl::exp2_fast(m - top); };
-  float total = 0;
+  for (int k = 0; k < R; ++k) {
+    State<D>& x = st[k];
+    // join the waves
+    if (lane < kRows) lds.m[wave][lane] = x.mc, lds.l[wave][lane] = x.l[0];
+    __syncthreads();
+    float top = lds.m[0][m16];
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) total += l_s[w][m16] * weight(m_s[w][m16]);
-  const float mine = weight(st.mc);
+    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, lds.m[w][m16]);
+    const auto weight = [&](float m) { return m == -INFINITY ? 0.0f : spl::exp2_fast(m - top); };
+    float total = 0;
 #pragma unroll
-  for (int k = 0; k < Gm::U; ++k) st.o[k] *= mine;
-  const auto give = [&](int buf) {
+    for (int w = 0; w < kWaves; ++w) total += lds.l[w][m16] * weight(lds.m[w][m16]);
+    const float mine = weight(x.mc);
 #pragma unroll
-    for (int k = 0; k < Gm::U; ++k)
+    for (int i = 0; i < Gm::U; ++i) x.o[i] *= mine;
+    const auto give = [&](int buf) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o_s[buf][4 * k + e][lane] = st.o[k][e];
-  };
-  const auto take = [&](int buf) {
+      for (int i = 0; i < Gm::U; ++i)
 #pragma unroll
-    for (int k = 0; k < Gm::U; ++k)
+        for (int e = 0; e < 4; ++e) lds.o[buf][4 * i + e][lane] = x.o[i][e];
+    };
+    const auto take = [&](int buf) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) st.o[k][e] += o_s[buf][4 * k + e][lane];
-  };
-  if (wave >= 2) give(wave - 2);
-  __syncthreads();
-  if (wave < 2) take(wave);
-  __syncthreads();
-  if (wave == 1) give(0);
-  __syncthreads();
-  if (wave != 0) return;
-  take(0);
-  if (m16 >= n) return;
-
-  const int64_t out_row = t_row * a.q.heads + h_row;
-  const spl::Parts w = spl::parts_of(a, D, splits);
-  if (splits > 1 && split == 0 && j == 1) w.counts[out_row] = only ? 1 : (ts.steps + ts.share - 1) / ts.share;
-  if (!only) {
-    const int64_t at = out_row * splits + split;
-    float* part = w.sums;
-    if (j == 0) w.stats[2 * at] = top, w.stats[2 * at + 1] = total;
+      for (int i = 0; i < Gm::U; ++i)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int ch = Gm::U * (4 * j + e);
-      if (ch >= D) break;
+        for (int e = 0; e < 4; ++e) x.o[i][e] += lds.o[buf][4 * i + e][lane];
+    };
+    if (wave >= 2) give(wave - 2);
+    __syncthreads();
+    if (wave < 2) take(wave);
+    __syncthreads();
+    if (wave == 1) give(0);
+    __syncthreads();
+    const int32_t at_row = 16 * k + m16;
+    if (wave == 0) take(0);
+    if (wave == 0 && at_row < n) {
+      const int32_t row = row0 + at_row, tok = row / group;
+      const int64_t out_row = (rows.first + tok) * a.q.heads + head * group + (row - tok * group);
+      if (splits > 1 && split == 0 && j == 1) part.counts[out_row] = only ? 1 : (ts.steps + ts.share - 1) / ts.share;
+      if (!only) {
+        const int64_t at = out_row * splits + split;
+        if (j == 0) part.stats[2 * at] = top, part.stats[2 * at + 1] = total;
 #pragma unroll
-      for (int k = 0; k < Gm::U; k += 4)
-        *reinterpret_cast<f32x4*>(part + at * D + ch + k) =
-            f32x4{st.o[k][e], st.o[k + 1][e], st.o[k + 2][e], st.o[k + 3][e]};
+        for (int e = 0; e < 4; ++e) {
+          const int ch = Gm::U * (4 * j + e);
+          if (ch >= D) break;
+#pragma unroll
+          for (int i = 0; i < Gm::U; i += 4)
+            *reinterpret_cast<f32x4*>(part.sums + at * D + ch + i) =
+                f32x4{x.o[i][e], x.o[i + 1][e], x.o[i + 2][e], x.o[i + 3][e]};
+        }
+      } else {
+        const float inv = total == 0.0f ? 0.0f : 1.0f / total;   // no key: 0 (a NaN stays one)
+        uint16_t* out = static_cast<uint16_t*>(a.out) + out_row * D;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int ch = Gm::U * (4 * j + e);
+          if (ch >= D) break;
+#pragma unroll
+          for (int i = 0; i < Gm::U; i += 4) {
+            u32x2 v;
+            v[0] = spl::pack2(T{}, x.o[i][e] * inv, x.o[i + 1][e] * inv);
+            v[1] = spl::pack2(T{}, x.o[i + 2][e] * inv, x.o[i + 3][e] * inv);
+            *reinterpret_cast<u32x2*>(out + ch + i) = v;
+          }
+        }
+        if (a.lse && j == 0)
+          a.lse[out_row] = total == 0.0f ? -INFINITY : (top + log2f(total)) * 0.6931471805599453f;
+      }
     }
-    return;
+    if (k + 1 < R) __syncthreads();
   }
-  const float inv = total == 0.0f ? 0.0f : 1.0f / total;         // no key: 0 (a NaN stays one)
-  uint16_t* out = static_cast<uint16_t*>(a.out) + out_row * D;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const int ch = Gm::U * (4 * j + e);
-    if (ch >= D) break;
-#pragma unroll
-    for (int k = 0; k < Gm::U; k += 4) {
-      u32x2 v;
-      v[0] = spl::pack2(T{}, st.o[k][e] * inv, st.o[k + 1][e] * inv);
-      v[1] = spl::pack2(T{}, st.o[k + 2][e] * inv, st.o[k + 3][e] * inv);
-      *reinterpret_cast<u32x2*>(out + ch + k) = v;
-    }
-  }
-  if (a.lse && j == 0) a.lse[out_row] = total == 0.0f ? -INFINITY : (top + log2f(total)) * 0.6931471805599453f;
 }
 
-// The splits of a row joined: a workgroup a row, its eight waves sharing the
-// splits, D / 64 channels a lane.  A lane knows the statistics of one split.
+// R: tiles of 16 rows that a workgroup takes where the request has them.
+template <class T, int D, int R>
+__global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : (R == 1 ? 3 : 2)) void k_attn_rows(
+    AttnArgs a, int group, int direct, int all_splits, int chunk, int snake, int most) {
+  const int splits = R == 1 ? all_splits : 1;    // enough workgroups: not split
+  __shared__ Shared<D> lds;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // heads fastest: consecutive workgroups go to different XCDs, so each has a
+  // share of every request, however their lengths differ
+  const int place = blockIdx.x / a.cache.heads, head = blockIdx.x - place * a.cache.heads, split = blockIdx.y;
+  spl::Tile tile{place, 0};
+  if (!direct) tile = spl::find_tile(a, group, R * kRows, 0, place);
+  else if (snake > 0) tile.request = ranked_request(a, place, snake);
+  const int32_t req = __builtin_amdgcn_readfirstlane((int)tile.request);
+  if (req < 0) return;
+  const LaneOff off = lane_off<D>(a.cache.page, lane);
+  // where the first step is known without the lengths, its data are requested before they are
+  Raw<D> r0;
+  Where w0;
+  const bool early = R == 1 && direct && splits == 1 && a.window == 0;
+  if (early) {
+    w0 = where(a, a.table + req * a.width, wave * kStep, __builtin_ctz((unsigned)a.cache.page));
+    load_step<D>(r0, a, head, wave * kStep, w0, off, lane);
+  }
+  const spl::Rows rows = spl::wave_rows_of(a, req);
+  const int32_t row0 = __builtin_amdgcn_readfirstlane((int)tile.index) * (R * kRows), all = rows.count * group;
+  if (row0 >= all || all > most) return;         // more rows than most: another kernel's
+  if (R > 1 && all - row0 > kRows)
+    rows_of_tile<T, D, R>(a, lds, group, head, split, splits, chunk, req, rows, row0, early, r0, w0, off, lane, wave);
+  else
+    rows_of_tile<T, D, 1>(a, lds, group, head, split, splits, chunk, req, rows, row0, early, r0, w0, off, lane, wave);
+}
+
+// The splits of a row joined: a workgroup a row (per > 0: of the first `per` of a
+// request and key head, if it has no more), its eight waves sharing the splits,
+// D / 64 channels a lane.  A lane knows the statistics of one split.
 // Loads go out in two rounds: the counts and statistics, then all sums.
 constexpr int kJoinWaves = 8;
 template <class T, int D>
-__global__ __launch_bounds__(kJoinWaves * 64) void k_attn_join(AttnArgs a, int splits) {
+__global__ __launch_bounds__(kJoinWaves * 64) void k_attn_join(AttnArgs a, int splits, int group, int per) {
   constexpr int C = D == 256 ? 4 : 2;                            // channels of a lane; D 64 and 96 leave lanes idle
   typedef float vec __attribute__((ext_vector_type(C)));
   __shared__ vec o_s[kJoinWaves - 1][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t row = blockIdx.x;
   const spl::Parts p = spl::parts_of(a, D, splits);
-  const int32_t t = (int32_t)blockIdx.x / a.q.heads;             // tokens * heads < 2^31
-  const int32_t t0 = a.row_start[0], t1 = a.row_start[a.requests];
+  int64_t row = blockIdx.x;
+  if (per > 0) {
+    const int32_t place = (int32_t)blockIdx.x / per, at = (int32_t)blockIdx.x - place * per;
+    const int32_t req = place / a.cache.heads, head = place - req * a.cache.heads;
+    const spl::Rows rows = spl::wave_rows_of(a, req);
+    if (at >= rows.count * group || rows.count * group > per) return;
+    const int32_t tok = at / group;
+    row = (rows.first + tok) * a.q.heads + head * group + (at - tok * group);
+  } else {
+    const int32_t t = (int32_t)blockIdx.x / a.q.heads;           // tokens * heads < 2^31
+    if (t < spl::uniform_load(a.row_start) || t >= spl::uniform_load(a.row_start + a.requests)) return;  // no request's
+  }
   int n = __builtin_amdgcn_readfirstlane(p.counts[row]);
   const float* st = p.stats + 2 * (row * splits + (lane < splits ? lane : 0));
   float m = st[0], l = st[1];
-  if (t < t0 || t >= t1 || n <= 1) return;                       // no request's, or written by its one split
+  if (n <= 1) return;                            // written by its one split
   n = n < splits ? n : splits;
   m = lane < n ? m : -INFINITY;
   l = lane < n ? l : 0.0f;
@@ -558,6 +627,12 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_attn_join(AttnArgs a, int s
 // Splits: twice as many workgroups as CUs are enough (16 requests of up to 4096
 // tokens, 32 heads: 512 workgroups 43.5 us, 1024 with the join 49; 64 requests of
 // up to 2000, 8 heads: 22.7 and 31), and a wave wants four steps.
+// Two tiles a workgroup, which halve the widening, where enough are left and
+// their tokens many.  us with one / two, bf16, 32 heads over 8, 128 channels, the
+// last 512 tokens of 1024: 23.2 / 21.9, of 2048 38.0 / 34.1, of 8192 130 / 102;
+// 64 channels of 2048 25.7 / 23.8; a 512-token prompt 14.6 / 15.1; 24 requests
+// under a window of 1024, 64 channels, 26.3 / 29.2; the last 256 tokens of 4096,
+// half the workgroups, 41 / 70.
 spl::AttnPlan plan_of(const AttnArgs& a) {
   const int64_t cus = spl::device_cus();
   spl::AttnPlan p{};
@@ -569,17 +644,23 @@ spl::AttnPlan plan_of(const AttnArgs& a) {
     p.prefill_tiles = a.requests == 1 ? (rows + spl::kPrefillRows - 1) / spl::kPrefillRows : (most < rows ? most : rows);
     p.direct = 1;                                // what is left
   }
-  const int64_t most = rows / kRows + a.requests;
-  p.tiles = p.direct ? a.requests : (most < rows ? most : rows);
-  if (p.prefill_tiles > 0 && a.requests == 1) p.tiles = rows > kRows ? 0 : 1;
-  // split the tokens into chunks while the launch has fewer workgroups than the chip takes
   int64_t len = a.width * (int64_t)a.cache.page;
   if (a.max_len > 0 && a.max_len < len) len = a.max_len;
   if (a.window > 0) {
     const int64_t seen = a.window + (a.max_new > 0 && a.max_new < kRows ? a.max_new : kRows);
     len = len < seen ? len : seen;
   }
-  const int64_t groups = p.tiles * a.cache.heads, steps = (len + kStep - 1) / kStep;
+  const int64_t steps = (len + kStep - 1) / kStep;
+  const auto tiles = [&](int size) {
+    const int64_t most = rows / size + a.requests;
+    return most < rows ? most : rows;
+  };
+  p.wide = !p.direct && a.cache.head_dim < 256 && steps >= kWideSteps &&
+           tiles(2 * kRows) * a.cache.heads >= kGroupsPerCu * cus;
+  p.tiles = p.direct ? a.requests : tiles(p.wide ? 2 * kRows : kRows);
+  if (p.prefill_tiles > 0 && a.requests == 1) p.tiles = rows > kRows ? 0 : 1;
+  // split the tokens into chunks while the launch has fewer workgroups than the chip takes
+  const int64_t groups = p.tiles * a.cache.heads;
   int64_t s = groups > 0 ? (kGroupsPerCu * cus + groups - 1) / groups : 1;
   s = s < 1 ? 1 : (s > kMaxSplits ? kMaxSplits : s);
   int64_t chunk = (steps + s - 1) / s;
@@ -597,15 +678,24 @@ template <class T, int D>
 hipError_t run(const AttnArgs& a, const spl::AttnPlan& p, hipStream_t s) {
   if (p.tiles > 0) {
     const dim3 grid((unsigned)(p.tiles * a.cache.heads), (unsigned)p.splits);
-    k_attn_rows<T, D><<<grid, kWaves * 64, 0, s>>>(a, p.group, p.direct, p.splits, p.chunk, p.snake,
-                                                   p.prefill_tiles > 0 ? kRows : INT32_MAX);
+    const int most = p.prefill_tiles > 0 ? kRows : INT32_MAX;
+    constexpr int kWide = D < 256 ? 2 : 1;
+    if (p.wide)
+      k_attn_rows<T, D, kWide><<<grid, kWaves * 64, 0, s>>>(a, p.group, p.direct, p.splits, p.chunk, p.snake, most);
+    else
+      k_attn_rows<T, D, 1><<<grid, kWaves * 64, 0, s>>>(a, p.group, p.direct, p.splits, p.chunk, p.snake, most);
   }
   if (p.prefill_tiles > 0) {
     const hipError_t e = spl::launch_attn_prefill(a, p, s);
     if (e != hipSuccess) return e;
   }
-  if (p.splits > 1)
-    k_attn_join<T, D><<<dim3((unsigned)(a.tokens * a.q.heads)), kJoinWaves * 64, 0, s>>>(a, p.splits);
+  if (p.splits > 1) {
+    // of a direct launch only requests of one tile are split
+    const int64_t one = a.max_new * p.group;
+    const int per = !p.direct ? 0 : (p.prefill_tiles > 0 || one > kRows ? kRows : (int)one);
+    const int64_t joins = per ? a.requests * a.cache.heads * per : a.tokens * a.q.heads;
+    k_attn_join<T, D><<<dim3((unsigned)joins), kJoinWaves * 64, 0, s>>>(a, p.splits, p.group, per);
+  }
   return hipGetLastError();
 }
 

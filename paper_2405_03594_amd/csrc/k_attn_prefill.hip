@@ -335,7 +335,7 @@ __device__ __forceinline__ void multiply(State<D>& st, const uint8_t* lds, const
 }
 
 template <class T, int D>
-__global__ __launch_bounds__(kThreads, 2) void k_attn_prefill(AttnArgs a, int group, int tiles, int mark) {
+__global__ __launch_bounds__(kThreads, 2) void k_attn_prefill(AttnArgs a, int group, int tiles) {
   using Gm = Geom<D>;
   __shared__ __attribute__((aligned(16))) uint8_t lds[2][Gm::kBytes];
   __shared__ uint8_t flags[2][2 * kFlags];
@@ -437,8 +437,6 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_prefill(AttnArgs a, int gr
       for (int e = 0; e < 16; ++e) st.o[g][e] = st.o[g][e] * mine + joint[(16 * g + e) * 64 + lane] * its;
   }
   const int64_t out_row = t_row * a.q.heads + h_row;
-  // rows of other requests may be split: these are whole
-  if (mark > 1 && half == 1) spl::parts_of(a, D, mark).counts[out_row] = 1;
   const float inv = total == 0.0f ? 0.0f : 1.0f / total;         // no key: 0 (a NaN stays one)
   uint16_t* out = static_cast<uint16_t*>(a.out) + out_row * D;
 #pragma unroll
@@ -456,7 +454,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_prefill(AttnArgs a, int gr
 template <class T, int D>
 hipError_t run(const AttnArgs& a, const spl::AttnPlan& p, hipStream_t s) {
   const dim3 grid((unsigned)(p.prefill_tiles * a.cache.heads));
-  k_attn_prefill<T, D><<<grid, kThreads, 0, s>>>(a, p.group, (int)p.prefill_tiles, p.splits);
+  k_attn_prefill<T, D><<<grid, kThreads, 0, s>>>(a, p.group, (int)p.prefill_tiles);
   return hipGetLastError();
 }
 

@@ -154,6 +154,50 @@ def test_long_requests_are_split_and_joined():
     b.check(max_new=0, window=3000)
 
 
+@pytest.mark.parametrize("D", [64, 96, 128])
+@pytest.mark.parametrize("dt", [BF, HF])
+@pytest.mark.parametrize("window", [0, 37])
+def test_tiles_of_twice_the_rows(D, dt, window):
+    """Many rows over a wide table: two tiles of 16 rows a workgroup; ends of 1 to 31 rows, some without any key."""
+    H = 64 * torch.cuda.get_device_properties(0).multi_processor_count // 256
+    new = [70, 1, 145, 31, 33, 17]                               # 297 rows of each head: tiles for every workgroup
+    b = Batch(new, [150, 60, 145, 33, 20, 0], H, H, D, 64, dt, seed=16, extra=40)
+    got = b.check(max_len=0, window=window)
+    assert (got[70 + 1 + 145 + 31:][:13] == 0).all() and (got[-17:] == 0).all()
+    _poison(b, 2, 100, 3, False, True)                           # seen by the last 45 rows of 145
+    _poison(b, 3, 32, 5, True, False)                            # by the last of 31
+    first = 70 + 1
+    got = b.check(max_len=0, window=window)
+    assert torch.isfinite(got[first:first + 100]).all() and torch.isnan(got[first + 100, 3, :32]).all()
+    assert torch.isnan(got[first + 145 + 30, 5]).all()
+
+
+def test_tiles_of_twice_the_rows_under_a_window():
+    H = 64 * torch.cuda.get_device_properties(0).multi_processor_count // 256
+    b = Batch([290], [2200], H, H, 64, 32, HF, seed=18)
+    got, lse = b.run(window=2040)
+    for t in (0, 1, 15, 16, 31, 32, 129, 130, 161, 288, 289):    # the window's start passes 0 at row 129
+        p = 2200 - 290 + t
+        w, l, m, top = ref.attention(b.q.double()[t:t + 1], b.keys, b.values, [0, 1], [p + 1], 64 ** -0.5, 2040)
+        tol = 3 * ref.UNIT[HF] + 2.0 ** -18 * (1 + top)
+        assert ((got[t] - w[0]).abs() <= tol * m[0] + ref.STEP[HF]).all(), t
+        assert ((lse[t] - l[0]).abs() <= tol).all(), t
+
+
+def test_split_requests_beside_prompts():
+    """Single rows over many tokens are split and joined in a call whose prompts are not."""
+    H = 64 * torch.cuda.get_device_properties(0).multi_processor_count // 256
+    b = Batch([1, 520, 3, 1, 16, 0], [1500, 520, 2100, 40, 1900, 700], H, H, 64, 64, BF, seed=17)
+    got, lse = b.run()
+    for r in (0, 2, 3, 4):
+        s, e = int(b.row_start[r]), int(b.row_start[r + 1])
+        w, l, m, top = ref.attention(b.q.double()[s:e], b.keys[r:r + 1], b.values[r:r + 1], [0, e - s], [b.lens[r]],
+                                     64 ** -0.5, 0)
+        tol = 3 * ref.UNIT[BF] + 2.0 ** -18 * (1 + top)
+        assert ((got[s:e] - w).abs() <= tol * m + ref.STEP[BF]).all(), r
+        assert ((lse[s:e] - l).abs() <= tol).all(), r
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.2, 1.0, 3e-3])
 def test_scales(scale):
     Batch([1, 20], [70, 45], 4, 4, 64, 16, BF, seed=8).check(scale=scale)
