@@ -215,68 +215,91 @@ __device__ __forceinline__ void store_codes(uint8_t* region, const spl::PageGeom
     region[g.page * (g.dim + g.scale_bytes) + ((b >> 3) * g.scale_bytes + (c >> 2)) * 8 + (b & 7)] = (uint8_t)scale;
 }
 
-// Waves of one token: first q's, then k's, then (with a cache) v's, each of
-// kIter slots of 64 / LPH heads.  A slot past the last head repeats it, and
-// writes nothing.
+// Where a task's heads are: a token's first tasks are q's, then k's, then (with
+// a cache) v's, each of kIter slots of 64 / LPH heads.
+struct Task {
+  int64_t token;
+  bool is_q, is_v;
+  int first;                                    // head
+};
+__device__ __forceinline__ Task task_of(int task, int q_tasks, int k_tasks, int all_tasks, int heads) {
+  const int t = task / all_tasks, part = task - t * all_tasks;
+  Task k;
+  k.token = t;
+  k.is_q = part < q_tasks;
+  k.is_v = part >= q_tasks + k_tasks;
+  k.first = (k.is_q ? part : (k.is_v ? part - q_tasks - k_tasks : part - q_tasks)) * heads;
+  return k;
+}
+
+// A wave takes tasks in a fixed stride, the next one's heads requested before
+// this one's are used.  A slot past the last head repeats it, and writes nothing.
 template <class T, int LPH, bool kInter, int kIter, bool kWhole>
-__global__ __launch_bounds__(kThreads) void k_norm_rope(spl::NormRopeArgs a, int q_waves, int k_waves, int all_waves,
+__global__ __launch_bounds__(kThreads) void k_norm_rope(spl::NormRopeArgs a, int q_tasks, int k_tasks, int all_tasks,
                                                         float inv_dim) {
   constexpr int kSlots = 64 / LPH;
-  const int task = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * kWaves + (threadIdx.x >> 6)));    // < 2^31
-  const int t32 = task / all_waves, part = task - t32 * all_waves;
-  const int64_t t = t32;
-  if (t >= a.tokens) return;
   const int lane = threadIdx.x & 63, chunk = lane & (LPH - 1);
-  const bool is_q = part < q_waves, is_v = part >= q_waves + k_waves;
-  const spl_heads& src = is_q ? a.q : (is_v ? a.v : a.k);
-  const int first = (is_q ? part : (is_v ? part - q_waves - k_waves : part - q_waves)) * kIter * kSlots;
-  const int mine = first + lane / LPH, last = src.heads - 1;
-  const bool live = kWhole || 8 * chunk < a.dim, full = kWhole && first + kIter * kSlots <= src.heads;
+  const bool live = kWhole || 8 * chunk < a.dim;
   const int at = live ? 8 * chunk : 0;
-  const uint16_t* in = static_cast<const uint16_t*>(src.data) + t * src.token_stride + at;
-
-  u32x4 x[kIter];
-#pragma unroll
-  for (int i = 0; i < kIter; ++i) {
-    const int h = mine + i * kSlots;
-    x[i] = *reinterpret_cast<const u32x4*>(in + (h < last ? h : last) * src.head_stride);
-  }
-  const int64_t slot = is_q || !a.cache.data ? -1 : a.slots[t];
-  const uint16_t* w16 = static_cast<const uint16_t*>(is_q ? a.wq : a.wk);
-  if (!is_v) {
-    float w[8], r[kIter];
-    if (w16) widen<T>(*reinterpret_cast<const u32x4*>(w16 + at), w);
-    const Turn<kInter> tr =
-        load_turn<LPH, kInter, kWhole>(a.rope, a.rope_rows, kWhole || a.rot ? a.positions[t] : 0, a.rot, chunk, lane);
-    uint16_t* out = static_cast<uint16_t*>(is_q ? a.q_out : a.k_out);
-    if (out) out += t * src.heads * (int64_t)a.dim + at;
-    if (w16) inverse_rms<T, LPH, kIter>(x, inv_dim, a.eps, !live, lane, r);
+  const int tasks = (int)a.tokens * all_tasks, stride = gridDim.x * kWaves;             // < 2^31
+  u32x4 x[kIter], ahead[kIter];
+  const auto fetch = [&](int task) {
+    const Task k = task_of(task, q_tasks, k_tasks, all_tasks, kIter * kSlots);
+    const spl_heads& src = k.is_q ? a.q : (k.is_v ? a.v : a.k);
+    const uint16_t* in = static_cast<const uint16_t*>(src.data) + k.token * src.token_stride + at;
+    const int mine = k.first + lane / LPH, last = src.heads - 1;
 #pragma unroll
     for (int i = 0; i < kIter; ++i) {
-      float f[8];
-      widen<T>(x[i], f);
-      if (w16) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = f[e] * r[i] * w[e];
-      }
-      if (kWhole || a.rot) turn<LPH, kInter, kWhole, false>(tr, f);
-      x[i] = narrow<T>(f);
       const int h = mine + i * kSlots;
-      if (out && (full || (live && h <= last))) *reinterpret_cast<u32x4*>(out + (int64_t)h * a.dim) = x[i];
+      ahead[i] = *reinterpret_cast<const u32x4*>(in + (h < last ? h : last) * src.head_stride);
     }
-  }
-  if (is_q || !a.cache.data) return;
-  const int shift = __builtin_ctz((unsigned)a.cache.page);
-  if (slot < 0 || (slot >> shift) >= a.cache.pages) return;
-  const spl::PageGeom g = spl::page_geom(a.dim, a.cache.page);
-  const int b = (int)(slot & (a.cache.page - 1));
-  uint8_t* page = static_cast<uint8_t*>(a.cache.data) + (slot >> shift) * (int64_t)a.cache.heads * g.bytes;
+  };
+  int task = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * kWaves + (threadIdx.x >> 6)));
+  if (task < tasks) fetch(task);
+  for (; task < tasks; task += stride) {
+    const Task k = task_of(task, q_tasks, k_tasks, all_tasks, kIter * kSlots);
+    const int64_t t = k.token;
+    const int heads = k.is_q ? a.q.heads : a.k.heads, mine = k.first + lane / LPH, last = heads - 1;
+    const bool full = kWhole && k.first + kIter * kSlots <= heads;
 #pragma unroll
-  for (int i = 0; i < kIter; ++i) {
-    uint32_t code;
-    const uint32_t scale = encode8<T>(x[i], &code);
-    const int h = mine + i * kSlots;
-    if (live && h <= last) store_codes(page + (int64_t)h * g.bytes, g, is_v, b, chunk, code, scale);
+    for (int i = 0; i < kIter; ++i) x[i] = ahead[i];
+    if (tasks - task > stride) fetch(task + stride);
+    const int64_t slot = k.is_q || !a.cache.data ? -1 : a.slots[t];
+    const uint16_t* w16 = static_cast<const uint16_t*>(k.is_q ? a.wq : a.wk);
+    if (!k.is_v) {
+      float w[8], r[kIter];
+      if (w16) widen<T>(*reinterpret_cast<const u32x4*>(w16 + at), w);
+      const Turn<kInter> tr =
+          load_turn<LPH, kInter, kWhole>(a.rope, a.rope_rows, kWhole || a.rot ? a.positions[t] : 0, a.rot, chunk, lane);
+      uint16_t* out = static_cast<uint16_t*>(k.is_q ? a.q_out : a.k_out);
+      if (out) out += t * heads * (int64_t)a.dim + at;
+      if (w16) inverse_rms<T, LPH, kIter>(x, inv_dim, a.eps, !live, lane, r);
+#pragma unroll
+      for (int i = 0; i < kIter; ++i) {
+        float f[8];
+        widen<T>(x[i], f);
+        if (w16) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[e] = f[e] * r[i] * w[e];
+        }
+        if (kWhole || a.rot) turn<LPH, kInter, kWhole, false>(tr, f);
+        x[i] = narrow<T>(f);
+        const int h = mine + i * kSlots;
+        if (out && (full || (live && h <= last))) *reinterpret_cast<u32x4*>(out + (int64_t)h * a.dim) = x[i];
+      }
+    }
+    const int shift = __builtin_ctz((unsigned)a.cache.page);
+    if (slot < 0 || (slot >> shift) >= a.cache.pages) continue;
+    const spl::PageGeom g = spl::page_geom(a.dim, a.cache.page);
+    const int b = (int)(slot & (a.cache.page - 1));
+    uint8_t* page = static_cast<uint8_t*>(a.cache.data) + (slot >> shift) * (int64_t)a.cache.heads * g.bytes;
+#pragma unroll
+    for (int i = 0; i < kIter; ++i) {
+      uint32_t code;
+      const uint32_t scale = encode8<T>(x[i], &code);
+      const int h = mine + i * kSlots;
+      if (live && h <= last) store_codes(page + (int64_t)h * g.bytes, g, k.is_v, b, chunk, code, scale);
+    }
   }
 }
 
@@ -448,11 +471,12 @@ int slots_of(int64_t tokens, int64_t heads, int lph) {
 }
 int lanes_of(int dim) { return dim <= 64 ? 8 : (dim <= 128 ? 16 : 32); }
 
-// Workgroups of the gradient for q and for k: shared out by heads, at most
-// four a CU, so that few rows of partial sums are left.
+// Workgroups of the gradient for q and for k: shared out by heads, at most as
+// many as the chip holds (134 registers; 2048 tokens of 32 + 32 heads of 128
+// channels: three a CU 23.8 us, four 27.1).
 void grad_groups(int64_t tokens, int32_t q_heads, int32_t k_heads, int32_t dim, int* q, int* k) {
   const int lph = lanes_of(dim), heads = slots_of(tokens, (int64_t)q_heads + k_heads, lph) * (64 / lph);
-  const int64_t most = 4 * (int64_t)spl::device_cus();
+  const int64_t most = 3 * (int64_t)spl::device_cus();
   const auto groups = [&](int64_t h) { return (tokens * ((h + heads - 1) / heads) + kWaves - 1) / kWaves; };
   const int64_t gq = groups(q_heads), gk = groups(k_heads);
   int64_t nq = gq, nk = gk;
@@ -496,7 +520,11 @@ hipError_t norm_rope(const spl::NormRopeArgs& a, hipStream_t s) {
   const int heads = iter * (64 / lph);
   const int qw = (a.q.heads + heads - 1) / heads, kw = (a.k.heads + heads - 1) / heads;
   const int all = qw + kw + (a.cache.data ? kw : 0);
-  const dim3 grid((unsigned)((a.tokens * all + kWaves - 1) / kWaves));
+  // as many waves as the chip holds (85 to 128 registers): 2048 tokens of 32 + 32
+  // heads of 128 channels 18.2 us with a wave a task, 17.5 so; 2 or 3 workgroups a
+  // CU 20.2, 18.3
+  const int64_t need = (a.tokens * all + kWaves - 1) / kWaves, most = 4 * (int64_t)spl::device_cus();
+  const dim3 grid((unsigned)(need < most ? need : most));
   const float inv = (float)(1.0 / a.dim);
   SPL_PICK(k_norm_rope, lph, a.interleaved, iter, a.rot == 8 * lph,
            <<<grid, kThreads, 0, s>>>(a, qw, kw, all, inv));
