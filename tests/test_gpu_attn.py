@@ -172,6 +172,17 @@ def test_tiles_of_twice_the_rows(D, dt, window):
     assert torch.isnan(got[first + 145 + 30, 5]).all()
 
 
+@pytest.mark.parametrize("requests", [33, 63, 64, 65])
+def test_many_requests_of_different_lengths(requests):
+    """Served in the order of their lengths up to 64 of them: each once, equal lengths among them, and none at all."""
+    heads = torch.cuda.get_device_properties(0).multi_processor_count // 16
+    lens = [(37 * i) % 90 if i % 5 else 40 for i in range(requests)]
+    lens[3] = lens[requests - 1] = 0
+    lens[7] = 530
+    b = Batch([1 + (i % 3 == 0) for i in range(requests)], lens, heads, heads, 64, 64, BF, seed=19)
+    b.check()
+
+
 def test_tiles_of_twice_the_rows_under_a_window():
     H = 64 * torch.cuda.get_device_properties(0).multi_processor_count // 256
     b = Batch([290], [2200], H, H, 64, 32, HF, seed=18)
