@@ -127,33 +127,47 @@ __device__ __forceinline__ Rows wave_rows_of(const AttnArgs& a, int32_t r) {
   return {s, e - s, len};
 }
 
+// Inclusive sum over the lanes of a wave: within rows of 16, then a row's or two
+// rows' last lane added to what follows.
+__device__ __forceinline__ int32_t lane_sums(int32_t x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return x;
+}
+
 // The request that owns tile `tile` when each of more than `few` rows (rows *
-// group) has ceil(rows * group / size) tiles, and the tile's number in it;
-// request -1 past the last.  Every lane of the wave calls it with the same tile.
+// group) has ceil(rows * group / size) tiles, the tile's number in it and its
+// rows; request -1 past the last.  Every lane of the wave calls it with the same
+// tile; the launch's tiles are fewer than 2^31.
 struct Tile {
-  int64_t request;
-  int64_t index;
+  int32_t request, index;
+  Rows rows;
 };
-__device__ __forceinline__ Tile find_tile(const AttnArgs& a, int group, int size, int few, int64_t tile) {
+__device__ __forceinline__ Tile find_tile(const AttnArgs& a, int group, int size, int few, int32_t tile) {
   const int lane = lane_id();
-  int64_t before = 0;
-  for (int64_t base = 0; base < a.requests; base += 64) {
-    int64_t n = 0;
-    if (base + lane < a.requests) n = (int64_t)rows_of(a, base + lane).count * group;
-    n = n > few ? (n + size - 1) / size : 0;
-    int64_t sum = n;
-    for (int d = 1; d < 64; d <<= 1) {
-      const int64_t y = __shfl_up(sum, d);
-      if (lane >= d) sum += y;
-    }
-    const uint64_t past = __ballot(before + sum > tile);
+  const int32_t requests = (int32_t)a.requests;
+  for (int32_t base = 0; base < requests; base += 64) {
+    const Rows r = rows_of(a, base + lane < requests ? base + lane : requests - 1);
+    int32_t n = base + lane < requests ? r.count * group : 0;
+    n = n > few ? (n - 1) / size + 1 : 0;
+    const int32_t sum = lane_sums(n);
+    const uint64_t past = __ballot(sum > tile);
     if (past) {
       const int k = __builtin_ctzll(past);
-      return {base + k, tile - before - __shfl(sum - n, k)};
+      const int32_t index = tile - __builtin_amdgcn_readlane(sum - n, k);
+      // requests that overlap may pass 2^31 tiles in all: none of theirs then
+      if ((uint32_t)index >= (uint32_t)__builtin_amdgcn_readlane(n, k)) break;
+      return {base + k, index,
+              {__builtin_amdgcn_readlane((int32_t)r.first, k), __builtin_amdgcn_readlane(r.count, k),
+               __builtin_amdgcn_readlane(r.len, k)}};
     }
-    before += __shfl(sum, 63);
+    tile -= __builtin_amdgcn_readlane(sum, 63);
   }
-  return {-1, 0};
+  return {-1, 0, {0, 0, 0}};
 }
 
 // The steps of `unit` tokens that any of the rows [row0, end_row) of a request

@@ -351,7 +351,7 @@ __device__ __forceinline__ void step(State<D> (&st)[R], Raw<D>& r, const u32x4 (
 // other round backwards, so that what a CU gets in two rounds is alike.
 // Requests up to 64: each lane ranks one (lengths past kMostRanked are alike).
 constexpr int32_t kMostRanked = (1 << 26) - 1;
-__device__ __forceinline__ int64_t ranked_request(const AttnArgs& a, int at, int round) {
+__device__ __forceinline__ int32_t ranked_request(const AttnArgs& a, int at, int round) {
   const int lane = spl::lane_id(), n = (int)a.requests;
   int32_t len = lane < n ? a.lens[lane] : 0;
   len = len < 0 ? 0 : (len > kMostRanked ? kMostRanked : len);
@@ -531,10 +531,10 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : (R == 1 ? 3 : 2)) void 
   // heads fastest: consecutive workgroups go to different XCDs, so each has a
   // share of every request, however their lengths differ
   const int place = blockIdx.x / a.cache.heads, head = blockIdx.x - place * a.cache.heads, split = blockIdx.y;
-  spl::Tile tile{place, 0};
+  spl::Tile tile{place, 0, {0, 0, 0}};
   if (!direct) tile = spl::find_tile(a, group, R * kRows, 0, place);
   else if (snake > 0) tile.request = ranked_request(a, place, snake);
-  const int32_t req = __builtin_amdgcn_readfirstlane((int)tile.request);
+  const int32_t req = tile.request;
   if (req < 0) return;
   const LaneOff off = lane_off<D>(a.cache.page, lane);
   // where the first step is known without the lengths, its data are requested before they are
@@ -545,8 +545,8 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : (R == 1 ? 3 : 2)) void 
     w0 = where(a, a.table + req * a.width, wave * kStep, __builtin_ctz((unsigned)a.cache.page));
     load_step<D>(r0, a, head, wave * kStep, w0, off, lane);
   }
-  const spl::Rows rows = spl::wave_rows_of(a, req);
-  const int32_t row0 = __builtin_amdgcn_readfirstlane((int)tile.index) * (R * kRows), all = rows.count * group;
+  const spl::Rows rows = direct ? spl::wave_rows_of(a, req) : tile.rows;
+  const int32_t row0 = tile.index * (R * kRows), all = rows.count * group;
   if (row0 >= all || all > most) return;         // more rows than most: another kernel's
   if (R > 1 && all - row0 > kRows)
     rows_of_tile<T, D, R>(a, lds, group, head, split, splits, chunk, req, rows, row0, early, r0, w0, off, lane, wave);

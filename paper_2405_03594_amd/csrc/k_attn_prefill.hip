@@ -343,12 +343,12 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_prefill(AttnArgs a, int gr
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int place = blockIdx.x / a.cache.heads, head = blockIdx.x - place * a.cache.heads;
   // the tiles that see the most first
-  const spl::Tile tile = a.requests == 1 ? spl::Tile{0, tiles - 1 - place}
+  const spl::Tile tile = a.requests == 1 ? spl::Tile{0, tiles - 1 - place, spl::wave_rows_of(a, 0)}
                                          : spl::find_tile(a, group, kRows, spl::kFewRows, tiles - 1 - place);
-  const int32_t req = __builtin_amdgcn_readfirstlane((int)tile.request);
+  const int32_t req = tile.request;
   if (req < 0) return;
-  const spl::Rows rows = spl::wave_rows_of(a, req);
-  const int32_t row0 = __builtin_amdgcn_readfirstlane((int)tile.index) * kRows, all = rows.count * group;
+  const spl::Rows rows = tile.rows;
+  const int32_t row0 = tile.index * kRows, all = rows.count * group;
   if (row0 >= all) return;
   const int32_t end_row = all - row0 < kRows ? all : row0 + kRows;
   const spl::Span span = spl::tile_span(rows, row0, end_row, group, a.window, Gm::kTok, 1, 0);

@@ -183,6 +183,15 @@ def test_many_requests_of_different_lengths(requests):
     b.check()
 
 
+def test_tiles_are_found_among_many_requests():
+    """More than a wave's lanes of requests, of no row to 90, the last ones empty."""
+    new = [(7 * i) % 4 for i in range(130)] + [90, 0, 0]
+    lens = [n + (13 * i) % 50 for i, n in enumerate(new)]
+    b = Batch(new, lens, 4, 2, 64, 16, HF, seed=20)
+    b.check()
+    b.check(max_new=0)
+
+
 def test_tiles_of_twice_the_rows_under_a_window():
     H = 64 * torch.cuda.get_device_properties(0).multi_processor_count // 256
     b = Batch([290], [2200], H, H, 64, 32, HF, seed=18)
