@@ -14,8 +14,13 @@
 // Codes are widened by v_cvt_scalef32_pk, scale applied, two a instruction;
 // values come as channels by token and are transposed two by two with v_perm.
 //
-// Bound: HBM; a step of 32 tokens is 32 (D + 2 S) bytes against some 200 vector
-// instructions and D / 8 matrix instructions of one wave.
+// Bound: HBM, then latency; a step of 32 tokens is 32 (D + 2 S) bytes against some
+// 200 vector instructions and D / 8 matrix instructions of one wave.  Measured, 128
+// channels: 16 requests of up to 4096 tokens, 32 heads, 36.5 us, 160 MB at 4.4 TB/s
+// (the loads alone 31.6, without any of the arithmetic); 64 requests of up to
+// 2000, 8 heads, 21.5 us, 79 MB at 3.7; one request of 131072 tokens, 8 heads, 31 us
+// and 5 for the join of 64 splits, 142 MB at 4.6; one of 93 tokens 5.2 us.  More
+// waves, deeper requests or more occupancy gain nothing.
 #include "attn_tile.h"
 
 namespace {
@@ -554,7 +559,9 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : (R == 1 ? 3 : 2)) void 
     rows_of_tile<T, D, 1>(a, lds, group, head, split, splits, chunk, req, rows, row0, early, r0, w0, off, lane, wave);
 }
 
-// The splits of a row joined: a workgroup a row (per > 0: of the first `per` of a
+// The splits of a row joined (by the last of its workgroups instead, with a fence
+// that writes the L2 back in each, 131072 tokens take 53 us and not 37; by a wave a
+// row 39): a workgroup a row (per > 0: of the first `per` of a
 // request and key head, if it has no more), its eight waves sharing the splits,
 // D / 64 channels a lane.  A lane knows the statistics of one split.
 // Loads go out in two rounds: the counts and statistics, then all sums.
@@ -622,19 +629,19 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_attn_join(AttnArgs a, int s
 }
 
 // k_attn_prefill takes over where its tiles give every CU a workgroup.  us of
-// k_attn_rows / k_attn_prefill, bf16, 128 channels, prompts of one request: 512
-// tokens of 32 heads 13.7 / 17.9, of 32 over 8 13.9 / 18.0, after 8192 tokens 134 /
-// 160; 1024 tokens 31.9 / 28.5, 31.4 / 28.0; 2048 of 32 83.1 / 58.4.  With 256
-// channels its registers do not hold a step (1024 tokens of 16 heads 51.6 / 85.4).
+// k_attn_rows / k_attn_prefill, bf16, 128 channels, one request: 512 tokens of 32
+// heads 13.5 / 17.9, the last 512 of 8192 100 / 150; 1024 tokens of 32 heads 32.1 /
+// 28.7, of 16 heads 18.7 / 26.5; 2048 of 32 80 / 56.  With 256 channels its
+// registers do not hold a step (1024 tokens of 16 heads 51.6 / 85.4).
 // Splits: twice as many workgroups as CUs are enough (16 requests of up to 4096
-// tokens, 32 heads: 512 workgroups 43.5 us, 1024 with the join 49; 64 requests of
-// up to 2000, 8 heads: 22.7 and 31), and a wave wants four steps.
+// tokens, 32 heads: 512 workgroups 37.0 us, 1024 with the join 40.2; 64 requests of
+// up to 2000, 8 heads: 21.6 and 31.4), and a wave wants four steps.
 // Two tiles a workgroup, which halve the widening, where enough are left and
 // their tokens many.  us with one / two, bf16, 32 heads over 8, 128 channels, the
-// last 512 tokens of 1024: 23.2 / 21.9, of 2048 38.0 / 34.1, of 8192 130 / 102;
-// 64 channels of 2048 25.7 / 23.8; a 512-token prompt 14.6 / 15.1; 24 requests
-// under a window of 1024, 64 channels, 26.3 / 29.2; the last 256 tokens of 4096,
-// half the workgroups, 41 / 70.
+// last 512 tokens of 1024: 22.5 / 21.8, of 2048 37.1 / 32.6, of 8192 130 / 100;
+// 64 channels of 2048 25.8 / 23.1; a 512-token prompt 14.8 / 15.8; 24 requests
+// under a window of 1024, 64 channels, 26.2 / 28.6; the last 256 tokens of 4096,
+// half the workgroups, 39.9 / 49.3.
 spl::AttnPlan plan_of(const AttnArgs& a) {
   const int64_t cus = spl::device_cus();
   spl::AttnPlan p{};
