@@ -204,6 +204,23 @@ def test_tiles_of_twice_the_rows_under_a_window():
         assert ((lse[t] - l[0]).abs() <= tol).all(), t
 
 
+@pytest.mark.parametrize("new,lens,extra", [([1, 3], [700, 90], 0), ([297], [310], 40), ([1040, 1], [1040, 70], 0)])
+def test_pages_past_four_gigabytes(new, lens, extra):
+    """The same bits where the pages lie past 4 GiB: single rows, two tiles a workgroup, many rows."""
+    H = 64 * torch.cuda.get_device_properties(0).multi_processor_count // 256
+    b = Batch(new, lens, H, H, 64, 64, BF, seed=21, extra=extra)
+    hint = 0 if extra else max(lens)
+    want = b.run(max_len=hint)
+    small = b.cache
+    more = (9 << 29) // (small.data.numel() // small.pages)      # 4.5 GiB before them
+    data = torch.zeros(more + small.pages, *small.data.shape[1:], dtype=torch.uint8, device="cuda")
+    data[more:] = small.data
+    b.cache = _spl().KVCache(data, 64, 64, BF)
+    b.table = torch.where(b.table >= 0, b.table + more, b.table).int()
+    got = b.run(max_len=hint)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_split_requests_beside_prompts():
     """Single rows over many tokens are split and joined in a call whose prompts are not."""
     H = 64 * torch.cuda.get_device_properties(0).multi_processor_count // 256
