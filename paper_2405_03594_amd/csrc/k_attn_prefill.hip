@@ -20,10 +20,12 @@
 // Bound: neither unit alone.  A step of 128 channels asks 0.85 us of the matrix
 // unit, 1.1 of the vector unit and 1.0 of LDS, and takes 2.3 on each CU; fewer
 // additions, operands read six ahead and other orders of the products change it by
-// 1%.  Measured, bf16, 32 heads of 128 channels: 1024 tokens 28.7 us, 2048 56 us
-// (610 TFLOP/s; 10 us are the launch's start, 4 each workgroup's start and end),
-// 4096 179 (768), 8192 640 (859, where the library's large product makes 1247); of
-// 64 channels 2048 35 us, 8192 392.
+// 1%; without widening, exponentials or operand reads (8192 tokens) it would take
+// 0.88, 0.92, 0.87 of the time, without all three 0.71, at the rate of the library's
+// large product.  Measured, bf16, 32 heads of 128 channels: 1024 tokens 28.1 us,
+// 2048 55.9 us (615 TFLOP/s; 10 us are the launch's start, 4 each workgroup's start
+// and end), 4096 178 (773), 8192 632 (870, the library 1247); of 64 channels 2048
+// 35 us, 8192 392.
 #include "attn_tile.h"
 
 namespace {
@@ -93,14 +95,17 @@ __device__ __forceinline__ void load_words(uint32_t* d, const uint8_t* p) {
   }
 }
 
-// Page numbers of a wave's keys and of both halves of its values; -1: none.
+// Page numbers of a wave's keys and of both halves of its values; -1: none.  What
+// the table holds past the request's pages may be anything: its tokens are past
+// every row.
 struct Pages {
   int32_t k, v[2];
 };
 __device__ __forceinline__ Pages pages_at(const AttnArgs& a, const int32_t* table, const Job& job, int32_t t0,
-                                          int32_t len, int shift) {
+                                          int shift) {
+  const int32_t last = (int32_t)a.width - 1;
   const auto page = [&](int32_t t) {
-    const int32_t p = t < len ? spl::uniform_load(table + (t >> shift)) : -1;
+    const int32_t at = t >> shift, p = spl::uniform_load(table + (at < last ? at : last));
     return p >= 0 && p < a.cache.pages ? p : -1;
   };
   return {page(t0 + job.key_unit), {page(t0 + job.value_unit), page(t0 + job.value_unit + 16)}};
@@ -350,6 +355,17 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_prefill(AttnArgs a, int gr
   __shared__ float stats_s[4][2][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int place = blockIdx.x / a.cache.heads, head = blockIdx.x - place * a.cache.heads;
+  const Job job = job_of<D>(a.cache.page, tid);
+  const int shift = __builtin_ctz((unsigned)a.cache.page);
+  Raw<D> raw, ahead;
+  const auto start = [&](const int32_t* table, int32_t t0, int32_t t1) {
+    const Pages p0 = pages_at(a, table, job, t0, shift), p1 = pages_at(a, table, job, t1, shift);
+    load_raw<D>(raw, a, head, job, t0, p0, lane);
+    load_raw<D>(ahead, a, head, job, t1, p1, lane);
+  };
+  // where the first steps are known without the lengths, their data are requested before they are
+  const bool early = a.requests == 1 && a.window == 0;
+  if (early) start(a.table, 0, Gm::kTok);
   // the tiles that see the most first
   const spl::Tile tile = a.requests == 1 ? spl::Tile{0, tiles - 1 - place, spl::wave_rows_of(a, 0)}
                                          : spl::find_tile(a, group, kRows, spl::kFewRows, tiles - 1 - place);
@@ -389,19 +405,15 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_prefill(AttnArgs a, int gr
       q[d] = (*reinterpret_cast<const u32x4*>(at + 16 * d + 8 * half) ^ flip) & keep;
   };
   if (steps > 0) {
-    const Job job = job_of<D>(a.cache.page, tid);
     if (tid < 4 * kFlags) (&flags[0][0])[tid] = 0;               // also the bytes that no thread writes
     const int32_t* table = a.table + req * a.width;
-    const int shift = __builtin_ctz((unsigned)a.cache.page);
     const auto at = [&](int32_t i) { return (span.s0 + (i < steps ? i : steps - 1)) * Gm::kTok; };
-    Raw<D> raw;
-    load_raw<D>(raw, a, head, job, at(0), pages_at(a, table, job, at(0), rows.len, shift), lane);
-    Pages pg = pages_at(a, table, job, at(1), rows.len, shift);
+    if (!early) start(table, at(0), at(1));
+    Pages pg = pages_at(a, table, job, at(2), shift);
     load_q();
     __syncthreads();
     widen<T, D>(lds[0], flags[0], raw, job);
-    load_raw<D>(raw, a, head, job, at(1), pg, lane);
-    pg = pages_at(a, table, job, at(2), rows.len, shift);
+    raw = ahead;
     __syncthreads();
     for (int32_t i = 0; i < steps; ++i) {
       const int now = i & 1;
@@ -411,7 +423,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_prefill(AttnArgs a, int gr
       const auto prepare = [&] {
         widen<T, D>(lds[now ^ 1], flags[now ^ 1], raw, job);
         load_raw<D>(raw, a, head, job, at(i + 2), pg, lane);
-        pg = pages_at(a, table, job, at(i + 3), rows.len, shift);
+        pg = pages_at(a, table, job, at(i + 3), shift);
       };
       if (more && th == 0) prepare();
       const int32_t t0 = at(i) + th * (Gm::kTok / 2);
