@@ -526,9 +526,10 @@ __device__ __forceinline__ void rows_of_tile(const AttnArgs& a, Shared<D>& lds, 
   }
 }
 
-// R: tiles of 16 rows that a workgroup takes where the request has them.
-template <class T, int D, int R>
-__global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : (R == 1 ? 3 : 2)) void k_attn_rows(
+// R: tiles of 16 rows that a workgroup takes where the request has them; O: waves
+// a SIMD.
+template <class T, int D, int R, int O>
+__global__ __launch_bounds__(kWaves * 64, O) void k_attn_rows(
     AttnArgs a, int group, int direct, int all_splits, int chunk, int snake, int most) {
   const int splits = R == 1 ? all_splits : 1;    // enough workgroups: not split
   __shared__ Shared<D> lds;
@@ -561,28 +562,30 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : (R == 1 ? 3 : 2)) void 
 
 // The splits of a row joined (by the last of its workgroups instead, with a fence
 // that writes the L2 back in each, 131072 tokens take 53 us and not 37; by a wave a
-// row 39): a workgroup a row (per > 0: of the first `per` of a
-// request and key head, if it has no more), its eight waves sharing the splits,
-// D / 64 channels a lane.  A lane knows the statistics of one split.
+// row 39): W waves a row (per > 0: of the first `per` of a
+// request and key head, if it has no more) that share the splits, D / 64 channels
+// a lane.  A lane knows the statistics of one split.
 // Loads go out in two rounds: the counts and statistics, then all sums.
-constexpr int kJoinWaves = 8;
-template <class T, int D>
-__global__ __launch_bounds__(kJoinWaves * 64) void k_attn_join(AttnArgs a, int splits, int group, int per) {
+constexpr int kJoinWaves = 8;                    // of a workgroup
+constexpr int kJoinDeep = kMaxSplits / kJoinWaves;               // splits of a wave
+template <class T, int D, int W>
+__global__ __launch_bounds__(kJoinWaves * 64) void k_attn_join(AttnArgs a, int splits, int group, int per, int joins) {
   constexpr int C = D == 256 ? 4 : 2;                            // channels of a lane; D 64 and 96 leave lanes idle
   typedef float vec __attribute__((ext_vector_type(C)));
-  __shared__ vec o_s[kJoinWaves - 1][64];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, in = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = in & (W - 1);
   const spl::Parts p = spl::parts_of(a, D, splits);
-  int64_t row = blockIdx.x;
+  const int32_t join = (int32_t)blockIdx.x * (kJoinWaves / W) + in / W;
+  if (join >= joins) return;                     // W 1: no wave waits for another
+  int64_t row = join;
   if (per > 0) {
-    const int32_t place = (int32_t)blockIdx.x / per, at = (int32_t)blockIdx.x - place * per;
+    const int32_t place = join / per, at = join - place * per;
     const int32_t req = place / a.cache.heads, head = place - req * a.cache.heads;
     const spl::Rows rows = spl::wave_rows_of(a, req);
     if (at >= rows.count * group || rows.count * group > per) return;
     const int32_t tok = at / group;
     row = (rows.first + tok) * a.q.heads + head * group + (at - tok * group);
   } else {
-    const int32_t t = (int32_t)blockIdx.x / a.q.heads;           // tokens * heads < 2^31
+    const int32_t t = join / a.q.heads;          // tokens * heads < 2^31
     if (t < spl::uniform_load(a.row_start) || t >= spl::uniform_load(a.row_start + a.requests)) return;  // no request's
   }
   int n = __builtin_amdgcn_readfirstlane(p.counts[row]);
@@ -594,11 +597,11 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_attn_join(AttnArgs a, int s
   l = lane < n ? l : 0.0f;
   const int ch = lane * C;
   const float* part = p.sums + row * splits * D + (ch < D ? ch : 0);
-  vec x[kMaxSplits / kJoinWaves];
+  vec x[kJoinDeep];
 #pragma unroll
-  for (int i = 0; i < kMaxSplits / kJoinWaves; ++i) {
-    const int s = wave + i * kJoinWaves;
-    if (i * kJoinWaves < n) x[i] = *reinterpret_cast<const vec*>(part + (int64_t)(s < n ? s : 0) * D);
+  for (int i = 0; i < kJoinDeep; ++i) {
+    const int s = wave + i * W;
+    if (i * W < n) x[i] = *reinterpret_cast<const vec*>(part + (int64_t)(s < n ? s : 0) * D);
   }
   float top = m;
   for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
@@ -607,18 +610,21 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_attn_join(AttnArgs a, int s
   for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d);
   vec o = 0;
 #pragma unroll
-  for (int i = 0; i < kMaxSplits / kJoinWaves; ++i) {
-    const int s = wave + i * kJoinWaves;
+  for (int i = 0; i < kJoinDeep; ++i) {
+    const int s = wave + i * W;
     if (s < n) {
       const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s));
       if (ws != 0.0f) o += ws * x[i];                            // the sums of a split that saw no key are 0
     }
   }
-  if (wave > 0) o_s[wave - 1][lane] = o;
-  __syncthreads();
-  if (wave > 0) return;
+  if constexpr (W > 1) {
+    __shared__ vec o_s[W - 1][64];
+    if (wave > 0) o_s[wave - 1][lane] = o;
+    __syncthreads();
+    if (wave > 0) return;
 #pragma unroll
-  for (int k = 0; k < kJoinWaves - 1; ++k) o += o_s[k][lane];
+    for (int k = 0; k < W - 1; ++k) o += o_s[k][lane];
+  }
   o *= total == 0.0f ? 0.0f : 1.0f / total;
   if (ch < D) {
     uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + row * D + ch);
@@ -694,11 +700,19 @@ hipError_t run(const AttnArgs& a, const spl::AttnPlan& p, hipStream_t s) {
   if (p.tiles > 0) {
     const dim3 grid((unsigned)(p.tiles * a.cache.heads), (unsigned)p.splits);
     const int most = p.prefill_tiles > 0 ? kRows : INT32_MAX;
-    constexpr int kWide = D < 256 ? 2 : 1;
-    if (p.wide)
-      k_attn_rows<T, D, kWide><<<grid, kWaves * 64, 0, s>>>(a, p.group, p.direct, p.splits, p.chunk, p.snake, most);
-    else
-      k_attn_rows<T, D, 1><<<grid, kWaves * 64, 0, s>>>(a, p.group, p.direct, p.splits, p.chunk, p.snake, most);
+    const auto go = [&](auto kernel) {
+      kernel<<<grid, kWaves * 64, 0, s>>>(a, p.group, p.direct, p.splits, p.chunk, p.snake, most);
+    };
+    // 256 channels hold a step in the registers of one wave a SIMD.  Tiles of prompts, whose keys come from the L2,
+    // gain more from a second than its spills cost (1112 tokens of 32 heads over 16 114 us and 95; 24 requests of up
+    // to 4000 tokens, 16 heads, 58 and 78).
+    if constexpr (D == 256) {
+      if (p.direct) go(k_attn_rows<T, D, 1, 1>);
+      else go(k_attn_rows<T, D, 1, 2>);
+    } else {
+      if (p.wide) go(k_attn_rows<T, D, 2, 2>);
+      else go(k_attn_rows<T, D, 1, 3>);
+    }
   }
   if (p.prefill_tiles > 0) {
     const hipError_t e = spl::launch_attn_prefill(a, p, s);
@@ -709,7 +723,13 @@ hipError_t run(const AttnArgs& a, const spl::AttnPlan& p, hipStream_t s) {
     const int64_t one = a.max_new * p.group;
     const int per = !p.direct ? 0 : (p.prefill_tiles > 0 || one > kRows ? kRows : (int)one);
     const int64_t joins = per ? a.requests * a.cache.heads * per : a.tokens * a.q.heads;
-    k_attn_join<T, D><<<dim3((unsigned)joins), kJoinWaves * 64, 0, s>>>(a, p.splits, p.group, per);
+    // few splits: a wave a row (2 splits of 5484 rows 22 us with eight, NEW with one; 64 of 32 rows 5.3 and 8)
+    if (p.splits <= kJoinDeep)
+      k_attn_join<T, D, 1><<<dim3((unsigned)((joins + kJoinWaves - 1) / kJoinWaves)), kJoinWaves * 64, 0, s>>>(
+          a, p.splits, p.group, per, (int)joins);
+    else
+      k_attn_join<T, D, kJoinWaves><<<dim3((unsigned)joins), kJoinWaves * 64, 0, s>>>(a, p.splits, p.group, per,
+                                                                                     (int)joins);
   }
   return hipGetLastError();
 }
