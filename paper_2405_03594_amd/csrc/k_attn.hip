@@ -39,6 +39,7 @@ constexpr int kGroupsPerCu = 2;
 constexpr int kMaxSplits = 64;
 constexpr int kMinChunk = 16;
 constexpr int kWideSteps = 64;
+constexpr int kShortSteps = 20;
 
 template <int D>
 struct Geom {
@@ -642,6 +643,13 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_attn_join(AttnArgs a, int s
 // Splits: twice as many workgroups as CUs are enough (16 requests of up to 4096
 // tokens, 32 heads: 512 workgroups 37.0 us, 1024 with the join 40.2; 64 requests of
 // up to 2000, 8 heads: 21.6 and 31.4), and a wave wants four steps.
+// 256 channels hold a step in the registers of one wave a SIMD, and one workgroup a
+// CU is enough then (us with two / one, 16 heads: 24 requests of up to 1200 tokens
+// 34.7 / 29.8, of 2000 43.7 / 39.9; 8 of 8000, 8 heads, 38.5 / 33.5).  Tiles of
+// prompts, whose keys come from the L2, and many short requests gain more from a
+// second wave than its spills cost (one / two: 1112 tokens of 32 heads over 16 114 /
+// 95; 24 requests of up to 300 tokens 18.9 / 15.7, of 600 23.0 / 21.4, of 1200 29.8 /
+// 35.7, of 4000 58 / 78).
 // Two tiles a workgroup, which halve the widening, where enough are left and
 // their tokens many.  us with one / two, bf16, 32 heads over 8, 128 channels, the
 // last 512 tokens of 1024: 22.5 / 21.8, of 2048 37.1 / 32.6, of 8192 130 / 100;
@@ -677,13 +685,15 @@ spl::AttnPlan plan_of(const AttnArgs& a) {
   if (p.prefill_tiles > 0 && a.requests == 1) p.tiles = rows > kRows ? 0 : 1;
   // split the tokens into chunks while the launch has fewer workgroups than the chip takes
   const int64_t groups = p.tiles * a.cache.heads;
-  int64_t s = groups > 0 ? (kGroupsPerCu * cus + groups - 1) / groups : 1;
+  const int64_t full = (p.direct && a.cache.head_dim == 256 ? 1 : kGroupsPerCu) * cus;
+  int64_t s = groups > 0 ? (full + groups - 1) / groups : 1;
   s = s < 1 ? 1 : (s > kMaxSplits ? kMaxSplits : s);
   int64_t chunk = (steps + s - 1) / s;
   chunk = chunk < kMinChunk ? kMinChunk : chunk;
   chunk = (chunk + kWaves - 1) / kWaves * kWaves;
   p.chunk = (int)chunk;
   p.splits = p.tiles > 0 ? (int)((steps + chunk - 1) / chunk) : 1;
+  p.two = a.cache.head_dim == 256 && (!p.direct || (groups > cus && steps <= kShortSteps));
   // several requests of unknown lengths, and more workgroups than CUs; ranking
   // them takes as long as they are many.  us in their order / ranked, bf16, 128
   // channels, 64 requests of 8 heads of up to 200, 400, 800, 1600, 8000 tokens 7.9 /
@@ -703,12 +713,9 @@ hipError_t run(const AttnArgs& a, const spl::AttnPlan& p, hipStream_t s) {
     const auto go = [&](auto kernel) {
       kernel<<<grid, kWaves * 64, 0, s>>>(a, p.group, p.direct, p.splits, p.chunk, p.snake, most);
     };
-    // 256 channels hold a step in the registers of one wave a SIMD.  Tiles of prompts, whose keys come from the L2,
-    // gain more from a second than its spills cost (1112 tokens of 32 heads over 16 114 us and 95; 24 requests of up
-    // to 4000 tokens, 16 heads, 58 and 78).
     if constexpr (D == 256) {
-      if (p.direct) go(k_attn_rows<T, D, 1, 1>);
-      else go(k_attn_rows<T, D, 1, 2>);
+      if (p.two) go(k_attn_rows<T, D, 1, 2>);
+      else go(k_attn_rows<T, D, 1, 1>);
     } else {
       if (p.wide) go(k_attn_rows<T, D, 2, 2>);
       else go(k_attn_rows<T, D, 1, 3>);
@@ -723,7 +730,7 @@ hipError_t run(const AttnArgs& a, const spl::AttnPlan& p, hipStream_t s) {
     const int64_t one = a.max_new * p.group;
     const int per = !p.direct ? 0 : (p.prefill_tiles > 0 || one > kRows ? kRows : (int)one);
     const int64_t joins = per ? a.requests * a.cache.heads * per : a.tokens * a.q.heads;
-    // few splits: a wave a row (2 splits of 5484 rows 22 us with eight, NEW with one; 64 of 32 rows 5.3 and 8)
+    // few splits: a wave a row (2 splits of 5484 rows 22 us with eight, 5.7 with one)
     if (p.splits <= kJoinDeep)
       k_attn_join<T, D, 1><<<dim3((unsigned)((joins + kJoinWaves - 1) / kJoinWaves)), kJoinWaves * 64, 0, s>>>(
           a, p.splits, p.group, per, (int)joins);

@@ -100,6 +100,7 @@ struct AttnPlan {
   int group;                                    // query heads of a key head
   int direct;                                   // a tile is a request
   int wide;                                     // tiles of twice the rows
+  int two;                                      // 256 channels: two waves a SIMD, not one
   int splits, chunk;                            // of the tokens in k_attn_rows; chunk in its steps
   int snake;                                    // requests of a round of the chip, 0: in their order
 };
