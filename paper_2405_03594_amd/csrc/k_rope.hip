@@ -221,14 +221,16 @@ __device__ __forceinline__ void store_codes(uint8_t* region, const spl::PageGeom
 }
 
 // Where a task's heads are: a token's first tasks are q's, then k's, then (with
-// a cache) v's, each of kIter slots of 64 / LPH heads.
+// a cache) v's, each of kIter slots of 64 / LPH heads.  Flat, for few heads: the
+// call's first tasks are q's, and their slots run on from token to token.
 struct Task {
-  int64_t token;
+  int token;
   bool is_q, is_v;
-  int first;                                    // head
+  int first;                                    // head, flat: row of (token, head)
 };
+template <bool kFlat>
 __device__ __forceinline__ Task task_of(int task, int q_tasks, int k_tasks, int all_tasks, int heads) {
-  const int t = task / all_tasks, part = task - t * all_tasks;
+  const int t = kFlat ? 0 : task / all_tasks, part = task - t * all_tasks;
   Task k;
   k.token = t;
   k.is_q = part < q_tasks;
@@ -236,51 +238,68 @@ __device__ __forceinline__ Task task_of(int task, int q_tasks, int k_tasks, int 
   k.first = (k.is_q ? part : (k.is_v ? part - q_tasks - k_tasks : part - q_tasks)) * heads;
   return k;
 }
+// The token and head of a slot; one past the last repeats it (in: it does not).
+struct Slot {
+  int64_t token;
+  int head;
+  bool in;
+};
+template <bool kFlat>
+__device__ __forceinline__ Slot slot_of(int token, int at, int heads, int64_t tokens) {
+  const int last = (kFlat ? (int)tokens * heads : heads) - 1, x = at < last ? at : last;
+  if (!kFlat) return {token, x, at <= last};
+  const int t = x / heads;
+  return {t, x - t * heads, at <= last};
+}
 
 // A wave takes tasks in a fixed stride, the next one's heads requested before
-// this one's are used.  A slot past the last head repeats it, and writes nothing.
-template <class T, int LPH, bool kInter, int kIter, bool kWhole>
+// this one's are used.
+template <class T, int LPH, bool kInter, int kIter, bool kWhole, bool kFlat>
 __global__ __launch_bounds__(kThreads) void k_norm_rope(spl::NormRopeArgs a, int q_tasks, int k_tasks, int all_tasks,
                                                         float inv_dim) {
   constexpr int kSlots = 64 / LPH;
   const int lane = threadIdx.x & 63, chunk = lane & (LPH - 1);
   const bool live = kWhole || 8 * chunk < a.dim;
   const int at = live ? 8 * chunk : 0;
-  const int tasks = (int)a.tokens * all_tasks, stride = gridDim.x * kWaves;             // < 2^31
+  const int tasks = kFlat ? all_tasks : (int)a.tokens * all_tasks, stride = gridDim.x * kWaves;        // < 2^31
   u32x4 x[kIter], ahead[kIter];
   const auto fetch = [&](int task) {
-    const Task k = task_of(task, q_tasks, k_tasks, all_tasks, kIter * kSlots);
+    const Task k = task_of<kFlat>(task, q_tasks, k_tasks, all_tasks, kIter * kSlots);
     const spl_heads& src = k.is_q ? a.q : (k.is_v ? a.v : a.k);
-    const uint16_t* in = static_cast<const uint16_t*>(src.data) + k.token * src.token_stride + at;
-    const int mine = k.first + lane / LPH, last = src.heads - 1;
+    const uint16_t* in = static_cast<const uint16_t*>(src.data) + at;
 #pragma unroll
     for (int i = 0; i < kIter; ++i) {
-      const int h = mine + i * kSlots;
-      ahead[i] = *reinterpret_cast<const u32x4*>(in + (h < last ? h : last) * src.head_stride);
+      const Slot s = slot_of<kFlat>(k.token, k.first + lane / LPH + i * kSlots, src.heads, a.tokens);
+      ahead[i] = *reinterpret_cast<const u32x4*>(in + s.token * src.token_stride + s.head * src.head_stride);
     }
+  };
+  const auto turn_of = [&](int64_t t) {
+    return load_turn<LPH, kInter, kWhole>(a.rope, a.rope_rows, kWhole || a.rot ? a.positions[t] : 0, a.rot, chunk, lane);
   };
   int task = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * kWaves + (threadIdx.x >> 6)));
   if (task < tasks) fetch(task);
   for (; task < tasks; task += stride) {
-    const Task k = task_of(task, q_tasks, k_tasks, all_tasks, kIter * kSlots);
-    const int64_t t = k.token;
-    const int heads = k.is_q ? a.q.heads : a.k.heads, mine = k.first + lane / LPH, last = heads - 1;
-    const bool full = kWhole && k.first + kIter * kSlots <= heads;
+    const Task k = task_of<kFlat>(task, q_tasks, k_tasks, all_tasks, kIter * kSlots);
+    const int heads = k.is_q ? a.q.heads : a.k.heads, mine = k.first + lane / LPH;
+    const bool full = kWhole && k.first + kIter * kSlots <= (kFlat ? (int)a.tokens * heads : heads);
 #pragma unroll
     for (int i = 0; i < kIter; ++i) x[i] = ahead[i];
     if (tasks - task > stride) fetch(task + stride);
-    const int64_t slot = k.is_q || !a.cache.data ? -1 : a.slots[t];
+    const bool store = !k.is_q && a.cache.data;
+    const int64_t slot = !kFlat && store ? a.slots[k.token] : -1;
     const uint16_t* w16 = static_cast<const uint16_t*>(k.is_q ? a.wq : a.wk);
     if (!k.is_v) {
       float w[8], r[kIter];
       if (w16) widen<T>(*reinterpret_cast<const u32x4*>(w16 + at), w);
-      const Turn<kInter> tr =
-          load_turn<LPH, kInter, kWhole>(a.rope, a.rope_rows, kWhole || a.rot ? a.positions[t] : 0, a.rot, chunk, lane);
+      Turn<kInter> tr;
+      if (!kFlat) tr = turn_of(k.token);
       uint16_t* out = static_cast<uint16_t*>(k.is_q ? a.q_out : a.k_out);
-      if (out) out += t * heads * (int64_t)a.dim + at;
+      if (out) out += at;
       if (w16) inverse_rms<T, LPH, kIter>(x, inv_dim, a.eps, !live, lane, r);
 #pragma unroll
       for (int i = 0; i < kIter; ++i) {
+        const Slot s = slot_of<kFlat>(k.token, mine + i * kSlots, heads, a.tokens);
+        if (kFlat) tr = turn_of(s.token);
         float f[8];
         widen<T>(x[i], f);
         if (w16) {
@@ -289,21 +308,23 @@ __global__ __launch_bounds__(kThreads) void k_norm_rope(spl::NormRopeArgs a, int
         }
         if (kWhole || a.rot) turn<LPH, kInter, kWhole, false>(tr, f);
         x[i] = narrow<T>(f);
-        const int h = mine + i * kSlots;
-        if (out && (full || (live && h <= last))) *reinterpret_cast<u32x4*>(out + (int64_t)h * a.dim) = x[i];
+        if (out && (full || (live && s.in)))
+          *reinterpret_cast<u32x4*>(out + (s.token * heads + s.head) * a.dim) = x[i];
       }
     }
+    if (!store) continue;
     const int shift = __builtin_ctz((unsigned)a.cache.page);
-    if (slot < 0 || (slot >> shift) >= a.cache.pages) continue;
     const spl::PageGeom g = spl::page_geom(a.dim, a.cache.page);
-    const int b = (int)(slot & (a.cache.page - 1));
-    uint8_t* page = static_cast<uint8_t*>(a.cache.data) + (slot >> shift) * (int64_t)a.cache.heads * g.bytes;
+    if (!kFlat && (slot < 0 || (slot >> shift) >= a.cache.pages)) continue;
 #pragma unroll
     for (int i = 0; i < kIter; ++i) {
       uint32_t code;
       const uint32_t scale = encode8<T>(x[i], &code);
-      const int h = mine + i * kSlots;
-      if (live && h <= last) store_codes(page + (int64_t)h * g.bytes, g, k.is_v, b, chunk, code, scale);
+      const Slot s = slot_of<kFlat>(k.token, mine + i * kSlots, heads, a.tokens);
+      const int64_t to = kFlat ? a.slots[s.token] : slot;
+      if (!(live && s.in) || (kFlat && (to < 0 || (to >> shift) >= a.cache.pages))) continue;
+      uint8_t* page = static_cast<uint8_t*>(a.cache.data) + (to >> shift) * (int64_t)a.cache.heads * g.bytes;
+      store_codes(page + (int64_t)s.head * g.bytes, g, k.is_v, (int)(to & (a.cache.page - 1)), chunk, code, scale);
     }
   }
 }
@@ -362,7 +383,7 @@ __global__ __launch_bounds__(kThreads) void k_cache_read(spl_kv_cache c, const i
 // channels, so dw's terms stay in registers; its sums go to one row of
 // `partial`, which k_norm_rope_dw adds up in order: the result does not change
 // from run to run.
-template <class T, int LPH, bool kInter, int kIter, bool kWhole>
+template <class T, int LPH, bool kInter, int kIter, bool kWhole, bool kFlat>
 __global__ __launch_bounds__(kThreads) void k_norm_rope_grad(spl::NormRopeGradArgs a, int q_groups, int groups,
                                                              float inv_dim) {
   constexpr int kSlots = 64 / LPH;
@@ -372,7 +393,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_rope_grad(spl::NormRopeGradAr
   const int group = is_q ? blockIdx.x : blockIdx.x - q_groups, count = is_q ? q_groups : groups - q_groups;
   const spl_heads& src = is_q ? a.q : a.k;
   const spl_heads& grad = is_q ? a.dq : a.dk;
-  const int at = live ? 8 * chunk : 0, last = src.heads - 1;
+  const int at = live ? 8 * chunk : 0;
   uint16_t* out = static_cast<uint16_t*>(is_q ? a.dq_out : a.dk_out) + at;
   const uint16_t* in = static_cast<const uint16_t*>(src.data) + at;
   const uint16_t* up = static_cast<const uint16_t*>(grad.data) + at;
@@ -381,28 +402,32 @@ __global__ __launch_bounds__(kThreads) void k_norm_rope_grad(spl::NormRopeGradAr
 #pragma unroll
   for (int e = 0; e < 8; ++e) dw[e] = 0.0f, w[e] = 1.0f;
   if (w16) widen<T>(*reinterpret_cast<const u32x4*>(w16 + at), w);
-  const int per = (src.heads + kIter * kSlots - 1) / (kIter * kSlots);       // waves of one token
-  const int64_t tasks = a.tokens * per;                         // < 2^31
+  // tasks of one token; flat: slots run on from token to token
+  const int rows = kFlat ? (int)a.tokens * src.heads : src.heads, per = (rows + kIter * kSlots - 1) / (kIter * kSlots);
+  const int64_t tasks = kFlat ? per : a.tokens * per;           // < 2^31
+  const auto turn_of = [&](int64_t t) {
+    return load_turn<LPH, kInter, kWhole>(a.rope, a.rope_rows, kWhole || a.rot ? a.positions[t] : 0, a.rot, chunk, lane);
+  };
   for (int64_t task = (int64_t)group * kWaves + wave; task < tasks; task += (int64_t)count * kWaves) {
-    const int task32 = __builtin_amdgcn_readfirstlane((int)task), t32 = task32 / per;
-    const int64_t t = t32;
+    const int task32 = __builtin_amdgcn_readfirstlane((int)task), t32 = kFlat ? 0 : task32 / per;
     const int first = (task32 - t32 * per) * kIter * kSlots, mine = first + lane / LPH;
-    const bool full = kWhole && first + kIter * kSlots <= src.heads;
+    const bool full = kWhole && first + kIter * kSlots <= rows;
     u32x4 x[kIter], g[kIter];
 #pragma unroll
     for (int i = 0; i < kIter; ++i) {
-      const int h = mine + i * kSlots < last ? mine + i * kSlots : last;
-      g[i] = *reinterpret_cast<const u32x4*>(up + t * grad.token_stride + h * grad.head_stride);
-      if (w16) x[i] = *reinterpret_cast<const u32x4*>(in + t * src.token_stride + h * src.head_stride);
+      const Slot s = slot_of<kFlat>(t32, mine + i * kSlots, src.heads, a.tokens);
+      g[i] = *reinterpret_cast<const u32x4*>(up + s.token * grad.token_stride + s.head * grad.head_stride);
+      if (w16) x[i] = *reinterpret_cast<const u32x4*>(in + s.token * src.token_stride + s.head * src.head_stride);
     }
-    const Turn<kInter> tr =
-        load_turn<LPH, kInter, kWhole>(a.rope, a.rope_rows, kWhole || a.rot ? a.positions[t] : 0, a.rot, chunk, lane);
+    Turn<kInter> tr;
+    if (!kFlat) tr = turn_of(t32);
     float r[kIter];
     if (w16) inverse_rms<T, LPH, kIter>(x, inv_dim, a.eps, !live, lane, r);
 #pragma unroll
     for (int i = 0; i < kIter; ++i) {
-      const int h = mine + i * kSlots;
-      const bool counts = full || (live && h <= last);          // a repeated head adds nothing to dw
+      const Slot s = slot_of<kFlat>(t32, mine + i * kSlots, src.heads, a.tokens);
+      const bool counts = full || (live && s.in);               // a repeated head adds nothing to dw
+      if (kFlat) tr = turn_of(s.token);
       float f[8], d[8];
       widen<T>(g[i], d);
       if (kWhole || a.rot) turn<LPH, kInter, kWhole, true>(tr, d);
@@ -420,7 +445,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_rope_grad(spl::NormRopeGradAr
 #pragma unroll
         for (int e = 0; e < 8; ++e) d[e] = r[i] * __builtin_fmaf(f[e], m, d[e]);
       }
-      if (counts) *reinterpret_cast<u32x4*>(out + (t * src.heads + h) * a.dim) = narrow<T>(d);
+      if (counts) *reinterpret_cast<u32x4*>(out + (s.token * src.heads + s.head) * a.dim) = narrow<T>(d);
     }
   }
   if (!w16) return;                                             // the same for the whole workgroup
@@ -476,13 +501,31 @@ int slots_of(int64_t tokens, int64_t heads, int lph) {
 }
 int lanes_of(int dim) { return dim <= 64 ? 8 : (dim <= 128 ? 16 : 32); }
 
+// Few heads: where those of a token fill less than half of its slots, the slots
+// run on over the tokens (two of a wave, with angles of their own).  us in a
+// token's slots / flat: 4 + 1 heads of 4096 tokens stored 15.6 / 11.8, 1 + 1 of
+// 87186 212 / 42; 6 + 1 of 64 channels, 7960 tokens, forward and backward 33.4 / 21.8.
+constexpr int kFlatSlots = 2;
+int wave_slots(int64_t tokens, int32_t q_heads, int32_t k_heads, int lph, bool cache, bool* flat) {
+  const int64_t all = q_heads + (cache ? 2 : 1) * (int64_t)k_heads;
+  const int iter = slots_of(tokens, all, lph), per = iter * (64 / lph);
+  const auto filled = [&](int64_t h) { return (h + per - 1) / per * per; };
+  *flat = 2 * all < filled(q_heads) + (cache ? 2 : 1) * filled(k_heads);
+  return *flat ? kFlatSlots : iter;
+}
+int64_t tasks_of(int64_t tokens, int64_t heads, int per, bool flat) {
+  return flat ? (tokens * heads + per - 1) / per : tokens * ((heads + per - 1) / per);
+}
+
 // Workgroups of the gradient for q and for k: shared out by heads, at most as
 // many as the chip holds (134 registers; 2048 tokens of 32 + 32 heads of 128
 // channels: three a CU 23.8 us, four 27.1).
 void grad_groups(int64_t tokens, int32_t q_heads, int32_t k_heads, int32_t dim, int* q, int* k) {
-  const int lph = lanes_of(dim), heads = slots_of(tokens, (int64_t)q_heads + k_heads, lph) * (64 / lph);
+  const int lph = lanes_of(dim);
+  bool flat;
+  const int per = wave_slots(tokens, q_heads, k_heads, lph, false, &flat) * (64 / lph);
   const int64_t most = 3 * (int64_t)spl::device_cus();
-  const auto groups = [&](int64_t h) { return (tokens * ((h + heads - 1) / heads) + kWaves - 1) / kWaves; };
+  const auto groups = [&](int64_t h) { return (tasks_of(tokens, h, per, flat) + kWaves - 1) / kWaves; };
   const int64_t gq = groups(q_heads), gk = groups(k_heads);
   int64_t nq = gq, nk = gk;
   if (gq + gk > most) {
@@ -509,26 +552,29 @@ void grad_groups(int64_t tokens, int32_t q_heads, int32_t k_heads, int32_t dim, 
   } while (0)
 #define SPL_PICK_N(kernel, L, I, iter, whole, ...)                                                       \
   do {                                                                                                   \
-    if ((iter) == 4) SPL_PICK_W(kernel, L, I, 4, whole, __VA_ARGS__);                                    \
-    else SPL_PICK_W(kernel, L, I, 2, whole, __VA_ARGS__);                                                \
+    if (flat) SPL_PICK_W(kernel, L, I, kFlatSlots, true, whole, __VA_ARGS__);                            \
+    else if ((iter) == 4) SPL_PICK_W(kernel, L, I, 4, false, whole, __VA_ARGS__);                        \
+    else SPL_PICK_W(kernel, L, I, 2, false, whole, __VA_ARGS__);                                         \
   } while (0)
-#define SPL_PICK_W(kernel, L, I, N, whole, ...)                                                          \
+#define SPL_PICK_W(kernel, L, I, N, F, whole, ...)                                                       \
   do {                                                                                                   \
-    if (whole) kernel<T, L, I, N, true> __VA_ARGS__;                                                     \
-    else kernel<T, L, I, N, false> __VA_ARGS__;                                                          \
+    if (whole) kernel<T, L, I, N, true, F> __VA_ARGS__;                                                  \
+    else kernel<T, L, I, N, false, F> __VA_ARGS__;                                                       \
   } while (0)
 
 template <class T>
 hipError_t norm_rope(const spl::NormRopeArgs& a, hipStream_t s) {
   const int lph = lanes_of(a.dim);
-  const int iter = slots_of(a.tokens, (int64_t)a.q.heads + (a.cache.data ? 2 : 1) * (int64_t)a.k.heads, lph);
-  const int heads = iter * (64 / lph);
-  const int qw = (a.q.heads + heads - 1) / heads, kw = (a.k.heads + heads - 1) / heads;
+  bool flat;
+  const int iter = wave_slots(a.tokens, a.q.heads, a.k.heads, lph, a.cache.data != nullptr, &flat);
+  const int64_t tokens = flat ? a.tokens : 1;    // that the tasks are counted over
+  const int per = iter * (64 / lph);
+  const int qw = (int)tasks_of(tokens, a.q.heads, per, flat), kw = (int)tasks_of(tokens, a.k.heads, per, flat);
   const int all = qw + kw + (a.cache.data ? kw : 0);
   // as many waves as the chip holds (85 to 128 registers): 2048 tokens of 32 + 32
   // heads of 128 channels 18.2 us with a wave a task, 17.5 so; 2 or 3 workgroups a
   // CU 20.2, 18.3
-  const int64_t need = (a.tokens * all + kWaves - 1) / kWaves, most = 4 * (int64_t)spl::device_cus();
+  const int64_t need = ((flat ? 1 : a.tokens) * all + kWaves - 1) / kWaves, most = 4 * (int64_t)spl::device_cus();
   const dim3 grid((unsigned)(need < most ? need : most));
   const float inv = (float)(1.0 / a.dim);
   SPL_PICK(k_norm_rope, lph, a.interleaved, iter, a.rot == 8 * lph,
@@ -540,7 +586,9 @@ template <class T>
 hipError_t norm_rope_grad(const spl::NormRopeGradArgs& a, hipStream_t s) {
   int nq, nk;
   grad_groups(a.tokens, a.q.heads, a.k.heads, a.dim, &nq, &nk);
-  const int lph = lanes_of(a.dim), iter = slots_of(a.tokens, (int64_t)a.q.heads + a.k.heads, lph);
+  const int lph = lanes_of(a.dim);
+  bool flat;
+  const int iter = wave_slots(a.tokens, a.q.heads, a.k.heads, lph, false, &flat);
   const float inv = (float)(1.0 / a.dim);
   SPL_PICK(k_norm_rope_grad, lph, a.interleaved, iter, a.rot == 8 * lph,
            <<<nq + nk, kThreads, 0, s>>>(a, nq, nq + nk, inv));

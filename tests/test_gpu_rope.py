@@ -238,6 +238,50 @@ def test_every_payload_is_stored_as_the_format_says(dt):
     _same(values.view(-1, 32)[sample.cuda()], want)
 
 
+FEW = [(1500, 1, 1, 96, 96, False, True, True), (2500, 4, 1, 128, 64, True, False, True),
+       (4001, 3, 1, 64, 32, True, True, True), (600, 1, 1, 256, 256, False, False, False),
+       (9000, 2, 1, 40, 32, False, False, True)]
+
+
+@pytest.mark.parametrize("dt", DTYPES)
+@pytest.mark.parametrize("case", FEW)
+def test_few_heads_of_many_tokens(case, dt):
+    """A wave's slots run on over the tokens: the forward pass and the gradient, and the bits of a call of many heads."""
+    test_forward(case, dt)
+    test_gradient(case, dt)
+    T, _, _, D, rot, inter, _, _ = case
+    _, _, _, _, (q, k, v), w, pos, rope = _make(T, 24, 24, D, rot, dt, 3)
+    spl = _spl()
+    args = dict(eps=1e-5, interleaved=inter)
+    many = spl.qk_norm_rope(q, k, pos, rope, w[0], w[1], **args)
+    few = spl.qk_norm_rope(q[:, 5:6], k[:, 7:8], pos, rope, w[0], w[1], **args)
+    torch.cuda.synchronize()
+    assert torch.equal(few[0], many[0][:, 5:6]) and torch.equal(few[1], many[1][:, 7:8])
+
+
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+def test_few_heads_stored(D):
+    """Slots of their own for each token of a wave, some of them none."""
+    T, page, dt = 1500, 32, torch.bfloat16
+    (q, k, v), w, pos, rope, (dq, dk, dv), dw, dpos, drope = _make(T, 3, 1, D, D, dt, 4)
+    spl = _spl()
+    pages = -(-T // page) + 3
+    slots = torch.randperm(pages * page, generator=torch.Generator().manual_seed(5))[:T].int()
+    slots[::7] = -1
+    slots[3::70] = pages * page + 5
+    cache = spl.KVCache.empty(pages, 1, D, page, dt)
+    ko = torch.empty_like(dk)
+    qo = spl.qk_norm_rope_append(dq, dk, dv, dpos, drope, slots.cuda(), cache, dw[0], dw[1], k_out=ko)
+    want = spl.qk_norm_rope(dq, dk, dpos, drope, dw[0], dw[1])
+    keys, values = spl.cache_read(cache, slots.cuda())
+    torch.cuda.synchronize()
+    assert torch.equal(qo, want[0]) and torch.equal(ko, want[1])
+    held = (slots >= 0) & (slots < pages * page)
+    _same(keys[held.cuda()], ref.stored(ko.cpu()[held]))
+    _same(values[held.cuda()], ref.stored(v[held]))
+    assert not keys[~held.cuda()].any() and not values[~held.cuda()].any()
+
+
 def test_a_cache_past_four_gigabytes():
     spl = _spl()
     D, page, Hk = 128, 256, 8
