@@ -18,7 +18,7 @@
 // 200 vector instructions and D / 8 matrix instructions of one wave.  Measured, 128
 // channels: 16 requests of up to 4096 tokens, 32 heads, 36.5 us, 160 MB at 4.4 TB/s
 // (the loads alone 31.6, without any of the arithmetic); 64 requests of up to
-// 2000, 8 heads, 21.5 us, 79 MB at 3.7; one request of 131072 tokens, 8 heads, 31 us
+// 2000, 8 heads, 21.3 us, 79 MB at 3.7; one request of 131072 tokens, 8 heads, 31 us
 // and 5 for the join of 64 splits, 142 MB at 4.6; one of 93 tokens 5.2 us.  More
 // waves, deeper requests or more occupancy gain nothing.
 #include "attn_tile.h"

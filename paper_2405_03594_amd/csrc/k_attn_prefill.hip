@@ -22,9 +22,9 @@
 // additions, operands read six ahead and other orders of the products change it by
 // 1%; without widening, exponentials or operand reads (8192 tokens) it would take
 // 0.88, 0.92, 0.87 of the time, without all three 0.71, at the rate of the library's
-// large product.  Measured, bf16, 32 heads of 128 channels: 1024 tokens 28.1 us,
-// 2048 55.9 us (615 TFLOP/s; 10 us are the launch's start, 4 each workgroup's start
-// and end), 4096 178 (773), 8192 632 (870, the library 1247); of 64 channels 2048
+// large product.  Measured, bf16, 32 heads of 128 channels: 1024 tokens 27.2 us,
+// 2048 55.3 us (622 TFLOP/s; 10 us are the launch's start, 4 each workgroup's start
+// and end), 4096 176 (780), 8192 632 (870, the library 1247); of 64 channels 2048
 // 35 us, 8192 392.
 #include "attn_tile.h"
 
