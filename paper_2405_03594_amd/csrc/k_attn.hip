@@ -693,6 +693,9 @@ spl::AttnPlan plan_of(const AttnArgs& a) {
   chunk = (chunk + kWaves - 1) / kWaves * kWaves;
   p.chunk = (int)chunk;
   p.splits = p.tiles > 0 ? (int)((steps + chunk - 1) / chunk) : 1;
+  // no fewer than any smaller number of steps is split into
+  const int64_t chunks = (steps + kMinChunk - 1) / kMinChunk;
+  p.most_splits = p.tiles > 0 ? (int)(s < chunks ? s : chunks) : 1;
   p.two = a.cache.head_dim == 256 && (!p.direct || (groups > cus && steps <= kShortSteps));
   // several requests of unknown lengths, and more workgroups than CUs; ranking
   // them takes as long as they are many.  us in their order / ranked, bf16, 128
@@ -757,8 +760,8 @@ namespace spl {
 
 int64_t attn_workspace_bytes(const AttnArgs& a) {
   const AttnPlan p = plan_of(a);
-  if (p.splits == 1) return 0;
-  return a.tokens * a.q.heads * ((int64_t)p.splits * (a.cache.head_dim + 2) + 1) * 4;
+  if (p.most_splits <= 1) return 0;
+  return a.tokens * a.q.heads * ((int64_t)p.most_splits * (a.cache.head_dim + 2) + 1) * 4;
 }
 
 hipError_t launch_attn(const AttnArgs& a, hipStream_t s) {

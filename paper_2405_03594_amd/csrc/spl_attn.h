@@ -102,10 +102,11 @@ struct AttnPlan {
   int wide;                                     // tiles of twice the rows
   int two;                                      // 256 channels: two waves a SIMD, not one
   int splits, chunk;                            // of the tokens in k_attn_rows; chunk in its steps
+  int most_splits;                              // of this call under any window: the workspace's
   int snake;                                    // requests of a round of the chip, 0: in their order
 };
 hipError_t launch_attn_prefill(const AttnArgs& a, const AttnPlan& p, hipStream_t s);
-int64_t attn_workspace_bytes(const AttnArgs& a);
+int64_t attn_workspace_bytes(const AttnArgs& a);                // the window does not count
 hipError_t launch_attn(const AttnArgs& a, hipStream_t s);
 
 }  // namespace spl

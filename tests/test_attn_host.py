@@ -218,6 +218,18 @@ def test_attention_checks(L):
         assert size(*a) == -1
 
 
+def test_the_workspace_holds_any_window(L):
+    """The size is asked without the window, which only takes tokens away: fewer tokens never need more."""
+    size = L.spl_attention_fp4_workspace_bytes
+    for requests, heads in ((1, 1), (3, 2), (26, 2), (7, 5), (40, 8), (1, 8)):
+        for dim in (64, 256):
+            last = 0
+            for steps in range(1, 420):
+                now = size(_c(heads=heads, head_dim=dim), requests, 4 * heads, requests, 5000, 1, 32 * steps)
+                assert now >= last, (requests, heads, dim, steps)
+                last = now
+
+
 # ---------------------------------------------------------------------------------------------- refusals (Python)
 
 

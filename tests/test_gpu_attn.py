@@ -235,6 +235,21 @@ def test_split_requests_beside_prompts():
         assert ((lse[s:e] - l).abs() <= tol).all(), r
 
 
+def test_a_window_that_is_split_further_than_its_requests():
+    """5440 tokens are split into 9, a window of 5100 of them into 10: the workspace has room."""
+    cus = torch.cuda.get_device_properties(0).multi_processor_count
+    R = 26 * cus // 256
+    lens = [5440] + [50] * (R - 2) + [5300]
+    b = Batch([1] * R, lens, 2, 2, 64, 64, BF, seed=22)
+    got, lse = b.run(window=5100)
+    for r in (0, 1, R - 1):
+        w, l, m, top = ref.attention(b.q.double()[r:r + 1], b.keys[r:r + 1], b.values[r:r + 1], [0, 1], [lens[r]],
+                                     64 ** -0.5, 5100)
+        tol = 3 * ref.UNIT[BF] + 2.0 ** -18 * (1 + top)
+        assert ((got[r] - w[0]).abs() <= tol * m[0] + ref.STEP[BF]).all(), r
+        assert ((lse[r] - l[0]).abs() <= tol).all(), r
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.2, 1.0, 3e-3])
 def test_scales(scale):
     Batch([1, 20], [70, 45], 4, 4, 64, 16, BF, seed=8).check(scale=scale)
