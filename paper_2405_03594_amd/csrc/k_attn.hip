@@ -563,14 +563,16 @@ __global__ __launch_bounds__(kWaves * 64, O) void k_attn_rows(
 
 // The splits of a row joined (by the last of its workgroups instead, with a fence
 // that writes the L2 back in each, 131072 tokens take 53 us and not 37; by a wave a
-// row 39): W waves a row (per > 0: of the first `per` of a
-// request and key head, if it has no more) that share the splits, D / 64 channels
-// a lane.  A lane knows the statistics of one split.
+// row 39): W waves a row that share the splits, D / 64 channels a lane.  per > 0: the
+// rows are the first `per` of a request and key head; a request of more than `most`
+// is another kernel's, one of more than `per` has its first ones joined.  A lane
+// knows the statistics of one split.
 // Loads go out in two rounds: the counts and statistics, then all sums.
 constexpr int kJoinWaves = 8;                    // of a workgroup
 constexpr int kJoinDeep = kMaxSplits / kJoinWaves;               // splits of a wave
 template <class T, int D, int W>
-__global__ __launch_bounds__(kJoinWaves * 64) void k_attn_join(AttnArgs a, int splits, int group, int per, int joins) {
+__global__ __launch_bounds__(kJoinWaves * 64) void k_attn_join(AttnArgs a, int splits, int group, int per, int joins,
+                                                            int most) {
   constexpr int C = D == 256 ? 4 : 2;                            // channels of a lane; D 64 and 96 leave lanes idle
   typedef float vec __attribute__((ext_vector_type(C)));
   const int lane = threadIdx.x & 63, in = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = in & (W - 1);
@@ -582,7 +584,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_attn_join(AttnArgs a, int s
     const int32_t place = join / per, at = join - place * per;
     const int32_t req = place / a.cache.heads, head = place - req * a.cache.heads;
     const spl::Rows rows = spl::wave_rows_of(a, req);
-    if (at >= rows.count * group || rows.count * group > per) return;
+    if (at >= rows.count * group || rows.count * group > most) return;
     const int32_t tok = at / group;
     row = (rows.first + tok) * a.q.heads + head * group + (at - tok * group);
   } else {
@@ -710,9 +712,9 @@ spl::AttnPlan plan_of(const AttnArgs& a) {
 
 template <class T, int D>
 hipError_t run(const AttnArgs& a, const spl::AttnPlan& p, hipStream_t s) {
+  const int most = p.prefill_tiles > 0 ? kRows : INT32_MAX;      // rows of a request that are not another kernel's
   if (p.tiles > 0) {
     const dim3 grid((unsigned)(p.tiles * a.cache.heads), (unsigned)p.splits);
-    const int most = p.prefill_tiles > 0 ? kRows : INT32_MAX;
     const auto go = [&](auto kernel) {
       kernel<<<grid, kWaves * 64, 0, s>>>(a, p.group, p.direct, p.splits, p.chunk, p.snake, most);
     };
@@ -736,10 +738,10 @@ hipError_t run(const AttnArgs& a, const spl::AttnPlan& p, hipStream_t s) {
     // few splits: a wave a row (2 splits of 5484 rows 22 us with eight, 5.7 with one)
     if (p.splits <= kJoinDeep)
       k_attn_join<T, D, 1><<<dim3((unsigned)((joins + kJoinWaves - 1) / kJoinWaves)), kJoinWaves * 64, 0, s>>>(
-          a, p.splits, p.group, per, (int)joins);
+          a, p.splits, p.group, per, (int)joins, most);
     else
       k_attn_join<T, D, kJoinWaves><<<dim3((unsigned)joins), kJoinWaves * 64, 0, s>>>(a, p.splits, p.group, per,
-                                                                                     (int)joins);
+                                                                                     (int)joins, most);
   }
   return hipGetLastError();
 }

@@ -424,3 +424,21 @@ def test_a_serving_step_in_a_graph():
         assert torch.equal(got, want), i
         assert torch.equal(state[2], eager[2]) and torch.equal(state[3].data, eager[3].data)
     assert eager[0].tolist() == [n + 6 for n in lens0]
+
+
+# (rows, lengths) of requests and their heads: 18, 6 and 1 splits of the longest
+LOW = [([2, 1, 3], [9000, 300, 2000], 4, 4), ([3, 1], [3000, 40], 8, 2), ([40, 2], [9000, 70], 4, 4),
+       ([2, 1, 5], [300, 40, 5], 4, 4)]
+
+
+@pytest.mark.parametrize("max_new", [1, 2])
+@pytest.mark.parametrize("new,lens,H,Hk", LOW)
+def test_the_first_rows_of_a_request_of_more_than_max_new(new, lens, H, Hk, max_new):
+    """Only rows past max_new may be left out, whether the request is split or not."""
+    b = Batch(new, lens, H, Hk, 128, 64, BF, seed=23)
+    got, lse = b.run(max_new=max_new)
+    want, want_lse, mag, top = ref.attention(b.q.double(), b.keys, b.values, b.row_start, lens, 128 ** -0.5, 0)
+    first = [int(b.row_start[r]) + t for r in range(len(new)) for t in range(min(new[r], max_new))]
+    tol = 3 * ref.UNIT[BF] + 2.0 ** -18 * (1 + top)
+    assert ((got[first] - want[first]).abs() <= tol * mag[first] + ref.STEP[BF]).all()
+    assert ((lse[first] - want_lse[first]).abs() <= tol).all()
