@@ -617,7 +617,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_attn_join(AttnArgs a, int s
     const int s = wave + i * W;
     if (s < n) {
       const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s));
-      if (ws != 0.0f) o += ws * x[i];                            // the sums of a split that saw no key are 0
+      o += ws * x[i];                            // a weight of 0 too: 0 times a NaN of the split is the row's NaN
     }
   }
   if constexpr (W > 1) {

@@ -442,3 +442,25 @@ def test_the_first_rows_of_a_request_of_more_than_max_new(new, lens, H, Hk, max_
     tol = 3 * ref.UNIT[BF] + 2.0 ** -18 * (1 + top)
     assert ((got[first] - want[first]).abs() <= tol * mag[first] + ref.STEP[BF]).all()
     assert ((lse[first] - want_lse[first]).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dt", [BF, HF])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("length", [300, 3000, 9000])
+def test_an_infinite_value_of_no_weight_reaches_its_row_however_it_is_split(length, D, dt):
+    """Weights below 2^-300 of the row's largest are 0, and 0 times an infinity is NaN: in one split, in 6, in 18."""
+    b = Batch([1], [length], 4, 2, D, 64, dt, seed=24)
+    spl = _spl()
+    k = torch.full((length, 2, D), 4.0, dtype=dt)                # scores of 16 sqrt(D), and their negatives before the middle
+    k[:length // 2] = -4.0
+    v = b.values[0].to(dt)
+    v[10, 1, 5] = float("inf")
+    at = torch.arange(length)
+    slots = (b.table[0].cpu()[at // 64] * 64 + at % 64).int().cuda()
+    spl.qk_norm_rope_append(k.cuda(), k.cuda(), v.cuda(), None, None, slots, b.cache)
+    b.q = torch.full((1, 4, D), 4.0, dtype=dt)
+    b.keys[0] = k.double()
+    b.values[0] = spl.cache_read(b.cache, slots)[1].cpu().double()
+    got = b.check()
+    assert torch.isnan(got[0, 2:, :32]).all() and torch.isfinite(got[0, :2]).all()
+    assert torch.isfinite(got[0, 2:, 32:]).all()
