@@ -960,20 +960,32 @@ class KVCache:
     data: uint8 [pages, heads, kv_page_bytes(head_dim, page)]; dtype: the type (fp16 or bf16) of what is stored and read
     back.  ``KVCache.empty`` allocates one."""
 
-    __slots__ = ("data", "pages", "heads", "page", "head_dim", "dtype", "_view")
+    __slots__ = ("data", "page", "head_dim", "dtype")
 
     def __init__(self, data: torch.Tensor, page: int, head_dim: int, dtype: torch.dtype):
+        self.data, self.page, self.head_dim, self.dtype = data, page, head_dim, dtype
+        self.view()
+
+    @property
+    def pages(self) -> int:
+        return self.data.shape[0]
+
+    @property
+    def heads(self) -> int:
+        return self.data.shape[1]
+
+    def view(self) -> _KVCache:
+        """The cache as a call takes it: of the attributes as they are now, so that it follows another `data`."""
+        data, dtype = self.data, self.dtype
         if dtype not in _HEAD_TYPES:
             raise ValueError("a cache holds fp16 or bf16 keys and values")
-        size = kv_page_bytes(head_dim, page)
+        size = kv_page_bytes(self.head_dim, self.page)
         if not isinstance(data, torch.Tensor) or data.dim() != 3 or data.shape[2] != size:
             raise ValueError(f"data must be [pages, heads, {size}]")
         if data.dtype != torch.uint8 or not data.is_contiguous():
             _arg(data, "data", dtype=torch.uint8, device=False)
-        self.data, self.page, self.head_dim, self.dtype = data, page, head_dim, dtype
-        self.pages, self.heads, _ = data.shape
-        self._view = _KVCache(data.data_ptr(), self.pages, data.numel(), page, self.heads, head_dim,
-                              _TORCH_DTYPE[dtype])
+        pages, heads, _ = data.shape
+        return _KVCache(data.data_ptr(), pages, pages * heads * size, self.page, heads, self.head_dim, _TORCH_DTYPE[dtype])
 
     @classmethod
     def empty(cls, pages: int, heads: int, head_dim: int, page: int, dtype: torch.dtype, device="cuda") -> "KVCache":
@@ -1178,7 +1190,8 @@ def qk_norm_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, posit
                         k_out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """q_out of qk_norm_rope; its keys and the values v go to `slots` of the cache in the same launch (and the keys to
     k_out, where given; see spl_qk_norm_rope_append)."""
-    D, dtype, heads = cache.head_dim, cache.dtype, cache.heads
+    view = cache.view()
+    D, dtype, heads = cache.head_dim, cache.dtype, view.heads
     hq = _heads(q, "q", None, D, dtype)
     T = q.shape[0]
     hk, hv = _heads(k, "k", T, D, dtype), _heads(v, "v", T, D, dtype)
@@ -1194,7 +1207,7 @@ def qk_norm_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, posit
         k_out = _heads_out(k_out, k, "k_out")
     _check("spl_qk_norm_rope_append",
            lib().spl_qk_norm_rope_append(hq, hk, hv, T, wq, wk, eps, at, angles, rows, rot, interleaved, to,
-                                         cache._view, q_out.data_ptr(), _ptr(k_out), _on(stream)))
+                                         view, q_out.data_ptr(), _ptr(k_out), _on(stream)))
     return q_out
 
 
@@ -1203,11 +1216,11 @@ def cache_read(cache: KVCache, slots: torch.Tensor, stream=None):
     if not isinstance(slots, torch.Tensor) or slots.dim() != 1:
         raise ValueError("slots must be 1-D")
     T = slots.shape[0]
-    at = _ints(slots, "slots", T)
+    at, view = _ints(slots, "slots", T), cache.view()
     _on_device("slots, the cache", slots, cache.data)
-    k = torch.empty((T, cache.heads, cache.head_dim), dtype=cache.dtype, device=slots.device)
+    k = torch.empty((T, view.heads, cache.head_dim), dtype=cache.dtype, device=slots.device)
     v = torch.empty_like(k)
-    _check("spl_cache_read", lib().spl_cache_read(cache._view, at, T, k.data_ptr(), v.data_ptr(), _on(stream)))
+    _check("spl_cache_read", lib().spl_cache_read(view, at, T, k.data_ptr(), v.data_ptr(), _on(stream)))
     return k, v
 
 
@@ -1218,18 +1231,18 @@ def attention_fp4(q: torch.Tensor, cache: KVCache, table: torch.Tensor, lens: to
     width] lists (see spl_attention_fp4).  `row_start` [requests + 1] and `lens` [requests] are those of block_tables;
     scale is 1 / sqrt(head_dim) unless given.  max_new (the most rows of a request) and max_len (about the most tokens)
     let the call choose its launch without asking the GPU.  lse: float32 [tokens, heads], written if given."""
-    L, D, view = lib(), cache.head_dim, cache._view
+    L, D, view = lib(), cache.head_dim, cache.view()
     hq = _heads(q, "q", None, D, cache.dtype)
     T, H, _ = q.shape
-    if H % cache.heads:
-        raise ValueError(f"q has {H} heads, not a multiple of the cache's {cache.heads}")
+    if H % view.heads:
+        raise ValueError(f"q has {H} heads, not a multiple of the cache's {view.heads}")
     R, width = _table(table)
     ends, starts = _ints(lens, "lens", R), _ints(row_start, "row_start", R + 1)
     if lse is not None:
         _arg(lse, "lse", shape=(T, H), dtype=torch.float32, device=False)
     _on_device("q, the cache, table, lens, row_start, lse", q, cache.data, table, lens, row_start, lse)
     out = _heads_out(out, q, "out")
-    need = _attention_workspace(cache.page, cache.heads, D, T, H, R, width, max_new, max_len)
+    need = _attention_workspace(cache.page, view.heads, D, T, H, R, width, max_new, max_len)
     ws = _workspace_on(need, q.device, stream) if need else None
     _check("spl_attention_fp4",
            L.spl_attention_fp4(hq, T, view, table.data_ptr(), R, width, ends, starts, max_new, max_len,

@@ -291,3 +291,61 @@ def test_wrappers_refuse_mismatched_tensors_before_any_launch():
         with pytest.raises(ValueError):
             call()
             pytest.fail(f"call {i} was accepted")
+
+
+class _Recorder:
+    """Stands for the library: keeps the arguments of each call, accepts them all.  Sizes are the library's."""
+
+    def __init__(self):
+        self.calls, self.spl_kv_page_bytes = [], spl.lib().spl_kv_page_bytes
+
+    def __getattr__(self, name):
+        return lambda *a: self.calls.append((name, a)) or 0
+
+
+def _calls(monkeypatch):
+    """The wrappers on CPU tensors, their calls recorded instead of made."""
+    rec = _Recorder()
+    monkeypatch.setattr(spl, "lib", lambda: rec)
+    monkeypatch.setattr(spl, "_on_device", lambda *a: None)
+    monkeypatch.setattr(spl, "_on", lambda stream: 0)
+    monkeypatch.setattr(spl, "_attention_workspace", lambda *a: 0)
+    return rec.calls
+
+
+def test_a_cache_whose_data_are_replaced_is_called_with_the_new_ones(monkeypatch):
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    data = lambda pages, dim: torch.zeros(pages, 2, spl.kv_page_bytes(dim, 16), dtype=torch.uint8)  # noqa: E731
+    cache = spl.KVCache(data(3, 128), 16, 128, torch.bfloat16)
+    calls = _calls(monkeypatch)
+
+    def step(D):
+        q, k, v = _qkv(D=D)
+        spl.qk_norm_rope_append(q, k, v, None, None, i32(2), cache)
+        spl.cache_read(cache, i32(2))
+        spl.attention_fp4(q, cache, i32(2, 4), i32(2), i32(3))
+        views = [next(a for a in args if isinstance(a, spl._KVCache)) for _, args in calls]
+        calls.clear()
+        assert len(views) == 3
+        for v in views:
+            assert (v.data, v.pages, v.data_bytes) == (cache.data.data_ptr(), len(cache.data), cache.data.numel())
+            assert (v.page, v.heads, v.head_dim) == (16, 2, D) and (cache.pages, cache.heads) == (len(cache.data), 2)
+
+    step(128)
+    cache.data = data(7, 128)                                    # grown
+    step(128)
+    cache.data, cache.head_dim = data(5, 64), 64
+    step(64)
+    for name, value in (("data", data(5, 128)), ("data", data(5, 64)[:, ::2]), ("data", data(5, 64).float()),
+                        ("data", None), ("page", 32), ("head_dim", 128), ("dtype", torch.float32)):
+        q, k, v = _qkv(D=64)
+        was = getattr(cache, name)
+        setattr(cache, name, value)
+        for call in (lambda: spl.qk_norm_rope_append(q, k, v, None, None, i32(2), cache),
+                     lambda: spl.cache_read(cache, i32(2)),
+                     lambda: spl.attention_fp4(q, cache, i32(2, 4), i32(2), i32(3))):
+            with pytest.raises(ValueError):
+                call()
+        assert not calls
+        setattr(cache, name, was)
+    step(64)
