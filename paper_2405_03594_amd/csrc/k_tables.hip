@@ -103,15 +103,17 @@ __global__ __launch_bounds__(kThreads) void k_block_tables(TablesArgs a) {
         row_s[k] = row, page_s[k] = pg, cached_s[k] = c[i], have_s[k] = have[i];
         if (blockIdx.x == 0) {
           a.row_start[base + k] = (int32_t)(row < INT32_MAX ? row : INT32_MAX);
-          // tokens in the page begun before, in new pages handed out, and the rest
-          const int64_t room = n[i] > 0 ? (int64_t)have[i] * page - c[i] : 0;
+          // of the tokens that have a row (the others are missing as such): those in the
+          // page begun before, in new pages handed out, and the rest
+          const int64_t in_rows = a.tokens - row, m = in_rows < 0 ? 0 : (in_rows < n[i] ? in_rows : n[i]);
+          const int64_t room = m > 0 ? (int64_t)have[i] * page - c[i] : 0;
           int64_t got = 0;
-          if (room > 0 && a.table[(base + k) * a.width + have[i] - 1] >= 0) got += room < n[i] ? room : n[i];
+          if (room > 0 && a.table[(base + k) * a.width + have[i] - 1] >= 0) got += room < m ? room : m;
           int64_t given = a.free_count - pg;
           given = given < 0 ? 0 : (given < need[i] ? given : need[i]);
-          const int64_t rest = n[i] - (room > 0 ? room : 0);
+          const int64_t rest = m - (room > 0 ? room : 0);
           if (rest > 0 && c[i] <= (int64_t)have[i] * page) got += rest < given * page ? rest : given * page;
-          missing += n[i] - got;
+          missing += m - got;
         }
       }
       row += n[i];

@@ -89,3 +89,21 @@ def test_negative_lengths_missing_pages_and_odd_heads():
     _check(cached, new, table, free, head, 32, int(np.maximum(new, 0).sum()))
     _check(cached, new, table, free, -5, 32, int(np.maximum(new, 0).sum()))
     _check(cached, new, table, free, len(free) + 9, 32, int(np.maximum(new, 0).sum()))
+
+
+@pytest.mark.parametrize("short", [0, 1, 4, 1000])
+@pytest.mark.parametrize("rows", [0, 1, 50, 300, 10 ** 6])
+def test_a_token_without_a_row_and_a_slot_is_missing_once(rows, short):
+    """Too few rows and a free list that runs out: what is missing is the tokens that lack one or both, token by token."""
+    cached, new, table, free, head = _case(11, 30, 16, 90, 40)
+    total = int(new.sum())
+    rows = min(rows, total + 20)
+    free = free[:max(head, len(free) - 5 - short)]
+    slots = ref.tables(cached, new, table, free, head, 16, total)["slots"]
+    want = sum(t >= rows or slots[t] < 0 for t in range(total))
+    assert _run(cached, new, table, free, head, 16, rows)["missing"] == want
+    gone = table.copy()
+    gone[::3] = -1                                   # requests whose pages are gone
+    slots = ref.tables(cached, new, gone, free, head, 16, total)["slots"]
+    want = sum(t >= rows or slots[t] < 0 for t in range(total))
+    assert _run(cached, new, gone, free, head, 16, rows)["missing"] == want
