@@ -606,7 +606,9 @@ int64_t spl_kv_page_bytes(int32_t head_dim, int32_t page);
  * position 0 and slot -1 (a batch padded for a captured graph), tokens past the
  * rows are counted in state[1].  The same arguments give the same results, so a
  * call can be repeated.  requests >= 1, 0 <= tokens < 2^31, page a power of two
- * from 16 to 256, 1 <= width, requests * width < 2^40; free_head may not be state. */
+ * from 16 to 256, 1 <= width, requests * width < 2^40.  What is written (table,
+ * row_start, lens, positions, slots, state) shares no memory with another array of
+ * the call: not lens with cached, nor state with free_head. */
 spl_status spl_block_tables(const int32_t* cached, const int32_t* fresh, int64_t requests, int64_t tokens,
                             int32_t page, int32_t* table, int64_t width, const int32_t* free_pages,
                             int64_t free_count, const int32_t* free_head, int32_t* row_start, int32_t* lens,

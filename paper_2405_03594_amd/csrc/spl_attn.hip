@@ -18,6 +18,21 @@ bool fp_dtype(int32_t d) { return d == SPL_F16 || d == SPL_BF16; }
 bool page_ok(int32_t page) { return page >= 16 && page <= 256 && (page & (page - 1)) == 0; }
 bool dim_ok(int32_t d) { return d == 64 || d == 96 || d == 128 || d == 256; }
 
+// Whether any of the first `outs` arrays shares memory with another one.
+struct Span {
+  const void* at;
+  int64_t ints;
+};
+bool overlap(const Span* a, int outs, int n) {
+  for (int i = 0; i < outs; ++i)
+    for (int j = i + 1; j < n; ++j) {
+      const uintptr_t x = reinterpret_cast<uintptr_t>(a[i].at), y = reinterpret_cast<uintptr_t>(a[j].at);
+      if (a[i].ints > 0 && a[j].ints > 0 && (x < y ? y - x < 4 * (uintptr_t)a[i].ints : x - y < 4 * (uintptr_t)a[j].ints))
+        return true;
+    }
+  return false;
+}
+
 spl_status launched(hipError_t e) {
   if (e == hipSuccess) return SPL_OK;
   return e == hipErrorNotSupported ? SPL_ERR_UNSUPPORTED : SPL_ERR_DEVICE;
@@ -75,8 +90,13 @@ spl_status spl_block_tables(const int32_t* cached, const int32_t* fresh, int64_t
   if (!page_ok(page)) return SPL_ERR_UNSUPPORTED;
   if (!given(cached, 4) || !given(fresh, 4) || !given(table, 4) || !given(free_head, 4) || !given(row_start, 4) ||
       !given(lens, 4) || !given(state, 4) || (free_count > 0 && !given(free_pages, 4)) ||
-      (tokens > 0 && (!given(positions, 4) || !given(slots, 4))) || free_head == state)
+      (tokens > 0 && (!given(positions, 4) || !given(slots, 4))))
     return SPL_ERR_INVALID_ARG;
+  // a workgroup reads what another one may have written by then
+  const Span arrays[] = {{table, requests * width}, {row_start, requests + 1}, {lens, requests}, {positions, tokens},
+                         {slots, tokens},           {state, 2},                {cached, requests}, {fresh, requests},
+                         {free_pages, free_count},  {free_head, 1}};
+  if (overlap(arrays, 6, 10)) return SPL_ERR_INVALID_ARG;
   (void)hipGetLastError();
   return launched(spl::launch_block_tables(cached, fresh, requests, tokens, page, table, width, free_pages, free_count,
                                            free_head, row_start, lens, positions, slots, state, stream));

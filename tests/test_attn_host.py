@@ -349,3 +349,20 @@ def test_a_cache_whose_data_are_replaced_is_called_with_the_new_ones(monkeypatch
         assert not calls
         setattr(cache, name, was)
     step(64)
+
+
+def test_block_tables_refuses_results_that_share_memory_with_another_array(L):
+    """Workgroups read the lengths and the free list while others write the results."""
+    size = dict(cached=8, fresh=8, table=32, free=36, head=4, row=12, lens=8, pos=16, slots=16, state=8)
+    at = {n: 0x1000 * (i + 1) for i, n in enumerate(size)}
+
+    def call(at):
+        return L.spl_block_tables(at["cached"], at["fresh"], 2, 4, 16, at["table"], 4, at["free"], 9, at["head"],
+                                  at["row"], at["lens"], at["pos"], at["slots"], at["state"], None)
+
+    for a in ("table", "row", "lens", "pos", "slots", "state"):
+        for b in size:
+            if a == b:
+                continue
+            for offset in (0, size[b] - 4, 4 - size[a]):         # the same start, one entry in common at either end
+                assert call(dict(at, **{a: at[b] + offset})) == INVALID, (a, b, offset)
