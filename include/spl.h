@@ -660,7 +660,9 @@ spl_status spl_qk_norm_rope_append(const spl_heads* q, const spl_heads* k, const
                                    hipStream_t stream);
 
 /* What the cache holds at slots[0 .. tokens): k, v out [tokens][heads][head_dim]
- * of the cache's type, either may be NULL; zeros for a slot outside the cache. */
+ * of the cache's type, either may be NULL; zeros for a slot outside the cache.
+ * tokens * heads * head_dim / 8 < 2^32 - 256, which one launch holds
+ * (SPL_ERR_UNSUPPORTED otherwise). */
 spl_status spl_cache_read(const spl_kv_cache* cache, const int32_t* slots, int64_t tokens, void* k, void* v,
                           hipStream_t stream);
 
@@ -688,7 +690,11 @@ spl_status spl_cache_read(const spl_kv_cache* cache, const int32_t* slots, int64
  * rounded to the cache's type before it meets the values, out once.  A row that
  * sees no key gives 0.  Keys and values of masked tokens have no influence,
  * whatever they hold.  The result of a row depends on the split, and so on the
- * sizes of the call, in the order of its sums only. */
+ * sizes of the call, in the order of its sums only.
+ * Sizes that one launch does not hold are SPL_ERR_UNSUPPORTED: with max_new rows of
+ * the heads of a key head at most 16, requests * cache heads from 2^24 on; else from
+ * 2^23 on (rows of a key head / 128 + requests) * cache heads, of 256 channels from
+ * 2^24 on (them / 16 + requests) * cache heads. */
 int64_t spl_attention_fp4_workspace_bytes(const spl_kv_cache* cache, int64_t tokens, int32_t heads, int64_t requests,
                                           int64_t width, int64_t max_new, int64_t max_len);
 spl_status spl_attention_fp4(const spl_heads* q, int64_t tokens, const spl_kv_cache* cache, const int32_t* table,

@@ -766,6 +766,13 @@ int64_t attn_workspace_bytes(const AttnArgs& a) {
   return a.tokens * a.q.heads * ((int64_t)p.most_splits * (a.cache.head_dim + 2) + 1) * 4;
 }
 
+// The joins are fewer: of at most 16 rows each of the tiles that are split.
+bool attn_fits(const AttnArgs& a) {
+  const AttnPlan p = plan_of(a);
+  return p.tiles * a.cache.heads <= kMaxThreads / (kWaves * 64) &&
+         p.prefill_tiles * a.cache.heads <= kMaxThreads / kPrefillThreads;
+}
+
 hipError_t launch_attn(const AttnArgs& a, hipStream_t s) {
   const AttnPlan p = plan_of(a);
   return a.cache.dtype == SPL_F16 ? run_dim<F16>(a, p, s) : run_dim<Bf16>(a, p, s);

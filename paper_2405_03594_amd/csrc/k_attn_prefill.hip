@@ -40,6 +40,7 @@ using spl::u32x4;
 
 constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * 64;
+static_assert(kThreads == spl::kPrefillThreads, "the launch's bound counts them");
 constexpr int kRows = spl::kPrefillRows;         // of a workgroup
 
 template <int D>

@@ -608,7 +608,7 @@ hipError_t launch_norm_rope(const NormRopeArgs& a, int32_t dtype, hipStream_t s)
 
 hipError_t launch_cache_read(const spl_kv_cache& c, const int32_t* slots, int64_t tokens, void* k, void* v,
                              hipStream_t s) {
-  const int64_t n = tokens * c.heads * (c.head_dim / 8);
+  const int64_t n = cache_read_threads(c, tokens);
   const dim3 grid((unsigned)((n + kThreads - 1) / kThreads));
   if (c.dtype == SPL_F16)
     k_cache_read<F16><<<grid, kThreads, 0, s>>>(c, slots, tokens, (uint16_t*)k, (uint16_t*)v);

@@ -26,6 +26,9 @@ inline __host__ __device__ PageGeom page_geom(int32_t dim, int32_t page) {
   return g;
 }
 
+// Threads that a launch can have in x.
+constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 1;
+
 struct NormRopeArgs {
   spl_heads q, k, v;                            // v only with a cache
   void* q_out;
@@ -44,6 +47,7 @@ struct NormRopeArgs {
   float eps;
 };
 hipError_t launch_norm_rope(const NormRopeArgs& a, int32_t dtype, hipStream_t s);
+inline int64_t cache_read_threads(const spl_kv_cache& c, int64_t tokens) { return tokens * c.heads * (c.head_dim / 8); }
 hipError_t launch_cache_read(const spl_kv_cache& c, const int32_t* slots, int64_t tokens, void* k, void* v,
                              hipStream_t s);
 
@@ -95,6 +99,7 @@ struct AttnArgs {
 // others, a tile each (tiles 0: there are none).
 constexpr int kFewRows = 16;                    // of a tile of k_attn_rows
 constexpr int kPrefillRows = 128;               // of a tile of k_attn_prefill
+constexpr int kPrefillThreads = 512;            // of a workgroup of it
 struct AttnPlan {
   int64_t tiles, prefill_tiles;
   int group;                                    // query heads of a key head
@@ -107,6 +112,7 @@ struct AttnPlan {
 };
 hipError_t launch_attn_prefill(const AttnArgs& a, const AttnPlan& p, hipStream_t s);
 int64_t attn_workspace_bytes(const AttnArgs& a);                // the window does not count
+bool attn_fits(const AttnArgs& a);                              // into launches; the window does not count
 hipError_t launch_attn(const AttnArgs& a, hipStream_t s);
 
 }  // namespace spl

@@ -155,6 +155,7 @@ spl_status spl_cache_read(const spl_kv_cache* cache, const int32_t* slots, int64
   if (!given(slots, 4) || (k && !aligned(k, 16)) || (v && !aligned(v, 16)) ||
       tokens > kMaxElems / 8 / ((int64_t)cache->heads * cache->head_dim))
     return SPL_ERR_INVALID_ARG;
+  if (spl::cache_read_threads(*cache, tokens) > spl::kMaxThreads - 255) return SPL_ERR_UNSUPPORTED;
   (void)hipGetLastError();
   return launched(spl::launch_cache_read(*cache, slots, tokens, k, v, stream));
 }
@@ -210,7 +211,7 @@ static spl_status attn_sizes(const spl_kv_cache* cache, int64_t tokens, int32_t 
   *a = spl::AttnArgs{};
   a->cache = *cache, a->tokens = tokens, a->requests = requests, a->width = width, a->max_new = max_new;
   a->max_len = max_len, a->q.heads = heads;
-  return SPL_OK;
+  return tokens == 0 || spl::attn_fits(*a) ? SPL_OK : SPL_ERR_UNSUPPORTED;
 }
 
 int64_t spl_attention_fp4_workspace_bytes(const spl_kv_cache* cache, int64_t tokens, int32_t heads, int64_t requests,

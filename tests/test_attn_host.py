@@ -366,3 +366,32 @@ def test_block_tables_refuses_results_that_share_memory_with_another_array(L):
                 continue
             for offset in (0, size[b] - 4, 4 - size[a]):         # the same start, one entry in common at either end
                 assert call(dict(at, **{a: at[b] + offset})) == INVALID, (a, b, offset)
+
+
+def test_sizes_past_one_launch_are_refused(L):
+    """A launch has fewer than 2^32 threads in x: past them a refusal before any launch, and no workspace."""
+    read = lambda heads, dim, tokens: L.spl_cache_read(_c(heads=heads, head_dim=dim, page=256), 0x7000, tokens, 0x10000,  # noqa: E731
+                                                       0, None)
+    assert read(8, 128, 1 << 25) == read(1, 64, 1 << 29) == read(4, 256, (1 << 25) - 1) == UNSUPPORTED
+    assert read(64, 128, 1 << 30) == INVALID         # past what the call takes at all
+
+    def call(cache, tokens, heads, requests, max_new):
+        sizes = (requests, 1, max_new, 16)
+        size = L.spl_attention_fp4_workspace_bytes(cache, tokens, heads, *sizes)
+        if size >= 0:
+            return size
+        assert size == -1
+        for window in (0, 5):
+            assert L.spl_attention_fp4(_h(heads), tokens, cache, 0x1000, requests, 1, 0x2000, 0x3000, max_new, 16, 0.1,
+                                       window, 0x4000, 0, 0x10000, None) == UNSUPPORTED
+        return -1
+
+    # single rows: requests * key heads workgroups of 256 threads
+    assert call(_c(), 1 << 22, 4, (1 << 22) - 1, 1) == 0 and call(_c(), 1 << 22, 4, 1 << 22, 1) == -1
+    assert call(_c(), 5, 4, (1 << 22) - 1, 1) == 0 and call(_c(), 5, 4, 1 << 22, 1) == -1
+    # many rows: workgroups of 512 threads for 128 rows and for each request
+    assert call(_c(), 1 << 21, 4, (1 << 21) - (1 << 14) - 1, 0) == 0
+    assert call(_c(), 1 << 21, 4, (1 << 21) - (1 << 14), 0) == -1
+    # 256 channels: workgroups of 256 threads for 16 rows and for each request
+    assert call(_c(head_dim=256), 1 << 22, 4, (1 << 22) - (1 << 18) - 1, 0) == 0
+    assert call(_c(head_dim=256), 1 << 22, 4, (1 << 22) - (1 << 18), 0) == -1
