@@ -996,7 +996,7 @@ class KVCache:
 @functools.lru_cache(maxsize=None)
 def kv_page_bytes(head_dim: int, page: int) -> int:
     """Bytes of one head's region of a page (see spl_kv_page_bytes)."""
-    size = lib().spl_kv_page_bytes(head_dim, page)
+    size = lib().spl_kv_page_bytes(_int32(head_dim, "head_dim"), _int32(page, "page"))
     if size == 0:
         raise ValueError(f"no cache of {head_dim} channels in pages of {page} tokens: 64, 96, 128 or 256 channels, a "
                          "power of two from 16 to 256 tokens")
@@ -1007,6 +1007,7 @@ def kv_page_bytes(head_dim: int, page: int) -> int:
 def _attention_workspace(page, cache_heads, head_dim, tokens, heads, requests, width, max_new, max_len) -> int:
     """spl_attention_fp4_workspace_bytes, a function of these sizes (and of the device, whose CUs are the same for all)."""
     view = _KVCache(16, 1, 1 << 62, page, cache_heads, head_dim, F16)
+    _int32(max_new, "max_new"), _int32(max_len, "max_len")
     need = lib().spl_attention_fp4_workspace_bytes(view, tokens, heads, requests, width, max_new, max_len)
     if need < 0:
         raise ValueError("spl_attention_fp4_workspace_bytes rejected the arguments")
@@ -1031,6 +1032,13 @@ def _on(stream) -> int:
     if stream is None:
         return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream
+
+
+def _int32(n: int, name: str) -> int:
+    """A number that the library takes in 32 bits, of which ctypes would pass the low ones of a larger one."""
+    if not -1 << 31 <= n < 1 << 31:
+        raise ValueError(f"{name} is {n}, past 32 bits")
+    return n
 
 
 def _on_device(names: str, *tensors) -> None:
@@ -1076,6 +1084,7 @@ def block_tables(cached: torch.Tensor, new: torch.Tensor, table: torch.Tensor, f
     head = _ints(free_head, "free_head", 1)
     if tokens < 0:
         raise ValueError("tokens must not be negative")
+    _int32(page, "page")
     _on_device("cached, new, table, free_pages, free_head", cached, new, table, free_pages, free_head)
     # one allocation for all results
     buf = torch.empty((2 * R + 2 * tokens + 3,), dtype=torch.int32, device=table.device)
@@ -1237,6 +1246,7 @@ def attention_fp4(q: torch.Tensor, cache: KVCache, table: torch.Tensor, lens: to
     if H % view.heads:
         raise ValueError(f"q has {H} heads, not a multiple of the cache's {view.heads}")
     R, width = _table(table)
+    _int32(window, "window")
     ends, starts = _ints(lens, "lens", R), _ints(row_start, "row_start", R + 1)
     if lse is not None:
         _arg(lse, "lse", shape=(T, H), dtype=torch.float32, device=False)

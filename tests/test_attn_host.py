@@ -395,3 +395,23 @@ def test_sizes_past_one_launch_are_refused(L):
     # 256 channels: workgroups of 256 threads for 16 rows and for each request
     assert call(_c(head_dim=256), 1 << 22, 4, (1 << 22) - (1 << 18) - 1, 0) == 0
     assert call(_c(head_dim=256), 1 << 22, 4, (1 << 22) - (1 << 18), 0) == -1
+
+
+def test_numbers_past_32_bits_are_refused_and_not_cut(monkeypatch):
+    """A window of 2^32 is not no window, and 2^32 + 64 is not a page of 64 tokens."""
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    cache = spl.KVCache(torch.zeros(3, 2, spl.kv_page_bytes(128, 16), dtype=torch.uint8), 16, 128, torch.bfloat16)
+    q, k, v = _qkv()
+    for n in (1 << 32, (1 << 32) + 64, (1 << 31), -(1 << 32) + 16, 1 << 64):
+        for call in (lambda: spl.kv_page_bytes(128, n + 16), lambda: spl.kv_page_bytes(n + 128, 16),
+                     lambda: spl._attention_workspace(16, 2, 128, 2, 4, 2, 4, n, 0),
+                     lambda: spl._attention_workspace(16, 2, 128, 2, 4, 2, 4, 0, n)):
+            with pytest.raises(ValueError):
+                call()
+    calls = _calls(monkeypatch)
+    for n in (1 << 32, (1 << 32) + 64, (1 << 31), -(1 << 32) + 16):
+        for call in (lambda: spl.block_tables(i32(2), i32(2), i32(2, 4), i32(9), i32(1), n + 64, 2),
+                     lambda: spl.attention_fp4(q, cache, i32(2, 4), i32(2), i32(3), window=n)):
+            with pytest.raises(ValueError):
+                call()
+    assert not calls
