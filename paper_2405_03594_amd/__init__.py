@@ -1071,6 +1071,21 @@ def _workspace_on(need: int, device, stream) -> torch.Tensor:
     return ws
 
 
+def _result(shape, dtype, device, stream) -> torch.Tensor:
+    """A result to be written on `stream` (None: the current one): from that stream's own pool, as a block of the current
+    one's may still be in use there, and not reused before the current stream is done with it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    here = torch.cuda.current_stream(device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if stream != here:
+        t.record_stream(here)
+    return t
+
+
 def block_tables(cached: torch.Tensor, new: torch.Tensor, table: torch.Tensor, free_pages: torch.Tensor,
                  free_head: torch.Tensor, page: int, tokens: int, stream=None) -> BlockPlan:
     """Pages from the free list for each request's `new` tokens after its `cached` ones, written into `table`
@@ -1087,7 +1102,7 @@ def block_tables(cached: torch.Tensor, new: torch.Tensor, table: torch.Tensor, f
     _int32(page, "page")
     _on_device("cached, new, table, free_pages, free_head", cached, new, table, free_pages, free_head)
     # one allocation for all results
-    buf = torch.empty((2 * R + 2 * tokens + 3,), dtype=torch.int32, device=table.device)
+    buf = _result((2 * R + 2 * tokens + 3,), torch.int32, table.device, stream)
     p = buf.data_ptr()
     _check("spl_block_tables",
            lib().spl_block_tables(*args, R, tokens, page, table.data_ptr(), width, free, free_pages.shape[0], head, p,
@@ -1135,9 +1150,9 @@ def _turn_args(tokens: int, positions, rope):
     return _ints(positions, "positions", tokens), rope.data_ptr(), rows, 2 * half
 
 
-def _heads_out(out, like: torch.Tensor, name: str) -> torch.Tensor:
+def _heads_out(out, like: torch.Tensor, name: str, stream) -> torch.Tensor:
     if out is None:
-        return torch.empty_like(like, memory_format=torch.contiguous_format)
+        return _result(like.shape, like.dtype, like.device, stream)
     return _arg(out, name, shape=like.shape, dtype=like.dtype)
 
 
@@ -1154,7 +1169,7 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor | Non
     wq, wk = _weight(q_weight, "q_weight", D, q.dtype), _weight(k_weight, "k_weight", D, q.dtype)
     at, angles, rows, rot = _turn_args(T, positions, rope)
     _on_device("q, k, weights, positions, rope", q, k, q_weight, k_weight, positions, rope)
-    q_out, k_out = _heads_out(q_out, q, "q_out"), _heads_out(k_out, k, "k_out")
+    q_out, k_out = _heads_out(q_out, q, "q_out", stream), _heads_out(k_out, k, "k_out", stream)
     _check("spl_qk_norm_rope",
            lib().spl_qk_norm_rope(hq, hk, T, D, _TORCH_DTYPE[q.dtype], wq, wk, eps, at, angles, rows, rot, interleaved,
                                   q_out.data_ptr(), k_out.data_ptr(), _on(stream)))
@@ -1181,9 +1196,8 @@ def qk_norm_rope_grad(dq: torch.Tensor, dk: torch.Tensor, q: torch.Tensor, k: to
     need = L.spl_qk_norm_rope_grad_workspace_bytes(T, H, hk.heads, D)
     if need < 0:
         raise ValueError("the workspace-size function rejected the shape")
-    dq_out, dk_out = _heads_out(dq_out, q, "dq_out"), _heads_out(dk_out, k, "dk_out")
-    dwq, dwk = (None if w is None else torch.empty((D,), dtype=torch.float32, device=q.device)
-                for w in (q_weight, k_weight))
+    dq_out, dk_out = _heads_out(dq_out, q, "dq_out", stream), _heads_out(dk_out, k, "dk_out", stream)
+    dwq, dwk = (None if w is None else _result((D,), torch.float32, q.device, stream) for w in (q_weight, k_weight))
     ws = _workspace_on(need, q.device, stream) if need else None
     _check("spl_qk_norm_rope_grad",
            L.spl_qk_norm_rope_grad(hdq, hdk, hq, hk, T, D, _TORCH_DTYPE[q.dtype], wq, wk, eps, at, angles, rows, rot,
@@ -1211,9 +1225,9 @@ def qk_norm_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, posit
     at, angles, rows, rot = _turn_args(T, positions, rope)
     _on_device("q, k, v, slots, the cache, weights, positions, rope", q, k, v, slots, cache.data, q_weight, k_weight,
                positions, rope)
-    q_out = _heads_out(q_out, q, "q_out")
+    q_out = _heads_out(q_out, q, "q_out", stream)
     if k_out is not None:
-        k_out = _heads_out(k_out, k, "k_out")
+        k_out = _heads_out(k_out, k, "k_out", stream)
     _check("spl_qk_norm_rope_append",
            lib().spl_qk_norm_rope_append(hq, hk, hv, T, wq, wk, eps, at, angles, rows, rot, interleaved, to,
                                          view, q_out.data_ptr(), _ptr(k_out), _on(stream)))
@@ -1227,8 +1241,7 @@ def cache_read(cache: KVCache, slots: torch.Tensor, stream=None):
     T = slots.shape[0]
     at, view = _ints(slots, "slots", T), cache.view()
     _on_device("slots, the cache", slots, cache.data)
-    k = torch.empty((T, view.heads, cache.head_dim), dtype=cache.dtype, device=slots.device)
-    v = torch.empty_like(k)
+    k, v = (_result((T, view.heads, cache.head_dim), cache.dtype, slots.device, stream) for _ in range(2))
     _check("spl_cache_read", lib().spl_cache_read(view, at, T, k.data_ptr(), v.data_ptr(), _on(stream)))
     return k, v
 
@@ -1251,7 +1264,7 @@ def attention_fp4(q: torch.Tensor, cache: KVCache, table: torch.Tensor, lens: to
     if lse is not None:
         _arg(lse, "lse", shape=(T, H), dtype=torch.float32, device=False)
     _on_device("q, the cache, table, lens, row_start, lse", q, cache.data, table, lens, row_start, lse)
-    out = _heads_out(out, q, "out")
+    out = _heads_out(out, q, "out", stream)
     need = _attention_workspace(cache.page, view.heads, D, T, H, R, width, max_new, max_len)
     ws = _workspace_on(need, q.device, stream) if need else None
     _check("spl_attention_fp4",

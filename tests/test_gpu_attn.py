@@ -464,3 +464,47 @@ def test_an_infinite_value_of_no_weight_reaches_its_row_however_it_is_split(leng
     got = b.check()
     assert torch.isnan(got[0, 2:, :32]).all() and torch.isfinite(got[0, :2]).all()
     assert torch.isfinite(got[0, 2:, 32:]).all()
+
+
+def test_results_belong_to_the_stream_that_writes_them():
+    """Not to blocks that the current stream freed and may still use, and kept while the current stream reads them."""
+    spl = _spl()
+    b = Batch([300, 9], [300, 40], 16, 4, 128, 16, BF, seed=27)
+    lens, rows, q = torch.tensor(b.lens).int().cuda(), b.row_start.int().cuda(), b.q.cuda()
+    k = torch.randn(309, 4, 128, device="cuda").to(BF)
+    w = torch.ones(128, dtype=BF, device="cuda")
+    slots = torch.arange(309, device="cuda").int() % (b.cache.pages * 16)
+    fresh = spl.KVCache.empty(40, 4, 128, 16, BF)
+    table, free = torch.zeros(2, 40, dtype=torch.int32, device="cuda"), torch.arange(60, device="cuda").int()
+    head = torch.zeros(1, dtype=torch.int32, device="cuda")
+    new = torch.tensor([300, 9], device="cuda").int()
+    calls = {
+        "block_tables": lambda s: spl.block_tables(new, new, table, free, head, 16, 309, stream=s).row_start,
+        "qk_norm_rope": lambda s: spl.qk_norm_rope(q, k, None, None, w, w, stream=s),
+        "qk_norm_rope_grad": lambda s: spl.qk_norm_rope_grad(q, k, q, k, None, None, w, w, stream=s),
+        "qk_norm_rope_append": lambda s: spl.qk_norm_rope_append(q, k, k, None, None, slots, fresh, stream=s),
+        "cache_read": lambda s: spl.cache_read(b.cache, slots, stream=s),
+        "attention_fp4": lambda s: spl.attention_fp4(q, b.cache, b.table, lens, rows, stream=s),
+    }
+    side = torch.cuda.Stream()
+    for name, call in calls.items():
+        as_list = lambda x: list(x) if isinstance(x, (tuple, list)) else [x]  # noqa: E731
+        want = [x.clone() for x in as_list(call(None))]
+        for stream in (side, torch.cuda.ExternalStream(side.cuda_stream)):
+            torch.cuda.synchronize()
+            freed = [torch.empty_like(x) for x in want]          # blocks of these sizes, back in the current stream's pool
+            places = {x.untyped_storage().data_ptr() for x in freed}
+            del freed
+            got = as_list(call(stream))
+            torch.cuda.current_stream().wait_stream(side)
+            at = [x.untyped_storage().data_ptr() for x in got]
+            assert not places & set(at), name
+            torch.cuda._sleep(20_000_000)                        # the current stream reads them late
+            copies = [x.clone() for x in got]
+            del got
+            again = as_list(call(stream))
+            assert not set(at) & {x.untyped_storage().data_ptr() for x in again}, name
+            torch.cuda.synchronize()
+            bits = lambda x: x.contiguous().view(torch.uint8)  # noqa: E731  (places without a token read back as NaN)
+            for x, y, z in zip(want, copies, again):
+                assert torch.equal(bits(x), bits(y)) and torch.equal(bits(x), bits(z)), name
