@@ -508,3 +508,31 @@ def test_results_belong_to_the_stream_that_writes_them():
             bits = lambda x: x.contiguous().view(torch.uint8)  # noqa: E731  (places without a token read back as NaN)
             for x, y, z in zip(want, copies, again):
                 assert torch.equal(bits(x), bits(y)) and torch.equal(bits(x), bits(z)), name
+
+
+@pytest.mark.parametrize("max_new", [0, 1100])
+def test_prompts_among_more_requests_than_a_wave_has_lanes(max_new):
+    """The kernel for many rows finds its tiles past the first 64 requests, and none at all in a batch of single rows."""
+    H = 64 * torch.cuda.get_device_properties(0).multi_processor_count // 256
+    new, lens = [1] * 150, [(37 * i) % 90 + 1 for i in range(150)]
+    new[70], lens[70] = 1100, 1130                               # the prompts in the second and third 64 requests
+    new[131], lens[131] = 17, 17
+    new[3] = lens[5] = 0
+    b = Batch(new, lens, H, H, 64, 64, BF, seed=25)
+    got, lse = b.run(max_new=max_new)
+    for r in range(150):
+        s, e = int(b.row_start[r]), int(b.row_start[r + 1])
+        for t in range(s, e) if r != 70 else (s, s + 1, s + 127, s + 128, s + 700, e - 1):
+            p = lens[r] - e + t
+            if p < 0:
+                assert (got[t] == 0).all() and torch.isneginf(lse[t]).all()
+                continue
+            w, l, m, top = ref.attention(b.q.double()[t:t + 1], b.keys[r:r + 1], b.values[r:r + 1], [0, 1], [p + 1],
+                                         64 ** -0.5, 0)
+            tol = 3 * ref.UNIT[BF] + 2.0 ** -18 * (1 + top)
+            assert ((got[t] - w[0]).abs() <= tol * m[0] + ref.STEP[BF]).all(), (r, t)
+            assert ((lse[t] - l[0]).abs() <= tol).all(), (r, t)
+    rows = 128 * torch.cuda.get_device_properties(0).multi_processor_count // H
+    one = Batch([1] * rows, [1 + i % 3 for i in range(rows)], H, H, 64, 16, BF, seed=26)      # no prompt, and max_new not known
+    want, known = one.run(max_new=0), one.run()
+    assert torch.equal(want[0], known[0]) and torch.equal(want[1], known[1])
