@@ -976,16 +976,17 @@ class KVCache:
 
     def view(self) -> _KVCache:
         """The cache as a call takes it: of the attributes as they are now, so that it follows another `data`."""
-        data, dtype = self.data, self.dtype
-        if dtype not in _HEAD_TYPES:
+        data, page, dim = self.data, self.page, self.head_dim
+        if self.dtype not in _HEAD_TYPES:
             raise ValueError("a cache holds fp16 or bf16 keys and values")
-        size = kv_page_bytes(self.head_dim, self.page)
-        if not isinstance(data, torch.Tensor) or data.dim() != 3 or data.shape[2] != size:
+        size = kv_page_bytes(dim, page)
+        shape = data.shape if isinstance(data, torch.Tensor) else ()
+        if len(shape) != 3 or shape[2] != size:
             raise ValueError(f"data must be [pages, heads, {size}]")
         if data.dtype != torch.uint8 or not data.is_contiguous():
             _arg(data, "data", dtype=torch.uint8, device=False)
-        pages, heads, _ = data.shape
-        return _KVCache(data.data_ptr(), pages, pages * heads * size, self.page, heads, self.head_dim, _TORCH_DTYPE[dtype])
+        pages, heads, _ = shape
+        return _KVCache(data.data_ptr(), pages, pages * heads * size, page, heads, dim, _TORCH_DTYPE[self.dtype])
 
     @classmethod
     def empty(cls, pages: int, heads: int, head_dim: int, page: int, dtype: torch.dtype, device="cuda") -> "KVCache":
@@ -1152,6 +1153,8 @@ def _turn_args(tokens: int, positions, rope):
 
 def _heads_out(out, like: torch.Tensor, name: str, stream) -> torch.Tensor:
     if out is None:
+        if stream is None:
+            return torch.empty_like(like, memory_format=torch.contiguous_format)
         return _result(like.shape, like.dtype, like.device, stream)
     return _arg(out, name, shape=like.shape, dtype=like.dtype)
 
@@ -1241,7 +1244,8 @@ def cache_read(cache: KVCache, slots: torch.Tensor, stream=None):
     T = slots.shape[0]
     at, view = _ints(slots, "slots", T), cache.view()
     _on_device("slots, the cache", slots, cache.data)
-    k, v = (_result((T, view.heads, cache.head_dim), cache.dtype, slots.device, stream) for _ in range(2))
+    k = _result((T, view.heads, cache.head_dim), cache.dtype, slots.device, stream)
+    v = _heads_out(None, k, "v", stream)
     _check("spl_cache_read", lib().spl_cache_read(view, at, T, k.data_ptr(), v.data_ptr(), _on(stream)))
     return k, v
 
