@@ -678,6 +678,8 @@ spl_status spl_cache_read(const spl_kv_cache* cache, const int32_t* slots, int64
  *   row_start   [requests + 1]: request r's rows are row_start[r] ..
  *               row_start[r + 1] - 1, at the last positions of the request:
  *               p = lens[r] - row_start[r + 1] + t.
+ *               Rows past `tokens` are not there; tokens past the table's pages hold
+ *               no keys.  Neither changes a row's p.
  *   max_new     the most rows of a request, 0 if not known: rows past it may be
  *               left out.  max_len  about the most tokens of a request, 0 if not
  *               known (a hint: it sets how far the work is split).

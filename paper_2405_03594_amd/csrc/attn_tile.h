@@ -101,30 +101,34 @@ __device__ __forceinline__ float quad_max(float x) {
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// Row indexes of a request, clamped to the call's rows, and its length.
+// Row indexes of a request, clamped to the call's rows, its length, clamped to the
+// table's, and its first row's position, which follows from both as they are given:
+// a request may have more rows than the call, and more tokens than pages.
 struct Rows {
   int64_t first;
-  int32_t count, len;
+  int32_t count, len, pos;
 };
 __device__ __forceinline__ Rows rows_of(const AttnArgs& a, int64_t r) {
   const int64_t t = a.tokens;
   int64_t s = a.row_start[r], e = a.row_start[r + 1];    // lane by lane: requests may differ
-  s = s < 0 ? 0 : (s > t ? t : s);
-  e = e < s ? s : (e > t ? t : e);
   const int64_t most = a.width * (int64_t)a.cache.page;
   int64_t len = a.lens[r];
-  len = len < 0 ? 0 : (len > most ? most : len);
-  return {s, (int32_t)(e - s), (int32_t)len};
+  len = len < 0 ? 0 : len;
+  s = s < 0 ? 0 : (s > t ? t : s);
+  const int32_t pos = (int32_t)(len - e + s);
+  e = e < s ? s : (e > t ? t : e);
+  return {s, (int32_t)(e - s), (int32_t)(len > most ? most : len), pos};
 }
 
 // The same for a request that is the wave's: scalar loads, all at once.
 __device__ __forceinline__ Rows wave_rows_of(const AttnArgs& a, int32_t r) {
   const int32_t t = (int32_t)a.tokens, most = (int32_t)(a.width * a.cache.page);          // < 2^31
   int32_t s = uniform_load(a.row_start + r), e = uniform_load(a.row_start + r + 1), len = uniform_load(a.lens + r);
+  len = len < 0 ? 0 : len;
   s = s < 0 ? 0 : (s > t ? t : s);
+  const int32_t pos = (int32_t)((uint32_t)len - (uint32_t)e + (uint32_t)s);
   e = e < s ? s : (e > t ? t : e);
-  len = len < 0 ? 0 : (len > most ? most : len);
-  return {s, e - s, len};
+  return {s, e - s, len > most ? most : len, pos};
 }
 
 // Inclusive sum over the lanes of a wave: within rows of 16, then a row's or two
@@ -163,11 +167,11 @@ __device__ __forceinline__ Tile find_tile(const AttnArgs& a, int group, int size
       if ((uint32_t)index >= (uint32_t)__builtin_amdgcn_readlane(n, k)) break;
       return {base + k, index,
               {__builtin_amdgcn_readlane((int32_t)r.first, k), __builtin_amdgcn_readlane(r.count, k),
-               __builtin_amdgcn_readlane(r.len, k)}};
+               __builtin_amdgcn_readlane(r.len, k), __builtin_amdgcn_readlane(r.pos, k)}};
     }
     tile -= __builtin_amdgcn_readlane(sum, 63);
   }
-  return {-1, 0, {0, 0, 0}};
+  return {-1, 0, {0, 0, 0, 0}};
 }
 
 // The steps of `unit` tokens that any of the rows [row0, end_row) of a request
@@ -180,9 +184,8 @@ struct Span {
 __device__ __forceinline__ Span tile_span(const Rows& rows, int32_t row0, int32_t end_row, int group, int32_t window,
                                           int unit, int splits, int chunk) {
   Span t;
-  const int32_t first_pos = rows.len - rows.count;
-  t.low = first_pos + row0 / group;
-  t.high = first_pos + (end_row - 1) / group;
+  t.low = rows.pos + row0 / group;
+  t.high = rows.pos + (end_row - 1) / group;
   const int32_t end = t.high + 1 < rows.len ? t.high + 1 : rows.len;
   const int32_t begin = window > 0 && t.low - window + 1 > 0 ? t.low - window + 1 : 0;
   t.s0 = begin / unit;

@@ -391,7 +391,6 @@ __device__ __forceinline__ void rows_of_tile(const AttnArgs& a, Shared<D>& lds, 
   const int32_t all = rows.count * group;
   const int n = all - row0 < R * kRows ? all - row0 : R * kRows;
   const int m16 = lane & 15, j = lane >> 4;
-  const int32_t first_pos = rows.len - rows.count;
   const int32_t* table = a.table + req * a.width;
   const int shift = __builtin_ctz((unsigned)a.cache.page);
   const spl::Span ts = spl::tile_span(rows, row0, row0 + n, group, a.window, kStep, splits, chunk);
@@ -413,7 +412,7 @@ __device__ __forceinline__ void rows_of_tile(const AttnArgs& a, Shared<D>& lds, 
   for (int k = 0; k < R; ++k) {
     const int at = 16 * k + m16;
     const int32_t row = row0 + (at < n ? at : n - 1), tok = row / group;
-    view.pos[k] = at < n ? first_pos + tok : -1;
+    view.pos[k] = at < n ? rows.pos + tok : -1;
     view.first[k] = a.window > 0 ? view.pos[k] - a.window + 1 : 0;
     const uint16_t* x = static_cast<const uint16_t*>(a.q.data) + (rows.first + tok) * a.q.token_stride +
                         (int64_t)(head * group + (row - tok * group)) * a.q.head_stride;
@@ -538,7 +537,7 @@ __global__ __launch_bounds__(kWaves * 64, O) void k_attn_rows(
   // heads fastest: consecutive workgroups go to different XCDs, so each has a
   // share of every request, however their lengths differ
   const int place = blockIdx.x / a.cache.heads, head = blockIdx.x - place * a.cache.heads, split = blockIdx.y;
-  spl::Tile tile{place, 0, {0, 0, 0}};
+  spl::Tile tile{place, 0, {0, 0, 0, 0}};
   if (!direct) tile = spl::find_tile(a, group, R * kRows, 0, place);
   else if (snake > 0) tile.request = ranked_request(a, place, snake);
   const int32_t req = tile.request;

@@ -263,11 +263,12 @@ __device__ __forceinline__ float pair_sum(float x) {
 }
 
 // A wave's rows against its part (th) of a step in LDS, whose first token is t0.
-// pos: the lane's row; low, high: the least and the most of the wave's.
+// first, last: what the lane's row sees; low: the least last of the wave's rows;
+// high: their most position.
 template <class T, int D>
 __device__ __forceinline__ void multiply(State<D>& st, const uint8_t* lds, const uint8_t* flags, const u32x4* q,
-                                         int th, int32_t t0, int32_t pos, int32_t low, int32_t high, int32_t window,
-                                         float c, int lane) {
+                                         int th, int32_t t0, int32_t first, int32_t last, int32_t low, int32_t high,
+                                         int32_t window, float c, int lane) {
   using Gm = Geom<D>;
   constexpr int kHalf = Gm::kTok / 2, kTiles = kHalf / 32;
   const int half = lane >> 5, col = lane & 31;
@@ -291,7 +292,7 @@ __device__ __forceinline__ void multiply(State<D>& st, const uint8_t* lds, const
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int at = 32 * t + 16 * (i >> 3) + 8 * half + (i & 7);
-        const bool see = t0 + at <= pos && (window == 0 || t0 + at > pos - window) &&
+        const bool see = t0 + at <= last && t0 + at >= first &&
                          !(flagged >> (kPageFlags + 2 * t + (i >> 3)) & 1);
         s[t][i] = see ? s[t][i] : -INFINITY;
       }
@@ -338,7 +339,7 @@ __device__ __forceinline__ void multiply(State<D>& st, const uint8_t* lds, const
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int32_t t = t0 + 8 * block + i;
-        hit |= (flags[f] >> i & 1) && t <= pos && (window == 0 || t > pos - window) &&
+        hit |= (flags[f] >> i & 1) && t <= last && t >= first &&
                !(flagged >> (kPageFlags + (block >> 1)) & 1);
       }
 #pragma unroll
@@ -382,13 +383,14 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_prefill(AttnArgs a, int gr
   // the wave's rows
   const int col = lane & 31, half = lane >> 5;
   const int th = wave >> 2;                      // its half of the tokens
-  const int32_t first_pos = rows.len - rows.count, wave0 = row0 + 32 * (wave & 3);
+  const int32_t wave0 = row0 + 32 * (wave & 3);
   const bool some = wave0 < end_row;             // the wave has rows
   const int32_t row = wave0 + col < end_row ? wave0 + col : end_row - 1, tok = row / group;
   const int64_t t_row = rows.first + tok, h_row = head * group + (row - tok * group);
-  const int32_t pos = wave0 + col < end_row ? first_pos + tok : -1;
-  const int32_t low = first_pos + wave0 / group;
-  const int32_t high = first_pos + ((wave0 + 32 < end_row ? wave0 + 32 : end_row) - 1) / group;
+  const int32_t pos = wave0 + col < end_row ? rows.pos + tok : -1, end = rows.len - 1;
+  const int32_t first = a.window > 0 ? pos - a.window + 1 : 0, last = pos < end ? pos : end;
+  const int32_t low = rows.pos + wave0 / group, least = low < end ? low : end;
+  const int32_t high = rows.pos + ((wave0 + 32 < end_row ? wave0 + 32 : end_row) - 1) / group;
   float c = fabsf(a.scale) * spl::kLog2e;
   const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u, keep = c > 0.0f ? 0xffffffffu : 0u;
   c = c > 0.0f ? c : 1.0f;
@@ -429,7 +431,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_prefill(AttnArgs a, int gr
       if (more && th == 0) prepare();
       const int32_t t0 = at(i) + th * (Gm::kTok / 2);
       if (some && t0 <= high && (a.window == 0 || t0 + Gm::kTok / 2 - 1 > low - a.window))
-        multiply<T, D>(st, lds[now], flags[now] + th * kFlags, q, th, t0, pos, low, high, a.window, c, lane);
+        multiply<T, D>(st, lds[now], flags[now] + th * kFlags, q, th, t0, first, last, least, high, a.window, c, lane);
       if (more && th == 1) prepare();
       __syncthreads();
     }

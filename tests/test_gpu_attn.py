@@ -536,3 +536,55 @@ def test_prompts_among_more_requests_than_a_wave_has_lanes(max_new):
     one = Batch([1] * rows, [1 + i % 3 for i in range(rows)], H, H, 64, 16, BF, seed=26)      # no prompt, and max_new not known
     want, known = one.run(max_new=0), one.run()
     assert torch.equal(want[0], known[0]) and torch.equal(want[1], known[1])
+
+
+# requests for each of the kernels: single rows, their splits, tiles of 16 rows, of 32, many rows of one request and of two
+GIVEN = {"rows": ([1, 1, 4], [30, 70, 90], 4, {}), "splits": ([1, 3], [9000, 8000], 4, {}),
+         "tiles": ([1, 20, 9], [30, 70, 60], 4, dict(max_new=0)), "wide": ([290], [2200], 64, dict(max_len=0)),
+         "prompt": ([700], [760], 64, {}), "prompts": ([600, 50], [640, 90], 64, {})}
+
+
+def _check_given(b, rows, tokens, window, **kw):
+    """The first `rows` rows, at the positions that lens and row_start give them, over the first `tokens` tokens."""
+    got, lse = b.run(q=b.q[:rows].cuda(), window=window, **kw)
+    for r in range(len(b.lens)):
+        s, e = int(b.row_start[r]), min(int(b.row_start[r + 1]), rows)
+        pick = range(s, e) if e - s < 40 else sorted({s, s + 1, s + 31, min(s + 128, e - 1), (s + e) // 2, *range(e - 12, e)})
+        for t in pick:
+            p = b.lens[r] - int(b.row_start[r + 1]) + t
+            lo, hi = max(0, p - window + 1) if window else 0, min(p + 1, tokens)
+            if hi <= lo:
+                assert (got[t] == 0).all() and torch.isneginf(lse[t]).all(), (r, t)
+                continue
+            w, l, m, top = ref.attention(b.q.double()[t:t + 1], [b.keys[r][lo:hi]], [b.values[r][lo:hi]], [0, 1], [hi - lo],
+                                         b.D ** -0.5, 0)
+            tol = 3 * ref.UNIT[b.dt] + 2.0 ** -18 * (1 + top)
+            assert ((got[t] - w[0]).abs() <= tol * m[0] + ref.STEP[b.dt]).all(), (r, t)
+            assert ((lse[t] - l[0]).abs() <= tol).all(), (r, t)
+
+
+@pytest.mark.parametrize("window", [0, 25])
+@pytest.mark.parametrize("kind", GIVEN)
+def test_rows_of_a_request_that_the_call_does_not_have(kind, window):
+    """A step with fewer rows than new tokens has the first rows of its last requests, not their last ones."""
+    new, lens, H, kw = GIVEN[kind]
+    H = H if H < 64 else 64 * torch.cuda.get_device_properties(0).multi_processor_count // 256
+    b = Batch(new, lens, H, H, 64, 32, BF, seed=28, extra=40 if kind == "wide" else 0)
+    _check_given(b, sum(new) - (1 if max(new) < 9 else 7), max(lens), window, **kw)
+
+
+@pytest.mark.parametrize("window", [0, 25])
+@pytest.mark.parametrize("kind", GIVEN)
+def test_tokens_past_the_table(kind, window):
+    """Requests longer than the table's pages: rows keep their positions and see the tokens that have pages."""
+    new, lens, H, kw = GIVEN[kind]
+    H = H if H < 64 else 64 * torch.cuda.get_device_properties(0).multi_processor_count // 256
+    b = Batch(new, lens, H, H, 64, 32, BF, seed=29)
+    width = max(2, b.table.shape[1] - 1)
+    if kind == "wide":                               # pages that no token has, so that the launch counts on many
+        kw = dict(max_len=2200)
+    b.table = b.table[:, :width].contiguous()
+    _check_given(b, sum(new), 32 * width, window, **kw)
+    if kind not in ("wide", "splits"):
+        b.table = b.table[:, :1].contiguous()
+        _check_given(b, sum(new), 32, window, **kw)
