@@ -690,13 +690,13 @@ spl_status spl_cache_read(const spl_kv_cache* cache, const int32_t* slots, int64
  *               arguments (-1 if they are rejected), 256-byte aligned, caller-owned.
  * Scores, softmax statistics and sums in fp32; a weight of the softmax is
  * rounded to the cache's type before it meets the values, out once.  A row that
- * sees no key gives 0.  Keys and values of masked tokens have no influence,
- * whatever they hold.  The result of a row depends on the split, and so on the
- * sizes of the call, in the order of its sums only.
- * Sizes that one launch does not hold are SPL_ERR_UNSUPPORTED: with max_new rows of
- * the heads of a key head at most 16, requests * cache heads from 2^24 on; else from
- * 2^23 on (rows of a key head / 128 + requests) * cache heads, of 256 channels from
- * 2^24 on (them / 16 + requests) * cache heads. */
+ * sees no key gives 0, as does one whose scores are all -inf.  Keys and values of
+ * masked tokens have no influence, whatever they hold.  The result of a row depends
+ * on the split, and so on the sizes of the call, in the order of its sums only.
+ * Sizes that one launch does not hold are SPL_ERR_UNSUPPORTED.  With g = heads /
+ * cache heads: requests * cache heads from 2^24 on where max_new * g is 1 to 16, else
+ * (tokens * g / 128 + requests) * cache heads from 2^23 on, and with 256 channels
+ * (tokens * g / 16 + requests) * cache heads from 2^24 on. */
 int64_t spl_attention_fp4_workspace_bytes(const spl_kv_cache* cache, int64_t tokens, int32_t heads, int64_t requests,
                                           int64_t width, int64_t max_new, int64_t max_len);
 spl_status spl_attention_fp4(const spl_heads* q, int64_t tokens, const spl_kv_cache* cache, const int32_t* table,

@@ -43,3 +43,14 @@ def test_no_private_memory(source, tmp_path_factory):
     if source == "k_int8_quad":
         eight = {k: v for k, v in kernels.items() if "Li8E" in k}
         assert len(eight) == 2 and all(v[1] >= 6 for v in eight.values()), eight
+
+
+def test_private_memory_of_the_attention_half(tmp_path_factory):
+    """Spills of few registers where a second wave or tile gains more than they cost, and nowhere else."""
+    for source in ("k_tables", "k_attn_prefill"):
+        kernels = _kernels(source, tmp_path_factory)
+        assert not any(v[0] for v in kernels.values()), kernels
+    known = {"Li96ELi2ELi2E": 28, "Li128ELi2ELi2E": 68, "Li256ELi1ELi2E": 120}
+    for name, (private, _) in _kernels("k_attn", tmp_path_factory).items():
+        limit = next((n for k, n in known.items() if "k_attn_rows" in name and k in name), 0)
+        assert private <= limit, (name, private)

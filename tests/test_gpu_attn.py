@@ -588,3 +588,21 @@ def test_tokens_past_the_table(kind, window):
     if kind not in ("wide", "splits"):
         b.table = b.table[:, :1].contiguous()
         _check_given(b, sum(new), 32, window, **kw)
+
+
+@pytest.mark.parametrize("new,length,H", [([1], 50, 4), ([1], 9000, 4), ([20], 50, 4), ([600], 600, 64)])
+def test_rows_whose_scores_are_all_minus_infinity(new, length, H):
+    """As rows that see no key: 0 and -inf; beside them a head whose scores are finite."""
+    H = H if H < 64 else 64 * torch.cuda.get_device_properties(0).multi_processor_count // 256
+    b = Batch(new, [length], H, H, 64, 64, BF, seed=30)
+    k = torch.full((length, H, 64), -2.0, dtype=BF)
+    at = torch.arange(length)
+    slots = (b.table[0].cpu()[at // 64] * 64 + at % 64).int().cuda()
+    _spl().qk_norm_rope_append(k.cuda(), k.cuda(), b.values[0].to(BF).cuda(), None, None, slots, b.cache)
+    clean = b.run()[0]
+    assert torch.isfinite(clean).all()
+    b.q[:, 1, 7] = float("inf")
+    got, lse = b.run()
+    assert (got[:, 1] == 0).all() and torch.isneginf(lse[:, 1]).all()
+    others = [h for h in range(H) if h != 1]
+    assert torch.equal(got[:, others], clean[:, others])
