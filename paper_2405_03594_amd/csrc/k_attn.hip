@@ -239,8 +239,8 @@ __device__ __forceinline__ void value_pair(const Raw<D>& r, int c, u32x4& even, 
 
 // The state of a tile's softmax: per lane the row's m, with mc = c m - lift; l
 // (four times the same) the sum of the weights 2^(c s - mc) as they meet the
-// values, rounded, so that what a rounding adds to a weight it adds to the sum
-// too; o[n] channels U (4 j + i) + n of the row.  l is a row of ones among the
+// values: rounded to 16 bits, which the matrix instruction multiplies, so that what
+// a rounding adds to a weight it adds to the sum too; o[n] channels U (4 j + i) + n of the row.  l is a row of ones among the
 // values: a matrix instruction adds it up.  m is a maximum of the scores so far,
 // but moves only when one passes it by the slack of reference_of.
 template <int D>
@@ -656,7 +656,8 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_attn_join(AttnArgs a, int s
 // last 512 tokens of 1024: 22.5 / 21.8, of 2048 37.1 / 32.6, of 8192 130 / 100;
 // 64 channels of 2048 25.8 / 23.1; a 512-token prompt 14.8 / 15.8; 24 requests
 // under a window of 1024, 64 channels, 26.2 / 28.6; the last 256 tokens of 4096,
-// half the workgroups, 39.9 / 49.3.
+// half the workgroups, 39.9 / 49.3.  They spill 16 registers at 128 channels and 6 at
+// 96 (68 and 28 bytes of scratch a lane), and gain that much over it.
 spl::AttnPlan plan_of(const AttnArgs& a) {
   const int64_t cus = spl::device_cus();
   spl::AttnPlan p{};

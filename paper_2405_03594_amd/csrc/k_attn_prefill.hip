@@ -244,7 +244,10 @@ __device__ __forceinline__ void widen(uint8_t* lds, uint8_t* flags, Raw<D>& r, c
 }
 
 // Per lane the row's m with mc = c m - lift (reference_of), the sum of the lane's
-// weights 2^(c s - mc), and the row's products with the values.
+// weights 2^(c s - mc), and the row's products with the values.  The weights are
+// rounded to 16 bits for those products alone, which 16-bit matrix instructions do;
+// the sum is of the exact ones, which are at hand in a register (rounded ones, added
+// by a product with ones, took no less time).
 template <int D>
 struct State {
   float m, mc, l;

@@ -14,7 +14,8 @@
 //
 // Bound: HBM at large sizes (2 + 2 bytes an element forward, 4 + 2 backward),
 // the launch at small ones.  Measured, bf16, 2048 tokens of 128 channels: 32 + 32
-// heads forward 17.8 us (67 MB at 3.8 TB/s, where a copy makes 5.2), the gradient
+// heads forward 17.8 us (67 MB at 3.8 TB/s; copies make 5.2 at 142 to 160 MB, 4.8 at
+// 4 GiB), the gradient
 // 23.6 (101 MB at 4.3) and 4 for the weights' sums; 32 + 8 heads stored in the
 // cache 15.0, read back 4.9.  16 tokens of 32 + 32 heads stored 4.6, read back 2.8.
 // What is left over a copy is the arithmetic of waves that all start together.
