@@ -82,8 +82,9 @@ typedef enum {
   SPL_ERR_DEVICE = 4         /* the HIP runtime reported an error */
 } spl_status;
 
-/* SPL_I4: 4-bit codes stored two per byte (spl_sparse_linear_int4 only). */
-typedef enum { SPL_F16 = 1, SPL_BF16 = 2, SPL_I8 = 3, SPL_I4 = 4 } spl_dtype;
+/* SPL_I4: 4-bit codes stored two per byte (spl_sparse_linear_int4 only).
+ * SPL_F32: of the 8-bit float linears and the optimizer step only. */
+typedef enum { SPL_F16 = 1, SPL_BF16 = 2, SPL_I8 = 3, SPL_I4 = 4, SPL_F32 = 5 } spl_dtype;
 
 /* Kernel family for spl_sparse_linear_ex / spl_dense_linear_ex.
  * AUTO picks by batch size M, and between kernels of one size by the matrices'
@@ -703,6 +704,170 @@ spl_status spl_attention_fp4(const spl_heads* q, int64_t tokens, const spl_kv_ca
                              int64_t requests, int64_t width, const int32_t* lens, const int32_t* row_start,
                              int64_t max_new, int64_t max_len, float scale, int32_t window, void* out, float* lse,
                              void* workspace, hipStream_t stream);
+
+/* Linear layers in 8-bit floats, their gradients and the optimizer step: what
+ * stays dense beside the sparse linears, for serving and for training (not a
+ * method of the paper).  One training step of such a layer is
+ *   spl_quantize_fp8 (X, rows and transposed), spl_linear_fp8 (Y),
+ *   spl_quantize_fp8 (dY, rows and transposed), spl_linear_fp8 (dX, dW),
+ *   spl_adamw_step, spl_quantize_fp8 (W and its transpose).
+ *
+ * Format: codes are 8-bit floats (1 sign, 4 exponent, 3 fraction bits; largest
+ * 448, no infinity, 0x7f and 0xff NaN), and a block of 128 columns of one row
+ * (block 1: activations, gradients) or of 128 x 128 entries (block 128:
+ * weights) shares a scale 2^e, held as the byte e + 127.  e is the least with
+ * |x| <= 448 * 2^e over the block, at least -127 (a block of zeros: -127);
+ * codes are x / 2^e to nearest, ties to the even code.  A block that held an
+ * infinity or a NaN has the byte 255 and NaN codes.  A power of two costs a
+ * float's codes no precision, and the matrix instructions apply it for nothing.
+ *
+ * A matrix [rows][cols] (or `count` of them, one after another):
+ *   codes    [count][rows][pitch], pitch = cols rounded up to 128; the columns
+ *            past cols are zero codes (or any, in a block of NaN).
+ *   scales   [count][ceil(rows / block)][spitch], spitch = pitch / 128 rounded
+ *            up to 4; bytes past pitch / 128 are not used.
+ * codes are 16-byte aligned, scales 4-byte aligned.  rows, cols, count >= 1;
+ * cols <= 2^22, count <= 65535, rows < 2^31, count * rows * pitch < 2^42. */
+typedef struct {
+  void* codes;
+  void* scales;
+  int64_t rows;
+  int64_t cols;
+  int64_t count;
+  int64_t codes_bytes;           /* allocated: >= spl_fp8_codes_bytes */
+  int64_t scales_bytes;          /* allocated: >= spl_fp8_scales_bytes */
+  int32_t block;                 /* rows that share a scale: 1 or 128 */
+} spl_fp8_matrix;
+
+/* Bytes of the two arrays; -1 for sizes that a matrix does not have. */
+int64_t spl_fp8_codes_bytes(int64_t rows, int64_t cols, int64_t count);
+int64_t spl_fp8_scales_bytes(int64_t rows, int64_t cols, int64_t count, int32_t block);
+
+/* X into that format: as it is, transposed, or both in one pass over it.
+ *   X            [count][rows][cols] of dtype (fp16, bf16 or fp32), rows
+ *                row_stride elements apart, matrices rows * row_stride apart.
+ *   out          rows x cols, or NULL.  out_t: the transpose, cols x rows, or
+ *                NULL; its blocks run along the rows of X.  Not both NULL; their
+ *                block is the same and their count that of X.
+ *   starts       NULL, or [groups + 1] int32 on the device (count 1): group g owns
+ *                rows starts[g] .. starts[g + 1] - 1 of X.  out_t then has a
+ *                group's rows of X from a multiple of 128 of its columns on:
+ *                group g begins at column 128 * sum over the groups before it of
+ *                ceil(rows of the group / 128), and zeros fill up its last block.
+ *                out_t->cols is at least spl_fp8_grouped_cols(rows, groups).
+ *                Rows of no group are in neither result; block is 1.  A start outside
+ *                [0, rows] counts as the nearer bound, one below the start before
+ *                it as no rows.
+ * What no entry of X falls to is left as it was: the bytes of scales past the
+ * last block, with starts also rows of no group and columns past the last.
+ * rows == 0 is a no-op.  rows and cols up to 2^22 each (SPL_ERR_UNSUPPORTED past
+ * that). */
+int64_t spl_fp8_grouped_cols(int64_t rows, int64_t groups);
+spl_status spl_quantize_fp8(const void* X, int32_t dtype, int64_t rows, int64_t cols, int64_t row_stride, int64_t count,
+                            const int32_t* starts, int64_t groups, const spl_fp8_matrix* out,
+                            const spl_fp8_matrix* out_t, hipStream_t stream);
+
+/* What a matrix in that format stands for: out [count][rows][cols] of dtype
+ * (fp16, bf16 or fp32), rounded once. */
+spl_status spl_dequantize_fp8(const spl_fp8_matrix* A, int32_t dtype, void* out, hipStream_t stream);
+
+/* Y [M][N] = X W^T of two such matrices that share cols: X of M rows, W of N, of
+ * either block.  fp32 sums, one rounding to dtype (fp16, bf16 or fp32).  With
+ * W and X the transposes of dY and of X it is the weight's gradient, with X = dY
+ * and W the transpose of the weight that of the activations.
+ *   Y            [M][N], 16-byte aligned, overwritten.
+ *   workspace    spl_linear_fp8_workspace_bytes(M, N, cols) bytes (-1 for sizes
+ *                that the call rejects, 0: NULL will do), 256-byte aligned,
+ *                caller-owned, overwritten.
+ * The order of a sum depends on the sizes only: the same call gives the same bits. */
+int64_t spl_linear_fp8_workspace_bytes(int64_t M, int64_t N, int64_t cols);
+spl_status spl_linear_fp8(const spl_fp8_matrix* X, const spl_fp8_matrix* W, int32_t dtype, void* Y, void* workspace,
+                          hipStream_t stream);
+
+/* The same from activations X [M][cols] of x_dtype (fp16 or bf16), rows
+ * row_stride elements apart, that are quantized on the way, block 1, as
+ * spl_quantize_fp8 does: the result is that of the two calls but for the order of
+ * the sums.  W as above, Y of dtype.
+ *   workspace    spl_linear_fp8_rows_workspace_bytes(...) bytes, 256-byte aligned. */
+int64_t spl_linear_fp8_rows_workspace_bytes(int64_t M, int64_t N, int64_t cols);
+spl_status spl_linear_fp8_rows(const void* X, int32_t x_dtype, int64_t M, int64_t row_stride, const spl_fp8_matrix* W,
+                               int32_t dtype, void* Y, void* workspace, hipStream_t stream);
+
+/* Linear layers of W->count experts: row m of X, in starts[e] <= m < starts[e + 1],
+ * is multiplied with matrix e.  starts [W->count + 1] int32 on the device, taken
+ * as by spl_quantize_fp8 (groups that overlap: which one a shared row's result is
+ * of is not defined); rows of no expert are left as they were in Y [M][N].
+ *   X            as spl_linear_fp8 takes it (block 1), or
+ *   spl_linear_fp8_grouped_rows: as spl_linear_fp8_rows takes it.
+ * The workspace-size functions as above, of M, N, cols and the experts. */
+spl_status spl_linear_fp8_grouped(const spl_fp8_matrix* X, const spl_fp8_matrix* W, const int32_t* starts,
+                                  int32_t dtype, void* Y, hipStream_t stream);
+int64_t spl_linear_fp8_grouped_rows_workspace_bytes(int64_t M, int64_t N, int64_t cols, int64_t experts);
+spl_status spl_linear_fp8_grouped_rows(const void* X, int32_t x_dtype, int64_t M, int64_t row_stride,
+                                       const spl_fp8_matrix* W, const int32_t* starts, int32_t dtype, void* Y,
+                                       void* workspace, hipStream_t stream);
+
+/* Their weights' gradients: dW [experts][N][K], dW[e] = sum over the rows m of
+ * expert e of dY[m][n] X[m][k], from the transposes that spl_quantize_fp8 makes of dY
+ * (N rows) and X (K rows) with the same starts.  dW of dtype, 16-byte aligned,
+ * fully written: zeros for an expert without rows. */
+spl_status spl_linear_fp8_grouped_weight_grad(const spl_fp8_matrix* dYt, const spl_fp8_matrix* Xt,
+                                              const int32_t* starts, int64_t experts, int64_t tokens, int32_t dtype,
+                                              void* dW, hipStream_t stream);
+
+/* AdamW over many tensors in one launch.  Per element, in fp32, every product and
+ * sum rounded on its own, with t = step:
+ *   g = grad * *grad_scale             (no product without grad_scale)
+ *   m = m beta1 + g (1 - beta1)        v = v beta2 + g g (1 - beta2)
+ *   p = p (1 - lr decay) - lr / (1 - beta1^t) * (m / (sqrt(v) / sqrt(1 - beta2^t) + eps))
+ * the factors of a tensor computed in 64 bits and rounded to fp32 once.
+ *
+ * A tensor: n elements of param (fp32, bf16, fp16), grad (the same, its own
+ * type) and, with copy_dtype, of copy (fp16 or bf16), the new p rounded to it
+ * (the values of a compressed matrix, say, whose fp32 master is p).  m and v are
+ * fp32, or in 8 bits: m and r = sqrt(v), each in the codes of the format above
+ * with a scale byte for every 128 elements of the tensor, codes 128 * ceil(n /
+ * 128) bytes, of which those past n are not used.  An 8-bit state is rounded to one of the two
+ * codes next to it, up where 20 random bits, which are a hash of (seed, step,
+ * the tensor's place in the plan, the element), reach the distance, so that
+ * small changes count on average; r > 0 does not become 0.  A block that gets an
+ * infinity or a NaN is NaN from then on.
+ *
+ * A plan lists the tensors: spl_adamw_plan writes spl_adamw_plan_bytes bytes of
+ * HOST memory, which the caller copies to the device (16-byte aligned) for
+ * the calls; it holds addresses only.  No two arrays of a plan overlap. */
+typedef struct {
+  void* param;
+  const void* grad;
+  void* m;                       /* fp32, or 8-bit codes (16-byte aligned) */
+  void* v;
+  uint8_t* m_scales;             /* 8-bit states: [ceil(n / 128)]; else NULL */
+  uint8_t* v_scales;
+  void* copy;                    /* or NULL */
+  int64_t n;                     /* >= 0, < 2^40 */
+  double decay;
+} spl_adamw_tensor;
+
+typedef struct {
+  int32_t param_dtype;           /* SPL_F32, SPL_BF16 or SPL_F16 */
+  int32_t grad_dtype;
+  int32_t copy_dtype;            /* 0: no copies */
+  int32_t state_bits;            /* 32 or 8 */
+} spl_adamw_types;
+
+/* Workgroups of a plan (what spl_adamw_step takes), and its bytes; -1 for
+ * tensors that it refuses. */
+int64_t spl_adamw_plan_chunks(const spl_adamw_tensor* tensors, int64_t count, const spl_adamw_types* types);
+int64_t spl_adamw_plan_bytes(const spl_adamw_tensor* tensors, int64_t count, const spl_adamw_types* types);
+spl_status spl_adamw_plan(const spl_adamw_tensor* tensors, int64_t count, const spl_adamw_types* types, void* host_plan);
+
+/* One step.  step: the number of this step, from 1 on; or, with step_on_device, an
+ * int32 there that is read when the step runs (a captured graph that is replayed
+ * adds to it), below 1 taken as 1.  grad_scale: NULL, or one float on the device; where it is not
+ * finite, nothing is updated.  lr finite, 0 <= beta < 1, eps >= 0. */
+spl_status spl_adamw_step(const void* plan, int64_t chunks, const spl_adamw_types* types, double lr, double beta1,
+                          double beta2, double eps, int64_t step, const int32_t* step_on_device,
+                          const float* grad_scale, uint32_t seed, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -18,7 +18,10 @@ Names follow the C ABI without its ``spl_`` prefix:
   the training step with the mask held fixed (Algorithm 1);
 * ``block_tables``, ``qk_norm_rope[_grad|_append]``, ``cache_read``,
   ``attention_fp4`` over a :class:`KVCache`: the attention half of a layer,
-  between the q, k, v projections and o.
+  between the q, k, v projections and o;
+* ``quantize_fp8[_both]``, ``linear_fp8[_grad]``, ``linear_fp8_grouped[_grad]``
+  over an :class:`Fp8Matrix`: dense linears in 8-bit floats, and of experts;
+* ``adamw_plan``, ``adamw_step``: the optimizer step over many tensors.
 """
 from __future__ import annotations
 
@@ -37,6 +40,7 @@ LAYOUT = {"rows": 0, "tile16": 1}
 ALGO = {"auto": 0, "decode": 1, "prefill": 2}
 _STATUS = {0: "ok", 1: "invalid argument", 2: "unsupported", 3: "overflow", 4: "HIP runtime error"}
 I4 = 4                                  # 4-bit codes, two per byte (values held as uint8)
+F32 = 5                                 # of the 8-bit float linears and the optimizer step
 _TORCH_DTYPE = {torch.float16: F16, torch.bfloat16: BF16, torch.int8: I8, torch.uint8: I4}
 _CODE_DTYPE = {F16: torch.float16, BF16: torch.bfloat16, I8: torch.int8, I4: torch.uint8}
 
@@ -90,6 +94,23 @@ class _KVCache(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("pages", ctypes.c_int64), ("data_bytes", ctypes.c_int64),
                 ("page", ctypes.c_int32), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("dtype", ctypes.c_int32)]
+
+
+class _Fp8(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64), ("count", ctypes.c_int64), ("codes_bytes", ctypes.c_int64),
+                ("scales_bytes", ctypes.c_int64), ("block", ctypes.c_int32)]
+
+
+class _AdamwTensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("m_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p), ("copy", ctypes.c_void_p),
+                ("n", ctypes.c_int64), ("decay", ctypes.c_double)]
+
+
+class _AdamwTypes(ctypes.Structure):
+    _fields_ = [("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32), ("copy_dtype", ctypes.c_int32),
+                ("state_bits", ctypes.c_int32)]
 
 
 class _DenseInt8Task(ctypes.Structure):
@@ -177,6 +198,27 @@ def lib() -> ctypes.CDLL:
         "spl_cache_read": (ctypes.c_int, [CP, P, I64, P, P, P]),
         "spl_attention_fp4_workspace_bytes": (I64, [CP, I64, I32, I64, I64, I64, I64]),
         "spl_attention_fp4": (ctypes.c_int, [HP, I64, CP, P, I64, I64, P, P, I64, I64, F32, I32, P, P, P, P]),
+    })
+    MQ, F64 = ctypes.POINTER(_Fp8), ctypes.c_double
+    TP, YP = ctypes.POINTER(_AdamwTensor), ctypes.POINTER(_AdamwTypes)
+    sigs.update({
+        "spl_fp8_codes_bytes": (I64, [I64, I64, I64]),
+        "spl_fp8_scales_bytes": (I64, [I64, I64, I64, I32]),
+        "spl_fp8_grouped_cols": (I64, [I64, I64]),
+        "spl_quantize_fp8": (ctypes.c_int, [P, I32, I64, I64, I64, I64, P, I64, MQ, MQ, P]),
+        "spl_dequantize_fp8": (ctypes.c_int, [MQ, I32, P, P]),
+        "spl_linear_fp8_workspace_bytes": (I64, [I64, I64, I64]),
+        "spl_linear_fp8": (ctypes.c_int, [MQ, MQ, I32, P, P, P]),
+        "spl_linear_fp8_rows_workspace_bytes": (I64, [I64, I64, I64]),
+        "spl_linear_fp8_rows": (ctypes.c_int, [P, I32, I64, I64, MQ, I32, P, P, P]),
+        "spl_linear_fp8_grouped": (ctypes.c_int, [MQ, MQ, P, I32, P, P]),
+        "spl_linear_fp8_grouped_rows_workspace_bytes": (I64, [I64, I64, I64, I64]),
+        "spl_linear_fp8_grouped_rows": (ctypes.c_int, [P, I32, I64, I64, MQ, P, I32, P, P, P]),
+        "spl_linear_fp8_grouped_weight_grad": (ctypes.c_int, [MQ, MQ, P, I64, I64, I32, P, P]),
+        "spl_adamw_plan_chunks": (I64, [TP, I64, YP]),
+        "spl_adamw_plan_bytes": (I64, [TP, I64, YP]),
+        "spl_adamw_plan": (ctypes.c_int, [TP, I64, YP, P]),
+        "spl_adamw_step": (ctypes.c_int, [P, I64, YP, F64, F64, F64, F64, I64, P, P, ctypes.c_uint32, P]),
     })
     for name, (res, args) in sigs.items():
         fn = getattr(L, name)
@@ -1276,3 +1318,422 @@ def attention_fp4(q: torch.Tensor, cache: KVCache, table: torch.Tensor, lens: to
                                D ** -0.5 if scale is None else scale, window, out.data_ptr(), _ptr(lse), _ptr(ws),
                                _on(stream)))
     return out
+
+
+# ------------------------------------------------------------------------------ linears in 8-bit floats
+
+
+_FLOAT_TYPES = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
+_CODE_TYPES = (torch.uint8, torch.float8_e4m3fn)
+
+
+def _here(names: str, stream, *tensors) -> torch.device:
+    """The device of the call, which is the current one: every tensor is on it, and so is the stream."""
+    at = torch._C._cuda_getDevice() if any(t is not None and t.is_cuda for t in tensors) else -1
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != at):
+            raise ValueError(f"{names}: tensors of the current device only")
+    if stream is not None and isinstance(stream, torch.cuda.Stream) and stream.device_index != at:
+        raise ValueError("the stream must be of the current device")
+    return tensors[0].device
+
+
+class Fp8Matrix:
+    """A matrix [rows, cols] (or `count` of them) in 8-bit floats with a power-of-two scale for each block of 128 columns
+    of one row (block 1) or of 128 rows (block 128); format: spl_fp8_matrix.
+
+    codes: uint8 or float8_e4m3fn [rows, pitch] or [count, rows, pitch], pitch = cols rounded up to 128; scales: uint8
+    [..., ceil(rows / block), spitch], spitch = pitch / 128 rounded up to 4.  ``quantize_fp8`` makes one, ``Fp8Matrix.of``
+    takes codes and scales that come from elsewhere."""
+
+    __slots__ = ("codes", "scales", "cols", "block")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, cols: int, block: int = 1):
+        self.codes, self.scales, self.cols, self.block = codes, scales, cols, block
+        self.view()
+
+    @property
+    def rows(self) -> int:
+        return self.codes.shape[-2]
+
+    @property
+    def count(self) -> int:
+        return 1 if self.codes.dim() == 2 else self.codes.shape[0]
+
+    def block_scales(self) -> torch.Tensor:
+        """The scale bytes (e + 127) without the padding of their rows: [..., ceil(rows / block), ceil(cols / 128)]."""
+        return self.scales[..., :(self.cols + 127) // 128]
+
+    def view(self) -> _Fp8:
+        """The matrix as a call takes it: of the attributes as they are now."""
+        codes, scales, cols, block = self.codes, self.scales, self.cols, self.block
+        shape = codes.shape
+        if block not in (1, 128):
+            raise ValueError("block must be 1 or 128")
+        pitch = (cols + 127) // 128 * 128
+        if cols < 1 or len(shape) not in (2, 3) or shape[-1] != pitch or codes.dtype not in _CODE_TYPES or \
+                not codes.is_contiguous():
+            raise ValueError(f"codes must be contiguous 8-bit floats [rows, {pitch}] or [count, rows, {pitch}]")
+        want = (*shape[:-2], (shape[-2] + block - 1) // block, (pitch // 128 + 3) // 4 * 4)
+        if scales.shape != want or scales.dtype != torch.uint8 or not scales.is_contiguous():
+            raise ValueError(f"scales must be contiguous uint8 {list(want)}")
+        return _Fp8(codes.data_ptr(), scales.data_ptr(), shape[-2], cols, 1 if len(shape) == 2 else shape[0],
+                    codes.numel(), scales.numel(), block)
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, block: int = 1, count: int | None = None, device="cuda", stream=None):
+        L, n = lib(), 1 if count is None else count
+        need = L.spl_fp8_scales_bytes(rows, cols, n, _int32(block, "block"))
+        if need < 0:
+            raise ValueError(f"no matrix of {n} x {rows} x {cols} with blocks of {block} rows")
+        lead = () if count is None else (count,)
+        codes = _result((*lead, rows, (cols + 127) // 128 * 128), torch.uint8, device, stream)
+        scales = _result((*lead, (rows + block - 1) // block, ((cols + 127) // 128 + 3) // 4 * 4), torch.uint8, device,
+                         stream)
+        m = object.__new__(cls)
+        m.codes, m.scales, m.cols, m.block = codes, scales, cols, block
+        return m
+
+    @classmethod
+    def of(cls, codes: torch.Tensor, scales: torch.Tensor, cols: int, block: int) -> "Fp8Matrix":
+        """From codes [..., rows, cols or more] and scale bytes [..., ceil(rows / block), ceil(cols / 128)], copied where
+        they are not laid out as here."""
+        if codes.dtype not in _CODE_TYPES or scales.dtype != torch.uint8 or block not in (1, 128) or cols < 1:
+            raise ValueError("codes of 8-bit floats, scales of uint8, block 1 or 128, at least one column")
+        blocks, rows = (cols + 127) // 128, codes.shape[-2]
+        if codes.shape[-1] < cols or scales.shape != (*codes.shape[:-2], (rows + block - 1) // block, blocks):
+            raise ValueError(f"codes {list(codes.shape)} and scales {list(scales.shape)} are not of {cols} columns")
+        codes = codes.view(torch.uint8)
+        if codes.shape[-1] != 128 * blocks or not codes.is_contiguous():
+            wide = torch.zeros((*codes.shape[:-1], 128 * blocks), dtype=torch.uint8, device=codes.device)
+            wide[..., :cols] = codes[..., :cols]
+            codes = wide
+        spitch = (blocks + 3) // 4 * 4
+        if spitch != blocks or not scales.is_contiguous():
+            wide = torch.zeros((*scales.shape[:-1], spitch), dtype=torch.uint8, device=scales.device)
+            wide[..., :blocks] = scales
+            scales = wide
+        return cls(codes, scales, cols, block)
+
+
+def _dense(X, name: str):
+    """(rows, cols, row stride, count) of a float matrix, or of several one after another."""
+    if not isinstance(X, torch.Tensor) or X.dim() not in (2, 3) or X.dtype not in _FLOAT_TYPES:
+        raise ValueError(f"{name} must be fp16, bf16 or fp32 [rows, cols] or [count, rows, cols]")
+    rows, cols = X.shape[-2:]
+    stride = X.stride(-2) if rows > 1 else max(cols, 1)
+    count = 1 if X.dim() == 2 else X.shape[0]
+    if cols < 1 or (cols > 1 and X.stride(-1) != 1) or stride < cols or (
+            X.dim() == 3 and count > 1 and X.stride(0) != rows * stride):
+        raise ValueError(f"{name}: columns must be contiguous, matrices one after another")
+    return rows, cols, stride, count
+
+
+def _starts(starts, experts: int | None = None) -> int:
+    """The groups of starts [groups + 1]."""
+    if not isinstance(starts, torch.Tensor) or starts.dim() != 1 or starts.shape[0] < 2:
+        raise ValueError("starts must be int32 [experts + 1]")
+    _ints(starts, "starts", starts.shape[0] if experts is None else experts + 1)
+    return starts.shape[0] - 1
+
+
+def _quantize(X, block, rows_too, cols_too, starts, stream):
+    rows, cols, stride, count = _dense(X, "X")
+    groups = 0 if starts is None else _starts(starts)
+    if rows < 1:
+        raise ValueError("X has no rows")
+    if block not in (1, 128):
+        raise ValueError("block must be 1 or 128")
+    if starts is not None and (X.dim() != 2 or block != 1):
+        raise ValueError("starts is for one matrix with blocks of one row")
+    device = _here("X, starts", stream, X, starts)
+    L, lead = lib(), None if X.dim() == 2 else count
+    out = Fp8Matrix.empty(rows, cols, block, lead, device, stream) if rows_too else None
+    out_t = None
+    if cols_too:
+        wide = rows if starts is None else L.spl_fp8_grouped_cols(rows, groups)
+        if wide < 0:
+            raise ValueError("too many rows or groups")
+        out_t = Fp8Matrix.empty(cols, wide, block, lead, device, stream)
+    _check("spl_quantize_fp8",
+           L.spl_quantize_fp8(X.data_ptr(), _FLOAT_TYPES[X.dtype], rows, cols, stride, count,
+                              None if starts is None else starts.data_ptr(), groups,
+                              None if out is None else out.view(), None if out_t is None else out_t.view(), _on(stream)))
+    return out, out_t
+
+
+def quantize_fp8(X: torch.Tensor, block: int = 1, transposed: bool = False, starts: torch.Tensor | None = None,
+                 stream=None) -> Fp8Matrix:
+    """X [rows, cols] (or [count, rows, cols]; fp16, bf16 or fp32) in 8-bit floats, or its transpose (see
+    spl_quantize_fp8).  block 1: a scale for 128 columns of a row, block 128: for 128 x 128 entries.  starts (int32
+    [groups + 1], transposed): each group's rows begin at a multiple of 128 of the result's columns."""
+    if starts is not None and not transposed:
+        raise ValueError("starts is for the transposed form")
+    return _quantize(X, block, not transposed, transposed, starts, stream)[transposed]
+
+
+def quantize_fp8_both(X: torch.Tensor, block: int = 1, starts: torch.Tensor | None = None, stream=None):
+    """(quantize_fp8(X), quantize_fp8(X, transposed=True)) in one pass over X.  With starts, rows of no group are in
+    neither."""
+    return _quantize(X, block, True, True, starts, stream)
+
+
+def dequantize_fp8(A: Fp8Matrix, dtype: torch.dtype = torch.float32, stream=None) -> torch.Tensor:
+    """What A stands for, [rows, cols] or [count, rows, cols] of dtype (see spl_dequantize_fp8)."""
+    if dtype not in _FLOAT_TYPES:
+        raise ValueError("dtype must be fp16, bf16 or fp32")
+    view, device = A.view(), _here("A", stream, A.codes, A.scales)
+    out = _result((*A.codes.shape[:-1], A.cols), dtype, device, stream)
+    _check("spl_dequantize_fp8", lib().spl_dequantize_fp8(view, _FLOAT_TYPES[dtype], out.data_ptr(), _on(stream)))
+    return out
+
+
+@functools.lru_cache(maxsize=1024)
+def _fp8_workspace(name: str, *sizes) -> int:
+    """A workspace-size function of sizes alone."""
+    need = getattr(lib(), name)(*sizes)
+    if need < 0:
+        raise ValueError(f"{name} rejected the sizes {sizes}")
+    return need
+
+
+def _fp8_out(out, M: int, N: int, dtype, X, device, stream) -> torch.Tensor:
+    """The result of a product, in dtype, else `out`'s, else X's type (bf16 where X holds codes)."""
+    if out is not None:
+        if dtype is not None and out.dtype != dtype:
+            raise ValueError(f"out has dtype {out.dtype}, expected {dtype}")
+        if out.dtype not in _FLOAT_TYPES:
+            raise ValueError("out must be fp16, bf16 or fp32")
+        _arg(out, "out", shape=(M, N), device=False)
+        _here("out", None, out)
+        return out
+    dtype = dtype or (torch.bfloat16 if isinstance(X, Fp8Matrix) else X.dtype)
+    if dtype not in _FLOAT_TYPES:
+        raise ValueError("dtype must be fp16, bf16 or fp32")
+    if stream is None:
+        return torch.empty((M, N), dtype=dtype, device=device)
+    return _result((M, N), dtype, device, stream)
+
+
+def _fp8_rows(X, cols: int):
+    """(rows, row stride) of the activations of a product: 16-bit floats."""
+    if not isinstance(X, torch.Tensor) or X.dim() != 2 or X.dtype not in _HEAD_TYPES or X.shape[1] != cols:
+        raise ValueError(f"X must be an Fp8Matrix or fp16 / bf16 [rows, {cols}]")
+    rows = X.shape[0]
+    stride = X.stride(0) if rows > 1 else cols
+    if (cols > 1 and X.stride(1) != 1) or stride < cols:
+        raise ValueError("X: columns must be contiguous")
+    return rows, stride
+
+
+def linear_fp8(X, W: Fp8Matrix, dtype: torch.dtype | None = None, out: torch.Tensor | None = None,
+               stream=None) -> torch.Tensor:
+    """Y [M, N] = X W^T in 8-bit floats (see spl_linear_fp8).  X: an Fp8Matrix, or fp16 / bf16 activations [M, K] that are
+    quantized on the way, a scale for 128 columns of a row.  Y: dtype, else that of out, else X's (bf16 for codes)."""
+    L, w = lib(), W.view()
+    if w.count != 1:
+        raise ValueError("W is several matrices: linear_fp8_grouped")
+    N, K = w.rows, w.cols
+    if isinstance(X, Fp8Matrix):
+        x = X.view()
+        if x.count != 1 or x.cols != K:
+            raise ValueError(f"X has {x.cols} columns, W {K}")
+        device = _here("X, W", stream, X.codes, X.scales, W.codes, W.scales)
+        out = _fp8_out(out, x.rows, N, dtype, X, device, stream)
+        need = _fp8_workspace("spl_linear_fp8_workspace_bytes", x.rows, N, K)
+        ws = _workspace_on(need, device, stream) if need else None
+        _check("spl_linear_fp8",
+               L.spl_linear_fp8(x, w, _FLOAT_TYPES[out.dtype], out.data_ptr(), _ptr(ws), _on(stream)))
+        return out
+    M, stride = _fp8_rows(X, K)
+    device = _here("X, W", stream, X, W.codes, W.scales)
+    out = _fp8_out(out, M, N, dtype, X, device, stream)
+    need = _fp8_workspace("spl_linear_fp8_rows_workspace_bytes", M, N, K)
+    ws = _workspace_on(need, device, stream) if need else None
+    _check("spl_linear_fp8_rows",
+           L.spl_linear_fp8_rows(X.data_ptr(), _TORCH_DTYPE[X.dtype], M, stride, w, _FLOAT_TYPES[out.dtype],
+                                 out.data_ptr(), _ptr(ws), _on(stream)))
+    return out
+
+
+def _gradient_args(dY, X, Wt: Fp8Matrix, grad_dtype):
+    for t, name in ((dY, "dY"), (X, "X")):
+        if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype not in _HEAD_TYPES:
+            raise ValueError(f"{name} must be fp16 or bf16 [rows, columns]")
+    if X.shape[0] != dY.shape[0] or X.dtype != dY.dtype or X.shape[1] != Wt.rows or dY.shape[1] != Wt.cols:
+        raise ValueError(f"dY {list(dY.shape)}, X {list(X.shape)} and the transposed weight [{Wt.rows}, {Wt.cols}] do not "
+                         "belong together")
+    if grad_dtype not in _FLOAT_TYPES:
+        raise ValueError("grad_dtype must be fp16, bf16 or fp32")
+
+
+def linear_fp8_grad(dY: torch.Tensor, X: torch.Tensor, Wt: Fp8Matrix, grad_dtype: torch.dtype = torch.float32,
+                    stream=None):
+    """(dX, dW) of Y = X W^T from dY [M, N] and X [M, K] (fp16 or bf16): dX = dY W in their type, dW = dY^T X in
+    grad_dtype, both sums in 8-bit floats, dY quantized along its columns for dX, dY and X along their rows for dW.
+    Wt: the transposed weight [K, N], as quantize_fp8_both makes it."""
+    _gradient_args(dY, X, Wt, grad_dtype)
+    if dY.shape[0] < 1:
+        raise ValueError("no rows")
+    q, qt = quantize_fp8_both(dY, stream=stream)
+    xt = quantize_fp8(X, transposed=True, stream=stream)
+    return linear_fp8(q, Wt, dtype=dY.dtype, stream=stream), linear_fp8(qt, xt, dtype=grad_dtype, stream=stream)
+
+
+def linear_fp8_grouped(X, W: Fp8Matrix, starts: torch.Tensor, dtype: torch.dtype | None = None,
+                       out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Y [M, N]: row m of X, starts[e] <= m < starts[e + 1], times matrix e of W (see spl_linear_fp8_grouped).  starts:
+    int32 [experts + 1] on the device.  X and Y as in linear_fp8.  Rows of no expert are not written: pass `out` where
+    there are some."""
+    L, w = lib(), W.view()
+    N, K = w.rows, w.cols
+    _starts(starts, w.count)
+    at = starts.data_ptr()
+    if isinstance(X, Fp8Matrix):
+        x = X.view()
+        if x.count != 1 or x.cols != K:
+            raise ValueError(f"X has {x.cols} columns, W {K}")
+        device = _here("X, W, starts", stream, X.codes, X.scales, W.codes, W.scales, starts)
+        out = _fp8_out(out, x.rows, N, dtype, X, device, stream)
+        _check("spl_linear_fp8_grouped",
+               L.spl_linear_fp8_grouped(x, w, at, _FLOAT_TYPES[out.dtype], out.data_ptr(), _on(stream)))
+        return out
+    M, stride = _fp8_rows(X, K)
+    device = _here("X, W, starts", stream, X, W.codes, W.scales, starts)
+    out = _fp8_out(out, M, N, dtype, X, device, stream)
+    need = _fp8_workspace("spl_linear_fp8_grouped_rows_workspace_bytes", M, N, K, w.count)
+    ws = _workspace_on(need, device, stream) if need else None
+    _check("spl_linear_fp8_grouped_rows",
+           L.spl_linear_fp8_grouped_rows(X.data_ptr(), _TORCH_DTYPE[X.dtype], M, stride, w, at,
+                                         _FLOAT_TYPES[out.dtype], out.data_ptr(), _ptr(ws), _on(stream)))
+    return out
+
+
+def linear_fp8_grouped_grad(dY: torch.Tensor, X: torch.Tensor, Wt: Fp8Matrix, starts: torch.Tensor,
+                            grad_dtype: torch.dtype = torch.float32, stream=None):
+    """(dX, dW) of linear_fp8_grouped as linear_fp8_grad's, Wt the transposed weights [experts, K, N], dW [experts, N, K]
+    with zeros for an expert without rows.  Rows of no expert are not written in dX."""
+    _gradient_args(dY, X, Wt, grad_dtype)
+    _starts(starts, Wt.count)
+    if dY.shape[0] < 1:
+        raise ValueError("no rows")
+    q, qt = quantize_fp8_both(dY, starts=starts, stream=stream)
+    xt = quantize_fp8(X, transposed=True, starts=starts, stream=stream)
+    dX = linear_fp8_grouped(q, Wt, starts, dtype=dY.dtype, stream=stream)
+    dW = _result((Wt.count, dY.shape[1], X.shape[1]), grad_dtype, dY.device, stream)
+    _check("spl_linear_fp8_grouped_weight_grad",
+           lib().spl_linear_fp8_grouped_weight_grad(qt.view(), xt.view(), starts.data_ptr(), Wt.count, dY.shape[0],
+                                                    _FLOAT_TYPES[grad_dtype], dW.data_ptr(), _on(stream)))
+    return dX, dW
+
+
+# ------------------------------------------------------------------------------ the optimizer step
+
+
+class Fp8Vector:
+    """An optimizer state of n elements in 8 bits: codes uint8 [128 * ceil(n / 128)] and a scale byte for every 128."""
+
+    __slots__ = ("codes", "scales", "n")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, n: int):
+        blocks = (n + 127) // 128
+        _arg(codes, "codes", shape=(128 * blocks,), dtype=torch.uint8, device=False)
+        _arg(scales, "scales", shape=(blocks,), dtype=torch.uint8, device=False)
+        self.codes, self.scales, self.n = codes, scales, n
+
+    @classmethod
+    def zeros(cls, n: int, device="cuda") -> "Fp8Vector":
+        blocks = (n + 127) // 128
+        return cls(torch.zeros((128 * blocks,), dtype=torch.uint8, device=device),
+                   torch.zeros((blocks,), dtype=torch.uint8, device=device), n)
+
+
+class AdamwPlan:
+    """The tensors of adamw_step, made by adamw_plan: it keeps them, and the list of their addresses on the device."""
+
+    __slots__ = ("tensors", "table", "chunks", "types", "device")
+
+    def __init__(self, tensors, table, chunks, types, device):
+        self.tensors, self.table, self.chunks, self.types, self.device = tensors, table, chunks, types, device
+
+
+def _one_type(tensors, name: str, allowed) -> int:
+    kinds = {t.dtype if isinstance(t, torch.Tensor) else type(t) for t in tensors}
+    if len(kinds) > 1 or not kinds <= set(allowed):
+        raise ValueError(f"{name}: tensors of one type of {', '.join(str(k) for k in allowed)}, got {kinds or 'none'}")
+    return allowed[kinds.pop()] if kinds else F32
+
+
+def adamw_plan(params, grads, exp_avg, exp_avg_sq, weight_decay=0.01, copies=None) -> AdamwPlan:
+    """The plan of adamw_step for lists of contiguous tensors (see spl_adamw_plan): params and grads in fp32, bf16 or
+    fp16 (one type for each list), both states float32 tensors or both Fp8Vector (exp_avg_sq then holds square roots),
+    copies (fp16 or bf16, or None) what receives the rounded params.  weight_decay: a number, or one for each tensor.
+    The plan keeps the tensors; where one gets another address, a new plan is needed.  Waits for the device once."""
+    lists = [list(x) for x in (params, grads, exp_avg, exp_avg_sq)] + ([] if copies is None else [list(copies)])
+    count = len(lists[0])
+    decays = [float(weight_decay)] * count if isinstance(weight_decay, (int, float)) else [float(d) for d in weight_decay]
+    if any(len(x) != count for x in lists) or len(decays) != count:
+        raise ValueError("params, grads, states, copies and weight_decay: one entry for each tensor")
+    P, G, M, V = lists[:4]
+    C = lists[4] if copies is not None else None
+    eight = any(isinstance(x, Fp8Vector) for x in M + V)
+    for i in range(count):
+        _arg(P[i], f"params[{i}]", device=False)
+        n = P[i].numel()
+        _arg(G[i], f"grads[{i}]", shape=P[i].shape, device=False)
+        if C is not None:
+            _arg(C[i], f"copies[{i}]", shape=P[i].shape, device=False)
+        for x, name in ((M[i], "exp_avg"), (V[i], "exp_avg_sq")):
+            if eight:
+                if not isinstance(x, Fp8Vector) or x.n != n:
+                    raise ValueError(f"{name}[{i}] must be an Fp8Vector of {n} elements, as the others")
+            else:
+                _arg(x, f"{name}[{i}]", shape=P[i].shape, dtype=torch.float32, device=False)
+    types = _AdamwTypes(_one_type(P, "params", _FLOAT_TYPES), _one_type(G, "grads", _FLOAT_TYPES),
+                        0 if C is None else _one_type(C, "copies", {torch.float16: F16, torch.bfloat16: BF16}),
+                        8 if eight else 32)
+    if copies is not None and count == 0:
+        types.copy_dtype = 0
+    states = [t for x in M + V for t in ((x.codes, x.scales) if eight else (x,))]
+    every = [*P, *G, *states, *(C or [])]
+    device = _here("params, grads, states, copies", None, *every) if every else torch.device("cuda")
+    rows = (_AdamwTensor * max(count, 1))()
+    for i in range(count):
+        m, v = M[i], V[i]
+        rows[i] = _AdamwTensor(P[i].data_ptr(), G[i].data_ptr(), (m.codes if eight else m).data_ptr(),
+                               (v.codes if eight else v).data_ptr(), m.scales.data_ptr() if eight else None,
+                               v.scales.data_ptr() if eight else None, C[i].data_ptr() if C is not None else None,
+                               P[i].numel(), decays[i])
+    L = lib()
+    need, chunks = L.spl_adamw_plan_bytes(rows, count, types), L.spl_adamw_plan_chunks(rows, count, types)
+    if need < 0:
+        raise ValueError("spl_adamw_plan_bytes rejected the tensors (addresses of their type's alignment, 8-bit codes 16-byte "
+                         "aligned, finite weight decay, fewer than 2^24 chunks of 8192 elements)")
+    host = torch.zeros((max(need, 16),), dtype=torch.uint8)
+    st = L.spl_adamw_plan(rows, count, types, host.data_ptr())
+    if st == 1:
+        raise ValueError("two arrays of the plan overlap")
+    _check("spl_adamw_plan", st)
+    table = host.to(device) if every else host
+    return AdamwPlan(every, table, chunks, types, device)
+
+
+def adamw_step(plan: AdamwPlan, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, step: int | torch.Tensor = 1,
+               grad_scale: torch.Tensor | None = None, seed: int = 0, stream=None) -> None:
+    """One AdamW step over the tensors of the plan, in one launch (see spl_adamw_step).  step: this step's number, from 1
+    on, or an int32 tensor [1] on the device that holds it when the step runs.  grad_scale: float32 [1] on the device that
+    the gradients are multiplied with (a clipping factor, the inverse of a loss scale); where it is not finite, nothing
+    is updated.  seed: of the rounding of 8-bit states."""
+    at, number = None, 1
+    if isinstance(step, torch.Tensor):
+        at = _ints(step, "step", 1)
+    else:
+        number = step
+    scale = None if grad_scale is None else _arg(grad_scale, "grad_scale", shape=(1,), dtype=torch.float32,
+                                                 device=False).data_ptr()
+    if not plan.chunks:
+        return
+    _here("the plan, step, grad_scale", stream, plan.table, step if at is not None else None, grad_scale)
+    _check("spl_adamw_step",
+           lib().spl_adamw_step(plan.table.data_ptr(), plan.chunks, plan.types, lr, betas[0], betas[1], eps, number, at,
+                                scale, seed & 0xFFFFFFFF, _on(stream)))

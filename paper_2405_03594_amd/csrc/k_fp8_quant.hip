@@ -1,0 +1,227 @@
+// Quantization to 8-bit floats with a power-of-two scale for each block of 128
+// (the format stands in spl.h), for gfx950.
+//
+// A workgroup of 256 threads takes 128 x 128 entries of X: thread (rg, cg) has rows
+// 8 rg .. 8 rg + 7 and columns 8 cg .. 8 cg + 7 in registers, so a row's 128
+// entries are 16 neighbouring lanes (their largest magnitude by four lane
+// moves) and a column's are 8 registers, 4 lanes and 4 waves.  Both results come
+// from one read.  Rows leave as 8 bytes a lane, 128 to a row; the transpose's codes
+// are converted two rows at a time, so that a thread's 8 rows of a column are 8
+// bytes, and go through LDS (their place in a row of 128 bytes turned by the
+// column) to leave as 16 bytes a lane.
+#include <type_traits>
+
+#include "spl_fp8.h"
+
+namespace spl {
+namespace {
+
+struct F32In {};
+template <class T>
+__device__ __forceinline__ float widen(const void* p, int64_t at) {
+  if constexpr (std::is_same<T, F32In>::value)
+    return static_cast<const float*>(p)[at];
+  else
+    return T::to_f32(static_cast<const uint16_t*>(p)[at]);
+}
+
+// 8 neighbours from an address of 16 bytes' alignment.
+template <class T>
+__device__ __forceinline__ void load8(const void* p, int64_t at, float (&v)[8]) {
+  if constexpr (std::is_same<T, F32In>::value) {
+    const f32x4* q = reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + at);
+    const f32x4 a = q[0], b = q[1];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = a[j], v[4 + j] = b[j];
+  } else {
+    const u32x4 a = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p) + at);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[2 * j] = T::to_f32(a[j] & 0xffffu), v[2 * j + 1] = T::to_f32(a[j] >> 16);
+  }
+}
+
+__device__ __forceinline__ uint32_t mag(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+template <class T, bool kRows, bool kCols, int kBlock>
+__global__ void __launch_bounds__(256) k_fp8_quantize(const Fp8QuantArgs a, const int wide) {
+  __shared__ __align__(16) uint8_t tile[kCols ? 128 * 128 : 16];
+  __shared__ uint32_t most[4][128];
+  const int tid = threadIdx.x, cg = tid & 15, rg = tid >> 4, wave = tid >> 6;
+  // my tile: rows [r0, rend) of X, which are block tb of a column of the transpose
+  int r0 = blockIdx.y * 128, rend = (int)a.rows;
+  const int tb = blockIdx.y;
+  if (a.starts) {
+    const Segment s = find_tile(a.starts, a.groups, (int)a.rows, 128, tb);
+    if (s.group < 0) return;
+    r0 = s.row, rend = s.end;
+  }
+  const int c0 = blockIdx.x * 128, z = blockIdx.z;
+  const int64_t base = (int64_t)z * a.rows * a.row_stride;
+  float v[8][8];
+  const int c = c0 + 8 * cg;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int r = r0 + 8 * rg + i;
+    const int64_t at = base + (int64_t)r * a.row_stride + c;
+    if (r < rend && wide && c + 8 <= a.cols) {
+      load8<T>(a.X, at, v[i]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] = r < rend && c + j < a.cols ? widen<T>(a.X, at + j) : 0.f;
+    }
+  }
+
+  uint32_t whole = 0;
+  if constexpr (kBlock == 128) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) whole = umax(whole, mag(v[i][j]));
+    whole = row16_max(whole);
+    if (cg == 0) most[0][rg] = whole;
+    __syncthreads();
+    whole = row16_max(most[0][cg]);
+    whole = fp8_scale_byte(whole);
+  }
+
+  if constexpr (kRows) {
+    uint8_t* codes = const_cast<uint8_t*>(a.out.codes) + z * a.out.code_stride;
+    uint8_t* scales = const_cast<uint8_t*>(a.out.scales) + z * a.out.scale_stride;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = r0 + 8 * rg + i;
+      uint32_t byte = whole;
+      if constexpr (kBlock == 1) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = umax(m, mag(v[i][j]));
+        byte = fp8_scale_byte(row16_max(m));
+      }
+      const float f = fp8_inverse(byte);
+      u32x2 q = {fp8_four(v[i][0] * f, v[i][1] * f, v[i][2] * f, v[i][3] * f),
+                 fp8_four(v[i][4] * f, v[i][5] * f, v[i][6] * f, v[i][7] * f)};
+      if (byte == 255) q = u32x2{0x7f7f7f7fu, 0x7f7f7f7fu};
+      if (r < rend) {
+        *reinterpret_cast<u32x2*>(codes + (int64_t)r * a.out.pitch + c) = q;
+        if (kBlock == 1 && cg == 0) scales[(int64_t)r * a.out.spitch + blockIdx.x] = (uint8_t)byte;
+      }
+    }
+    if (kBlock == 128 && tid == 0) scales[(int64_t)tb * a.out.spitch + blockIdx.x] = (uint8_t)whole;
+  }
+
+  if constexpr (kCols) {
+    uint8_t* codes = const_cast<uint8_t*>(a.out_t.codes) + z * a.out_t.code_stride;
+    uint8_t* scales = const_cast<uint8_t*>(a.out_t.scales) + z * a.out_t.scale_stride;
+    uint32_t byte[8];
+    if constexpr (kBlock == 1) {
+      uint32_t m[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        m[j] = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m[j] = umax(m[j], mag(v[i][j]));
+        m[j] = umax(m[j], (uint32_t)__shfl_xor((int)m[j], 16));
+        m[j] = umax(m[j], (uint32_t)__shfl_xor((int)m[j], 32));
+      }
+      if ((rg & 3) == 0) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) most[wave][8 * cg + j] = m[j];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int k = 8 * cg + j;
+        byte[j] = fp8_scale_byte(umax(umax(most[0][k], most[1][k]), umax(most[2][k], most[3][k])));
+        if (rg == 0 && c + j < a.cols) scales[(int64_t)(c + j) * a.out_t.spitch + tb] = (uint8_t)byte[j];
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) byte[j] = whole;
+      if (tid == 0) scales[(int64_t)blockIdx.x * a.out_t.spitch + tb] = (uint8_t)whole;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float f = fp8_inverse(byte[j]);
+      u32x2 q = {fp8_four(v[0][j] * f, v[1][j] * f, v[2][j] * f, v[3][j] * f),
+                 fp8_four(v[4][j] * f, v[5][j] * f, v[6][j] * f, v[7][j] * f)};
+      if (byte[j] == 255) q = u32x2{0x7f7f7f7fu, 0x7f7f7f7fu};
+      *reinterpret_cast<u32x2*>(tile + (8 * cg + j) * 128 + 8 * (rg ^ cg)) = q;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int k = 32 * q + (tid >> 3), u = 2 * (tid & 7);
+      const u32x2 lo = *reinterpret_cast<const u32x2*>(tile + k * 128 + 8 * (u ^ (k >> 3)));
+      const u32x2 hi = *reinterpret_cast<const u32x2*>(tile + k * 128 + 8 * ((u + 1) ^ (k >> 3)));
+      if (c0 + k < a.cols)
+        *reinterpret_cast<u32x4*>(codes + (int64_t)(c0 + k) * a.out_t.pitch + (int64_t)tb * 128 + 8 * u) =
+            u32x4{lo.x, lo.y, hi.x, hi.y};
+    }
+  }
+}
+
+template <class T>
+hipError_t quantize(const Fp8QuantArgs& a, hipStream_t s) {
+  const int64_t tiles = a.starts ? most_tiles(a.rows, a.groups, 128) : (a.rows + 127) / 128;
+  if (tiles < 1) return hipSuccess;
+  if (tiles > 65535) return hipErrorNotSupported;
+  const dim3 grid((unsigned)((a.cols + 127) / 128), (unsigned)tiles, (unsigned)a.count);
+  constexpr int E = std::is_same<T, F32In>::value ? 4 : 2;
+  const int wide = (reinterpret_cast<uintptr_t>(a.X) & 15) == 0 && a.row_stride * E % 16 == 0;
+  const bool r = a.out.codes, c = a.out_t.codes, big = (r ? a.out : a.out_t).shift == 7;
+#define SPL_Q(R, C, B) hipLaunchKernelGGL((k_fp8_quantize<T, R, C, B>), grid, dim3(256), 0, s, a, wide)
+  if (r && c) {
+    if (big) SPL_Q(true, true, 128); else SPL_Q(true, true, 1);
+  } else if (r) {
+    if (big) SPL_Q(true, false, 128); else SPL_Q(true, false, 1);
+  } else {
+    if (big) SPL_Q(false, true, 128); else SPL_Q(false, true, 1);
+  }
+#undef SPL_Q
+  return hipGetLastError();
+}
+
+// out = code * 2^e, one rounding: a thread an entry's group of 8.
+template <class T>
+__global__ void __launch_bounds__(256) k_fp8_dequantize(const Fp8View m, int64_t cols, int64_t groups, void* out) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= groups) return;
+  const int64_t per = (cols + 7) / 8, row = i / per, c = 8 * (i - row * per);
+  const int64_t z = row / m.rows, r = row - z * m.rows;
+  const u32x2 q = *reinterpret_cast<const u32x2*>(m.codes + z * m.code_stride + r * m.pitch + c);
+  const uint32_t byte = m.scales[z * m.scale_stride + (r >> m.shift) * m.spitch + c / 128];
+  const float f = byte == 255 ? __uint_as_float(0x7fc00000u) : (byte == 0 ? 0x1p-127f : __uint_as_float(byte << 23));
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    if (c + j >= cols) break;
+    const uint32_t w = j < 4 ? q.x : q.y;
+    const float v = __builtin_amdgcn_cvt_f32_fp8((int)(w >> (8 * (j & 3))), 0) * f;
+    const int64_t at = row * cols + c + j;
+    if constexpr (std::is_same<T, F32In>::value)
+      static_cast<float*>(out)[at] = v;
+    else
+      static_cast<uint16_t*>(out)[at] = T::from_f32(v);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_fp8_quantize(const Fp8QuantArgs& a, int32_t dtype, hipStream_t s) {
+  if (dtype == SPL_F32) return quantize<F32In>(a, s);
+  return dtype == SPL_BF16 ? quantize<Bf16>(a, s) : quantize<F16>(a, s);
+}
+
+hipError_t launch_fp8_dequantize(const Fp8View& m, int64_t cols, int64_t count, int32_t dtype, void* out, hipStream_t s) {
+  const int64_t groups = count * m.rows * ((cols + 7) / 8), blocks = (groups + 255) / 256;
+  if (blocks > ((int64_t)1 << 24) - 1) return hipErrorNotSupported;
+  const dim3 grid((unsigned)blocks);
+  if (dtype == SPL_F32)
+    hipLaunchKernelGGL(k_fp8_dequantize<F32In>, grid, dim3(256), 0, s, m, cols, groups, out);
+  else if (dtype == SPL_BF16)
+    hipLaunchKernelGGL(k_fp8_dequantize<Bf16>, grid, dim3(256), 0, s, m, cols, groups, out);
+  else
+    hipLaunchKernelGGL(k_fp8_dequantize<F16>, grid, dim3(256), 0, s, m, cols, groups, out);
+  return hipGetLastError();
+}
+
+}  // namespace spl

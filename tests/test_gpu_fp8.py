@@ -1,0 +1,379 @@
+"""8-bit float linears on the GPU: the format bit for bit, the products and their gradients, experts.
+
+Tolerances.  Codes and scales are exact.  A product of K terms x w with 16-bit results: half a unit of the result's last
+place, eps / 2 of it, and the sum's own error.  The 8-bit matrix instructions align the products that they add at once
+(at most 128 of a block) to the largest of them and drop what is below 2^-16 of it; that is at most 128 * 2^-16 of the
+block's largest product for each block, 2^-9 of it, so 2^-9 * sum over the blocks of max |x w| bounds it, and the fp32 sum
+over blocks adds 2^-24 a block.  With fp32 results the products are exact in bf16 instructions whose sums are fp32:
+(K + 2) * 2^-24 of sum |x w|."""
+import numpy as np
+import pytest
+import torch
+
+import _fp8_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+EPS = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11, torch.float32: 2.0 ** -24}
+FLOATS = [torch.bfloat16, torch.float16, torch.float32]
+
+
+def _spl():
+    import paper_2405_03594_amd as spl
+
+    return spl
+
+
+def _x(shape, dtype, seed, spread=1.0):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(shape, generator=g) * torch.exp(spread * torch.randn((*shape[:-1], 1), generator=g))
+    return x.to(dtype)
+
+
+def _np(t):
+    return t.detach().cpu().double().numpy()
+
+
+def _same(q, want, what):
+    codes, scale = want
+    assert np.array_equal(q.block_scales().cpu().numpy(), scale), what + " scales"
+    assert np.array_equal(q.codes.view(torch.uint8).cpu().numpy(), codes), what + " codes"
+
+
+def _bound(x, w, dtype):
+    """How far a product of the held values x [M, K], w [N, K] may be off, [M, N]."""
+    y = np.abs(x @ w.T)
+    K = x.shape[1]
+    if dtype == torch.float32:
+        return EPS[dtype] * ((K + 2) * (np.abs(x) @ np.abs(w).T)) + 1e-38
+    worst = np.zeros_like(y)
+    for k in range(0, K, 128):
+        a, b = np.abs(x[:, k:k + 128]), np.abs(w[:, k:k + 128])
+        worst += (a[:, None, :] * b[None, :, :]).max(-1) if a.shape[0] * b.shape[0] < 60000 else \
+            a.max(1)[:, None] * b.max(1)[None, :]
+    tiny = 2.0 ** -24 if dtype == torch.float16 else 1e-38
+    return EPS[dtype] * y * (1 + 2.0 ** -7) + 2.0 ** -9 * worst + K / 128 * 2.0 ** -24 * (np.abs(x) @ np.abs(w).T) + tiny
+
+
+def _near(got, want, bound, what=""):
+    bad = ~(np.abs(_np(got) - want) <= bound)
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.size}, worst {np.max(np.abs(_np(got) - want) / bound):.2f}"
+
+
+# ------------------------------------------------------------------------------------------------ the format
+
+
+SHAPES = [(1, 1), (1, 128), (1, 4096), (3, 129), (128, 128), (127, 255), (129, 7), (200, 300), (17, 1000), (257, 384)]
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("block", [1, 128])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_quantize(shape, block, dtype):
+    spl = _spl()
+    x = _x(shape, dtype, sum(shape) + block)
+    want, want_t = ref.quantize(_np(x), block), ref.quantize(_np(x).T, block)
+    dev = x.cuda()
+    _same(spl.quantize_fp8(dev, block), want, "rows")
+    _same(spl.quantize_fp8(dev, block, transposed=True), want_t, "transposed")
+    q, t = spl.quantize_fp8_both(dev, block)
+    _same(q, want, "both, rows")
+    _same(t, want_t, "both, transposed")
+    for dt in FLOATS:
+        back = spl.dequantize_fp8(q, dt)
+        held = torch.from_numpy(ref.held(*want, block, shape[1])).to(torch.float32).to(dt)
+        assert torch.equal(back.cpu(), held), dt
+
+
+def test_quantize_every_border():
+    """Every value next to and between codes, at scales from the smallest on, and both sides of 448 2^e."""
+    spl = _spl()
+    grid = ref.values(np.arange(127))
+    mid = (grid[1:] + grid[:-1]) / 2
+    rows = []
+    for e in (-127, -100, -10, 0, 3, 100):
+        v = np.concatenate([grid, mid, -mid, mid * (1 + 2.0 ** -12), mid * (1 - 2.0 ** -12)])
+        for part in np.array_split(v, 6):
+            row = np.zeros(128)
+            row[0] = 448.0
+            row[1:1 + len(part)] = part
+            rows.append(row * 2.0 ** e)
+        for top in (448.0, 448.5, 447.5, 464.0, 240.0, 1e-3):
+            row = np.linspace(-1, 1, 128) * top
+            rows.append(row * 2.0 ** e)
+    x = torch.from_numpy(np.array(rows)).float()
+    q = spl.quantize_fp8(x.cuda())
+    _same(q, ref.quantize(_np(x)), "borders")
+
+
+def test_quantize_special_values():
+    """Zeros of both signs, subnormals, the largest numbers, infinities and NaN, which take their block along."""
+    spl = _spl()
+    x = torch.randn(130, 300, generator=torch.Generator().manual_seed(1))
+    x[0] = 0.0
+    x[1, :128] = -0.0
+    x[2, :128] = 2.0 ** -149
+    x[3] = 3.3e38
+    x[4, 130] = float("inf")
+    x[5, 5] = float("nan")
+    x[6, 299] = -float("inf")
+    x[129, 0] = float("nan")
+    for block in (1, 128):
+        q, t = spl.quantize_fp8_both(x.cuda(), block)
+        for got, want in ((q, ref.quantize(_np(x), block)), (t, ref.quantize(_np(x).T, block))):
+            assert np.array_equal(got.block_scales().cpu().numpy(), want[1])
+            a, b = (ref.held(c, want[1], block, got.cols) for c in (got.codes.cpu().numpy(), want[0]))
+            assert np.array_equal(a, b, equal_nan=True)
+            assert np.array_equal(_np(spl.dequantize_fp8(got)), b.astype(np.float32).astype(np.float64), equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+def test_quantize_strided_and_counted(dtype):
+    """A slice of a wider product (odd strides and addresses too), and several matrices at once."""
+    spl = _spl()
+    wide = _x((70, 517), dtype, 3)
+    for c0, c1 in ((0, 256), (8, 300), (3, 400), (1, 2)):
+        x = wide[:, c0:c1]
+        q, t = spl.quantize_fp8_both(wide.cuda()[:, c0:c1])
+        _same(q, ref.quantize(_np(x)), "slice")
+        _same(t, ref.quantize(_np(x).T), "slice transposed")
+    many = _x((3, 140, 130), dtype, 4)
+    for block in (1, 128):
+        q, t = spl.quantize_fp8_both(many.cuda(), block)
+        for i in range(3):
+            for got, want in ((q, ref.quantize(_np(many[i]), block)), (t, ref.quantize(_np(many[i]).T, block))):
+                assert np.array_equal(got.codes[i].cpu().numpy(), want[0])
+                assert np.array_equal(got.block_scales()[i].cpu().numpy(), want[1])
+
+
+STARTS = [[0, 0, 5, 5, 130, 300], [0, 300], [10, 138, 138, 290], [0] * 70 + [1, 129, 129, 300], [300, 300, 300]]
+
+
+@pytest.mark.parametrize("starts", STARTS)
+def test_quantize_groups(starts):
+    spl = _spl()
+    x = _x((300, 150), torch.bfloat16, 5)
+    at = torch.tensor(starts, dtype=torch.int32).cuda()
+    q, t = spl.quantize_fp8_both(x.cuda(), starts=at)
+    alone = spl.quantize_fp8(x.cuda(), transposed=True, starts=at)
+    block = 0
+    want_q = ref.quantize(_np(x))
+    for a, b in zip(starts, starts[1:]):
+        n = b - a
+        if n == 0:
+            continue
+        want, scale = ref.quantize(_np(x[a:b]).T)
+        k = want.shape[1] // 128
+        for got in (t, alone):
+            assert np.array_equal(got.codes[:, 128 * block:128 * (block + k)].cpu().numpy(), want)
+            assert np.array_equal(got.block_scales()[:, block:block + k].cpu().numpy(), scale)
+        assert np.array_equal(q.codes[a:b].cpu().numpy(), want_q[0][a:b])
+        assert np.array_equal(q.block_scales()[a:b].cpu().numpy(), want_q[1][a:b])
+        block += k
+
+
+# ------------------------------------------------------------------------------------------------ products
+
+
+PRODUCTS = [(1, 1, 1), (1, 16, 128), (1, 100, 4096), (2, 257, 640), (5, 33, 130), (16, 64, 1000), (17, 1111, 257),
+            (33, 48, 2048), (64, 129, 384), (65, 130, 512), (100, 300, 896), (129, 257, 129), (256, 256, 256),
+            (300, 520, 700), (513, 1030, 1100), (1000, 77, 2100)]
+
+
+@pytest.mark.parametrize("dtype", FLOATS)
+@pytest.mark.parametrize("wblock", [1, 128])
+@pytest.mark.parametrize("mnk", PRODUCTS)
+def test_linear_codes(mnk, wblock, dtype):
+    spl = _spl()
+    M, N, K = mnk
+    x, w = _x((M, K), torch.float32, M + K), _x((N, K), torch.float32, N + 7)
+    q, wq = spl.quantize_fp8(x.cuda()), spl.quantize_fp8(w.cuda(), wblock)
+    hx, hw = ref.round_trip(_np(x)), ref.round_trip(_np(w), wblock)
+    y = spl.linear_fp8(q, wq, dtype=dtype)
+    assert y.dtype == dtype
+    _near(y, hx @ hw.T, _bound(hx, hw, dtype), f"{mnk}")
+    assert torch.equal(spl.linear_fp8(q, wq, dtype=dtype), y)      # the same bits again
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("mnk", PRODUCTS)
+def test_linear_rows(mnk, dtype):
+    """Activations in 16 bits: the product of what quantize_fp8 makes of them."""
+    spl = _spl()
+    M, N, K = mnk
+    x, w = _x((M, K), dtype, M + K), _x((N, K), torch.float32, N + 7)
+    wq = spl.quantize_fp8(w.cuda(), 128)
+    hx, hw = ref.round_trip(_np(x)), ref.round_trip(_np(w), 128)
+    y = spl.linear_fp8(x.cuda(), wq)
+    assert y.dtype == dtype
+    _near(y, hx @ hw.T, _bound(hx, hw, dtype), f"{mnk}")
+    wide = torch.zeros((M, K + 13), dtype=dtype)
+    wide[:, 5:5 + K] = x
+    y32 = spl.linear_fp8(wide.cuda()[:, 5:5 + K], wq, dtype=torch.float32)
+    _near(y32, hx @ hw.T, _bound(hx, hw, torch.float32), f"strided {mnk}")
+
+
+def test_linear_exact_and_poisoned():
+    """Small integers: every sum is exact in every type.  A NaN or an infinity reaches its rows and columns, no others."""
+    spl = _spl()
+    g = torch.Generator().manual_seed(2)
+    for M, N, K in ((3, 40, 300), (140, 200, 520), (300, 300, 1024)):
+        x = torch.randint(-2, 3, (M, K), generator=g).float()
+        w = torch.randint(-1, 2, (N, K), generator=g).float() * (torch.rand((N, K), generator=g) < 0.1)
+        want = (x.double() @ w.double().T)
+        assert want.abs().max() <= 256
+        for dt in FLOATS:
+            assert torch.equal(spl.linear_fp8(spl.quantize_fp8(x.cuda()), spl.quantize_fp8(w.cuda(), 128), dtype=dt).cpu(),
+                               want.to(dt)), (M, dt)
+        x[1, 5], w[30, K - 1] = float("nan"), float("inf")
+        for dt in FLOATS:
+            y = spl.linear_fp8(spl.quantize_fp8(x.cuda()), spl.quantize_fp8(w.cuda()), dtype=dt).cpu()
+            bad = torch.zeros((M, N), dtype=torch.bool)
+            bad[1], bad[:, 30] = True, True
+            assert torch.equal(torch.isnan(y), bad), (M, dt)
+
+
+@pytest.mark.parametrize("mnk", [(8, 130, 257), (300, 260, 520), (1000, 128, 384)])
+def test_linear_grad(mnk):
+    spl = _spl()
+    M, N, K = mnk
+    x, dy = _x((M, K), torch.bfloat16, 1), _x((M, N), torch.bfloat16, 2)
+    w = _x((N, K), torch.float32, 3)
+    _, wt = spl.quantize_fp8_both(w.cuda(), 128)
+    dx, dw = spl.linear_fp8_grad(dy.cuda(), x.cuda(), wt)
+    hdy, hw = ref.round_trip(_np(dy)), ref.round_trip(_np(w), 128)
+    _near(dx, hdy @ hw, _bound(hdy, hw.T, torch.bfloat16), "dX")
+    a, b = ref.round_trip(_np(dy).T), ref.round_trip(_np(x).T)
+    assert dw.dtype == torch.float32
+    _near(dw, a @ b.T, _bound(a, b, torch.float32), "dW")
+    half = spl.linear_fp8_grad(dy.cuda(), x.cuda(), wt, grad_dtype=torch.bfloat16)[1]
+    _near(half, a @ b.T, _bound(a, b, torch.bfloat16), "dW in bf16")
+
+
+def test_gradients_against_differences():
+    """The gradients of sum(dY * Y) along random directions, by central differences of the plain product: where x, dY
+    and w are codes already, quantizing changes nothing and the product is bilinear, so that differences are exact."""
+    spl = _spl()
+    g = torch.Generator().manual_seed(9)
+    M, N, K = 128, 64, 96
+    pick = lambda *s: torch.randint(-4, 5, s, generator=g).float()  # noqa: E731
+    x, w, dy = pick(M, K), pick(N, K), pick(M, N)
+    _, wt = spl.quantize_fp8_both(w.cuda(), 128)
+    dx, dw = spl.linear_fp8_grad(dy.bfloat16().cuda(), x.bfloat16().cuda(), wt)
+    loss = lambda a, b: float((dy.double() * (a.double() @ b.double().T)).sum())  # noqa: E731
+    for _ in range(4):
+        u, v = pick(M, K), pick(N, K)
+        along_x = (loss(x + u, w) - loss(x - u, w)) / 2
+        along_w = (loss(x, w + v) - loss(x, w - v)) / 2
+        # sums of up to 64 products of at most 16: exact in fp32, rounded to bf16 in dX (2^-9 each)
+        err = 2.0 ** -9 * float((dx.cpu().double().abs() * u.double().abs()).sum())
+        assert abs(float((dx.cpu().double() * u.double()).sum()) - along_x) <= err
+        assert float((dw.cpu().double() * v.double()).sum()) == along_w
+
+
+# ------------------------------------------------------------------------------------------------ experts
+
+
+GROUPED = [([0, 1], 1, 64, 128), ([0, 0, 3, 3, 4, 9, 20, 32, 32], 32, 150, 260), ([0, 16, 33, 33, 64], 64, 128, 512),
+           ([0, 90, 90, 91, 300, 420], 420, 270, 300), ([5, 40, 300], 310, 130, 384), ([0] * 66 + [2, 7, 50], 50, 40, 130),
+           ([0, 700, 1300], 1300, 600, 640)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("case", range(len(GROUPED)))
+def test_grouped(case, dtype):
+    spl = _spl()
+    starts, M, N, K = GROUPED[case]
+    E = len(starts) - 1
+    x, w = _x((M, K), torch.bfloat16, case), _x((E, N, K), torch.float32, case + 1)
+    at = torch.tensor(starts, dtype=torch.int32).cuda()
+    hx = ref.round_trip(_np(x))
+    for block in (1, 128):
+        wq = spl.quantize_fp8(w.cuda(), block)
+        for given in (x.cuda(), spl.quantize_fp8(x.cuda())):
+            out = torch.full((M, N), 7.0, dtype=dtype, device="cuda")
+            y = spl.linear_fp8_grouped(given, wq, at, out=out)
+            assert y is out
+            owned = torch.zeros(M, dtype=torch.bool)
+            for e, (a, b) in enumerate(zip(starts, starts[1:])):
+                if b > a:
+                    owned[a:b] = True
+                    hw = ref.round_trip(_np(w[e]), block)
+                    _near(y[a:b], hx[a:b] @ hw.T, _bound(hx[a:b], hw, dtype), f"expert {e}")
+            assert (y.cpu()[~owned] == 7.0).all()
+
+
+@pytest.mark.parametrize("case", range(len(GROUPED)))
+def test_grouped_grad(case):
+    spl = _spl()
+    starts, M, N, K = GROUPED[case]
+    E = len(starts) - 1
+    x, dy = _x((M, K), torch.bfloat16, 1), _x((M, N), torch.bfloat16, 2)
+    w = _x((E, N, K), torch.float32, 3)
+    at = torch.tensor(starts, dtype=torch.int32).cuda()
+    _, wt = spl.quantize_fp8_both(w.cuda(), 128)
+    for dt in (torch.float32, torch.bfloat16):
+        dx, dw = spl.linear_fp8_grouped_grad(dy.cuda(), x.cuda(), wt, at, grad_dtype=dt)
+        assert dw.shape == (E, N, K) and dw.dtype == dt
+        for e, (a, b) in enumerate(zip(starts, starts[1:])):
+            if b == a:
+                assert (dw[e] == 0).all()
+                continue
+            hdy, hw = ref.round_trip(_np(dy[a:b])), ref.round_trip(_np(w[e]), 128)
+            _near(dx[a:b], hdy @ hw, _bound(hdy, hw.T, torch.bfloat16), f"dX of {e}")
+            p, q = ref.round_trip(_np(dy[a:b]).T), ref.round_trip(_np(x[a:b]).T)
+            _near(dw[e], p @ q.T, _bound(p, q, dt), f"dW of {e}")
+
+
+def test_grouped_bad_starts():
+    """Starts out of range or falling: nothing past the tensors is touched, rows that no expert owns stay."""
+    spl = _spl()
+    M, N, K, E = 200, 64, 256, 4
+    x, w = _x((M, K), torch.bfloat16, 1).cuda(), _x((E, N, K), torch.float32, 2).cuda()
+    wq, hx = spl.quantize_fp8(w, 128), ref.round_trip(_np(x))
+    for starts, owned in (([-5, 10, 20, 1000, 2000], {0: (0, 10), 1: (10, 20), 2: (20, 200)}),
+                          ([50, 20, 30, 30, 40], {1: (20, 30), 3: (30, 40)}),
+                          ([2 ** 31 - 1] * 5, {}), ([-2 ** 31, -1, -1, -1, 0], {})):
+        at = torch.tensor(starts, dtype=torch.int32).cuda()
+        out = torch.full((M, N), 7.0, dtype=torch.bfloat16, device="cuda")
+        spl.linear_fp8_grouped(x, wq, at, out=out)
+        rest = torch.ones(M, dtype=torch.bool)
+        for e, (a, b) in owned.items():
+            hw = ref.round_trip(_np(w[e]), 128)
+            _near(out[a:b], hx[a:b] @ hw.T, _bound(hx[a:b], hw, torch.bfloat16), f"{starts} {e}")
+            rest[a:b] = False
+        assert (out.cpu()[rest] == 7.0).all()
+
+
+# ------------------------------------------------------------------------------------------------ as a program calls them
+
+
+def test_streams_and_graphs():
+    """The calls on another stream, and a captured graph replayed with new inputs between eager work."""
+    spl = _spl()
+    M, N, K = 40, 300, 520
+    w = _x((N, K), torch.float32, 1)
+    wq, wt = spl.quantize_fp8_both(w.cuda(), 128)
+    xs = [_x((M, K), torch.bfloat16, s).cuda() for s in range(4)]
+    dys = [_x((M, N), torch.bfloat16, 10 + s).cuda() for s in range(4)]
+    eager = [(spl.linear_fp8(x, wq), *spl.linear_fp8_grad(d, x, wt)) for x, d in zip(xs, dys)]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    other = [(spl.linear_fp8(x, wq, stream=side), *spl.linear_fp8_grad(d, x, wt, stream=side)) for x, d in zip(xs, dys)]
+    torch.cuda.current_stream().wait_stream(side)
+    for a, b in zip(eager, other):
+        assert all(torch.equal(p, q) for p, q in zip(a, b))
+    x, d = xs[0].clone(), dys[0].clone()
+    with torch.cuda.stream(side):
+        spl.linear_fp8(x, wq), spl.linear_fp8_grad(d, x, wt)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = (spl.linear_fp8(x, wq), *spl.linear_fp8_grad(d, x, wt))
+    for r in (1, 2, 3, 0, 2):
+        x.copy_(xs[r]), d.copy_(dys[r])
+        torch.mm(torch.ones(64, 64, device="cuda"), torch.ones(64, 64, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(got, eager[r])), r
