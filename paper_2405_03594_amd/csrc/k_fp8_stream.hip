@@ -144,6 +144,4 @@ hipError_t launch_fp8_stream(const Fp8GemmArgs& a, hipStream_t s) {
   return a.x16_dtype == SPL_BF16 ? by_type<Bf16>(a, wide, s) : by_type<F16>(a, wide, s);
 }
 
-hipError_t launch_fp8_gemm(const Fp8GemmArgs& a, hipStream_t s) { return launch_fp8_stream(a, s); }
-
 }  // namespace spl
