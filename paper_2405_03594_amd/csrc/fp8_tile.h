@@ -46,6 +46,10 @@ __device__ __forceinline__ f32x4 fp8_mfma_wide(const Wide8& a, const Wide8& b, f
 
 // The part of a call that a workgroup computes: rows [m0, mend) of X, the
 // blocks [k0, k1) of the sum, which matrix of W, which result.
+struct F32Out {
+  static constexpr int32_t code = SPL_F32;
+};
+
 struct Fp8Part {
   int m0, mend;
   int k0, k1;
@@ -98,6 +102,17 @@ __device__ __forceinline__ void fp8_store4(const Fp8GemmArgs& a, int64_t row, in
       if (n + 2 < a.N) y[2] = (uint16_t)h2;
       if (n + 3 < a.N) y[3] = (uint16_t)h3;
     }
+  }
+}
+
+// Two results of 16 bits, the first in the low half.
+template <class T>
+__device__ __forceinline__ uint32_t fp8_pack2(float a, float b) {
+  if constexpr (T::code == SPL_BF16) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+  } else {
+    return (uint32_t)T::from_f32(a) | ((uint32_t)T::from_f32(b) << 16);
   }
 }
 

@@ -55,9 +55,11 @@ __device__ __forceinline__ void settle(f32x4 (&acc)[FN][FM]) {
 
 constexpr int tile_waves(int FN, int FM) { return FN * FM > 32 ? 1 : 2; }   // a SIMD's waves that the registers are held to
 
-template <int FN, int FM, int WN, int WM, bool kExact>
+// T: of the results; fp32 ones are summed by bf16 instructions.
+template <class T, int FN, int FM, int WN, int WM>
 __global__ void __launch_bounds__(64 * WN * WM, tile_waves(FN, FM)) k_fp8_tile(const Fp8GemmArgs a, const int tn,
                                                                                const int tm) {
+  constexpr bool kExact = T::code == SPL_F32;
   constexpr int NW = WN * WM, BN = 16 * FN * WN, BM = 16 * FM * WM;
   constexpr int PW = BN / 8 / NW, PX = BM / 8 / NW;   // requests of 8 rows a wave and stage
   constexpr int SZ = (BN + BM) * 128, RQ = PW + PX;
@@ -135,14 +137,13 @@ __global__ void __launch_bounds__(64 * WN * WM, tile_waves(FN, FM)) k_fp8_tile(c
     }
   };
   const uint32_t sbase = lds_off(dsm) + 2 * SZ + 4 * fr;
-  uint32_t sc[FN + FM];
-  auto read_scales = [&](int st) {                   // 0 past the last stage, whose codes are zeros
+  uint32_t sc[FN + FM], coming[FN + FM];              // the scale bytes of this stage, of the next one
+  auto read_scales = [&](int st) {
     const int b = (p.k0 & 3) + st;
     const uint32_t at = sbase + (uint32_t)(((b >> 2) & 3) * (BN + BM) * 4 + (b & 3));
-    const uint32_t mask = st < nst ? 255u : 0u;
 #pragma unroll
     for (int i = 0; i < FN + FM; ++i)
-      sc[i] = lds_load1(at + 4 * (i < FN ? 16 * (FN * wn + i) : BN + 16 * (FM * wm + i - FN))) & mask;
+      coming[i] = lds_load1(at + 4 * (i < FN ? 16 * (FN * wn + i) : BN + 16 * (FM * wm + i - FN)));
   };
 
   // a row's pieces fg and fg + 4, in the first stage buffer and in the second
@@ -201,17 +202,21 @@ __global__ void __launch_bounds__(64 * WN * WM, tile_waves(FN, FM)) k_fp8_tile(c
     request_scales(1);
     wait_vm0();
     tile_barrier();
+    read_scales(0);
     read_a(A[0], 0, 0);
 #pragma unroll
     for (int j = 0; j < FM; ++j) read_b(j, 0);
     auto stage = [&](int st, auto x) {
       constexpr int buf = decltype(x)::value;
-      read_scales(st);
+      const uint32_t mask = st < nst ? 255u : 0u;    // the stage past the last has codes of zero, and 0 as its scale
+#pragma unroll
+      for (int i = 0; i < FN + FM; ++i) sc[i] = coming[i] & mask;
       widen_b();
 #pragma unroll
       for (int step = 0; step < FN / 2 - 1; ++step) {
         __builtin_amdgcn_sched_barrier(0);
         read_a(A[(step + 1) & 1], step + 1, buf);
+        if (step == FN / 2 - 2) read_scales(st + 1);
         __builtin_amdgcn_sched_barrier(0);
         widen_a(A[step & 1], step);
 #pragma unroll
@@ -247,21 +252,56 @@ __global__ void __launch_bounds__(64 * WN * WM, tile_waves(FN, FM)) k_fp8_tile(c
     wait_vm0();                                      // no request outlives the workgroup's LDS
   }
 
+  // Results: 16 rows of the wave's at a time through LDS, so that a row's leave as 16-byte pieces.  A lane has columns
+  // 4 fg .. 4 fg + 3 of each fragment, row fr; piece c of a row sits at c ^ row.
+  constexpr int E = kExact ? 4 : 2, CH = 16 * FN * E / 16;   // bytes of a result, pieces of a row
+  tile_barrier();                                    // the other waves have read their last stage
+  unsigned char* out = dsm + wave * (2 * 16 * CH * 16);
+  const int64_t nw = n0 + 16 * FN * wn;
+  const bool whole = nw + 16 * FN <= a.N && (a.N * E) % 16 == 0;
 #pragma unroll
   for (int j = 0; j < FM; ++j) {
-    const int m = 16 * (FM * wm + j) + fr;
-    if (m >= Mr) continue;
+    unsigned char* half = out + (j & 1) * (16 * CH * 16);
 #pragma unroll
-    for (int i = 0; i < FN; ++i)
-      fp8_store4(a, p.m0 + m, n0 + 16 * (FN * wn + i) + 4 * fg, acc[i][j], p.y);
+    for (int i = 0; i < FN; ++i) {
+      const f32x4 v = acc[i][j];
+      if constexpr (kExact) {
+        *reinterpret_cast<f32x4*>(half + fr * (CH * 16) + 16 * ((4 * i + fg) ^ (fr & (CH - 1)))) = v;
+      } else {
+        *reinterpret_cast<u32x2*>(half + fr * (CH * 16) + 16 * ((2 * i + (fg >> 1)) ^ (fr & (CH - 1))) + 8 * (fg & 1)) =
+            u32x2{fp8_pack2<T>(v[0], v[1]), fp8_pack2<T>(v[2], v[3])};
+      }
+    }
+    wave_lds_sync();
+#pragma unroll
+    for (int q = 0; q < 16 * CH / 64; ++q) {
+      const int e = 64 * q + lane, row = e / CH, c = e % CH;
+      const u32x4 v = *reinterpret_cast<const u32x4*>(half + row * (CH * 16) + 16 * (c ^ (row & (CH - 1))));
+      const int m = 16 * (FM * wm + j) + row;
+      if (m >= Mr) continue;
+      const int64_t n = nw + c * (16 / E), at = p.y + (p.m0 + m) * a.N + n;
+      unsigned char* y = static_cast<unsigned char*>(a.y) + at * E;
+      if (whole) {
+        *reinterpret_cast<u32x4*>(y) = v;
+      } else {
+#pragma unroll
+        for (int k = 0; k < 16 / E; ++k) {
+          if (n + k >= a.N) break;
+          if constexpr (kExact)
+            reinterpret_cast<uint32_t*>(y)[k] = v[k];
+          else
+            reinterpret_cast<uint16_t*>(y)[k] = (uint16_t)(v[k >> 1] >> (16 * (k & 1)));
+        }
+      }
+    }
   }
 }
 
-template <int FN, int FM, int WN, int WM, bool kExact>
+template <class T, int FN, int FM, int WN, int WM>
 hipError_t launch_tile(const Fp8GemmArgs& a, hipStream_t s) {
   constexpr int BN = 16 * FN * WN, BM = 16 * FM * WM, LDS = 2 * (BN + BM) * 128 + 4 * (BN + BM) * 4;
   static PerDeviceFlag done;
-  auto* kernel = k_fp8_tile<FN, FM, WN, WM, kExact>;
+  auto* kernel = k_fp8_tile<T, FN, FM, WN, WM>;
   const hipError_t e = allow_lds_once(done, kernel, LDS);
   if (e != hipSuccess) return e;
   const int64_t tn = (a.N + BN - 1) / BN, tm = fp8_row_tiles(a, BM);
@@ -271,20 +311,21 @@ hipError_t launch_tile(const Fp8GemmArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <bool kExact>
+template <class T>
 hipError_t by_size(const Fp8GemmArgs& a, hipStream_t s) {
-  if constexpr (!kExact) {
+  if constexpr (T::code != SPL_F32) {
     const int64_t big = ((a.N + 255) / 256) * fp8_row_tiles(a, 256) * (a.mode == kFp8Sum ? a.groups : 1);
-    if (big >= 128) return launch_tile<8, 8, 2, 2, false>(a, s);
+    if (big >= 128) return launch_tile<T, 8, 8, 2, 2>(a, s);
   }
-  return launch_tile<4, 4, 2, 2, kExact>(a, s);
+  return launch_tile<T, 4, 4, 2, 2>(a, s);
 }
 
 }  // namespace
 
 hipError_t launch_fp8_gemm(const Fp8GemmArgs& a, hipStream_t s) {
   if (a.x16 || a.M <= 64) return launch_fp8_stream(a, s);
-  return a.dtype == SPL_F32 ? by_size<true>(a, s) : by_size<false>(a, s);
+  if (a.dtype == SPL_F32) return by_size<F32Out>(a, s);
+  return a.dtype == SPL_BF16 ? by_size<Bf16>(a, s) : by_size<F16>(a, s);
 }
 
 }  // namespace spl
