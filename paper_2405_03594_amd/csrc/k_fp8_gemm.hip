@@ -8,6 +8,8 @@
 // read from LDS, one a quadrant, into the registers that the quadrant before has left: By, A1, then A0 and By of the
 // next stage.  The one barrier of a stage stands before its third quadrant: the buffer has been read by then and is
 // refilled with the stage after the next, and the next stage's has been waited for.
+#include <math.h>
+
 #include <type_traits>
 
 #include "fp8_tile.h"
@@ -20,7 +22,12 @@ constexpr uint32_t kOob = 0x80000000u;
 __device__ __forceinline__ void dma16(__amdgpu_buffer_rsrc_t src, unsigned char* dst, uint32_t voff, int soff) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (__attribute__((address_space(3))) void*)dst, 16, voff, soff, 0, 0);
 }
-__device__ __forceinline__ void wait_vm0() { __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8)); }
+// At most N of this wave's vector-memory requests remain, and no LDS read.
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+  static_assert(N >= 0 && N < 64, "vmcnt");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | ((N >> 4) << 14));
+}
 __device__ __forceinline__ void tile_barrier() {
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_barrier();
@@ -30,10 +37,6 @@ __device__ __forceinline__ void tile_barrier() {
 struct alignas(32) Codes32 {
   u32x4 lo, hi;
 };
-
-__device__ __forceinline__ uint32_t lds_load1(uint32_t addr) {
-  return *reinterpret_cast<const __attribute__((address_space(3))) uint8_t*>((uintptr_t)addr);
-}
 
 // The same instruction with its sums in accumulator registers, which the compiler does not keep there by itself when
 // they are all of them (it moves and spills).  What it cannot know of this text is kept by hand: two wait states after
@@ -55,10 +58,9 @@ __device__ __forceinline__ void settle(f32x4 (&acc)[FN][FM]) {
 
 constexpr int tile_waves(int FN, int FM) { return FN * FM > 32 ? 1 : 2; }   // a SIMD's waves that the registers are held to
 
-// T: of the results; fp32 ones are summed by bf16 instructions.
-template <class T, int FN, int FM, int WN, int WM>
-__global__ void __launch_bounds__(64 * WN * WM, tile_waves(FN, FM)) k_fp8_tile(const Fp8GemmArgs a, const int tn,
-                                                                               const int tm) {
+// Tile w of tn x tm (columns from nbase on).  T: of the results; fp32 ones are summed by bf16 instructions.
+template <class T, int FN, int FM, int WN, int WM, int R>
+__device__ __forceinline__ void tile_body(const Fp8GemmArgs& a, int w, int tn, int tm, int64_t nbase) {
   constexpr bool kExact = T::code == SPL_F32;
   constexpr int NW = WN * WM, BN = 16 * FN * WN, BM = 16 * FM * WM;
   constexpr int PW = BN / 8 / NW, PX = BM / 8 / NW;   // requests of 8 rows a wave and stage
@@ -68,7 +70,7 @@ __global__ void __launch_bounds__(64 * WN * WM, tile_waves(FN, FM)) k_fp8_tile(c
   // the XCDs (blockIdx % 8) take contiguous runs of tiles, four row tiles to a column of column tiles
   int bn, bm;
   {
-    const int total = tm * tn, w = (int)blockIdx.x;
+    const int total = tm * tn;
     const int q = total / 8, r = total % 8, x = w % 8, i = w / 8;
     const int t = x * q + (x < r ? x : r) + i;
     const int gsz = 4 * tn, grp = t / gsz, h = tm - grp * 4 < 4 ? tm - grp * 4 : 4, in = t - grp * gsz;
@@ -79,7 +81,7 @@ __global__ void __launch_bounds__(64 * WN * WM, tile_waves(FN, FM)) k_fp8_tile(c
   if (p.none) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int wn = wave % WN, wm = wave / WN, fr = lane & 15, fg = lane >> 4;
-  const int64_t n0 = (int64_t)bn * BN;
+  const int64_t n0 = nbase + (int64_t)bn * BN;
   const int Nr = (int)(a.N - n0 < BN ? a.N - n0 : BN), Mr = p.mend - p.m0 < BM ? p.mend - p.m0 : BM;
   const int nst = p.k1 - p.k0;
 
@@ -97,8 +99,8 @@ __global__ void __launch_bounds__(64 * WN * WM, tile_waves(FN, FM)) k_fp8_tile(c
     const int row = 8 * (PX * wave + i) + (lane >> 3);
     xoff[i] = row < Mr ? (uint32_t)row * (uint32_t)a.x.pitch + piece : kOob;
   }
-  // Request i of a stage; stages past the last read through empty descriptors: zeros.
-  auto request = [&](int i, int st, int buf) {
+  // Request i of a stage, into stage buffer `buf`; stages past the last read through empty descriptors: zeros.
+  auto request_codes = [&](int i, int st, int buf) {
     const bool w = i < PW;
     const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<unsigned char*>(w ? wbase : xbase), (short)0, st < nst ? (w ? Nr * a.w.pitch : Mr * a.x.pitch) : 0, 0x00020000);
@@ -109,59 +111,63 @@ __global__ void __launch_bounds__(64 * WN * WM, tile_waves(FN, FM)) k_fp8_tile(c
       dma16(r, dsm + buf * SZ + BN * 128 + (PX * wave + i - PW) * 1024, xoff[i - PW], at);
   };
   // The rows' scale bytes, four stages a word, in a ring of four words a row behind the stage buffers: 64 rows a request.
-  constexpr int SQ = (BN + BM) / 64 / NW;
-  static_assert((BN + BM) % (64 * NW) == 0 && BN % 64 == 0, "whole requests");
+  constexpr int SW = (BN + BM) / 64, SQ = (SW + NW - 1) / NW;
+  static_assert(BM % 64 == 0 && BN % 64 == 0, "whole requests");
+  const auto scale_request = [&](int i) { return NW * i + wave < SW ? NW * i + wave : SW - 1; };   // the last one again
   const uint8_t* wsc = a.w.scales + p.w_scales + (n0 >> a.w.shift) * a.w.spitch;
   const uint8_t* xsc = a.x.scales + ((int64_t)p.m0 >> a.x.shift) * a.x.spitch;
   uint32_t soff[SQ];
 #pragma unroll
   for (int i = 0; i < SQ; ++i) {
-    const int q = NW * i + wave, row = 64 * (q < BN / 64 ? q : q - BN / 64) + lane;
+    const int q = scale_request(i), row = 64 * (q < BN / 64 ? q : q - BN / 64) + lane;
     if (q < BN / 64)
       soff[i] = row < Nr ? (uint32_t)(row >> a.w.shift) * (uint32_t)a.w.spitch : kOob;
     else
       soff[i] = row < Mr ? (uint32_t)(((p.m0 + row) >> a.x.shift) - (p.m0 >> a.x.shift)) * (uint32_t)a.x.spitch : kOob;
   }
-  const int kal = p.k0 & ~3;
-  auto request_scales = [&](int word) {              // the word'th from the one that k0 is in
-    const int at = kal + 4 * word;
-#pragma unroll
-    for (int i = 0; i < SQ; ++i) {
-      const int q = NW * i + wave;
-      const bool w = q < BN / 64;
-      const int rows = w ? ((Nr - 1) >> a.w.shift) + 1 : ((p.m0 + Mr - 1) >> a.x.shift) - (p.m0 >> a.x.shift) + 1;
-      const int bytes = at < a.w.spitch ? rows * (w ? a.w.spitch : a.x.spitch) : 0;   // words past a row: zeros
-      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(w ? wsc : xsc), (short)0, bytes, 0x00020000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          r, (__attribute__((address_space(3))) void*)(dsm + 2 * SZ + (word & 3) * (BN + BM) * 4 + 256 * q), 4, soff[i], at, 0, 0);
-    }
+  const int lead = p.k0 & 3;                         // stages from a word's begin to mine
+  auto request_scales = [&](int i, int st) {         // the word of stage st, which four stages request (the same bytes)
+    const int word = (lead + st) >> 2, at = (p.k0 - lead) + 4 * word;
+    const int q = scale_request(i);
+    const bool w = q < BN / 64;
+    const int rows = w ? ((Nr - 1) >> a.w.shift) + 1 : ((p.m0 + Mr - 1) >> a.x.shift) - (p.m0 >> a.x.shift) + 1;
+    const int bytes = at < a.w.spitch ? rows * (w ? a.w.spitch : a.x.spitch) : 0;   // words past a row: zeros
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(w ? wsc : xsc), (short)0, bytes, 0x00020000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        r, (__attribute__((address_space(3))) void*)(dsm + R * SZ + (word & 3) * (BN + BM) * 4 + 256 * q), 4, soff[i], at, 0, 0);
   };
-  const uint32_t sbase = lds_off(dsm) + 2 * SZ + 4 * fr;
-  uint32_t sc[FN + FM], coming[FN + FM];              // the scale bytes of this stage, of the next one
-  auto read_scales = [&](int st) {
-    const int b = (p.k0 & 3) + st;
-    const uint32_t at = sbase + (uint32_t)(((b >> 2) & 3) * (BN + BM) * 4 + (b & 3));
-#pragma unroll
-    for (int i = 0; i < FN + FM; ++i)
-      coming[i] = lds_load1(at + 4 * (i < FN ? 16 * (FN * wn + i) : BN + 16 * (FM * wm + i - FN)));
+  constexpr int G = RQ + SQ;                         // a stage's requests
+  auto request = [&](int i, int st, int buf) {
+    if (i < SQ)
+      request_scales(i, st);
+    else
+      request_codes(i - SQ, st, buf);
+  };
+  // My rows' scales, of W's fragments, then of X's: the word as it is read, then shifted so that the stage's byte is the
+  // low one (the matrix instruction looks at no other).
+  uint32_t sc[FN + FM];
+  const uint32_t wscale = lds_off(dsm) + R * SZ + 4 * (16 * FN * wn + fr);
+  const uint32_t xscale = lds_off(dsm) + R * SZ + 4 * (BN + 16 * FM * wm + fr);
+  auto scale_place = [&](int st) { return (uint32_t)((((lead + st) >> 2) & 3) * (BN + BM) * 4); };
+  auto read_scale = [&](int i, uint32_t place) {
+    sc[i] = i < FN ? lds_load4(wscale + place + 64 * i) : lds_load4(xscale + place + 64 * (i - FN));
   };
 
-  // a row's pieces fg and fg + 4, in the first stage buffer and in the second
+  // a row's pieces fg and fg + 4 in a stage buffer
   const uint32_t turn = 16 * (uint32_t)(fg ^ (fr & 7));
   const uint32_t arow = lds_off(dsm) + 128 * (16 * FN * wn + fr), brow = lds_off(dsm) + BN * 128 + 128 * (16 * FM * wm + fr);
-  const uint32_t al[2] = {arow + turn, arow + turn + SZ}, ah[2] = {arow + (turn ^ 64u), arow + (turn ^ 64u) + SZ};
-  const uint32_t bl[2] = {brow + turn, brow + turn + SZ}, bh[2] = {brow + (turn ^ 64u), brow + (turn ^ 64u) + SZ};
   Codes32 A[2][2], B[FM];
-  auto read_a = [&](Codes32 (&d)[2], int step, int buf) {
+  auto read_a = [&](Codes32 (&d)[2], int step, uint32_t off) {
+    const uint32_t lo = arow + turn + off, hi = arow + (turn ^ 64u) + off;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      d[i].lo = lds_load16(al[buf] + 2048 * (2 * step + i));
-      d[i].hi = lds_load16(ah[buf] + 2048 * (2 * step + i));
+      d[i].lo = lds_load16(lo + 2048 * (2 * step + i));
+      d[i].hi = lds_load16(hi + 2048 * (2 * step + i));
     }
   };
-  auto read_b = [&](int j, int buf) {
-    B[j].lo = lds_load16(bl[buf] + 2048 * j);
-    B[j].hi = lds_load16(bh[buf] + 2048 * j);
+  auto read_b = [&](int j, uint32_t off) {
+    B[j].lo = lds_load16(brow + turn + off + 2048 * j);
+    B[j].hi = lds_load16(brow + (turn ^ 64u) + off + 2048 * j);
   };
   f32x4 acc[FN][FM];
 #pragma unroll
@@ -169,17 +175,17 @@ __global__ void __launch_bounds__(64 * WN * WM, tile_waves(FN, FM)) k_fp8_tile(c
 #pragma unroll
     for (int j = 0; j < FM; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   Wide8 aw[kExact ? 2 : 1], bw[kExact ? FM : 1];
-  auto widen_a = [&](const Codes32 (&w)[2], int step) {
-    if constexpr (kExact) {
+  // the stage's scales of two fragments of W, of a fragment of X (and, for fp32 results, their values)
+  auto ready_a = [&](const Codes32 (&w)[2], int step, int shift) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) aw[i] = fp8_widen32(w[i].lo, w[i].hi, sc[2 * step + i]);
+    for (int i = 0; i < 2; ++i) {
+      sc[2 * step + i] >>= shift;
+      if constexpr (kExact) aw[i] = fp8_widen32(w[i].lo, w[i].hi, sc[2 * step + i] & 255u);
     }
   };
-  auto widen_b = [&]() {
-    if constexpr (kExact) {
-#pragma unroll
-      for (int j = 0; j < FM; ++j) bw[j] = fp8_widen32(B[j].lo, B[j].hi, sc[FN + j]);
-    }
+  auto ready_b = [&](int j, int shift) {
+    sc[FN + j] >>= shift;
+    if constexpr (kExact) bw[j] = fp8_widen32(B[j].lo, B[j].hi, sc[FN + j] & 255u);
   };
   // two fragments of W by fragment j of X
   auto multiply = [&](const Codes32 (&w)[2], int step, int j) {
@@ -195,61 +201,72 @@ __global__ void __launch_bounds__(64 * WN * WM, tile_waves(FN, FM)) k_fp8_tile(c
     }
   };
 
+  // Stage st + R - 1's requests: the first half behind the barrier of stage st - 1, which frees their buffer, the second
+  // in the first step of stage st.  At the barrier of stage st those up to stage st + 1 have to be there.
+  constexpr int H = G / 2;
+  static_assert(R >= 2 && R <= 7 && (R - 2) * G + H < 64, "counted waits; a ring of four words of four stages");
   if (nst > 0) {
 #pragma unroll
-    for (int i = 0; i < RQ + RQ / 2; ++i) request(i % RQ, i / RQ, i / RQ);
-    request_scales(0);
-    request_scales(1);
-    wait_vm0();
+    for (int i = 0; i < (R - 1) * G + H; ++i) request(i % G, i / G, i / G);
+    wait_vm<(R - 2) * G + H>();
     tile_barrier();
-    read_scales(0);
+#pragma unroll
+    for (int i = 0; i < FN + FM; ++i) read_scale(i, scale_place(0));
     read_a(A[0], 0, 0);
 #pragma unroll
     for (int j = 0; j < FM; ++j) read_b(j, 0);
-    auto stage = [&](int st, auto x) {
-      constexpr int buf = decltype(x)::value;
-      const uint32_t mask = st < nst ? 255u : 0u;    // the stage past the last has codes of zero, and 0 as its scale
-#pragma unroll
-      for (int i = 0; i < FN + FM; ++i) sc[i] = coming[i] & mask;
-      widen_b();
+    __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 0) | (3 << 14));   // else the loop would wait here for its own later reads
+    int buf = 0;
+#pragma unroll 1
+    for (int st = 0; st < nst; ++st) {
+      const uint32_t here = (uint32_t)(buf * SZ);
+      const int shift = 8 * ((lead + st) & 3);
+      const int after = buf + 1 == R ? 0 : buf + 1, last = buf == 0 ? R - 1 : buf - 1;
 #pragma unroll
       for (int step = 0; step < FN / 2 - 1; ++step) {
         __builtin_amdgcn_sched_barrier(0);
-        read_a(A[(step + 1) & 1], step + 1, buf);
-        if (step == FN / 2 - 2) read_scales(st + 1);
-        __builtin_amdgcn_sched_barrier(0);
-        widen_a(A[step & 1], step);
+        ready_a(A[step & 1], step, shift);
 #pragma unroll
         for (int j = 0; j < FM; ++j) {
+          if (step == 0) ready_b(j, shift);
           multiply(A[step & 1], step, j);
-          if (step == 0) {                           // the second half of stage st + 1's
+          if (j == 0) {                              // behind the first product, which has waited long enough
+            __builtin_amdgcn_sched_barrier(0);
+            read_a(A[(step + 1) & 1], step + 1, here);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          if (step == 0) {
 #pragma unroll
-            for (int i = RQ * (FM + j) / (2 * FM); i < RQ * (FM + j + 1) / (2 * FM); ++i) request(i, st + 1, 1 - buf);
+            for (int i = H + (G - H) * j / FM; i < H + (G - H) * (j + 1) / FM; ++i) request(i, st + R - 1, last);
           }
         }
       }
       __builtin_amdgcn_sched_barrier(0);
-      __builtin_amdgcn_s_waitcnt(0);                 // my reads of this buffer, my requests for the next
+      wait_vm<(R - 2) * G>();                        // and for my reads of this buffer
       tile_barrier();
-      if (buf == 0) request_scales(st / 4 + 2);      // (twice the same: a branch here would cost more)
-      read_a(A[0], 0, 1 - buf);
-      __builtin_amdgcn_sched_barrier(0);
-      widen_a(A[1], FN / 2 - 1);
+      const uint32_t place = scale_place(st + 1);
+      ready_a(A[1], FN / 2 - 1, shift);
 #pragma unroll
       for (int j = 0; j < FM; ++j) {
         multiply(A[1], FN / 2 - 1, j);
-        read_b(j, 1 - buf);
+        if (j == 0) {
+          __builtin_amdgcn_sched_barrier(0);
+          read_a(A[0], 0, (uint32_t)(after * SZ));
 #pragma unroll
-        for (int i = RQ * j / (2 * FM); i < RQ * (j + 1) / (2 * FM); ++i) request(i, st + 2, buf);
+          for (int i = 0; i < FN - 2; ++i) read_scale(i, place);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        read_b(j, (uint32_t)(after * SZ));
+        read_scale(FN + j, place);
+        if (j == FM - 1) read_scale(FN - 2, place), read_scale(FN - 1, place);
+#pragma unroll
+        for (int i = H * j / FM; i < H * (j + 1) / FM; ++i) request(i, st + R, buf);
       }
       __builtin_amdgcn_sched_barrier(0);
-    };
-    for (int st = 0; st < nst; st += 2) {            // the stage past an odd number's last multiplies zeros
-      stage(st, std::integral_constant<int, 0>{});
-      stage(st + 1, std::integral_constant<int, 1>{});
+      buf = after;
     }
     if constexpr (FN * FM > 32) settle(acc);
-    wait_vm0();                                      // no request outlives the workgroup's LDS
+    wait_vm<0>();                                    // no request outlives the workgroup's LDS
   }
 
   // Results: 16 rows of the wave's at a time through LDS, so that a row's leave as 16-byte pieces.  A lane has columns
@@ -258,7 +275,6 @@ __global__ void __launch_bounds__(64 * WN * WM, tile_waves(FN, FM)) k_fp8_tile(c
   tile_barrier();                                    // the other waves have read their last stage
   unsigned char* out = dsm + wave * (2 * 16 * CH * 16);
   const int64_t nw = n0 + 16 * FN * wn;
-  const bool whole = nw + 16 * FN <= a.N && (a.N * E) % 16 == 0;
 #pragma unroll
   for (int j = 0; j < FM; ++j) {
     unsigned char* half = out + (j & 1) * (16 * CH * 16);
@@ -273,51 +289,129 @@ __global__ void __launch_bounds__(64 * WN * WM, tile_waves(FN, FM)) k_fp8_tile(c
       }
     }
     wave_lds_sync();
+    const int m = 16 * (FM * wm + j);
+    unsigned char* y = static_cast<unsigned char*>(a.y) + (p.y + (p.m0 + m) * a.N + nw) * E;
 #pragma unroll
     for (int q = 0; q < 16 * CH / 64; ++q) {
       const int e = 64 * q + lane, row = e / CH, c = e % CH;
-      const u32x4 v = *reinterpret_cast<const u32x4*>(half + row * (CH * 16) + 16 * (c ^ (row & (CH - 1))));
-      const int m = 16 * (FM * wm + j) + row;
-      if (m >= Mr) continue;
-      const int64_t n = nw + c * (16 / E), at = p.y + (p.m0 + m) * a.N + n;
-      unsigned char* y = static_cast<unsigned char*>(a.y) + at * E;
-      if (whole) {
-        *reinterpret_cast<u32x4*>(y) = v;
+      const unsigned char* from = half + row * (CH * 16) + 16 * (c ^ (row & (CH - 1)));
+      unsigned char* to = y + (int64_t)row * a.N * E + 16 * c;
+      const int have = m + row < Mr ? (int)(a.N - nw < 16 * FN ? a.N - nw : 16 * FN) - c * (16 / E) : 0;
+      if (have >= 16 / E) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(from);
+        __builtin_memcpy(to, &v, 16);                // (rows of any length: their starts have E bytes' alignment)
       } else {
-#pragma unroll
-        for (int k = 0; k < 16 / E; ++k) {
-          if (n + k >= a.N) break;
-          if constexpr (kExact)
-            reinterpret_cast<uint32_t*>(y)[k] = v[k];
-          else
-            reinterpret_cast<uint16_t*>(y)[k] = (uint16_t)(v[k >> 1] >> (16 * (k & 1)));
-        }
+#pragma unroll 1
+        for (int k = 0; k < have; ++k) __builtin_memcpy(to + E * k, from + E * k, E);
       }
     }
   }
 }
 
-template <class T, int FN, int FM, int WN, int WM>
+template <class T, int FN, int FM, int WN, int WM, int R>
+__global__ void __launch_bounds__(64 * WN * WM, tile_waves(FN, FM)) k_fp8_tile(const Fp8GemmArgs a, const int tn,
+                                                                               const int tm) {
+  tile_body<T, FN, FM, WN, WM, R>(a, (int)blockIdx.x, tn, tm, 0);
+}
+
+// `big` tiles of 256 x 256, which fill the chip whole times, then the rest of the columns in tiles of 256 x 128.
+template <class T>
+__global__ void __launch_bounds__(256, 1) k_fp8_mixed(const Fp8GemmArgs a, const int tnb, const int tmb, const int tn,
+                                                      const int tm) {
+  const int big = tnb * tmb, w = (int)blockIdx.x;
+  if (w < big)
+    tile_body<T, 8, 8, 2, 2, 2>(a, w, tnb, tmb, 0);
+  else
+    tile_body<T, 8, 4, 2, 2, 2>(a, w - big, tn, tm, (int64_t)tnb * 256);
+}
+
+constexpr int tile_lds(int BN, int BM, int R) { return R * (BN + BM) * 128 + 4 * (BN + BM) * 4; }
+constexpr int64_t kMostTiles = (int64_t)1 << 22;
+
+template <class T, int FN, int FM, int WN, int WM, int R>
 hipError_t launch_tile(const Fp8GemmArgs& a, hipStream_t s) {
-  constexpr int BN = 16 * FN * WN, BM = 16 * FM * WM, LDS = 2 * (BN + BM) * 128 + 4 * (BN + BM) * 4;
+  constexpr int BN = 16 * FN * WN, BM = 16 * FM * WM, LDS = tile_lds(BN, BM, R);
   static PerDeviceFlag done;
-  auto* kernel = k_fp8_tile<T, FN, FM, WN, WM>;
+  auto* kernel = k_fp8_tile<T, FN, FM, WN, WM, R>;
   const hipError_t e = allow_lds_once(done, kernel, LDS);
   if (e != hipSuccess) return e;
   const int64_t tn = (a.N + BN - 1) / BN, tm = fp8_row_tiles(a, BM);
-  if (tn * tm >= (int64_t)1 << 22) return hipErrorNotSupported;
+  if (tn * tm >= kMostTiles) return hipErrorNotSupported;
   const dim3 grid((unsigned)(tn * tm), 1u, a.mode == kFp8Sum ? (unsigned)a.groups : 1u);
   hipLaunchKernelGGL(kernel, grid, dim3(64 * WN * WM), LDS, s, a, (int)tn, (int)tm);
   return hipGetLastError();
 }
 
 template <class T>
-hipError_t by_size(const Fp8GemmArgs& a, hipStream_t s) {
-  if constexpr (T::code != SPL_F32) {
-    const int64_t big = ((a.N + 255) / 256) * fp8_row_tiles(a, 256) * (a.mode == kFp8Sum ? a.groups : 1);
-    if (big >= 128) return launch_tile<T, 8, 8, 2, 2>(a, s);
+hipError_t launch_mixed(const Fp8GemmArgs& a, int64_t tnb, hipStream_t s) {
+  constexpr int LDS = tile_lds(256, 256, 2);
+  static PerDeviceFlag done;
+  const hipError_t e = allow_lds_once(done, k_fp8_mixed<T>, LDS);
+  if (e != hipSuccess) return e;
+  const int64_t tmb = fp8_row_tiles(a, 256), tm = fp8_row_tiles(a, 128), tn = (a.N + 255) / 256 - tnb;
+  if (tnb * tmb + tn * tm >= kMostTiles) return hipErrorNotSupported;
+  hipLaunchKernelGGL(k_fp8_mixed<T>, dim3((unsigned)(tnb * tmb + tn * tm)), dim3(256), LDS, s, a, (int)tnb, (int)tmb,
+                     (int)tn, (int)tm);
+  return hipGetLastError();
+}
+
+// How long a call takes, in us, in tiles of one kind: rounds of the chip, each a fixed part and one for each stage, which
+// differs where a CU has one workgroup only.  Fitted to launches of 128 to 8192 rows (us, 256 x 256 tiles / 128 x 128 / the
+// same, one a CU and four stage buffers / 128 x 64): 8192 x 8192 x 8192 437 / 569 / 652 / 714, 2048 x 11008 x 4096 107 / 108 /
+// 126 / 132 (256 x 256 and then 256 x 128: 99), 2048 x 4096 x 4096 50 / 37.0 / 42.5 / 45.6, 1000 x 4096 x 4096 50 / 29.2 / 23.3 /
+// 25.4, 512 x 4096 x 4096 48 / 28.0 / 20.7 / 16.1; fp32 results, 128 x 256 / 128 x 128 / 128 x 64: 4096 x 4096 x 2048 67 / 69 / 82,
+// 1024 x 1024 x 2048 27 / 20.5 / 15.0.
+struct Cost {
+  double fixed, full, alone;                         // a stage: with every place taken, with at most one workgroup a CU
+  int places;                                        // workgroups of a CU
+  double rounds(double tiles, double stages, int cus) const {
+    const double room = (double)cus * places, whole = floor(tiles / room), rest = tiles - whole * room;
+    return whole * (fixed + full * stages) + (rest <= 0 ? 0 : fixed + (rest <= cus ? alone : full) * stages);
   }
-  return launch_tile<T, 4, 4, 2, 2>(a, s);
+};
+constexpr Cost kLarge{12, 1.45, 1.45, 1}, kMiddle{9, 0.85, 0.85, 1}, kSmall{6, 0.97, 0.72, 2}, kDeep{6.5, 0.53, 0.53, 1},
+    kNarrow{5, 0.6, 0.32, 2};
+constexpr Cost kLarge32{8, 1.6, 1.6, 1}, kSmall32{6, 1.75, 0.85, 2}, kNarrow32{5, 1.15, 0.6, 2};
+
+// Tiles of the call, as far as the host can tell: groups are taken as equal.
+double about_tiles(const Fp8GemmArgs& a, int BN, int BM) {
+  const double tn = (double)((a.N + BN - 1) / BN);
+  if (a.mode != kFp8Rows) return tn * (double)((a.M + BM - 1) / BM) * (a.mode == kFp8Sum ? a.groups : 1);
+  const int64_t groups = a.M < a.groups ? a.M : a.groups;
+  return tn * (double)groups * (double)((a.M / groups + BM - 1) / BM);
+}
+double about_stages(const Fp8GemmArgs& a) {
+  if (a.mode != kFp8Sum) return a.blocks;
+  return (double)((a.tokens / a.groups + 127) / 128 + (a.tokens > 0 ? 0 : 1));
+}
+
+template <class T>
+hipError_t by_size(const Fp8GemmArgs& a, hipStream_t s) {
+  const int cus = device_cus();
+  const double st = about_stages(a), t64 = about_tiles(a, 128, 64), t128 = about_tiles(a, 128, 128);
+  if constexpr (T::code == SPL_F32) {
+    const double large = kLarge32.rounds(about_tiles(a, 128, 256), st, cus), small = kSmall32.rounds(t128, st, cus),
+                 narrow = kNarrow32.rounds(t64, st, cus);
+    if (narrow <= small && narrow <= large) return launch_tile<T, 4, 2, 2, 2, 3>(a, s);
+    return small <= large ? launch_tile<T, 4, 4, 2, 2, 2>(a, s) : launch_tile<T, 4, 4, 2, 4, 3>(a, s);
+  } else {
+    const double t256 = about_tiles(a, 256, 256);
+    const double large = kLarge.rounds(t256, st, cus), small = kSmall.rounds(t128, st, cus),
+                 deep = kDeep.rounds(t128, st, cus), narrow = kNarrow.rounds(t64, st, cus);
+    double best = large < small ? large : small;
+    best = deep < best ? deep : best;
+    best = narrow < best ? narrow : best;
+    if (a.mode == kFp8Plain && t256 > cus) {           // whole rounds of large tiles, the rest of the columns in middle ones
+      const int64_t tm = (a.M + 255) / 256, tn = (a.N + 255) / 256;
+      const int64_t tnb = (int64_t)(t256 / cus) * cus / tm;
+      const double mixed = kLarge.rounds((double)(tnb * tm), st, cus) +
+                           kMiddle.rounds((double)(tn - tnb) * (double)((a.M + 127) / 128), st, cus);
+      if (tnb > 0 && tnb < tn && mixed < best) return launch_mixed<T>(a, tnb, s);
+    }
+    if (best == narrow) return launch_tile<T, 4, 2, 2, 2, 3>(a, s);
+    if (best == deep) return launch_tile<T, 4, 4, 2, 2, 4>(a, s);
+    return best == small ? launch_tile<T, 4, 4, 2, 2, 2>(a, s) : launch_tile<T, 8, 8, 2, 2, 2>(a, s);
+  }
 }
 
 }  // namespace
