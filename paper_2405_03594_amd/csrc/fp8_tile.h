@@ -121,6 +121,11 @@ inline int64_t fp8_row_tiles(const Fp8GemmArgs& a, int64_t size) {
   return a.mode == kFp8Rows ? most_tiles(a.M, a.groups, size) : (a.M + size - 1) / size;
 }
 
+// Rows of X that a matrix of W meets, about: of a group one and a half times the mean.
+inline double fp8_rows_each(const Fp8GemmArgs& a) {
+  return a.mode == kFp8Rows ? 1.5 * (double)a.M / a.groups : (double)a.M;
+}
+
 hipError_t launch_fp8_stream(const Fp8GemmArgs& a, hipStream_t s);
 
 }  // namespace spl

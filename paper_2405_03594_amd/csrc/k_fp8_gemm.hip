@@ -373,16 +373,15 @@ constexpr Cost kLarge{12, 1.45, 1.45, 1}, kMiddle{9, 0.85, 0.85, 1}, kSmall{6, 0
     kNarrow{5, 0.6, 0.32, 2};
 constexpr Cost kLarge32{8, 1.6, 1.6, 1}, kSmall32{6, 1.75, 0.85, 2}, kNarrow32{5, 1.15, 0.6, 2};
 
-// Tiles of the call, as far as the host can tell: groups are taken as equal.
+// Tiles and stages of the call, as far as the host can tell: groups are taken as equal, each with half a tile to spare.
 double about_tiles(const Fp8GemmArgs& a, int BN, int BM) {
   const double tn = (double)((a.N + BN - 1) / BN);
   if (a.mode != kFp8Rows) return tn * (double)((a.M + BM - 1) / BM) * (a.mode == kFp8Sum ? a.groups : 1);
-  const int64_t groups = a.M < a.groups ? a.M : a.groups;
-  return tn * (double)groups * (double)((a.M / groups + BM - 1) / BM);
+  const double groups = (double)(a.M < a.groups ? a.M : a.groups);
+  return tn * groups * ((double)a.M / groups / BM + 0.5);
 }
 double about_stages(const Fp8GemmArgs& a) {
-  if (a.mode != kFp8Sum) return a.blocks;
-  return (double)((a.tokens / a.groups + 127) / 128 + (a.tokens > 0 ? 0 : 1));
+  return a.mode == kFp8Sum ? (double)a.tokens / a.groups / 128 + 0.5 : (double)a.blocks;
 }
 
 template <class T>
@@ -414,10 +413,21 @@ hipError_t by_size(const Fp8GemmArgs& a, hipStream_t s) {
   }
 }
 
+// Whether the streaming kernel is the one: up to 32 rows of a matrix; up to 64 where tiles of 128 x 64 would take longer
+// (us, streaming / tiles, 64 rows: 4096 x 4096 11.1 / 16.2, 4096 x 11008 25.5 / 33, 11008 x 4096 31 / 20.6).
+bool streams(const Fp8GemmArgs& a) {
+  const double each = fp8_rows_each(a);
+  if (each <= 32) return true;
+  if (each > 64 || a.mode != kFp8Plain) return false;
+  const double cus = device_cus(), wgs = (double)((a.N + 31) / 32) * 2 / cus;
+  const Cost& narrow = a.dtype == SPL_F32 ? kNarrow32 : kNarrow;
+  return 4 + (wgs > 1 ? wgs : 1) * a.blocks * 0.27 < narrow.rounds(about_tiles(a, 128, 64), a.blocks, (int)cus);
+}
+
 }  // namespace
 
 hipError_t launch_fp8_gemm(const Fp8GemmArgs& a, hipStream_t s) {
-  if (a.x16 || a.M <= 64) return launch_fp8_stream(a, s);
+  if (a.x16 || streams(a)) return launch_fp8_stream(a, s);
   if (a.dtype == SPL_F32) return by_size<F32Out>(a, s);
   return a.dtype == SPL_BF16 ? by_size<Bf16>(a, s) : by_size<F16>(a, s);
 }

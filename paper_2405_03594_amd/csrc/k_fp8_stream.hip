@@ -1,10 +1,12 @@
-// Products of 8-bit floats for few rows, for gfx950: a workgroup streams 16 rows
-// of W past up to 64 rows of X.
+// Products of 8-bit floats for few rows, for gfx950: a workgroup streams 16 NR rows
+// of W past up to 16 MT rows of X.
 //
-// Its waves share the sum, a run of blocks each: a wave loads 16 rows x 128
+// Its four or eight waves share the sum, a run of blocks each: a wave loads 16 rows x 128
 // columns of W straight into the operand of one scaled matrix instruction (two
 // requests of 16 bytes a lane, 64 neighbouring bytes of a row by 4 lanes), and
-// one for each 16 rows of X.  Partial sums are added in LDS, in the waves' order.
+// of X likewise; what several blocks need is requested together, before the first
+// of them is multiplied, so that a wave of a 4096-column sum waits for memory
+// once.  Partial sums are added in LDS, in the waves' order.
 // Rows of X may also come in 16 bits: a lane then has 32 of a block's 128
 // entries, the largest magnitude is found by two lane moves, and the codes are
 // those of k_fp8_quantize.
@@ -15,38 +17,90 @@
 namespace spl {
 namespace {
 
-constexpr int kWaves = 8;
+struct Codes {};                                // X is quantized already
+
+// A lane's part of a block of X: 32 codes (a quarter's pieces fg and fg + 4), or as many values of 16 bits.
+template <class T>
+struct Part {
+  u32x4 q[std::is_same<T, Codes>::value ? 2 : 4];
+};
 
 // 16 entries of a row in 16 bits from column c on, zeros past the last.
-template <class T>
-__device__ __forceinline__ void load16(const uint16_t* row, int c, int cols, bool wide, float (&v)[16]) {
+__device__ __forceinline__ void load16(const uint16_t* row, int c, int cols, bool wide, u32x4& p, u32x4& q) {
   if (wide && c + 16 <= cols) {
-    const u32x4 p = *reinterpret_cast<const u32x4*>(row + c), q = *reinterpret_cast<const u32x4*>(row + c + 8);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      v[2 * j] = T::to_f32(p[j] & 0xffffu), v[2 * j + 1] = T::to_f32(p[j] >> 16);
-      v[8 + 2 * j] = T::to_f32(q[j] & 0xffffu), v[9 + 2 * j] = T::to_f32(q[j] >> 16);
-    }
+    p = *reinterpret_cast<const u32x4*>(row + c), q = *reinterpret_cast<const u32x4*>(row + c + 8);
   } else {
 #pragma unroll
-    for (int j = 0; j < 16; ++j) v[j] = c + j < cols ? T::to_f32(row[c + j]) : 0.f;
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t lo = c + 2 * j < cols ? row[c + 2 * j] : 0u, hi = c + 2 * j + 1 < cols ? row[c + 2 * j + 1] : 0u;
+      (j < 4 ? p : q)[j & 3] = lo | (hi << 16);
+    }
   }
 }
 
-struct Codes {};                                // X is quantized already
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t max16(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+// Four values of 16 bits, divided by a power of two, to codes.
+template <class T>
+__device__ __forceinline__ uint32_t code4(uint32_t a, uint32_t b, float scale) {
+  s16x2 z = {0, 0};
+  if constexpr (std::is_same<T, Bf16>::value) {
+    z = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(z, __builtin_bit_cast(bf16x2, a), scale, false);
+    z = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(z, __builtin_bit_cast(bf16x2, b), scale, true);
+  } else {
+    z = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(z, __builtin_bit_cast(f16x2, a), scale, false);
+    z = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(z, __builtin_bit_cast(f16x2, b), scale, true);
+  }
+  return __builtin_bit_cast(uint32_t, z);
+}
+// The block's scale byte, and the lane's codes.
+template <class T>
+__device__ __forceinline__ uint32_t quantize(const Part<T>& v, u32x4& x0, u32x4& x1) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m = max16(m, v.q[i][j] & 0x7fff7fffu);
+  m = umax(m & 0xffffu, m >> 16);
+  m = umax(m, (uint32_t)__shfl_xor((int)m, 16));
+  m = umax(m, (uint32_t)__shfl_xor((int)m, 32));
+  const uint32_t byte = fp8_scale_byte(__float_as_uint(T::to_f32(m)));
+  // 2^-127, which blocks of zeros have, and of bf16 those whose largest is below 2^-118, is no normal number: taken by 2^-126
+  // and 2^-1 (of bf16: values below 2^-126 are none that the conversion keeps)
+  const float scale = byte == 0 ? 0x1p-127f : __uint_as_float(byte << 23);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    x0[2 * j] = code4<T>(v.q[j][0], v.q[j][1], scale), x0[2 * j + 1] = code4<T>(v.q[j][2], v.q[j][3], scale);
+    x1[2 * j] = code4<T>(v.q[2 + j][0], v.q[2 + j][1], scale), x1[2 * j + 1] = code4<T>(v.q[2 + j][2], v.q[2 + j][3], scale);
+  }
+  if (byte == 255) x0 = x1 = u32x4{0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu};
+  return byte;
+}
 
-template <class T, int MT, bool kExact>
-__global__ void __launch_bounds__(64 * kWaves) k_fp8_stream(const Fp8GemmArgs a, const int wide) {
+// U: blocks requested together, of kWaves waves.  kEach: waves that a SIMD's registers are to hold.
+template <class T, int MT, int NR, int U, int kWaves, int kEach, bool kExact>
+__global__ void __launch_bounds__(64 * kWaves, kEach) k_fp8_stream(const Fp8GemmArgs a, const int wide) {
   constexpr bool kCodes = std::is_same<T, Codes>::value;
-  __shared__ f32x4 sums[kWaves][MT][64];
+  __shared__ f32x4 sums[kWaves][NR * MT][64];
   const Fp8Part p = fp8_part(a, 16 * MT, blockIdx.y, blockIdx.z);
   if (p.none) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int fr = lane & 15, fg = lane >> 4;
-  const int64_t n0 = 16 * (int64_t)blockIdx.x;
-  const int64_t wr = n0 + fr < a.N ? n0 + fr : a.N - 1;             // rows past the last repeat it and are not stored
-  const uint8_t* wp = a.w.codes + p.w_codes + wr * a.w.pitch + 16 * fg;
-  const uint8_t* ws = a.w.scales + p.w_scales + (wr >> a.w.shift) * a.w.spitch;
+  const int64_t n0 = 16 * NR * (int64_t)blockIdx.x;
+  const uint8_t* wp[NR];
+  const uint8_t* ws[NR];
+#pragma unroll
+  for (int i = 0; i < NR; ++i) {
+    int64_t wr = n0 + 16 * i + fr;
+    wr = wr < a.N ? wr : a.N - 1;                // rows past the last repeat it and are not stored
+    wp[i] = a.w.codes + p.w_codes + wr * a.w.pitch + 16 * fg;
+    ws[i] = a.w.scales + p.w_scales + (wr >> a.w.shift) * a.w.spitch;
+  }
   const uint8_t* xp[MT];
   const uint8_t* xs[MT];
   const uint16_t* xh[MT];
@@ -54,94 +108,149 @@ __global__ void __launch_bounds__(64 * kWaves) k_fp8_stream(const Fp8GemmArgs a,
   for (int j = 0; j < MT; ++j) {
     int64_t m = p.m0 + 16 * j + fr;
     m = m < p.mend ? m : p.mend - 1;
-    xp[j] = a.x.codes + m * a.x.pitch + 16 * fg;
-    xs[j] = a.x.scales + (m >> a.x.shift) * a.x.spitch;
-    xh[j] = static_cast<const uint16_t*>(a.x16) + m * a.x16_stride;
+    if constexpr (kCodes) {
+      xp[j] = a.x.codes + m * a.x.pitch + 16 * fg;
+      xs[j] = a.x.scales + (m >> a.x.shift) * a.x.spitch;
+    } else {
+      xh[j] = static_cast<const uint16_t*>(a.x16) + m * a.x16_stride;
+    }
   }
-  const int per = (p.k1 - p.k0 + kWaves - 1) / kWaves;
-  const int b0 = p.k0 + wave * per, b1 = b0 + per < p.k1 ? b0 + per : p.k1;
-  f32x4 acc[MT];
+  // A wave's blocks: 1, 2 or a multiple of 4 of them, so that the scale bytes of those requested together are of one word.
+  // Blocks before k0 and from k1 on are read and multiplied as zeros.
+  static_assert(U == 4 || U == 2, "a word's blocks");
+  const int start = p.k0 & ~3;
+  int per = (p.k1 - start + kWaves - 1) / kWaves;
+  per = per < 3 ? per : (per + 3) & ~3;
+  const int b0 = start + wave * per, b1 = b0 + per < p.k1 ? b0 + per : p.k1;
+  f32x4 acc[NR][MT];
 #pragma unroll
-  for (int j = 0; j < MT; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int b = b0; b < b1; ++b) {
-    const u32x4 a0 = *reinterpret_cast<const u32x4*>(wp + 128 * (int64_t)b);
-    const u32x4 a1 = *reinterpret_cast<const u32x4*>(wp + 128 * (int64_t)b + 64);
-    const uint32_t sa = ws[b];
-    Wide8 aw;
-    if constexpr (kExact) aw = fp8_widen32(a0, a1, sa);
+  for (int i = 0; i < NR; ++i)
 #pragma unroll
-    for (int j = 0; j < MT; ++j) {
-      u32x4 x0, x1;
-      uint32_t sb;
-      if constexpr (kCodes) {
-        x0 = *reinterpret_cast<const u32x4*>(xp[j] + 128 * (int64_t)b);
-        x1 = *reinterpret_cast<const u32x4*>(xp[j] + 128 * (int64_t)b + 64);
-        sb = xs[j][b];
-      } else {
-        float u[16], v[16];
-        load16<T>(xh[j], 128 * b + 16 * fg, a.cols, wide, u);
-        load16<T>(xh[j], 128 * b + 64 + 16 * fg, a.cols, wide, v);
-        uint32_t m = 0;
+    for (int j = 0; j < MT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int b = b0; b < b1; b += U) {
+    // X first: it is near, and in 16 bits it is quantized while W is on its way
+    Part<T> x[U][MT];
+    Part<Codes> w[U][NR];
+    uint32_t sw[NR], sx[MT];
+    const int word = b & ~3, shift = 8 * (b & 3);
+    if constexpr (kCodes) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          m = umax(m, umax(__float_as_uint(u[i]) & 0x7fffffffu, __float_as_uint(v[i]) & 0x7fffffffu));
-        m = umax(m, (uint32_t)__shfl_xor((int)m, 16));
-        m = umax(m, (uint32_t)__shfl_xor((int)m, 32));
-        sb = fp8_scale_byte(m);
-        const float f = fp8_inverse(sb);
+      for (int j = 0; j < MT; ++j) sx[j] = *reinterpret_cast<const uint32_t*>(xs[j] + word);
+    }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          x0[i] = fp8_four(u[4 * i] * f, u[4 * i + 1] * f, u[4 * i + 2] * f, u[4 * i + 3] * f);
-          x1[i] = fp8_four(v[4 * i] * f, v[4 * i + 1] * f, v[4 * i + 2] * f, v[4 * i + 3] * f);
+    for (int u = 0; u < U; ++u) {
+      const int at = b + u < b1 ? b + u : b1 - 1;
+#pragma unroll
+      for (int j = 0; j < MT; ++j) {
+        if constexpr (kCodes) {
+          x[u][j].q[0] = *reinterpret_cast<const u32x4*>(xp[j] + 128 * (int64_t)at);
+          x[u][j].q[1] = *reinterpret_cast<const u32x4*>(xp[j] + 128 * (int64_t)at + 64);
+        } else {
+          load16(xh[j], 128 * at + 16 * fg, a.cols, wide, x[u][j].q[0], x[u][j].q[1]);
+          load16(xh[j], 128 * at + 64 + 16 * fg, a.cols, wide, x[u][j].q[2], x[u][j].q[3]);
         }
-        if (sb == 255) x0 = x1 = u32x4{0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu};
       }
-      if constexpr (kExact)
-        acc[j] = fp8_mfma_wide(aw, fp8_widen32(x0, x1, sb), acc[j]);
-      else
-        acc[j] = fp8_mfma(a0, a1, x0, x1, acc[j], sa, sb);
+    }
+    if constexpr (!kCodes) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < NR; ++i) sw[i] = *reinterpret_cast<const uint32_t*>(ws[i] + word);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int at = b + u < b1 ? b + u : b1 - 1;
+#pragma unroll
+      for (int i = 0; i < NR; ++i) {
+        w[u][i].q[0] = *reinterpret_cast<const u32x4*>(wp[i] + 128 * (int64_t)at);
+        w[u][i].q[1] = *reinterpret_cast<const u32x4*>(wp[i] + 128 * (int64_t)at + 64);
+      }
+    }
+    if constexpr (!kCodes) __builtin_amdgcn_sched_barrier(0);
+    u32x4 x0[U][MT], x1[U][MT];
+    uint32_t sb[U][MT];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t live = b + u >= p.k0 && b + u < b1 ? ~0u : 0u;   // (a branch here would take the requests along)
+#pragma unroll
+      for (int j = 0; j < MT; ++j) {
+        if constexpr (kCodes)
+          x0[u][j] = x[u][j].q[0], x1[u][j] = x[u][j].q[1], sb[u][j] = sx[j] >> (shift + 8 * u);
+        else
+          sb[u][j] = quantize<T>(x[u][j], x0[u][j], x1[u][j]);
+        x0[u][j] &= live, x1[u][j] &= live, sb[u][j] &= live;
+      }
+    }
+    if constexpr (!kCodes) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t live = b + u >= p.k0 && b + u < b1 ? ~0u : 0u;
+#pragma unroll
+      for (int i = 0; i < NR; ++i) {
+        const uint32_t sa = (sw[i] >> (shift + 8 * u)) & live;      // the matrix instruction takes the low byte
+        if constexpr (kExact) {
+          const Wide8 v = fp8_widen32(w[u][i].q[0], w[u][i].q[1], sa & 255u);
+#pragma unroll
+          for (int j = 0; j < MT; ++j)
+            acc[i][j] = fp8_mfma_wide(v, fp8_widen32(x0[u][j], x1[u][j], sb[u][j] & 255u), acc[i][j]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < MT; ++j)
+            acc[i][j] = fp8_mfma(w[u][i].q[0], w[u][i].q[1], x0[u][j], x1[u][j], acc[i][j], sa, sb[u][j]);
+        }
+      }
     }
   }
 #pragma unroll
-  for (int j = 0; j < MT; ++j) sums[wave][j][lane] = acc[j];
+  for (int i = 0; i < NR; ++i)
+#pragma unroll
+    for (int j = 0; j < MT; ++j) sums[wave][i * MT + j][lane] = acc[i][j];
   __syncthreads();
 #pragma unroll
-  for (int q = 0; q < (MT + kWaves - 1) / kWaves; ++q) {
-    const int j = wave + kWaves * q;
-    if (j >= MT) break;
-    f32x4 v = sums[0][j][lane];
+  for (int q = 0; q < (NR * MT + kWaves - 1) / kWaves; ++q) {
+    const int f = wave + kWaves * q, i = f / MT, j = f % MT;
+    if (f >= NR * MT) break;
+    f32x4 v = sums[0][f][lane];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) v += sums[w][j][lane];
+    for (int w = 1; w < kWaves; ++w) v += sums[w][f][lane];
     const int64_t m = p.m0 + 16 * j + fr;
-    if (m < p.mend) fp8_store4(a, m, n0 + 4 * fg, v, p.y);
+    if (m < p.mend) fp8_store4(a, m, n0 + 16 * i + 4 * fg, v, p.y);
   }
 }
 
-template <class T, bool kExact>
-hipError_t stream(const Fp8GemmArgs& a, int wide, hipStream_t s) {
-  const int mt = a.M <= 16 ? 1 : (a.M <= 32 ? 2 : 4);
-  const int64_t tiles = fp8_row_tiles(a, 16 * mt);
+template <class T, int MT, int NR, int U, int W, int E>
+hipError_t launch(const Fp8GemmArgs& a, int wide, hipStream_t s) {
+  const int64_t tiles = fp8_row_tiles(a, 16 * MT);
   if (tiles > 65535) return hipErrorNotSupported;
-  const dim3 grid((unsigned)((a.N + 15) / 16), (unsigned)tiles, a.mode == kFp8Sum ? (unsigned)a.groups : 1u);
-  if (mt == 1)
-    hipLaunchKernelGGL((k_fp8_stream<T, 1, kExact>), grid, dim3(64 * kWaves), 0, s, a, wide);
-  else if (mt == 2)
-    hipLaunchKernelGGL((k_fp8_stream<T, 2, kExact>), grid, dim3(64 * kWaves), 0, s, a, wide);
+  const dim3 grid((unsigned)((a.N + 16 * NR - 1) / (16 * NR)), (unsigned)tiles, a.mode == kFp8Sum ? (unsigned)a.groups : 1u);
+  if (a.dtype == SPL_F32)
+    hipLaunchKernelGGL((k_fp8_stream<T, MT, NR, U, W, E, true>), grid, dim3(64 * W), 0, s, a, wide);
   else
-    hipLaunchKernelGGL((k_fp8_stream<T, 4, kExact>), grid, dim3(64 * kWaves), 0, s, a, wide);
+    hipLaunchKernelGGL((k_fp8_stream<T, MT, NR, U, W, E, false>), grid, dim3(64 * W), 0, s, a, wide);
   return hipGetLastError();
 }
+// Four waves for up to 16 blocks of 128 columns, which would leave eight of them two or fewer each (us, 4 / 8 waves:
+// 5632 x 2048 6.0 / 8.2, 1111 x 1000 3.9 / 5.0, 4096 x 4096 7.6 / 6.5, 4096 x 11008 16.3 / 13.0).
+template <class T, int MT, int NR, int U, int E>
+hipError_t by_sum(const Fp8GemmArgs& a, int wide, hipStream_t s) {
+  if (a.blocks <= 16) return launch<T, MT, NR, U, 4, E>(a, wide, s);
+  return launch<T, MT, NR, U, 8, E>(a, wide, s);
+}
+// Rows in 16 bits are quantized by each workgroup anew, which is most of its arithmetic: two blocks of 16 rows of W a
+// workgroup where those still fill the chip.
 template <class T>
-hipError_t by_type(const Fp8GemmArgs& a, int wide, hipStream_t s) {
-  return a.dtype == SPL_F32 ? stream<T, true>(a, wide, s) : stream<T, false>(a, wide, s);
+hipError_t rows16(const Fp8GemmArgs& a, hipStream_t s) {
+  const int wide = (reinterpret_cast<uintptr_t>(a.x16) & 15) == 0 && a.x16_stride % 8 == 0;
+  const int64_t wgs = (a.N + 31) / 32 * (a.mode == kFp8Rows ? (a.M < a.groups ? a.M : a.groups) : 1);
+  if (wgs >= device_cus()) return by_sum<T, 1, 2, 2, 5>(a, wide, s);
+  return by_sum<T, 1, 1, 2, 6>(a, wide, s);
 }
 
 }  // namespace
 
 hipError_t launch_fp8_stream(const Fp8GemmArgs& a, hipStream_t s) {
-  if (!a.x16) return by_type<Codes>(a, 0, s);
-  const int wide = (reinterpret_cast<uintptr_t>(a.x16) & 15) == 0 && a.x16_stride % 8 == 0;
-  return a.x16_dtype == SPL_BF16 ? by_type<Bf16>(a, wide, s) : by_type<F16>(a, wide, s);
+  if (a.x16) return a.x16_dtype == SPL_BF16 ? rows16<Bf16>(a, s) : rows16<F16>(a, s);
+  const double each = fp8_rows_each(a);
+  if (each <= 16) return by_sum<Codes, 1, 1, 4, 6>(a, 0, s);
+  if (each <= 32) return by_sum<Codes, 2, 1, 4, 4>(a, 0, s);
+  return by_sum<Codes, 2, 2, 4, 2>(a, 0, s);
 }
 
 }  // namespace spl

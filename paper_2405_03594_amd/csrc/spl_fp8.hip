@@ -45,10 +45,10 @@ spl_status check_matrix(const spl_fp8_matrix* m) {
 }
 
 // Activations of 16 bits that a product quantizes itself: a row is read by every
-// workgroup of 16 rows of W, so only few are.
-bool fused(int64_t M) { return M <= 16; }
-int64_t rows_workspace(int64_t M, int64_t N, int64_t cols) {
-  if (fused(M)) return 0;
+// workgroup of 16 rows of W, so only few are (of a group, where there are groups).
+bool fused(int64_t M, int64_t experts) { return M <= 16 * experts && M <= 64; }
+int64_t rows_workspace(int64_t M, int64_t cols, int64_t experts) {
+  if (fused(M, experts)) return 0;
   return align256(M * spl::fp8_pitch(cols)) + align256(M * spl::fp8_spitch(cols));
 }
 bool product_ok(int64_t M, int64_t N, int64_t cols, int64_t experts) {
@@ -66,7 +66,7 @@ spl_status rows_product(const void* X, int32_t x_dtype, int64_t M, int64_t row_s
   if (M == 0) return SPL_OK;
   if (row_stride < W->cols || row_stride > kMaxBytes / M || !given(X, 2) || !given(Y, 16) || !aligned(starts, 4))
     return SPL_ERR_INVALID_ARG;
-  const int64_t need = rows_workspace(M, W->rows, W->cols);
+  const int64_t need = rows_workspace(M, W->cols, W->count);
   if (need > 0 && !given(workspace, 256)) return SPL_ERR_INVALID_ARG;
   if (M > kMaxCols) return SPL_ERR_UNSUPPORTED;
   (void)hipGetLastError();
@@ -168,7 +168,7 @@ spl_status spl_linear_fp8(const spl_fp8_matrix* X, const spl_fp8_matrix* W, int3
 }
 
 int64_t spl_linear_fp8_rows_workspace_bytes(int64_t M, int64_t N, int64_t cols) {
-  return product_ok(M, N, cols, 1) ? (M == 0 ? 0 : rows_workspace(M, N, cols)) : -1;
+  return product_ok(M, N, cols, 1) ? (M == 0 ? 0 : rows_workspace(M, cols, 1)) : -1;
 }
 spl_status spl_linear_fp8_rows(const void* X, int32_t x_dtype, int64_t M, int64_t row_stride, const spl_fp8_matrix* W,
                                int32_t dtype, void* Y, void* workspace, hipStream_t stream) {
@@ -194,7 +194,7 @@ spl_status spl_linear_fp8_grouped(const spl_fp8_matrix* X, const spl_fp8_matrix*
 }
 
 int64_t spl_linear_fp8_grouped_rows_workspace_bytes(int64_t M, int64_t N, int64_t cols, int64_t experts) {
-  return product_ok(M, N, cols, experts) ? (M == 0 ? 0 : rows_workspace(M, N, cols)) : -1;
+  return product_ok(M, N, cols, experts) ? (M == 0 ? 0 : rows_workspace(M, cols, experts)) : -1;
 }
 spl_status spl_linear_fp8_grouped_rows(const void* X, int32_t x_dtype, int64_t M, int64_t row_stride,
                                        const spl_fp8_matrix* W, const int32_t* starts, int32_t dtype, void* Y,
