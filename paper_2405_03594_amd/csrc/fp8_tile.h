@@ -57,7 +57,7 @@ struct Fp8Part {
   int64_t y;                                    // element offset of the result
   bool none;
 };
-// t: the tile of `size` rows; z: the group (kFp8Sum).
+// t: the tile of `size` rows; z: the group (kFp8Sum) or the split.
 __device__ __forceinline__ Fp8Part fp8_part(const Fp8GemmArgs& a, int size, int t, int z) {
   Fp8Part p{t * size, (int)a.M, 0, a.blocks, 0, 0, 0, false};
   if (a.mode == kFp8Rows) {
@@ -69,6 +69,11 @@ __device__ __forceinline__ Fp8Part fp8_part(const Fp8GemmArgs& a, int size, int 
     const Segment s = find_group(a.starts, z, a.tokens, 128);
     p.k0 = s.tile, p.k1 = s.tile + (s.end - s.row + 127) / 128;
     p.k1 = p.k1 < a.blocks ? p.k1 : a.blocks;
+    p.y = (int64_t)z * a.M * a.N;
+  } else if (a.splits > 1) {                     // z: the split
+    const int each = (a.blocks + a.splits - 1) / a.splits;
+    p.k0 = z * each < a.blocks ? z * each : a.blocks;
+    p.k1 = p.k0 + each < a.blocks ? p.k0 + each : a.blocks;
     p.y = (int64_t)z * a.M * a.N;
   }
   return p;

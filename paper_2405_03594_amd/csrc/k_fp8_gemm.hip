@@ -58,10 +58,9 @@ __device__ __forceinline__ void settle(f32x4 (&acc)[FN][FM]) {
 
 constexpr int tile_waves(int FN, int FM) { return FN * FM > 32 ? 1 : 2; }   // a SIMD's waves that the registers are held to
 
-// Tile w of tn x tm (columns from nbase on).  T: of the results; fp32 ones are summed by bf16 instructions.
-template <class T, int FN, int FM, int WN, int WM, int R>
+// Tile w of tn x tm (columns from nbase on).  T: of the results; kExact: summed by bf16 instructions.
+template <class T, bool kExact, int FN, int FM, int WN, int WM, int R>
 __device__ __forceinline__ void tile_body(const Fp8GemmArgs& a, int w, int tn, int tm, int64_t nbase) {
-  constexpr bool kExact = T::code == SPL_F32;
   constexpr int NW = WN * WM, BN = 16 * FN * WN, BM = 16 * FM * WM;
   constexpr int PW = BN / 8 / NW, PX = BM / 8 / NW;   // requests of 8 rows a wave and stage
   constexpr int SZ = (BN + BM) * 128, RQ = PW + PX;
@@ -271,7 +270,7 @@ __device__ __forceinline__ void tile_body(const Fp8GemmArgs& a, int w, int tn, i
 
   // Results: 16 rows of the wave's at a time through LDS, so that a row's leave as 16-byte pieces.  A lane has columns
   // 4 fg .. 4 fg + 3 of each fragment, row fr; piece c of a row sits at c ^ row.
-  constexpr int E = kExact ? 4 : 2, CH = 16 * FN * E / 16;   // bytes of a result, pieces of a row
+  constexpr int E = T::code == SPL_F32 ? 4 : 2, CH = 16 * FN * E / 16;   // bytes of a result, pieces of a row
   tile_barrier();                                    // the other waves have read their last stage
   unsigned char* out = dsm + wave * (2 * 16 * CH * 16);
   const int64_t nw = n0 + 16 * FN * wn;
@@ -281,7 +280,7 @@ __device__ __forceinline__ void tile_body(const Fp8GemmArgs& a, int w, int tn, i
 #pragma unroll
     for (int i = 0; i < FN; ++i) {
       const f32x4 v = acc[i][j];
-      if constexpr (kExact) {
+      if constexpr (E == 4) {
         *reinterpret_cast<f32x4*>(half + fr * (CH * 16) + 16 * ((4 * i + fg) ^ (fr & (CH - 1)))) = v;
       } else {
         *reinterpret_cast<u32x2*>(half + fr * (CH * 16) + 16 * ((2 * i + (fg >> 1)) ^ (fr & (CH - 1))) + 8 * (fg & 1)) =
@@ -308,10 +307,10 @@ __device__ __forceinline__ void tile_body(const Fp8GemmArgs& a, int w, int tn, i
   }
 }
 
-template <class T, int FN, int FM, int WN, int WM, int R>
+template <class T, bool kExact, int FN, int FM, int WN, int WM, int R>
 __global__ void __launch_bounds__(64 * WN * WM, tile_waves(FN, FM)) k_fp8_tile(const Fp8GemmArgs a, const int tn,
                                                                                const int tm) {
-  tile_body<T, FN, FM, WN, WM, R>(a, (int)blockIdx.x, tn, tm, 0);
+  tile_body<T, kExact, FN, FM, WN, WM, R>(a, (int)blockIdx.x, tn, tm, 0);
 }
 
 // `big` tiles of 256 x 256, which fill the chip whole times, then the rest of the columns in tiles of 256 x 128.
@@ -320,24 +319,24 @@ __global__ void __launch_bounds__(256, 1) k_fp8_mixed(const Fp8GemmArgs a, const
                                                       const int tm) {
   const int big = tnb * tmb, w = (int)blockIdx.x;
   if (w < big)
-    tile_body<T, 8, 8, 2, 2, 2>(a, w, tnb, tmb, 0);
+    tile_body<T, false, 8, 8, 2, 2, 2>(a, w, tnb, tmb, 0);
   else
-    tile_body<T, 8, 4, 2, 2, 2>(a, w - big, tn, tm, (int64_t)tnb * 256);
+    tile_body<T, false, 8, 4, 2, 2, 2>(a, w - big, tn, tm, (int64_t)tnb * 256);
 }
 
 constexpr int tile_lds(int BN, int BM, int R) { return R * (BN + BM) * 128 + 4 * (BN + BM) * 4; }
 constexpr int64_t kMostTiles = (int64_t)1 << 22;
 
-template <class T, int FN, int FM, int WN, int WM, int R>
+template <class T, bool kExact, int FN, int FM, int WN, int WM, int R>
 hipError_t launch_tile(const Fp8GemmArgs& a, hipStream_t s) {
   constexpr int BN = 16 * FN * WN, BM = 16 * FM * WM, LDS = tile_lds(BN, BM, R);
   static PerDeviceFlag done;
-  auto* kernel = k_fp8_tile<T, FN, FM, WN, WM, R>;
+  auto* kernel = k_fp8_tile<T, kExact, FN, FM, WN, WM, R>;
   const hipError_t e = allow_lds_once(done, kernel, LDS);
   if (e != hipSuccess) return e;
   const int64_t tn = (a.N + BN - 1) / BN, tm = fp8_row_tiles(a, BM);
   if (tn * tm >= kMostTiles) return hipErrorNotSupported;
-  const dim3 grid((unsigned)(tn * tm), 1u, a.mode == kFp8Sum ? (unsigned)a.groups : 1u);
+  const dim3 grid((unsigned)(tn * tm), 1u, a.mode == kFp8Sum ? (unsigned)a.groups : (unsigned)a.splits);
   hipLaunchKernelGGL(kernel, grid, dim3(64 * WN * WM), LDS, s, a, (int)tn, (int)tm);
   return hipGetLastError();
 }
@@ -384,6 +383,22 @@ double about_stages(const Fp8GemmArgs& a) {
   return a.mode == kFp8Sum ? (double)a.tokens / a.groups / 128 + 0.5 : (double)a.blocks;
 }
 
+// Workgroups that share a tile's sum, joined by a second launch (3 us and the partial sums): as many as are worth
+// it where the tiles of 128 x 64 leave CUs without work.
+int splits_of(int64_t M, int64_t N, int32_t blocks) {
+  if (M <= 32) return 1;
+  const int cus = device_cus();
+  const double tiles = (double)((N + 127) / 128) * (double)((M + 63) / 64);
+  double best = kNarrow.rounds(tiles, blocks, cus);
+  int splits = 1;
+  for (int n = 2; n <= 16 && blocks / n >= 4; ++n) {
+    const double join = 3 + (double)M * N * 4 * (n + 1) / 4e6;
+    const double t = kNarrow.rounds(tiles * n, (double)((blocks + n - 1) / n), cus) + join;
+    if (t < 0.9 * best) best = t, splits = n;
+  }
+  return splits;
+}
+
 template <class T>
 hipError_t by_size(const Fp8GemmArgs& a, hipStream_t s) {
   const int cus = device_cus();
@@ -391,8 +406,8 @@ hipError_t by_size(const Fp8GemmArgs& a, hipStream_t s) {
   if constexpr (T::code == SPL_F32) {
     const double large = kLarge32.rounds(about_tiles(a, 128, 256), st, cus), small = kSmall32.rounds(t128, st, cus),
                  narrow = kNarrow32.rounds(t64, st, cus);
-    if (narrow <= small && narrow <= large) return launch_tile<T, 4, 2, 2, 2, 3>(a, s);
-    return small <= large ? launch_tile<T, 4, 4, 2, 2, 2>(a, s) : launch_tile<T, 4, 4, 2, 4, 3>(a, s);
+    if (narrow <= small && narrow <= large) return launch_tile<T, true, 4, 2, 2, 2, 3>(a, s);
+    return small <= large ? launch_tile<T, true, 4, 4, 2, 2, 2>(a, s) : launch_tile<T, true, 4, 4, 2, 4, 3>(a, s);
   } else {
     const double t256 = about_tiles(a, 256, 256);
     const double large = kLarge.rounds(t256, st, cus), small = kSmall.rounds(t128, st, cus),
@@ -407,9 +422,9 @@ hipError_t by_size(const Fp8GemmArgs& a, hipStream_t s) {
                            kMiddle.rounds((double)(tn - tnb) * (double)((a.M + 127) / 128), st, cus);
       if (tnb > 0 && tnb < tn && mixed < best) return launch_mixed<T>(a, tnb, s);
     }
-    if (best == narrow) return launch_tile<T, 4, 2, 2, 2, 3>(a, s);
-    if (best == deep) return launch_tile<T, 4, 4, 2, 2, 4>(a, s);
-    return best == small ? launch_tile<T, 4, 4, 2, 2, 2>(a, s) : launch_tile<T, 8, 8, 2, 2, 2>(a, s);
+    if (best == narrow) return launch_tile<T, false, 4, 2, 2, 2, 3>(a, s);
+    if (best == deep) return launch_tile<T, false, 4, 4, 2, 2, 4>(a, s);
+    return best == small ? launch_tile<T, false, 4, 4, 2, 2, 2>(a, s) : launch_tile<T, false, 8, 8, 2, 2, 2>(a, s);
   }
 }
 
@@ -418,16 +433,63 @@ hipError_t by_size(const Fp8GemmArgs& a, hipStream_t s) {
 bool streams(const Fp8GemmArgs& a) {
   const double each = fp8_rows_each(a);
   if (each <= 32) return true;
-  if (each > 64 || a.mode != kFp8Plain) return false;
+  if (each > 64 || a.mode != kFp8Plain || splits_of(a.M, a.N, a.blocks) > 1) return false;
   const double cus = device_cus(), wgs = (double)((a.N + 31) / 32) * 2 / cus;
   const Cost& narrow = a.dtype == SPL_F32 ? kNarrow32 : kNarrow;
   return 4 + (wgs > 1 ? wgs : 1) * a.blocks * 0.27 < narrow.rounds(about_tiles(a, 128, 64), a.blocks, (int)cus);
 }
 
+// The sum of the splits, in their order: 4 results a thread.
+template <class T>
+__global__ void __launch_bounds__(256) k_fp8_join(const float* partial, int splits, int64_t n, void* y) {
+  const int64_t i = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x);
+  if (i >= n) return;
+  if (i + 4 <= n && (n & 3) == 0) {
+    f32x4 v = *reinterpret_cast<const f32x4*>(partial + i);
+    for (int s = 1; s < splits; ++s) v += *reinterpret_cast<const f32x4*>(partial + s * n + i);
+    if constexpr (T::code == SPL_F32)
+      *reinterpret_cast<f32x4*>(static_cast<float*>(y) + i) = v;
+    else
+      *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(y) + i) = u32x2{fp8_pack2<T>(v[0], v[1]), fp8_pack2<T>(v[2], v[3])};
+  } else {
+    for (int k = 0; k < 4 && i + k < n; ++k) {
+      float v = partial[i + k];
+      for (int s = 1; s < splits; ++s) v += partial[s * n + i + k];
+      if constexpr (T::code == SPL_F32)
+        static_cast<float*>(y)[i + k] = v;
+      else
+        static_cast<uint16_t*>(y)[i + k] = T::from_f32(v);
+    }
+  }
+}
+
 }  // namespace
 
-hipError_t launch_fp8_gemm(const Fp8GemmArgs& a, hipStream_t s) {
+int64_t fp8_partial_bytes(int64_t M, int64_t N, int32_t blocks) {
+  const int splits = splits_of(M, N, blocks);
+  return splits > 1 ? 4 * M * N * splits : 0;
+}
+
+hipError_t launch_fp8_gemm(const Fp8GemmArgs& given, hipStream_t s) {
+  Fp8GemmArgs a = given;
+  a.splits = 1;
   if (a.x16 || streams(a)) return launch_fp8_stream(a, s);
+  if (a.mode == kFp8Plain && a.partial) {
+    a.splits = splits_of(a.M, a.N, a.blocks);
+    a.y = a.partial;
+    hipError_t e = a.dtype == SPL_F32 ? launch_tile<F32Out, true, 4, 2, 2, 2, 3>(a, s) : launch_tile<F32Out, false, 4, 2, 2, 2, 3>(a, s);
+    if (e != hipSuccess) return e;
+    const int64_t n = a.M * a.N;
+    const dim3 grid((unsigned)((n + 1023) / 1024));
+    const float* from = static_cast<const float*>(a.partial);
+    if (a.dtype == SPL_F32)
+      hipLaunchKernelGGL(k_fp8_join<F32Out>, grid, dim3(256), 0, s, from, a.splits, n, given.y);
+    else if (a.dtype == SPL_BF16)
+      hipLaunchKernelGGL(k_fp8_join<Bf16>, grid, dim3(256), 0, s, from, a.splits, n, given.y);
+    else
+      hipLaunchKernelGGL(k_fp8_join<F16>, grid, dim3(256), 0, s, from, a.splits, n, given.y);
+    return hipGetLastError();
+  }
   if (a.dtype == SPL_F32) return by_size<F32Out>(a, s);
   return a.dtype == SPL_BF16 ? by_size<Bf16>(a, s) : by_size<F16>(a, s);
 }

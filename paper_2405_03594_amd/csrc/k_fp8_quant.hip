@@ -160,6 +160,32 @@ __global__ void __launch_bounds__(256) k_fp8_quantize(const Fp8QuantArgs a, cons
   }
 }
 
+// Rows only, a scale a row: 16 rows of 128 entries a workgroup, for calls of so few rows that waiting is their time.
+template <class T>
+__global__ void __launch_bounds__(256) k_fp8_quantize_rows(const Fp8QuantArgs a, const int wide) {
+  const int cg = threadIdx.x & 15, c = blockIdx.x * 128 + 8 * cg;
+  const int r = blockIdx.y * 16 + (threadIdx.x >> 4);
+  const int64_t z = blockIdx.z, at = (z * a.rows + r) * a.row_stride + c;
+  float v[8];
+  if (r < a.rows && wide && c + 8 <= a.cols) {
+    load8<T>(a.X, at, v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = r < a.rows && c + j < a.cols ? widen<T>(a.X, at + j) : 0.f;
+  }
+  uint32_t m = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) m = umax(m, mag(v[j]));
+  const uint32_t byte = fp8_scale_byte(row16_max(m));
+  const float f = fp8_inverse(byte);
+  u32x2 q = {fp8_four(v[0] * f, v[1] * f, v[2] * f, v[3] * f), fp8_four(v[4] * f, v[5] * f, v[6] * f, v[7] * f)};
+  if (byte == 255) q = u32x2{0x7f7f7f7fu, 0x7f7f7f7fu};
+  if (r >= a.rows) return;
+  *reinterpret_cast<u32x2*>(const_cast<uint8_t*>(a.out.codes) + z * a.out.code_stride + (int64_t)r * a.out.pitch + c) = q;
+  if (cg == 0)
+    const_cast<uint8_t*>(a.out.scales)[z * a.out.scale_stride + (int64_t)r * a.out.spitch + blockIdx.x] = (uint8_t)byte;
+}
+
 template <class T>
 hipError_t quantize(const Fp8QuantArgs& a, hipStream_t s) {
   const int64_t tiles = a.starts ? most_tiles(a.rows, a.groups, 128) : (a.rows + 127) / 128;
@@ -169,6 +195,11 @@ hipError_t quantize(const Fp8QuantArgs& a, hipStream_t s) {
   constexpr int E = std::is_same<T, F32In>::value ? 4 : 2;
   const int wide = (reinterpret_cast<uintptr_t>(a.X) & 15) == 0 && a.row_stride * E % 16 == 0;
   const bool r = a.out.codes, c = a.out_t.codes, big = (r ? a.out : a.out_t).shift == 7;
+  if (r && !c && !big && !a.starts && a.rows <= 1024) {
+    const dim3 few((unsigned)((a.cols + 127) / 128), (unsigned)((a.rows + 15) / 16), (unsigned)a.count);
+    hipLaunchKernelGGL(k_fp8_quantize_rows<T>, few, dim3(256), 0, s, a, wide);
+    return hipGetLastError();
+  }
 #define SPL_Q(R, C, B) hipLaunchKernelGGL((k_fp8_quantize<T, R, C, B>), grid, dim3(256), 0, s, a, wide)
   if (r && c) {
     if (big) SPL_Q(true, true, 128); else SPL_Q(true, true, 1);

@@ -239,6 +239,7 @@ template <class T>
 hipError_t rows16(const Fp8GemmArgs& a, hipStream_t s) {
   const int wide = (reinterpret_cast<uintptr_t>(a.x16) & 15) == 0 && a.x16_stride % 8 == 0;
   const int64_t wgs = (a.N + 31) / 32 * (a.mode == kFp8Rows ? (a.M < a.groups ? a.M : a.groups) : 1);
+  if (fp8_rows_each(a) > 16) return by_sum<T, 2, 1, 2, 4>(a, wide, s);
   if (wgs >= device_cus()) return by_sum<T, 1, 2, 2, 5>(a, wide, s);
   return by_sum<T, 1, 1, 2, 6>(a, wide, s);
 }

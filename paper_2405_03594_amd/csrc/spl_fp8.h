@@ -140,6 +140,7 @@ struct Fp8GemmArgs {
   int32_t blocks;                               // of 128 columns: the whole sum's, or (kFp8Sum) the most there can be
   int32_t dtype;                                // of y
   int32_t mode;
+  int32_t splits;                               // of the sum (set by the launcher)
   const int32_t* starts;
   int32_t groups;
   int32_t tokens;                               // kFp8Sum: the rows that starts counts
@@ -147,8 +148,15 @@ struct Fp8GemmArgs {
   int64_t x16_stride;
   int32_t x16_dtype;
   int32_t cols;                                 // of x16
+  void* partial;                                // fp8_partial_bytes, or NULL where that is 0
 };
 hipError_t launch_fp8_gemm(const Fp8GemmArgs& a, hipStream_t s);
+// Scratch of a plain product of codes whose sum is split over workgroups: fp32 [splits][M][N]; 0: it is not.  The same for
+// every type of y.
+int64_t fp8_partial_bytes(int64_t M, int64_t N, int32_t blocks);
+// Whether the kernel for few rows quantizes rows of 16 bits itself: each is read by every workgroup of 16 or 32 rows of W, so
+// only few are (of a group, where there are groups).
+inline bool fp8_fused(int64_t M, int64_t experts) { return M <= 32 || (experts > 1 && 3 * M <= 64 * experts); }
 
 struct AdamwHyper {
   double lr, beta1, beta2, eps;

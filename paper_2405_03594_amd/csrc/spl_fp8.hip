@@ -44,12 +44,13 @@ spl_status check_matrix(const spl_fp8_matrix* m) {
   return SPL_OK;
 }
 
-// Activations of 16 bits that a product quantizes itself: a row is read by every
-// workgroup of 16 rows of W, so only few are (of a group, where there are groups).
-bool fused(int64_t M, int64_t experts) { return M <= 16 * experts && M <= 64; }
-int64_t rows_workspace(int64_t M, int64_t cols, int64_t experts) {
-  if (fused(M, experts)) return 0;
-  return align256(M * spl::fp8_pitch(cols)) + align256(M * spl::fp8_spitch(cols));
+int64_t codes_workspace(int64_t M, int64_t N, int64_t cols) {
+  return align256(spl::fp8_partial_bytes(M, N, (int32_t)(spl::fp8_pitch(cols) / 128)));
+}
+int64_t rows_workspace(int64_t M, int64_t N, int64_t cols, int64_t experts) {
+  if (spl::fp8_fused(M, experts)) return 0;
+  return align256(M * spl::fp8_pitch(cols)) + align256(M * spl::fp8_spitch(cols)) +
+         (experts == 1 ? codes_workspace(M, N, cols) : 0);
 }
 bool product_ok(int64_t M, int64_t N, int64_t cols, int64_t experts) {
   return M >= 0 && M < kMaxRows && (M == 0 || sizes_ok(M, cols, 1)) && sizes_ok(N, cols, experts) &&
@@ -66,7 +67,7 @@ spl_status rows_product(const void* X, int32_t x_dtype, int64_t M, int64_t row_s
   if (M == 0) return SPL_OK;
   if (row_stride < W->cols || row_stride > kMaxBytes / M || !given(X, 2) || !given(Y, 16) || !aligned(starts, 4))
     return SPL_ERR_INVALID_ARG;
-  const int64_t need = rows_workspace(M, W->cols, W->count);
+  const int64_t need = rows_workspace(M, W->rows, W->cols, W->count);
   if (need > 0 && !given(workspace, 256)) return SPL_ERR_INVALID_ARG;
   if (M > kMaxCols) return SPL_ERR_UNSUPPORTED;
   (void)hipGetLastError();
@@ -86,6 +87,8 @@ spl_status rows_product(const void* X, int32_t x_dtype, int64_t M, int64_t row_s
   const hipError_t e = spl::launch_fp8_quantize(z, x_dtype, stream);
   if (e != hipSuccess) return launched(e);
   a.x = z.out;
+  const int64_t codes = align256(M * a.w.pitch) + align256(M * a.w.spitch);
+  if (!starts && need > codes) a.partial = base + codes;
   return launched(spl::launch_fp8_gemm(a, stream));
 }
 
@@ -150,7 +153,7 @@ spl_status spl_dequantize_fp8(const spl_fp8_matrix* A, int32_t dtype, void* out,
 }
 
 int64_t spl_linear_fp8_workspace_bytes(int64_t M, int64_t N, int64_t cols) {
-  return M >= 1 && product_ok(M, N, cols, 1) ? 0 : -1;
+  return M >= 1 && product_ok(M, N, cols, 1) ? codes_workspace(M, N, cols) : -1;
 }
 spl_status spl_linear_fp8(const spl_fp8_matrix* X, const spl_fp8_matrix* W, int32_t dtype, void* Y, void* workspace,
                           hipStream_t stream) {
@@ -163,12 +166,16 @@ spl_status spl_linear_fp8(const spl_fp8_matrix* X, const spl_fp8_matrix* W, int3
   Fp8GemmArgs a{};
   a.x = spl::fp8_view(*X), a.w = spl::fp8_view(*W);
   a.M = X->rows, a.N = W->rows, a.blocks = a.w.pitch / 128, a.dtype = dtype, a.y = Y, a.mode = spl::kFp8Plain;
+  if (spl::fp8_partial_bytes(a.M, a.N, a.blocks) > 0) {
+    if (!given(workspace, 256)) return SPL_ERR_INVALID_ARG;
+    a.partial = workspace;
+  }
   (void)hipGetLastError();
   return launched(spl::launch_fp8_gemm(a, stream));
 }
 
 int64_t spl_linear_fp8_rows_workspace_bytes(int64_t M, int64_t N, int64_t cols) {
-  return product_ok(M, N, cols, 1) ? (M == 0 ? 0 : rows_workspace(M, cols, 1)) : -1;
+  return product_ok(M, N, cols, 1) ? (M == 0 ? 0 : rows_workspace(M, N, cols, 1)) : -1;
 }
 spl_status spl_linear_fp8_rows(const void* X, int32_t x_dtype, int64_t M, int64_t row_stride, const spl_fp8_matrix* W,
                                int32_t dtype, void* Y, void* workspace, hipStream_t stream) {
@@ -194,7 +201,7 @@ spl_status spl_linear_fp8_grouped(const spl_fp8_matrix* X, const spl_fp8_matrix*
 }
 
 int64_t spl_linear_fp8_grouped_rows_workspace_bytes(int64_t M, int64_t N, int64_t cols, int64_t experts) {
-  return product_ok(M, N, cols, experts) ? (M == 0 ? 0 : rows_workspace(M, cols, experts)) : -1;
+  return product_ok(M, N, cols, experts) ? (M == 0 ? 0 : rows_workspace(M, N, cols, experts)) : -1;
 }
 spl_status spl_linear_fp8_grouped_rows(const void* X, int32_t x_dtype, int64_t M, int64_t row_stride,
                                        const spl_fp8_matrix* W, const int32_t* starts, int32_t dtype, void* Y,
