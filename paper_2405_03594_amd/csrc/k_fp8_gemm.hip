@@ -428,10 +428,12 @@ hipError_t by_size(const Fp8GemmArgs& a, hipStream_t s) {
   }
 }
 
-// Whether the streaming kernel is the one: up to 32 rows of a matrix; up to 64 where tiles of 128 x 64 would take longer
+// Whether the streaming kernel is the one: up to 32 rows of a matrix, of a group 16 (us, streaming / tiles, 5632 x 2048, 8
+// experts: 32 rows 17.7 / 20.1, 64 22.9 / 22.1, 128 31.3 / 23.6); up to 64 where tiles of 128 x 64 would take longer
 // (us, streaming / tiles, 64 rows: 4096 x 4096 11.1 / 16.2, 4096 x 11008 25.5 / 33, 11008 x 4096 31 / 20.6).
 bool streams(const Fp8GemmArgs& a) {
   const double each = fp8_rows_each(a);
+  if (a.mode == kFp8Rows) return each <= 16;
   if (each <= 32) return true;
   if (each > 64 || a.mode != kFp8Plain || splits_of(a.M, a.N, a.blocks) > 1) return false;
   const double cus = device_cus(), wgs = (double)((a.N + 31) / 32) * 2 / cus;

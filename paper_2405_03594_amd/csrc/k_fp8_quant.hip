@@ -160,7 +160,8 @@ __global__ void __launch_bounds__(256) k_fp8_quantize(const Fp8QuantArgs a, cons
   }
 }
 
-// Rows only, a scale a row: 16 rows of 128 entries a workgroup, for calls of so few rows that waiting is their time.
+// Rows only, a scale a row: 16 rows of 128 entries a workgroup, a piece a thread (us, so / by the kernel above: 1 x 4096 2.4 /
+// 4.1, 1024 x 4096 3.9 / 6.0, 2048 x 11008 12.2 / 14.2, 5.5 TB/s).
 template <class T>
 __global__ void __launch_bounds__(256) k_fp8_quantize_rows(const Fp8QuantArgs a, const int wide) {
   const int cg = threadIdx.x & 15, c = blockIdx.x * 128 + 8 * cg;
@@ -195,7 +196,7 @@ hipError_t quantize(const Fp8QuantArgs& a, hipStream_t s) {
   constexpr int E = std::is_same<T, F32In>::value ? 4 : 2;
   const int wide = (reinterpret_cast<uintptr_t>(a.X) & 15) == 0 && a.row_stride * E % 16 == 0;
   const bool r = a.out.codes, c = a.out_t.codes, big = (r ? a.out : a.out_t).shift == 7;
-  if (r && !c && !big && !a.starts && a.rows <= 1024) {
+  if (r && !c && !big && !a.starts) {
     const dim3 few((unsigned)((a.cols + 127) / 128), (unsigned)((a.rows + 15) / 16), (unsigned)a.count);
     hipLaunchKernelGGL(k_fp8_quantize_rows<T>, few, dim3(256), 0, s, a, wide);
     return hipGetLastError();
@@ -203,8 +204,10 @@ hipError_t quantize(const Fp8QuantArgs& a, hipStream_t s) {
 #define SPL_Q(R, C, B) hipLaunchKernelGGL((k_fp8_quantize<T, R, C, B>), grid, dim3(256), 0, s, a, wide)
   if (r && c) {
     if (big) SPL_Q(true, true, 128); else SPL_Q(true, true, 1);
+  } else if (r && big) {
+    SPL_Q(true, false, 128);
   } else if (r) {
-    if (big) SPL_Q(true, false, 128); else SPL_Q(true, false, 1);
+    SPL_Q(true, false, 1);                           // rows of groups
   } else {
     if (big) SPL_Q(false, true, 128); else SPL_Q(false, true, 1);
   }

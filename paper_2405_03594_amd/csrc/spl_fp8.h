@@ -154,9 +154,13 @@ hipError_t launch_fp8_gemm(const Fp8GemmArgs& a, hipStream_t s);
 // Scratch of a plain product of codes whose sum is split over workgroups: fp32 [splits][M][N]; 0: it is not.  The same for
 // every type of y.
 int64_t fp8_partial_bytes(int64_t M, int64_t N, int32_t blocks);
-// Whether the kernel for few rows quantizes rows of 16 bits itself: each is read by every workgroup of 16 or 32 rows of W, so
-// only few are (of a group, where there are groups).
-inline bool fp8_fused(int64_t M, int64_t experts) { return M <= 32 || (experts > 1 && 3 * M <= 64 * experts); }
+// Whether the kernel for few rows quantizes rows of 16 bits itself, which every workgroup of 16 or 32 rows of W does anew:
+// up to 16 rows of a matrix, up to 32 of a small one (us, fused / two launches: 24 x 1111 x 1000 6.3 / 9.3, 24 x 4096 x 4096 12.6 / 12.2,
+// 24 x 11008 x 4096 28 / 24, 16 x 11008 x 4096 20 / 19 and a launch's host time).
+inline bool fp8_fused(int64_t M, int64_t N, int64_t cols, int64_t experts) {
+  if (experts > 1) return 3 * M <= 32 * experts;
+  return M <= 16 || (M <= 32 && N * cols <= (int64_t)1 << 24);
+}
 
 struct AdamwHyper {
   double lr, beta1, beta2, eps;

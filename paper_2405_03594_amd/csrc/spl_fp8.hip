@@ -48,7 +48,7 @@ int64_t codes_workspace(int64_t M, int64_t N, int64_t cols) {
   return align256(spl::fp8_partial_bytes(M, N, (int32_t)(spl::fp8_pitch(cols) / 128)));
 }
 int64_t rows_workspace(int64_t M, int64_t N, int64_t cols, int64_t experts) {
-  if (spl::fp8_fused(M, experts)) return 0;
+  if (spl::fp8_fused(M, N, cols, experts)) return 0;
   return align256(M * spl::fp8_pitch(cols)) + align256(M * spl::fp8_spitch(cols)) +
          (experts == 1 ? codes_workspace(M, N, cols) : 0);
 }
