@@ -815,6 +815,23 @@ spl_status spl_linear_fp8_grouped_weight_grad(const spl_fp8_matrix* dYt, const s
                                               const int32_t* starts, int64_t experts, int64_t tokens, int32_t dtype,
                                               void* dW, hipStream_t stream);
 
+/* Both gradients of spl_linear_fp8_rows or, with starts, of spl_linear_fp8_grouped_rows, from dY [M][N] and X [M][K] of
+ * dtype (fp16 or bf16), rows dy_stride and x_stride elements apart:
+ *   dX [M][K] = dY W, of dtype;    dW [experts][N][K] = dY^T X, of grad_dtype;
+ * both sums in 8-bit floats, dY quantized along its columns for dX, dY and X along their
+ * rows (a group's from its own start on) for dW, as by the calls above.
+ *   Wt           the transposed weights: Wt->count matrices [K][N].
+ *   starts       NULL (Wt->count 1), or as above: rows of no expert are not written
+ *                in dX, an expert without rows has a dW of zeros.
+ *   dX, dW       16-byte aligned; one of them may be NULL.
+ *   workspace    spl_linear_fp8_grad_workspace_bytes(M, N, K, experts) bytes (experts 0:
+ *                without starts), 256-byte aligned.
+ * M == 0: dW is zeros. */
+int64_t spl_linear_fp8_grad_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t experts);
+spl_status spl_linear_fp8_grad(const void* dY, int64_t dy_stride, const void* X, int64_t x_stride, int32_t dtype,
+                               int64_t M, const spl_fp8_matrix* Wt, const int32_t* starts, int32_t grad_dtype,
+                               void* dX, void* dW, void* workspace, hipStream_t stream);
+
 /* AdamW over many tensors in one launch.  Per element, in fp32, every product and
  * sum rounded on its own, with t = step:
  *   g = grad * *grad_scale             (no product without grad_scale)

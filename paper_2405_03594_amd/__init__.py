@@ -215,6 +215,8 @@ def lib() -> ctypes.CDLL:
         "spl_linear_fp8_grouped_rows_workspace_bytes": (I64, [I64, I64, I64, I64]),
         "spl_linear_fp8_grouped_rows": (ctypes.c_int, [P, I32, I64, I64, MQ, P, I32, P, P, P]),
         "spl_linear_fp8_grouped_weight_grad": (ctypes.c_int, [MQ, MQ, P, I64, I64, I32, P, P]),
+        "spl_linear_fp8_grad_workspace_bytes": (I64, [I64, I64, I64, I64]),
+        "spl_linear_fp8_grad": (ctypes.c_int, [P, I64, P, I64, I32, I64, MQ, P, I32, P, P, P, P]),
         "spl_adamw_plan_chunks": (I64, [TP, I64, YP]),
         "spl_adamw_plan_bytes": (I64, [TP, I64, YP]),
         "spl_adamw_plan": (ctypes.c_int, [TP, I64, YP, P]),
@@ -1329,13 +1331,14 @@ _CODE_TYPES = (torch.uint8, torch.float8_e4m3fn)
 
 def _here(names: str, stream, *tensors) -> torch.device:
     """The device of the call, which is the current one: every tensor is on it, and so is the stream."""
-    at = torch._C._cuda_getDevice() if any(t is not None and t.is_cuda for t in tensors) else -1
+    first = tensors[0]
+    at = torch._C._cuda_getDevice() if first.is_cuda else -1
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != at):
+        if t is not None and (t.get_device() != at or at < 0):
             raise ValueError(f"{names}: tensors of the current device only")
     if stream is not None and isinstance(stream, torch.cuda.Stream) and stream.device_index != at:
         raise ValueError("the stream must be of the current device")
-    return tensors[0].device
+    return first.device
 
 
 class Fp8Matrix:
@@ -1362,7 +1365,8 @@ class Fp8Matrix:
 
     def block_scales(self) -> torch.Tensor:
         """The scale bytes (e + 127) without the padding of their rows: [..., ceil(rows / block), ceil(cols / 128)]."""
-        return self.scales[..., :(self.cols + 127) // 128]
+        scales, blocks = self.scales, (self.cols + 127) // 128
+        return scales if scales.shape[-1] == blocks else scales[..., :blocks]
 
     def view(self) -> _Fp8:
         """The matrix as a call takes it: of the attributes as they are now."""
@@ -1382,16 +1386,14 @@ class Fp8Matrix:
 
     @classmethod
     def empty(cls, rows: int, cols: int, block: int = 1, count: int | None = None, device="cuda", stream=None):
-        L, n = lib(), 1 if count is None else count
-        need = L.spl_fp8_scales_bytes(rows, cols, n, _int32(block, "block"))
-        if need < 0:
-            raise ValueError(f"no matrix of {n} x {rows} x {cols} with blocks of {block} rows")
-        lead = () if count is None else (count,)
-        codes = _result((*lead, rows, (cols + 127) // 128 * 128), torch.uint8, device, stream)
-        scales = _result((*lead, (rows + block - 1) // block, ((cols + 127) // 128 + 3) // 4 * 4), torch.uint8, device,
-                         stream)
+        _fp8_workspace("spl_fp8_scales_bytes", rows, cols, 1 if count is None else count, block)   # refuses the sizes
+        blocks = (cols + 127) // 128
+        codes, scales = (rows, 128 * blocks), ((rows + block - 1) // block, (blocks + 3) // 4 * 4)
+        if count is not None:
+            codes, scales = (count, *codes), (count, *scales)
         m = object.__new__(cls)
-        m.codes, m.scales, m.cols, m.block = codes, scales, cols, block
+        m.codes, m.scales = _result(codes, torch.uint8, device, stream), _result(scales, torch.uint8, device, stream)
+        m.cols, m.block = cols, block
         return m
 
     @classmethod
@@ -1515,14 +1517,16 @@ def _fp8_out(out, M: int, N: int, dtype, X, device, stream) -> torch.Tensor:
     return _result((M, N), dtype, device, stream)
 
 
-def _fp8_rows(X, cols: int):
+def _fp8_rows(X, cols: int, name: str = "X"):
     """(rows, row stride) of the activations of a product: 16-bit floats."""
     if not isinstance(X, torch.Tensor) or X.dim() != 2 or X.dtype not in _HEAD_TYPES or X.shape[1] != cols:
-        raise ValueError(f"X must be an Fp8Matrix or fp16 / bf16 [rows, {cols}]")
+        raise ValueError(f"{name} must be an Fp8Matrix or fp16 / bf16 [rows, {cols}]")
     rows = X.shape[0]
-    stride = X.stride(0) if rows > 1 else cols
-    if (cols > 1 and X.stride(1) != 1) or stride < cols:
-        raise ValueError("X: columns must be contiguous")
+    stride, step = X.stride()
+    if rows <= 1:
+        stride = cols
+    if (step != 1 and cols > 1) or stride < cols:
+        raise ValueError(f"{name}: columns must be contiguous")
     return rows, stride
 
 
@@ -1556,28 +1560,39 @@ def linear_fp8(X, W: Fp8Matrix, dtype: torch.dtype | None = None, out: torch.Ten
     return out
 
 
-def _gradient_args(dY, X, Wt: Fp8Matrix, grad_dtype):
+def _gradients(dY, X, Wt: Fp8Matrix, starts, grad_dtype, stream):
     for t, name in ((dY, "dY"), (X, "X")):
         if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype not in _HEAD_TYPES:
             raise ValueError(f"{name} must be fp16 or bf16 [rows, columns]")
-    if X.shape[0] != dY.shape[0] or X.dtype != dY.dtype or X.shape[1] != Wt.rows or dY.shape[1] != Wt.cols:
-        raise ValueError(f"dY {list(dY.shape)}, X {list(X.shape)} and the transposed weight [{Wt.rows}, {Wt.cols}] do not "
-                         "belong together")
+    view = Wt.view()
+    K, N, E = view.rows, view.cols, view.count
+    M = X.shape[0]
+    if dY.shape[0] != M or X.dtype != dY.dtype or X.shape[1] != K or dY.shape[1] != N:
+        raise ValueError(f"dY {list(dY.shape)}, X {list(X.shape)} and the transposed weight [{K}, {N}] do not belong "
+                         "together")
     if grad_dtype not in _FLOAT_TYPES:
         raise ValueError("grad_dtype must be fp16, bf16 or fp32")
+    if starts is None and E != 1:
+        raise ValueError("Wt is several matrices: linear_fp8_grouped_grad")
+    (_, dys), (_, xs) = _fp8_rows(dY, N, "dY"), _fp8_rows(X, K)
+    device = _here("dY, X, Wt, starts", stream, dY, X, Wt.codes, Wt.scales, starts)
+    dX = _result((M, K), dY.dtype, device, stream)
+    dW = _result((N, K) if starts is None else (E, N, K), grad_dtype, device, stream)
+    need = _fp8_workspace("spl_linear_fp8_grad_workspace_bytes", M, N, K, 0 if starts is None else E)
+    ws = _workspace_on(need, device, stream) if need else None
+    _check("spl_linear_fp8_grad",
+           lib().spl_linear_fp8_grad(dY.data_ptr(), dys, X.data_ptr(), xs, _TORCH_DTYPE[X.dtype], M, view,
+                                     None if starts is None else starts.data_ptr(), _FLOAT_TYPES[grad_dtype],
+                                     dX.data_ptr(), dW.data_ptr(), _ptr(ws), _on(stream)))
+    return dX, dW
 
 
 def linear_fp8_grad(dY: torch.Tensor, X: torch.Tensor, Wt: Fp8Matrix, grad_dtype: torch.dtype = torch.float32,
                     stream=None):
     """(dX, dW) of Y = X W^T from dY [M, N] and X [M, K] (fp16 or bf16): dX = dY W in their type, dW = dY^T X in
-    grad_dtype, both sums in 8-bit floats, dY quantized along its columns for dX, dY and X along their rows for dW.
-    Wt: the transposed weight [K, N], as quantize_fp8_both makes it."""
-    _gradient_args(dY, X, Wt, grad_dtype)
-    if dY.shape[0] < 1:
-        raise ValueError("no rows")
-    q, qt = quantize_fp8_both(dY, stream=stream)
-    xt = quantize_fp8(X, transposed=True, stream=stream)
-    return linear_fp8(q, Wt, dtype=dY.dtype, stream=stream), linear_fp8(qt, xt, dtype=grad_dtype, stream=stream)
+    grad_dtype, both sums in 8-bit floats (see spl_linear_fp8_grad).  Wt: the transposed weight [K, N], as
+    quantize_fp8_both makes it.  A dW of 16 bits is summed at twice the rate of an fp32 one."""
+    return _gradients(dY, X, Wt, None, grad_dtype, stream)
 
 
 def linear_fp8_grouped(X, W: Fp8Matrix, starts: torch.Tensor, dtype: torch.dtype | None = None,
@@ -1613,18 +1628,23 @@ def linear_fp8_grouped_grad(dY: torch.Tensor, X: torch.Tensor, Wt: Fp8Matrix, st
                             grad_dtype: torch.dtype = torch.float32, stream=None):
     """(dX, dW) of linear_fp8_grouped as linear_fp8_grad's, Wt the transposed weights [experts, K, N], dW [experts, N, K]
     with zeros for an expert without rows.  Rows of no expert are not written in dX."""
-    _gradient_args(dY, X, Wt, grad_dtype)
     _starts(starts, Wt.count)
-    if dY.shape[0] < 1:
-        raise ValueError("no rows")
-    q, qt = quantize_fp8_both(dY, starts=starts, stream=stream)
-    xt = quantize_fp8(X, transposed=True, starts=starts, stream=stream)
-    dX = linear_fp8_grouped(q, Wt, starts, dtype=dY.dtype, stream=stream)
-    dW = _result((Wt.count, dY.shape[1], X.shape[1]), grad_dtype, dY.device, stream)
+    return _gradients(dY, X, Wt, starts, grad_dtype, stream)
+
+
+def linear_fp8_grouped_weight_grad(dYt: Fp8Matrix, Xt: Fp8Matrix, starts: torch.Tensor, tokens: int,
+                                   dtype: torch.dtype = torch.float32, stream=None) -> torch.Tensor:
+    """dW [experts, N, K] from the transposes of dY and X, `tokens` rows each, that quantize_fp8 made with the same starts
+    (see spl_linear_fp8_grouped_weight_grad): for a program that quantizes X once for both passes."""
+    a, b, E = dYt.view(), Xt.view(), _starts(starts)
+    if dtype not in _FLOAT_TYPES:
+        raise ValueError("dtype must be fp16, bf16 or fp32")
+    device = _here("dYt, Xt, starts", stream, dYt.codes, dYt.scales, Xt.codes, Xt.scales, starts)
+    dW = _result((E, a.rows, b.rows), dtype, device, stream)
     _check("spl_linear_fp8_grouped_weight_grad",
-           lib().spl_linear_fp8_grouped_weight_grad(qt.view(), xt.view(), starts.data_ptr(), Wt.count, dY.shape[0],
-                                                    _FLOAT_TYPES[grad_dtype], dW.data_ptr(), _on(stream)))
-    return dX, dW
+           lib().spl_linear_fp8_grouped_weight_grad(a, b, starts.data_ptr(), E, tokens, _FLOAT_TYPES[dtype],
+                                                    dW.data_ptr(), _on(stream)))
+    return dW
 
 
 # ------------------------------------------------------------------------------ the optimizer step

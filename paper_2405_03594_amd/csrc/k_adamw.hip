@@ -1,7 +1,7 @@
 // AdamW over many tensors in one launch, for gfx950 (the formulas stand in spl.h).
 //
-// A plan lists the tensors and cuts them into chunks of 8192 elements, one a
-// workgroup; a thread has 8 neighbouring elements at a time, so that 8-bit
+// A plan lists the tensors and cuts them into chunks of 2048 or 8192 elements, one
+// a workgroup; a thread has 8 neighbouring elements at a time, so that 8-bit
 // states' blocks of 128 are 16 neighbouring lanes and their scales come from
 // four lane moves.  Everything is read and written once.
 #include <string.h>
@@ -13,7 +13,9 @@
 namespace spl {
 namespace {
 
-constexpr int kThreads = 256, kEach = 8, kChunk = 8192;
+constexpr int kThreads = 256, kEach = 8;
+// Elements of a chunk: a workgroup's one turn where all tensors together do not fill the chip anyway, else four of them.
+constexpr int64_t kTurn = kThreads * kEach, kFew = 2048 * kTurn;
 
 struct Tensor {
   void* p;
@@ -29,10 +31,15 @@ struct Tensor {
   int32_t pad_;
 };
 struct Chunk {
+  int64_t begin;
   int32_t tensor;
-  int32_t at;                                   // in chunks
+  int32_t size;
 };
-int64_t chunks_of(int64_t n) { return (n + kChunk - 1) / kChunk; }
+int64_t chunk_size(const spl_adamw_tensor* t, int64_t count) {
+  int64_t n = 0;
+  for (int64_t i = 0; i < count; ++i) n += t[i].n;
+  return n <= kFew ? kTurn : 4 * kTurn;
+}
 
 struct F32P {};
 template <class T>
@@ -158,8 +165,7 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const Tensor* tensors, const
   const float eps = (float)h.eps;
   uint32_t key = 0;
   if constexpr (k8) key = mix(mix(h.seed ^ ((uint32_t)step * 0x6A09E667u)) + (uint32_t)k.tensor);
-  const int64_t begin = (int64_t)k.at * kChunk;
-  const int64_t end = begin + kChunk < t.n ? begin + kChunk : t.n;
+  const int64_t begin = k.begin, end = begin + k.size;
   // whole waves go through the loop together: 8-bit blocks ask their neighbours
   for (int64_t at = begin; at < end; at += kThreads * kEach) {
     const int64_t i = at + kEach * (int64_t)threadIdx.x;
@@ -213,7 +219,7 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const Tensor* tensors, const
 template <class P, class G>
 hipError_t launch(const void* plan, int64_t chunks, const spl_adamw_types& ty, const AdamwHyper& h, hipStream_t s) {
   const Chunk* c = static_cast<const Chunk*>(plan);
-  const Tensor* t = reinterpret_cast<const Tensor*>(c + (chunks + 1) / 2 * 2);
+  const Tensor* t = reinterpret_cast<const Tensor*>(c + chunks);
   if (ty.state_bits == 8)
     hipLaunchKernelGGL((k_adamw<P, G, true>), dim3((unsigned)chunks), dim3(kThreads), 0, s, t, c, h, ty.copy_dtype);
   else
@@ -229,27 +235,30 @@ hipError_t by_grad(const void* plan, int64_t chunks, const spl_adamw_types& ty, 
 }  // namespace
 
 int64_t adamw_plan_chunks(const spl_adamw_tensor* t, int64_t count) {
+  const int64_t size = chunk_size(t, count);
   int64_t c = 0;
-  for (int64_t i = 0; i < count; ++i) c += chunks_of(t[i].n);
+  for (int64_t i = 0; i < count; ++i) c += (t[i].n + size - 1) / size;
   return c;
 }
 int64_t adamw_plan_bytes(const spl_adamw_tensor* t, int64_t count) {
-  return (adamw_plan_chunks(t, count) + 1) / 2 * 2 * (int64_t)sizeof(Chunk) + count * (int64_t)sizeof(Tensor);
+  return adamw_plan_chunks(t, count) * (int64_t)sizeof(Chunk) + count * (int64_t)sizeof(Tensor);
 }
 
-// The chunks, then (16-byte aligned) the tensors.
+// The chunks, then the tensors (both of 16 bytes' multiples).
+static_assert(sizeof(Chunk) % 16 == 0 && sizeof(Tensor) % 16 == 0, "alignment");
 void adamw_plan_write(const spl_adamw_tensor* t, int64_t count, const spl_adamw_types& ty, void* host) {
-  const int64_t chunks = adamw_plan_chunks(t, count);
+  const int64_t chunks = adamw_plan_chunks(t, count), size = chunk_size(t, count);
   memset(host, 0, (size_t)adamw_plan_bytes(t, count));
   Chunk* c = static_cast<Chunk*>(host);
-  Tensor* out = reinterpret_cast<Tensor*>(c + (chunks + 1) / 2 * 2);
+  Tensor* out = reinterpret_cast<Tensor*>(c + chunks);
   for (int64_t i = 0; i < count; ++i) {
     const spl_adamw_tensor& x = t[i];
     uintptr_t all = reinterpret_cast<uintptr_t>(x.param) | reinterpret_cast<uintptr_t>(x.grad);
     if (ty.state_bits == 32) all |= reinterpret_cast<uintptr_t>(x.m) | reinterpret_cast<uintptr_t>(x.v);
     if (ty.copy_dtype) all |= reinterpret_cast<uintptr_t>(x.copy);
     out[i] = Tensor{x.param, x.grad, x.m, x.v, x.m_scales, x.v_scales, x.copy, x.n, x.decay, (all & 15) == 0, 0};
-    for (int64_t k = 0; k < chunks_of(x.n); ++k) *c++ = Chunk{(int32_t)i, (int32_t)k};
+    for (int64_t k = 0; k < x.n; k += size)
+      *c++ = Chunk{k, (int32_t)i, (int32_t)(x.n - k < size ? x.n - k : size)};
   }
 }
 

@@ -229,6 +229,98 @@ spl_status spl_linear_fp8_grouped_weight_grad(const spl_fp8_matrix* dYt, const s
   return launched(spl::launch_fp8_gemm(a, stream));
 }
 
+// The workspace of both gradients: dY's codes, its transpose's, those of X's transpose, the split sums of either product.
+struct GradSpace {
+  int64_t tokens;                                       // columns of the transposes
+  int64_t q, q_scales, qt, qt_scales, xt, xt_scales, partial, bytes;   // offsets
+};
+static bool grad_space(int64_t M, int64_t N, int64_t K, int64_t experts, GradSpace* g) {
+  if (M < 1 || M > kMaxCols || N < 1 || N > kMaxCols || K < 1 || K > kMaxCols || experts < 0 || experts > kMaxCount)
+    return false;
+  g->tokens = experts ? spl_fp8_grouped_cols(M, experts) : M;
+  if (g->tokens < 0 || !sizes_ok(M, N, 1) || !sizes_ok(K, N, experts ? experts : 1) || !sizes_ok(N, g->tokens, 1) ||
+      !sizes_ok(K, g->tokens, 1))
+    return false;
+  int64_t at = 0;
+  const auto take = [&](int64_t n) {
+    const int64_t here = at;
+    at += align256(n);
+    return here;
+  };
+  g->q = take(M * spl::fp8_pitch(N)), g->q_scales = take(M * spl::fp8_spitch(N));
+  g->qt = take(N * spl::fp8_pitch(g->tokens)), g->qt_scales = take(N * spl::fp8_spitch(g->tokens));
+  g->xt = take(K * spl::fp8_pitch(g->tokens)), g->xt_scales = take(K * spl::fp8_spitch(g->tokens));
+  int64_t most = 0;
+  if (!experts) {
+    const int64_t x = codes_workspace(M, K, N), w = codes_workspace(N, K, M);
+    most = x > w ? x : w;
+  }
+  g->partial = take(most);
+  g->bytes = at;
+  return true;
+}
+
+int64_t spl_linear_fp8_grad_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t experts) {
+  GradSpace g;
+  if (M == 0) return N >= 1 && N <= kMaxCols && K >= 1 && K <= kMaxCols && experts >= 0 && experts <= kMaxCount ? 0 : -1;
+  return grad_space(M, N, K, experts, &g) ? g.bytes : -1;
+}
+spl_status spl_linear_fp8_grad(const void* dY, int64_t dy_stride, const void* X, int64_t x_stride, int32_t dtype,
+                               int64_t M, const spl_fp8_matrix* Wt, const int32_t* starts, int32_t grad_dtype,
+                               void* dX, void* dW, void* workspace, hipStream_t stream) {
+  const spl_status st = check_matrix(Wt);
+  if (st != SPL_OK) return st;
+  if (!half_type(dtype) || !float_type(grad_dtype)) return SPL_ERR_UNSUPPORTED;
+  const int64_t N = Wt->cols, K = Wt->rows, experts = starts ? Wt->count : 0;
+  if (M < 0 || (!starts && Wt->count != 1) || !aligned(starts, 4) || !aligned(dX, 16) || !aligned(dW, 16) || (!dX && !dW) ||
+      N > kMaxBytes / K / Wt->count)
+    return SPL_ERR_INVALID_ARG;
+  (void)hipGetLastError();
+  if (M == 0) {
+    if (!dW) return SPL_OK;
+    return launched(spl::launch_zero_fill(dW, Wt->count * N * K * (grad_dtype == SPL_F32 ? 2 : 1), stream));
+  }
+  GradSpace g;
+  if (!grad_space(M, N, K, experts, &g)) return SPL_ERR_UNSUPPORTED;
+  if (!given(dY, 2) || !given(X, 2) || dy_stride < N || x_stride < K || dy_stride > kMaxBytes / M ||
+      x_stride > kMaxBytes / M || !given(workspace, 256))
+    return SPL_ERR_INVALID_ARG;
+  uint8_t* base = static_cast<uint8_t*>(workspace);
+  const auto view = [&](int64_t codes, int64_t scales, int64_t rows, int64_t cols) {
+    spl_fp8_matrix m{};
+    m.codes = base + codes, m.scales = base + scales, m.rows = rows, m.cols = cols, m.count = 1, m.block = 1;
+    return spl::fp8_view(m);
+  };
+  const spl::Fp8View q = view(g.q, g.q_scales, M, N), qt = view(g.qt, g.qt_scales, N, g.tokens),
+                     xt = view(g.xt, g.xt_scales, K, g.tokens);
+  spl::Fp8QuantArgs z{};
+  z.X = dY, z.row_stride = dy_stride, z.rows = M, z.cols = N, z.count = 1, z.starts = starts, z.groups = (int32_t)experts;
+  if (dX) z.out = q;
+  if (dW) z.out_t = qt;
+  hipError_t e = spl::launch_fp8_quantize(z, dtype, stream);
+  if (e == hipSuccess && dW) {
+    z.X = X, z.row_stride = x_stride, z.cols = K, z.out = spl::Fp8View{}, z.out_t = xt;
+    e = spl::launch_fp8_quantize(z, dtype, stream);
+  }
+  void* partial = base + g.partial;
+  if (e == hipSuccess && dX) {
+    Fp8GemmArgs a{};
+    a.x = q, a.w = spl::fp8_view(*Wt), a.M = M, a.N = K, a.blocks = a.w.pitch / 128, a.dtype = dtype, a.y = dX;
+    a.mode = starts ? spl::kFp8Rows : spl::kFp8Plain, a.starts = starts, a.groups = (int32_t)experts;
+    if (!starts && spl::fp8_partial_bytes(M, K, a.blocks) > 0) a.partial = partial;
+    e = spl::launch_fp8_gemm(a, stream);
+  }
+  if (e == hipSuccess && dW) {
+    Fp8GemmArgs a{};
+    a.x = qt, a.w = xt, a.M = N, a.N = K, a.blocks = a.w.pitch / 128, a.dtype = grad_dtype, a.y = dW;
+    a.mode = starts ? spl::kFp8Sum : spl::kFp8Plain, a.starts = starts, a.groups = (int32_t)experts;
+    a.tokens = (int32_t)M;
+    if (!starts && spl::fp8_partial_bytes(N, K, a.blocks) > 0) a.partial = partial;
+    e = spl::launch_fp8_gemm(a, stream);
+  }
+  return launched(e);
+}
+
 static bool adamw_types(const spl_adamw_types* ty) {
   return ty && float_type(ty->param_dtype) && float_type(ty->grad_dtype) &&
          (ty->copy_dtype == 0 || half_type(ty->copy_dtype)) && (ty->state_bits == 32 || ty->state_bits == 8);
@@ -237,18 +329,17 @@ static bool adamw_tensors(const spl_adamw_tensor* t, int64_t count, const spl_ad
   if (!adamw_types(ty) || count < 0 || count >= kMaxRows || (count > 0 && !t)) return false;
   const int64_t pb = ty->param_dtype == SPL_F32 ? 4 : 2, gb = ty->grad_dtype == SPL_F32 ? 4 : 2;
   const bool eight = ty->state_bits == 8;
-  int64_t chunks = 0;
+  int64_t total = 0;
   for (int64_t i = 0; i < count; ++i) {
     if (t[i].n < 0 || t[i].n >= (int64_t)1 << 40 || !isfinite(t[i].decay)) return false;
+    if ((total += t[i].n) >= (int64_t)1 << 40) return false;
     if (t[i].n == 0) continue;
     if (!given(t[i].param, pb) || !given(t[i].grad, gb) || !given(t[i].m, eight ? 16 : 4) ||
         !given(t[i].v, eight ? 16 : 4) || (eight && (!t[i].m_scales || !t[i].v_scales)) ||
         (ty->copy_dtype != 0 && !given(t[i].copy, 2)))
       return false;
-    chunks += spl::adamw_plan_chunks(t + i, 1);
-    if (chunks >= (int64_t)1 << 24) return false;                   // workgroups of one launch
   }
-  return true;
+  return spl::adamw_plan_chunks(t, count) < (int64_t)1 << 24;       // workgroups of one launch
 }
 
 int64_t spl_adamw_plan_chunks(const spl_adamw_tensor* tensors, int64_t count, const spl_adamw_types* types) {

@@ -248,6 +248,28 @@ def test_linear_grad(mnk):
     _near(dw, a @ b.T, _bound(a, b, torch.float32), "dW")
     half = spl.linear_fp8_grad(dy.cuda(), x.cuda(), wt, grad_dtype=torch.bfloat16)[1]
     _near(half, a @ b.T, _bound(a, b, torch.bfloat16), "dW in bf16")
+    # the same from the calls that it stands for, bit for bit; from slices of wider products too
+    q, qt = spl.quantize_fp8_both(dy.cuda())
+    xt = spl.quantize_fp8(x.cuda(), transposed=True)
+    assert torch.equal(spl.linear_fp8(q, wt), dx)
+    assert torch.equal(spl.linear_fp8(qt, xt, dtype=torch.float32), dw)
+    wide = torch.cat((dy, x), 1).cuda()
+    again = spl.linear_fp8_grad(wide[:, :N], wide[:, N:], wt)
+    assert torch.equal(again[0], dx) and torch.equal(again[1], dw)
+
+
+def test_linear_grad_without_rows():
+    spl = _spl()
+    none = torch.zeros((0, 40), dtype=torch.bfloat16, device="cuda")
+    _, wt = spl.quantize_fp8_both(torch.ones((40, 40), device="cuda"), 128)
+    for dt in FLOATS:
+        dx, dw = spl.linear_fp8_grad(none, none, wt, grad_dtype=dt)
+        assert dx.shape == (0, 40) and (dw == 0).all()
+    many = spl.Fp8Matrix(wt.codes.repeat(3, 1, 1), wt.scales.repeat(3, 1, 1), 40, 128)
+    dx, dw = spl.linear_fp8_grouped_grad(none, none, many, torch.zeros(4, dtype=torch.int32, device="cuda"))
+    assert dx.shape == (0, 40) and dw.shape == (3, 40, 40) and (dw == 0).all()
+    assert spl.linear_fp8(none, wt).shape == (0, 40)
+    assert spl.linear_fp8_grouped(none, many, torch.zeros(4, dtype=torch.int32, device="cuda")).shape == (0, 40)
 
 
 def test_gradients_against_differences():
@@ -323,6 +345,8 @@ def test_grouped_grad(case):
             _near(dx[a:b], hdy @ hw, _bound(hdy, hw.T, torch.bfloat16), f"dX of {e}")
             p, q = ref.round_trip(_np(dy[a:b]).T), ref.round_trip(_np(x[a:b]).T)
             _near(dw[e], p @ q.T, _bound(p, q, dt), f"dW of {e}")
+        qt, xt = (spl.quantize_fp8(t.cuda(), transposed=True, starts=at) for t in (dy, x))
+        assert torch.equal(spl.linear_fp8_grouped_weight_grad(qt, xt, at, M, dtype=dt), dw)
 
 
 def test_grouped_bad_starts():
