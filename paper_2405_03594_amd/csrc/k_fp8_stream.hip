@@ -38,26 +38,6 @@ __device__ __forceinline__ void load16(const uint16_t* row, int c, int cols, boo
   }
 }
 
-typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-typedef short s16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ uint32_t max16(uint32_t a, uint32_t b) {
-  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
-}
-// Four values of 16 bits, divided by a power of two, to codes.
-template <class T>
-__device__ __forceinline__ uint32_t code4(uint32_t a, uint32_t b, float scale) {
-  s16x2 z = {0, 0};
-  if constexpr (std::is_same<T, Bf16>::value) {
-    z = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(z, __builtin_bit_cast(bf16x2, a), scale, false);
-    z = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(z, __builtin_bit_cast(bf16x2, b), scale, true);
-  } else {
-    z = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(z, __builtin_bit_cast(f16x2, a), scale, false);
-    z = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(z, __builtin_bit_cast(f16x2, b), scale, true);
-  }
-  return __builtin_bit_cast(uint32_t, z);
-}
 // The block's scale byte, and the lane's codes.
 template <class T>
 __device__ __forceinline__ uint32_t quantize(const Part<T>& v, u32x4& x0, u32x4& x1) {
@@ -65,18 +45,16 @@ __device__ __forceinline__ uint32_t quantize(const Part<T>& v, u32x4& x0, u32x4&
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) m = max16(m, v.q[i][j] & 0x7fff7fffu);
+    for (int j = 0; j < 4; ++j) m = max16(m, mag16(v.q[i][j]));
   m = umax(m & 0xffffu, m >> 16);
   m = umax(m, (uint32_t)__shfl_xor((int)m, 16));
   m = umax(m, (uint32_t)__shfl_xor((int)m, 32));
   const uint32_t byte = fp8_scale_byte(__float_as_uint(T::to_f32(m)));
-  // 2^-127, which blocks of zeros have, and of bf16 those whose largest is below 2^-118, is no normal number: taken by 2^-126
-  // and 2^-1 (of bf16: values below 2^-126 are none that the conversion keeps)
-  const float scale = byte == 0 ? 0x1p-127f : __uint_as_float(byte << 23);
+  const float scale = fp8_scale(byte);
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    x0[2 * j] = code4<T>(v.q[j][0], v.q[j][1], scale), x0[2 * j + 1] = code4<T>(v.q[j][2], v.q[j][3], scale);
-    x1[2 * j] = code4<T>(v.q[2 + j][0], v.q[2 + j][1], scale), x1[2 * j + 1] = code4<T>(v.q[2 + j][2], v.q[2 + j][3], scale);
+    x0[2 * j] = fp8_code4<T>(v.q[j][0], v.q[j][1], scale), x0[2 * j + 1] = fp8_code4<T>(v.q[j][2], v.q[j][3], scale);
+    x1[2 * j] = fp8_code4<T>(v.q[2 + j][0], v.q[2 + j][1], scale), x1[2 * j + 1] = fp8_code4<T>(v.q[2 + j][2], v.q[2 + j][3], scale);
   }
   if (byte == 255) x0 = x1 = u32x4{0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu};
   return byte;

@@ -53,6 +53,30 @@ __device__ __forceinline__ uint32_t fp8_four(float a, float b, float c, float d)
   return fp8_pair<true>(c, d, fp8_pair<false>(a, b, 0u));
 }
 
+// Two values of 16 bits in a word: the larger magnitudes of two words; four values, divided by the scale of a byte (bytes up
+// to 247 occur), to codes.  Exact powers of two, so the codes are those of the fp32 way.
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t max16(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+__device__ __forceinline__ uint32_t mag16(uint32_t a) { return a & 0x7fff7fffu; }
+__device__ __forceinline__ float fp8_scale(uint32_t byte) { return byte == 0 ? 0x1p-127f : __uint_as_float(byte << 23); }
+template <class T>
+__device__ __forceinline__ uint32_t fp8_code4(uint32_t a, uint32_t b, float scale) {
+  s16x2 z = {0, 0};
+  if constexpr (T::code == SPL_BF16) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    z = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(z, __builtin_bit_cast(bf16x2, a), scale, false);
+    z = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(z, __builtin_bit_cast(bf16x2, b), scale, true);
+  } else {
+    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+    z = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(z, __builtin_bit_cast(f16x2, a), scale, false);
+    z = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(z, __builtin_bit_cast(f16x2, b), scale, true);
+  }
+  return __builtin_bit_cast(uint32_t, z);
+}
+
 // The largest of a value over the 16 lanes of a row (unsigned compares: magnitudes' bits).
 __device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
 __device__ __forceinline__ uint32_t row16_max(uint32_t x) {

@@ -127,6 +127,49 @@ def test_quantize_special_values():
             assert np.array_equal(_np(spl.dequantize_fp8(got)), b.astype(np.float32).astype(np.float64), equal_nan=True)
 
 
+def _far(dtype):
+    """Rows of 16-bit values at both ends of the type: subnormals, the smallest normal ones, the largest, with zeros between."""
+    bits = [0x0001, 0x0003, 0x007F, 0x0080, 0x0081, 0x0100, 0x03FF, 0x0400, 0x0401, 0x0777, 0x0FFF, 0x1234]
+    top = 0x7F7F if dtype == torch.bfloat16 else 0x7BFF
+    rows = []
+    for hi in bits + [top, 0x3F80, 0x4321]:
+        row = torch.zeros(256, dtype=torch.int32)
+        row[0], row[129] = hi, hi
+        row[1:1 + len(bits)] = torch.tensor([min(b, hi) for b in bits])
+        row[140:140 + len(bits)] = torch.tensor([min(b, hi) | 0x8000 for b in bits])
+        rows.append(row)
+    return torch.stack(rows).to(torch.int16).view(dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_quantize_ends_of_the_type(dtype):
+    """The conversions of 16-bit types take their scale as it is, down to 2^-127, and subnormals as numbers."""
+    spl = _spl()
+    x = _far(dtype)
+    q, t = spl.quantize_fp8_both(x.cuda())
+    _same(q, ref.quantize(_np(x)), "rows")
+    _same(t, ref.quantize(_np(x).T), "transposed")
+    _same(spl.quantize_fp8(x.cuda()), ref.quantize(_np(x)), "rows alone")
+    for block in (1, 128):
+        big = x.repeat(20, 3)[:, :700]
+        a, b = spl.quantize_fp8_both(big.cuda(), block)
+        _same(a, ref.quantize(_np(big), block), "rows")
+        _same(b, ref.quantize(_np(big).T, block), "transposed")
+    # and in the product that quantizes on the way: rows times the identity are what the codes stand for.  bf16's largest
+    # number is 255 2^120, whose code is 256: 2^128, an infinity in every type of the result (and, where the sum is one of
+    # bf16 numbers, as for fp32 results, in all of the row)
+    eye = spl.quantize_fp8(torch.eye(256).cuda())
+    held = ref.round_trip(_np(x)[:15])
+    past = (np.abs(held) >= 2.0 ** 128).any(1)
+    assert past.sum() == (dtype == torch.bfloat16)
+    y = _np(spl.linear_fp8(x[:15].cuda(), eye, dtype=torch.float32))
+    normal = np.abs(held) >= 2.0 ** -126
+    assert np.array_equal(np.where(normal, y, 0)[~past], np.where(normal, held, 0)[~past])
+    assert (np.abs(y - held) <= 2.0 ** -126)[~past].all()
+    y = _np(spl.linear_fp8(x[:15].cuda(), eye, dtype=torch.bfloat16))
+    assert np.array_equal(np.where(normal, y, 0), np.where(np.abs(held) >= 2.0 ** 128, np.copysign(np.inf, held), np.where(normal, held, 0)))
+
+
 @pytest.mark.parametrize("dtype", FLOATS)
 def test_quantize_strided_and_counted(dtype):
     """A slice of a wider product (odd strides and addresses too), and several matrices at once."""
