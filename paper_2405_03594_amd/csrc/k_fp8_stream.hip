@@ -94,18 +94,20 @@ __global__ void __launch_bounds__(64 * kWaves, kEach) k_fp8_stream(const Fp8Gemm
     }
   }
   // A wave's blocks: 1, 2 or a multiple of 4 of them, so that the scale bytes of those requested together are of one word.
-  // Blocks before k0 and from k1 on are read and multiplied as zeros.
+  // Places before k0 and from k1 on take a block of the wave's again, with codes of zero for X: a NaN in it is in the sum anyway.
   static_assert(U == 4 || U == 2, "a word's blocks");
   const int start = p.k0 & ~3;
   int per = (p.k1 - start + kWaves - 1) / kWaves;
   per = per < 3 ? per : (per + 3) & ~3;
   const int b0 = start + wave * per, b1 = b0 + per < p.k1 ? b0 + per : p.k1;
+  const int first = b0 > p.k0 ? b0 : p.k0;
+  const auto block = [&](int b) { return b < first ? first : (b < b1 ? b : b1 - 1); };
   f32x4 acc[NR][MT];
 #pragma unroll
   for (int i = 0; i < NR; ++i)
 #pragma unroll
     for (int j = 0; j < MT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int b = b0; b < b1; b += U) {
+  for (int b = b0; b < b1 && first < b1; b += U) {
     // X first: it is near, and in 16 bits it is quantized while W is on its way
     Part<T> x[U][MT];
     Part<Codes> w[U][NR];
@@ -117,7 +119,7 @@ __global__ void __launch_bounds__(64 * kWaves, kEach) k_fp8_stream(const Fp8Gemm
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int at = b + u < b1 ? b + u : b1 - 1;
+      const int at = block(b + u);
 #pragma unroll
       for (int j = 0; j < MT; ++j) {
         if constexpr (kCodes) {
@@ -134,7 +136,7 @@ __global__ void __launch_bounds__(64 * kWaves, kEach) k_fp8_stream(const Fp8Gemm
     for (int i = 0; i < NR; ++i) sw[i] = *reinterpret_cast<const uint32_t*>(ws[i] + word);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int at = b + u < b1 ? b + u : b1 - 1;
+      const int at = block(b + u);
 #pragma unroll
       for (int i = 0; i < NR; ++i) {
         w[u][i].q[0] = *reinterpret_cast<const u32x4*>(wp[i] + 128 * (int64_t)at);

@@ -392,6 +392,36 @@ def test_grouped_grad(case):
         assert torch.equal(spl.linear_fp8_grouped_weight_grad(qt, xt, at, M, dtype=dt), dw)
 
 
+@pytest.mark.parametrize("N", [20, 200])
+@pytest.mark.parametrize("bad", [0, 1, 3, 4])
+def test_grouped_poisoned(N, bad):
+    """A NaN in one expert's rows is in its results alone, also where experts share a word of scales or a tile's edge."""
+    spl = _spl()
+    starts, K = [0, 130, 300, 300, 310, 440, 900], 150
+    at = torch.tensor(starts, dtype=torch.int32).cuda()
+    M, E = starts[-1], len(starts) - 1
+    x, dy = _x((M, K), torch.bfloat16, 1), _x((M, N), torch.bfloat16, 2)
+    w, wt = spl.quantize_fp8_both(_x((E, N, K), torch.float32, 3).cuda(), 128)
+    calls = lambda: (spl.linear_fp8_grouped(x.cuda(), w, at), *spl.linear_fp8_grouped_grad(dy.cuda(), x.cuda(), wt, at))  # noqa: E731
+    clean = calls()
+    row = starts[bad + 1] - 1
+    x[row, 7], dy[row, 3] = float("nan"), float("inf")
+    y, dx, dw = calls()
+    for e, (a, b) in enumerate(zip(starts, starts[1:])):
+        keep = torch.ones(M, dtype=torch.bool)
+        keep[row] = False
+        keep = keep[a:b]
+        assert torch.equal(y[a:b].cpu()[keep], clean[0][a:b].cpu()[keep]) and torch.equal(dx[a:b].cpu()[keep], clean[1][a:b].cpu()[keep])
+        if e == bad:
+            assert torch.isnan(y[row]).all() and torch.isnan(dx[row]).all()
+            assert torch.isnan(dw[e][3]).all() and torch.isnan(dw[e][:, 7]).all()
+            rest = torch.ones((N, K), dtype=torch.bool)
+            rest[3], rest[:, 7] = False, False
+            assert torch.equal(dw[e].cpu()[rest], clean[2][e].cpu()[rest])
+        else:
+            assert torch.equal(dw[e], clean[2][e]), e
+
+
 def test_grouped_bad_starts():
     """Starts out of range or falling: nothing past the tensors is touched, rows that no expert owns stay."""
     spl = _spl()
