@@ -17,7 +17,8 @@ constexpr int kThreads = 256, kEach = 8;
 // Elements of a chunk: a workgroup's one turn where all tensors together do not fill the chip anyway, else four of them.
 constexpr int64_t kTurn = kThreads * kEach, kFew = 2048 * kTurn;
 
-struct Tensor {
+// A chunk with its tensor's addresses, so that a workgroup's data is two trips to memory away.
+struct Chunk {
   void* p;
   const void* g;
   void* m;
@@ -25,15 +26,12 @@ struct Tensor {
   uint8_t* ms;
   uint8_t* vs;
   void* copy;
-  int64_t n;
-  double decay;
-  int32_t wide;                                 // every array is aligned for 16-byte (8-bit codes: 8-byte) accesses
-  int32_t pad_;
-};
-struct Chunk {
   int64_t begin;
-  int32_t tensor;
+  double decay;
   int32_t size;
+  int32_t tensor;
+  int32_t wide;                                 // every array is aligned for 16-byte (8-bit codes: 8-byte) accesses
+  int32_t pad_[3];
 };
 int64_t chunk_size(const spl_adamw_tensor* t, int64_t count) {
   int64_t n = 0;
@@ -151,12 +149,9 @@ __device__ __forceinline__ void decode8(const uint8_t* c, const uint8_t* s, int6
 }
 
 template <class P, class G, bool k8>
-__global__ void __launch_bounds__(kThreads) k_adamw(const Tensor* tensors, const Chunk* chunks, const AdamwHyper h,
-                                                    const int copy) {
+__global__ void __launch_bounds__(kThreads) k_adamw(const Chunk* chunks, const AdamwHyper h, const int copy) {
   const float gs = h.grad_scale ? *h.grad_scale : 1.f;
-  if (!isfinite(gs)) return;
-  const Chunk k = chunks[blockIdx.x];
-  const Tensor t = tensors[k.tensor];
+  const Chunk t = chunks[blockIdx.x];
   int64_t step = h.step_on_device ? *h.step_on_device : h.step;
   step = step < 1 ? 1 : step;
   const float keep = (float)(1.0 - h.lr * t.decay), rate = (float)(h.lr / (1.0 - power(h.beta1, step)));
@@ -164,8 +159,8 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const Tensor* tensors, const
   const float b1 = (float)h.beta1, c1 = (float)(1.0 - h.beta1), b2 = (float)h.beta2, c2 = (float)(1.0 - h.beta2);
   const float eps = (float)h.eps;
   uint32_t key = 0;
-  if constexpr (k8) key = mix(mix(h.seed ^ ((uint32_t)step * 0x6A09E667u)) + (uint32_t)k.tensor);
-  const int64_t begin = k.begin, end = begin + k.size;
+  if constexpr (k8) key = mix(mix(h.seed ^ ((uint32_t)step * 0x6A09E667u)) + (uint32_t)t.tensor);
+  const int64_t begin = t.begin, end = isfinite(gs) ? begin + t.size : begin;   // a scale that is not finite: nothing is updated
   // whole waves go through the loop together: 8-bit blocks ask their neighbours
   for (int64_t at = begin; at < end; at += kThreads * kEach) {
     const int64_t i = at + kEach * (int64_t)threadIdx.x;
@@ -219,11 +214,10 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const Tensor* tensors, const
 template <class P, class G>
 hipError_t launch(const void* plan, int64_t chunks, const spl_adamw_types& ty, const AdamwHyper& h, hipStream_t s) {
   const Chunk* c = static_cast<const Chunk*>(plan);
-  const Tensor* t = reinterpret_cast<const Tensor*>(c + chunks);
   if (ty.state_bits == 8)
-    hipLaunchKernelGGL((k_adamw<P, G, true>), dim3((unsigned)chunks), dim3(kThreads), 0, s, t, c, h, ty.copy_dtype);
+    hipLaunchKernelGGL((k_adamw<P, G, true>), dim3((unsigned)chunks), dim3(kThreads), 0, s, c, h, ty.copy_dtype);
   else
-    hipLaunchKernelGGL((k_adamw<P, G, false>), dim3((unsigned)chunks), dim3(kThreads), 0, s, t, c, h, ty.copy_dtype);
+    hipLaunchKernelGGL((k_adamw<P, G, false>), dim3((unsigned)chunks), dim3(kThreads), 0, s, c, h, ty.copy_dtype);
   return hipGetLastError();
 }
 template <class P>
@@ -241,24 +235,22 @@ int64_t adamw_plan_chunks(const spl_adamw_tensor* t, int64_t count) {
   return c;
 }
 int64_t adamw_plan_bytes(const spl_adamw_tensor* t, int64_t count) {
-  return adamw_plan_chunks(t, count) * (int64_t)sizeof(Chunk) + count * (int64_t)sizeof(Tensor);
+  return adamw_plan_chunks(t, count) * (int64_t)sizeof(Chunk);
 }
 
-// The chunks, then the tensors (both of 16 bytes' multiples).
-static_assert(sizeof(Chunk) % 16 == 0 && sizeof(Tensor) % 16 == 0, "alignment");
+static_assert(sizeof(Chunk) % 16 == 0, "alignment");
 void adamw_plan_write(const spl_adamw_tensor* t, int64_t count, const spl_adamw_types& ty, void* host) {
-  const int64_t chunks = adamw_plan_chunks(t, count), size = chunk_size(t, count);
+  const int64_t size = chunk_size(t, count);
   memset(host, 0, (size_t)adamw_plan_bytes(t, count));
   Chunk* c = static_cast<Chunk*>(host);
-  Tensor* out = reinterpret_cast<Tensor*>(c + chunks);
   for (int64_t i = 0; i < count; ++i) {
     const spl_adamw_tensor& x = t[i];
     uintptr_t all = reinterpret_cast<uintptr_t>(x.param) | reinterpret_cast<uintptr_t>(x.grad);
     if (ty.state_bits == 32) all |= reinterpret_cast<uintptr_t>(x.m) | reinterpret_cast<uintptr_t>(x.v);
     if (ty.copy_dtype) all |= reinterpret_cast<uintptr_t>(x.copy);
-    out[i] = Tensor{x.param, x.grad, x.m, x.v, x.m_scales, x.v_scales, x.copy, x.n, x.decay, (all & 15) == 0, 0};
     for (int64_t k = 0; k < x.n; k += size)
-      *c++ = Chunk{k, (int32_t)i, (int32_t)(x.n - k < size ? x.n - k : size)};
+      *c++ = Chunk{x.param, x.grad, x.m, x.v, x.m_scales, x.v_scales, x.copy, k, x.decay,
+                   (int32_t)(x.n - k < size ? x.n - k : size), (int32_t)i, (all & 15) == 0, {0, 0, 0}};
   }
 }
 

@@ -68,7 +68,12 @@ __global__ void __launch_bounds__(256) k_fp8_quantize(const Fp8QuantArgs a, cons
       load8<T>(a.X, at, v[i]);
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = r < rend && c + j < a.cols ? widen<T>(a.X, at + j) : 0.f;
+      for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+      if (r < rend && c < a.cols) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (c + j < a.cols) v[i][j] = widen<T>(a.X, at + j);
+      }
     }
   }
 
@@ -186,11 +191,13 @@ __global__ void __launch_bounds__(256) k_fp8_quantize16(const Fp8QuantArgs a, co
     if (r < rend && wide && c + 8 <= a.cols) {
       v[i] = *reinterpret_cast<const u32x4*>(row);
     } else {
+      v[i] = u32x4{0u, 0u, 0u, 0u};
+      if (r < rend && c < a.cols) {                  // (lanes past the columns do not wait for single loads)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t lo = r < rend && c + 2 * j < a.cols ? row[2 * j] : 0u;
-        const uint32_t hi = r < rend && c + 2 * j + 1 < a.cols ? row[2 * j + 1] : 0u;
-        v[i][j] = lo | (hi << 16);
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t lo = c + 2 * j < a.cols ? row[2 * j] : 0u, hi = c + 2 * j + 1 < a.cols ? row[2 * j + 1] : 0u;
+          v[i][j] = lo | (hi << 16);
+        }
       }
     }
   }
@@ -300,7 +307,12 @@ __global__ void __launch_bounds__(256) k_fp8_quantize_rows(const Fp8QuantArgs a,
     load8<T>(a.X, at, v);
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = r < a.rows && c + j < a.cols ? widen<T>(a.X, at + j) : 0.f;
+    for (int j = 0; j < 8; ++j) v[j] = 0.f;
+    if (r < a.rows && c < a.cols) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (c + j < a.cols) v[j] = widen<T>(a.X, at + j);
+    }
   }
   uint32_t m = 0;
 #pragma unroll
