@@ -355,11 +355,11 @@ hipError_t launch_mixed(const Fp8GemmArgs& a, int64_t tnb, hipStream_t s) {
 }
 
 // How long a call takes, in us, in tiles of one kind: rounds of the chip, each a fixed part and one for each stage, which
-// differs where a CU has one workgroup only.  Fitted to launches of 128 to 8192 rows (us, 256 x 256 tiles / 128 x 128 / the
-// same, one a CU and four stage buffers / 128 x 64): 8192 x 8192 x 8192 437 / 569 / 652 / 714, 2048 x 11008 x 4096 107 / 108 /
-// 126 / 132 (256 x 256 and then 256 x 128: 99), 2048 x 4096 x 4096 50 / 37.0 / 42.5 / 45.6, 1000 x 4096 x 4096 50 / 29.2 / 23.3 /
-// 25.4, 512 x 4096 x 4096 48 / 28.0 / 20.7 / 16.1; fp32 results, 128 x 256 / 128 x 128 / 128 x 64: 4096 x 4096 x 2048 67 / 69 / 82,
-// 1024 x 1024 x 2048 27 / 20.5 / 15.0.
+// differs where a CU has one workgroup only.  Fitted to launches of 128 to 8192 rows (us; 256 x 256 tiles / 256 x 128 of eight
+// waves and three stage buffers / 128 x 128, four stage buffers / 128 x 64): 8192 x 8192 x 8192 437 / 538 / 652 / 714, 2048 x
+// 11008 x 4096 107 / - / 126 / 132 (256 x 256, then 256 x 128 of four waves: 99), 2048 x 4096 x 4096 50 / 36.3 / 42.5 / 45.6, 1000 x
+// 4096 x 4096 50 / 30 / 23.3 / 25.4, 512 x 4096 x 4096 48 / 29 / 20.7 / 16.1, 4096 rows of 16 experts x 5632 x 2048 104 / 102 / 122 /
+// 116; fp32 results, 128 x 256 / 128 x 128 / 128 x 64: 4096 x 4096 x 2048 67 / 69 / 82, 1024 x 1024 x 2048 27 / 20.5 / 15.0.
 struct Cost {
   double fixed, full, alone;                         // a stage: with every place taken, with at most one workgroup a CU
   int places;                                        // workgroups of a CU
@@ -368,7 +368,7 @@ struct Cost {
     return whole * (fixed + full * stages) + (rest <= 0 ? 0 : fixed + (rest <= cus ? alone : full) * stages);
   }
 };
-constexpr Cost kLarge{12, 1.45, 1.45, 1}, kMiddle{9, 0.85, 0.85, 1}, kSmall{6, 0.97, 0.72, 2}, kDeep{6.5, 0.53, 0.53, 1},
+constexpr Cost kLarge{12, 1.45, 1.45, 1}, kMiddle{8, 0.88, 0.88, 1}, kRest{9, 0.85, 0.85, 1}, kDeep{6.5, 0.53, 0.53, 1},
     kNarrow{5, 0.6, 0.32, 2};
 constexpr Cost kLarge32{8, 1.6, 1.6, 1}, kSmall32{6, 1.75, 0.85, 2}, kNarrow32{5, 1.15, 0.6, 2};
 
@@ -410,21 +410,21 @@ hipError_t by_size(const Fp8GemmArgs& a, hipStream_t s) {
     return small <= large ? launch_tile<T, true, 4, 4, 2, 2, 2>(a, s) : launch_tile<T, true, 4, 4, 2, 4, 3>(a, s);
   } else {
     const double t256 = about_tiles(a, 256, 256);
-    const double large = kLarge.rounds(t256, st, cus), small = kSmall.rounds(t128, st, cus),
+    const double large = kLarge.rounds(t256, st, cus), middle = kMiddle.rounds(about_tiles(a, 256, 128), st, cus),
                  deep = kDeep.rounds(t128, st, cus), narrow = kNarrow.rounds(t64, st, cus);
-    double best = large < small ? large : small;
+    double best = large < middle ? large : middle;
     best = deep < best ? deep : best;
     best = narrow < best ? narrow : best;
     if (a.mode == kFp8Plain && t256 > cus) {           // whole rounds of large tiles, the rest of the columns in middle ones
       const int64_t tm = (a.M + 255) / 256, tn = (a.N + 255) / 256;
       const int64_t tnb = (int64_t)(t256 / cus) * cus / tm;
       const double mixed = kLarge.rounds((double)(tnb * tm), st, cus) +
-                           kMiddle.rounds((double)(tn - tnb) * (double)((a.M + 127) / 128), st, cus);
+                           kRest.rounds((double)(tn - tnb) * (double)((a.M + 127) / 128), st, cus);
       if (tnb > 0 && tnb < tn && mixed < best) return launch_mixed<T>(a, tnb, s);
     }
     if (best == narrow) return launch_tile<T, false, 4, 2, 2, 2, 3>(a, s);
     if (best == deep) return launch_tile<T, false, 4, 4, 2, 2, 4>(a, s);
-    return best == small ? launch_tile<T, false, 4, 4, 2, 2, 2>(a, s) : launch_tile<T, false, 8, 8, 2, 2, 2>(a, s);
+    return best == middle ? launch_tile<T, false, 4, 4, 4, 2, 3>(a, s) : launch_tile<T, false, 8, 8, 2, 2, 2>(a, s);
   }
 }
 
