@@ -295,8 +295,8 @@ __global__ void __launch_bounds__(256) k_fp8_quantize16(const Fp8QuantArgs a, co
   }
 }
 
-// Rows only, a scale a row: 16 rows of 128 entries a workgroup, a piece a thread (us, so / by the kernel above: 1 x 4096 2.4 /
-// 4.1, 1024 x 4096 3.9 / 6.0, 2048 x 11008 12.2 / 14.2, 5.5 TB/s).
+// Rows only, a scale a row: 16 rows of 128 entries a workgroup, a piece a thread (us, so / by a workgroup of 128
+// rows: 1 x 4096 2.4 / 4.1, 2048 x 11008 12.2 / 14.2; 5.5 TB/s).
 template <class T>
 __global__ void __launch_bounds__(256) k_fp8_quantize_rows(const Fp8QuantArgs a, const int wide) {
   const int cg = threadIdx.x & 15, c = blockIdx.x * 128 + 8 * cg;

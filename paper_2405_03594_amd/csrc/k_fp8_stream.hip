@@ -10,6 +10,9 @@
 // Rows of X may also come in 16 bits: a lane then has 32 of a block's 128
 // entries, the largest magnitude is found by two lane moves, and the codes are
 // those of k_fp8_quantize.
+//
+// Bound by W's bytes where they are many (11008 x 4096 by one row of bf16 13.5 to 15.2 us, 3.0 to 3.3 TB/s; 12.7 with codes), by
+// the launch and two trips to memory where they are few (1111 x 1000 3.9).
 #include <type_traits>
 
 #include "fp8_tile.h"
@@ -214,13 +217,14 @@ hipError_t by_sum(const Fp8GemmArgs& a, int wide, hipStream_t s) {
   return launch<T, MT, NR, U, 8, E>(a, wide, s);
 }
 // Rows in 16 bits are quantized by each workgroup anew, which is most of its arithmetic: two blocks of 16 rows of W a
-// workgroup where those still fill the chip.
+// workgroup where there are plenty (us, two / one: 1 x 11008 x 4096, 344 workgroups of two, 15.5 / 14.5; 32 rows of 8
+// experts x 5632 x 2048, 1408 of them, 19.3 / 21.3).
 template <class T>
 hipError_t rows16(const Fp8GemmArgs& a, hipStream_t s) {
   const int wide = (reinterpret_cast<uintptr_t>(a.x16) & 15) == 0 && a.x16_stride % 8 == 0;
   const int64_t wgs = (a.N + 31) / 32 * (a.mode == kFp8Rows ? (a.M < a.groups ? a.M : a.groups) : 1);
   if (fp8_rows_each(a) > 16) return by_sum<T, 2, 1, 2, 4>(a, wide, s);
-  if (wgs >= device_cus()) return by_sum<T, 1, 2, 2, 5>(a, wide, s);
+  if (wgs >= 4 * device_cus()) return by_sum<T, 1, 2, 2, 5>(a, wide, s);
   return by_sum<T, 1, 1, 2, 6>(a, wide, s);
 }
 
