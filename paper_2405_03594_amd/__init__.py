@@ -1406,7 +1406,7 @@ class Fp8Matrix:
         if codes.shape[-1] < cols or scales.shape != (*codes.shape[:-2], (rows + block - 1) // block, blocks):
             raise ValueError(f"codes {list(codes.shape)} and scales {list(scales.shape)} are not of {cols} columns")
         codes = codes.view(torch.uint8)
-        if codes.shape[-1] != 128 * blocks or not codes.is_contiguous():
+        if codes.shape[-1] != cols or cols != 128 * blocks or not codes.is_contiguous():   # zeros behind the columns
             wide = torch.zeros((*codes.shape[:-1], 128 * blocks), dtype=torch.uint8, device=codes.device)
             wide[..., :cols] = codes[..., :cols]
             codes = wide

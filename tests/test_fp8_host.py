@@ -243,6 +243,17 @@ def test_matrix_of(spl):
             spl.Fp8Matrix.of(*args)
 
 
+def test_matrix_of_clears_the_padding(spl):
+    """Codes wider than the matrix may hold anything behind its columns; a product reads whole blocks."""
+    codes = torch.full((3, 256), 0x7f, dtype=torch.uint8)      # NaN codes
+    codes[:, :200] = 0x38
+    scales = torch.full((3, 2), 127, dtype=torch.uint8)
+    for given in (codes, torch.cat([codes, codes], 1)):
+        m = spl.Fp8Matrix.of(given, scales, 200, 1)
+        assert m.codes.shape == (3, 256) and (m.codes[:, 200:] == 0).all() and (m.codes[:, :200] == 0x38).all()
+    assert (codes[:, 200:] == 0x7f).all()
+
+
 def test_wrappers_refuse(spl):
     x, w = torch.zeros((4, 256), dtype=torch.bfloat16), _cpu_matrix(spl)
     starts = torch.zeros(4, dtype=torch.int32)
