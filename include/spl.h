@@ -726,6 +726,8 @@ spl_status spl_attention_fp4(const spl_heads* q, int64_t tokens, const spl_kv_ca
  *            past cols are zero codes (or any, in a block of NaN).
  *   scales   [count][ceil(rows / block)][spitch], spitch = pitch / 128 rounded
  *            up to 4; bytes past pitch / 128 are not used.
+ * Results in the memory of a call's matrices, rows or workspace, or of each other, are
+ * SPL_ERR_INVALID_ARG (but for spl_linear_fp8_grad's on dY's or X's, read by then).
  * codes are 16-byte aligned, scales 4-byte aligned.  rows, cols, count >= 1;
  * cols <= 2^22, count <= 65535, rows < 2^31, count * rows * pitch < 2^42. */
 typedef struct {

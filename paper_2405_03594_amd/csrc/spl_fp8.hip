@@ -44,6 +44,23 @@ spl_status check_matrix(const spl_fp8_matrix* m) {
   return SPL_OK;
 }
 
+// Whether a result, fully in [p, p + bytes), is apart from other memory of the call: workgroups write it while others read.
+bool apart(const void* p, int64_t bytes, const void* q, int64_t more) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return !p || !q || a + (uintptr_t)bytes <= b || b + (uintptr_t)more <= a;
+}
+bool apart(const void* p, int64_t bytes, const spl_fp8_matrix& m) {
+  return apart(p, bytes, m.codes, spl_fp8_codes_bytes(m.rows, m.cols, m.count)) &&
+         apart(p, bytes, m.scales, spl_fp8_scales_bytes(m.rows, m.cols, m.count, m.block));
+}
+bool apart(const spl_fp8_matrix& out, const void* q, int64_t more) { return apart(q, more, out); }
+bool apart(const spl_fp8_matrix& a, const spl_fp8_matrix& b) {
+  return apart(a.codes, spl_fp8_codes_bytes(a.rows, a.cols, a.count), b) &&
+         apart(a.scales, spl_fp8_scales_bytes(a.rows, a.cols, a.count, a.block), b);
+}
+int64_t type_bytes(int32_t d) { return d == SPL_F32 ? 4 : 2; }
+int64_t rows_bytes(int64_t rows, int64_t stride, int64_t cols, int32_t d) { return ((rows - 1) * stride + cols) * type_bytes(d); }
+
 int64_t codes_workspace(int64_t M, int64_t N, int64_t cols) {
   return align256(spl::fp8_partial_bytes(M, N, (int32_t)(spl::fp8_pitch(cols) / 128)));
 }
@@ -69,6 +86,10 @@ spl_status rows_product(const void* X, int32_t x_dtype, int64_t M, int64_t row_s
     return SPL_ERR_INVALID_ARG;
   const int64_t need = rows_workspace(M, W->rows, W->cols, W->count);
   if (need > 0 && !given(workspace, 256)) return SPL_ERR_INVALID_ARG;
+  const int64_t bytes = M * W->rows * type_bytes(dtype);
+  if (!apart(Y, bytes, *W) || !apart(Y, bytes, X, rows_bytes(M, row_stride, W->cols, x_dtype)) ||
+      !apart(Y, bytes, workspace, need))
+    return SPL_ERR_INVALID_ARG;
   if (M > kMaxCols) return SPL_ERR_UNSUPPORTED;
   (void)hipGetLastError();
   Fp8GemmArgs a{};
@@ -121,11 +142,13 @@ spl_status spl_quantize_fp8(const void* X, int32_t dtype, int64_t rows, int64_t 
   if (row_stride < cols || row_stride > kMaxBytes / rows / count || !given(X, dtype == SPL_F32 ? 4 : 2))
     return SPL_ERR_INVALID_ARG;
   spl::Fp8QuantArgs a{};
+  const int64_t bytes = rows_bytes(count * rows, row_stride, cols, dtype);
   if (out) {
     const spl_status st = check_matrix(out);
     if (st != SPL_OK) return st;
     if (out->rows != rows || out->cols != cols || out->count != count || (starts && out->block != 1))
       return SPL_ERR_INVALID_ARG;
+    if (!apart(*out, X, bytes)) return SPL_ERR_INVALID_ARG;
     a.out = spl::fp8_view(*out);
   }
   if (out_t) {
@@ -135,6 +158,7 @@ spl_status spl_quantize_fp8(const void* X, int32_t dtype, int64_t rows, int64_t 
     if (out_t->rows != cols || out_t->count != count || want < 0 || (starts ? out_t->cols < want : out_t->cols != want) ||
         (starts && out_t->block != 1) || (out && out->block != out_t->block))
       return SPL_ERR_INVALID_ARG;
+    if (!apart(*out_t, X, bytes) || (out && !apart(*out, *out_t))) return SPL_ERR_INVALID_ARG;
     a.out_t = spl::fp8_view(*out_t);
   }
   a.X = X, a.row_stride = row_stride, a.rows = rows, a.cols = cols, a.count = count, a.starts = starts;
@@ -147,7 +171,7 @@ spl_status spl_dequantize_fp8(const spl_fp8_matrix* A, int32_t dtype, void* out,
   const spl_status st = check_matrix(A);
   if (st != SPL_OK) return st;
   if (!float_type(dtype)) return SPL_ERR_UNSUPPORTED;
-  if (!given(out, 16)) return SPL_ERR_INVALID_ARG;
+  if (!given(out, 16) || !apart(out, A->count * A->rows * A->cols * type_bytes(dtype), *A)) return SPL_ERR_INVALID_ARG;
   (void)hipGetLastError();
   return launched(spl::launch_fp8_dequantize(spl::fp8_view(*A), A->cols, A->count, dtype, out, stream));
 }
@@ -163,11 +187,14 @@ spl_status spl_linear_fp8(const spl_fp8_matrix* X, const spl_fp8_matrix* W, int3
   if (!float_type(dtype)) return SPL_ERR_UNSUPPORTED;
   if (X->cols != W->cols || X->count != 1 || W->count != 1 || !product_ok(X->rows, W->rows, W->cols, 1) || !given(Y, 16))
     return SPL_ERR_INVALID_ARG;
+  const int64_t bytes = X->rows * W->rows * type_bytes(dtype);
+  if (!apart(Y, bytes, *X) || !apart(Y, bytes, *W)) return SPL_ERR_INVALID_ARG;
   Fp8GemmArgs a{};
   a.x = spl::fp8_view(*X), a.w = spl::fp8_view(*W);
   a.M = X->rows, a.N = W->rows, a.blocks = a.w.pitch / 128, a.dtype = dtype, a.y = Y, a.mode = spl::kFp8Plain;
-  if (spl::fp8_partial_bytes(a.M, a.N, a.blocks) > 0) {
-    if (!given(workspace, 256)) return SPL_ERR_INVALID_ARG;
+  const int64_t partial = spl::fp8_partial_bytes(a.M, a.N, a.blocks);
+  if (partial > 0) {
+    if (!given(workspace, 256) || !apart(Y, bytes, workspace, partial)) return SPL_ERR_INVALID_ARG;
     a.partial = workspace;
   }
   (void)hipGetLastError();
@@ -191,6 +218,8 @@ spl_status spl_linear_fp8_grouped(const spl_fp8_matrix* X, const spl_fp8_matrix*
   if (X->cols != W->cols || X->count != 1 || !product_ok(X->rows, W->rows, W->cols, W->count) || !given(Y, 16) ||
       !given(starts, 4))
     return SPL_ERR_INVALID_ARG;
+  const int64_t bytes = X->rows * W->rows * type_bytes(dtype);
+  if (!apart(Y, bytes, *X) || !apart(Y, bytes, *W)) return SPL_ERR_INVALID_ARG;
   if (X->rows > kMaxCols) return SPL_ERR_UNSUPPORTED;
   Fp8GemmArgs a{};
   a.x = spl::fp8_view(*X), a.w = spl::fp8_view(*W);
@@ -221,6 +250,8 @@ spl_status spl_linear_fp8_grouped_weight_grad(const spl_fp8_matrix* dYt, const s
   if (want < 0 || dYt->cols != Xt->cols || dYt->cols < want || dYt->count != 1 || Xt->count != 1 || !given(starts, 4) ||
       !given(dW, 16) || Xt->rows > kMaxBytes / dYt->rows / experts)
     return SPL_ERR_INVALID_ARG;
+  const int64_t bytes = experts * dYt->rows * Xt->rows * type_bytes(dtype);
+  if (!apart(dW, bytes, *dYt) || !apart(dW, bytes, *Xt)) return SPL_ERR_INVALID_ARG;
   Fp8GemmArgs a{};
   a.x = spl::fp8_view(*dYt), a.w = spl::fp8_view(*Xt);
   a.M = dYt->rows, a.N = Xt->rows, a.blocks = a.w.pitch / 128, a.dtype = dtype, a.y = dW;
@@ -285,6 +316,10 @@ spl_status spl_linear_fp8_grad(const void* dY, int64_t dy_stride, const void* X,
   if (!given(dY, 2) || !given(X, 2) || dy_stride < N || x_stride < K || dy_stride > kMaxBytes / M ||
       x_stride > kMaxBytes / M || !given(workspace, 256))
     return SPL_ERR_INVALID_ARG;
+  const int64_t dx_bytes = M * K * 2, dw_bytes = Wt->count * N * K * type_bytes(grad_dtype);
+  if (!apart(dX, dx_bytes, *Wt) || !apart(dW, dw_bytes, *Wt) || !apart(dX, dx_bytes, dW, dw_bytes) ||
+      !apart(dX, dx_bytes, workspace, g.bytes) || !apart(dW, dw_bytes, workspace, g.bytes))
+    return SPL_ERR_INVALID_ARG;                         // (dY and X have been read when these are written)
   uint8_t* base = static_cast<uint8_t*>(workspace);
   const auto view = [&](int64_t codes, int64_t scales, int64_t rows, int64_t cols) {
     spl_fp8_matrix m{};

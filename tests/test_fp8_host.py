@@ -149,6 +149,33 @@ def test_refused_products(L):
     assert L.spl_linear_fp8_grouped_weight_grad(x, w, P(0x60000), 0, 100, F32, Y, None) == INVALID
 
 
+def test_refused_shared_memory(L):
+    """Results in the memory of what the same call reads or writes: refused before anything runs (64 x 256 codes at 0x10000
+    are 0x4000 bytes, 64 x 4 scales at 0x20000 are 0x100)."""
+    x, w = _m(codes=P(0x100000), scales=P(0x110000)), _m()
+    starts = P(0x600000)
+    for y in (0x100000, 0x103ff0, 0x110000, 0x10000, 0x13ff0, 0x20000, 0xff010, 0x10010):
+        assert L.spl_linear_fp8(x, w, BF16, P(y), None, None) == INVALID, hex(y)
+        assert L.spl_linear_fp8_grouped(x, w, starts, BF16, P(y), None) == INVALID, hex(y)
+    X = P(0x50000)                                            # 4 rows of 256, 300 apart: 3 * 600 + 512 bytes
+    for y in (0x50000, 0x50900, 0x4fe10, 0x10000, 0x20000):
+        assert L.spl_linear_fp8_rows(X, BF16, 4, 300, w, BF16, P(y), None, None) == INVALID, hex(y)
+        assert L.spl_linear_fp8_grouped_rows(X, BF16, 4, 300, w, starts, BF16, P(y), None, None) == INVALID, hex(y)
+    q = L.spl_quantize_fp8
+    t = _m(rows=256, cols=64, codes=P(0x200000), scales=P(0x300000))
+    assert q(P(0x10000), BF16, 64, 256, 256, 1, None, 0, w, None, None) == INVALID
+    assert q(P(0x1fe00), BF16, 64, 256, 256, 1, None, 0, w, None, None) == INVALID           # its scales
+    assert q(P(0x200000), BF16, 64, 256, 256, 1, None, 0, w, t, None) == INVALID
+    assert q(P(0x700000), BF16, 64, 256, 256, 1, None, 0, w, _m(rows=256, cols=64), None) == INVALID   # both at one place
+    g = L.spl_linear_fp8_grad                                 # M 64, N 256, K 64: dX 0x2000 bytes, dW 0x10000
+    a = (P(0x700000), 256, P(0x800000), 64, BF16, 64, _m())
+    ws = P(0x900000)
+    for dx, dw in ((0x400000, 0x401000), (0x10000, 0x400000), (0x400000, 0x20000), (0x900000, 0x400000)):
+        assert g(*a, None, F32, P(dx), P(dw), ws, None) == INVALID, (hex(dx), hex(dw))
+    assert L.spl_linear_fp8_grouped_weight_grad(x, w, starts, 1, 100, F32, P(0x10000), None) == INVALID
+    assert L.spl_dequantize_fp8(w, F32, P(0x13ff0), None) == INVALID
+
+
 def test_refused_quantize(L):
     X, o, t = P(0x50000), _m(), _m(rows=256, cols=64)
     q = L.spl_quantize_fp8
