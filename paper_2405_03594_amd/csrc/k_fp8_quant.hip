@@ -336,7 +336,7 @@ hipError_t quantize(const Fp8QuantArgs& a, hipStream_t s) {
   constexpr int E = std::is_same<T, F32In>::value ? 4 : 2;
   const int wide = (reinterpret_cast<uintptr_t>(a.X) & 15) == 0 && a.row_stride * E % 16 == 0;
   const bool r = a.out.codes, c = a.out_t.codes, big = (r ? a.out : a.out_t).shift == 7;
-  if (r && !c && !big && !a.starts) {
+  if (r && !c && !big && !a.starts && (a.rows + 15) / 16 <= 65535) {   // (what a grid's second axis holds)
     const dim3 few((unsigned)((a.cols + 127) / 128), (unsigned)((a.rows + 15) / 16), (unsigned)a.count);
     hipLaunchKernelGGL(k_fp8_quantize_rows<T>, few, dim3(256), 0, s, a, wide);
     return hipGetLastError();
@@ -353,7 +353,7 @@ hipError_t quantize(const Fp8QuantArgs& a, hipStream_t s) {
   } else if (r && big) {
     SPL_Q(true, false, 128);
   } else if (r) {
-    SPL_Q(true, false, 1);                           // rows of groups
+    SPL_Q(true, false, 1);                           // rows of groups, or more than the kernel above is launched for
   } else if (big) {
     SPL_Q(false, true, 128);
   } else {

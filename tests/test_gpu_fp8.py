@@ -192,6 +192,20 @@ def test_quantize_strided_and_counted(dtype):
 STARTS = [[0, 0, 5, 5, 130, 300], [0, 300], [10, 138, 138, 290], [0] * 70 + [1, 129, 129, 300], [300, 300, 300]]
 
 
+@pytest.mark.parametrize("rows", [16 * 65535, 16 * 65535 + 1, (1 << 22) - 3])
+def test_quantize_many_rows(rows):
+    """Past what one grid of 16 rows a workgroup holds: the same 4099 rows over and over give the same codes."""
+    spl = _spl()
+    x = _x((4099, 5), torch.bfloat16, 3).cuda()
+    want = spl.quantize_fp8(x)
+    got = spl.quantize_fp8(x.repeat((rows + 4098) // 4099, 1)[:rows])
+    at = torch.arange(rows, device="cuda") % 4099
+    for a in range(0, rows, 1 << 19):
+        here = at[a:a + (1 << 19)]
+        assert torch.equal(got.codes[a:a + (1 << 19)], want.codes[here]), a
+        assert torch.equal(got.scales[a:a + (1 << 19), :1], want.scales[here, :1]), a
+
+
 @pytest.mark.parametrize("starts", STARTS)
 def test_quantize_groups(starts):
     spl = _spl()
