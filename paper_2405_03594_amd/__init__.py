@@ -1386,7 +1386,13 @@ class Fp8Matrix:
 
     @classmethod
     def empty(cls, rows: int, cols: int, block: int = 1, count: int | None = None, device="cuda", stream=None):
-        _fp8_workspace("spl_fp8_scales_bytes", rows, cols, 1 if count is None else count, block)   # refuses the sizes
+        return cls._made(rows, cols, block, count, device, stream)[0]
+
+    @classmethod
+    def _made(cls, rows: int, cols: int, block: int, count: int | None, device, stream):
+        """A matrix to be written, and its view (right as made: view()'s checks are 1 us of a short call's 10.6)."""
+        n = 1 if count is None else count
+        scales_bytes = _fp8_workspace("spl_fp8_scales_bytes", rows, cols, n, block)   # refuses the sizes
         blocks = (cols + 127) // 128
         codes, scales = (rows, 128 * blocks), ((rows + block - 1) // block, (blocks + 3) // 4 * 4)
         if count is not None:
@@ -1394,7 +1400,7 @@ class Fp8Matrix:
         m = object.__new__(cls)
         m.codes, m.scales = _result(codes, torch.uint8, device, stream), _result(scales, torch.uint8, device, stream)
         m.cols, m.block = cols, block
-        return m
+        return m, _Fp8(m.codes.data_ptr(), m.scales.data_ptr(), rows, cols, n, n * rows * 128 * blocks, scales_bytes, block)
 
     @classmethod
     def of(cls, codes: torch.Tensor, scales: torch.Tensor, cols: int, block: int) -> "Fp8Matrix":
@@ -1450,17 +1456,17 @@ def _quantize(X, block, rows_too, cols_too, starts, stream):
         raise ValueError("starts is for one matrix with blocks of one row")
     device = _here("X, starts", stream, X, starts)
     L, lead = lib(), None if X.dim() == 2 else count
-    out = Fp8Matrix.empty(rows, cols, block, lead, device, stream) if rows_too else None
-    out_t = None
+    out, view = Fp8Matrix._made(rows, cols, block, lead, device, stream) if rows_too else (None, None)
+    out_t = view_t = None
     if cols_too:
         wide = rows if starts is None else L.spl_fp8_grouped_cols(rows, groups)
         if wide < 0:
             raise ValueError("too many rows or groups")
-        out_t = Fp8Matrix.empty(cols, wide, block, lead, device, stream)
+        out_t, view_t = Fp8Matrix._made(cols, wide, block, lead, device, stream)
     _check("spl_quantize_fp8",
            L.spl_quantize_fp8(X.data_ptr(), _FLOAT_TYPES[X.dtype], rows, cols, stride, count,
                               None if starts is None else starts.data_ptr(), groups,
-                              None if out is None else out.view(), None if out_t is None else out_t.view(), _on(stream)))
+                              view, view_t, _on(stream)))
     return out, out_t
 
 
