@@ -4,7 +4,7 @@
 // a workgroup; a thread has 8 neighbouring elements at a time, so that 8-bit
 // states' blocks of 128 are 16 neighbouring lanes and their scales come from
 // four lane moves.  Everything is read and written once, which bounds it: 60.8 million elements, fp32 p, bf16
-// gradient and copy, 340 us (5.0 TB/s); 8-bit states 210 (4.6).  16 small tensors 4.4 us.
+// gradient and copy, 340 us (5.0 TB/s); 8-bit states 205 to 210 (4.6 to 4.7).  16 small tensors 4.4 us.
 #include <string.h>
 
 #include <type_traits>
