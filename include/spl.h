@@ -802,8 +802,9 @@ spl_status spl_linear_fp8_rows(const void* X, int32_t x_dtype, int64_t M, int64_
 
 /* Linear layers of W->count experts: row m of X, in starts[e] <= m < starts[e + 1],
  * is multiplied with matrix e.  starts [W->count + 1] int32 on the device, taken
- * as by spl_quantize_fp8 (groups that overlap: which one a shared row's result is
- * of is not defined); rows of no expert are left as they were in Y [M][N].
+ * as by spl_quantize_fp8; rows of no expert are left as they were in Y [M][N].  Where
+ * starts fall and groups overlap, which group a shared row's result is of is not
+ * defined, and the launch may have no tile for the last groups' rows, which then stay too.
  *   X            as spl_linear_fp8 takes it (block 1), or
  *   spl_linear_fp8_grouped_rows: as spl_linear_fp8_rows takes it.
  * The workspace-size functions as above, of M, N, cols and the experts. */
@@ -817,7 +818,8 @@ spl_status spl_linear_fp8_grouped_rows(const void* X, int32_t x_dtype, int64_t M
 /* Their weights' gradients: dW [experts][N][K], dW[e] = sum over the rows m of
  * expert e of dY[m][n] X[m][k], from the transposes that spl_quantize_fp8 makes of dY
  * (N rows) and X (K rows) with the same starts.  dW of dtype, 16-byte aligned,
- * fully written: zeros for an expert without rows. */
+ * fully written: zeros for an expert without rows; of groups that overlap, undefined
+ * numbers. */
 spl_status spl_linear_fp8_grouped_weight_grad(const spl_fp8_matrix* dYt, const spl_fp8_matrix* Xt,
                                               const int32_t* starts, int64_t experts, int64_t tokens, int32_t dtype,
                                               void* dW, hipStream_t stream);
@@ -828,8 +830,8 @@ spl_status spl_linear_fp8_grouped_weight_grad(const spl_fp8_matrix* dYt, const s
  * both sums in 8-bit floats, dY quantized along its columns for dX, dY and X along their
  * rows (a group's from its own start on) for dW, as by the calls above.
  *   Wt           the transposed weights: Wt->count matrices [K][N].
- *   starts       NULL (Wt->count 1), or as above: rows of no expert are not written
- *                in dX, an expert without rows has a dW of zeros.
+ *   starts       NULL (Wt->count 1), or as above: rows of no expert are zeros in dX,
+ *                an expert without rows has a dW of zeros.
  *   dX, dW       16-byte aligned; one of them may be NULL.
  *   workspace    spl_linear_fp8_grad_workspace_bytes(M, N, K, experts) bytes (experts 0:
  *                without starts), 256-byte aligned.

@@ -1633,7 +1633,7 @@ def linear_fp8_grouped(X, W: Fp8Matrix, starts: torch.Tensor, dtype: torch.dtype
 def linear_fp8_grouped_grad(dY: torch.Tensor, X: torch.Tensor, Wt: Fp8Matrix, starts: torch.Tensor,
                             grad_dtype: torch.dtype = torch.float32, stream=None):
     """(dX, dW) of linear_fp8_grouped as linear_fp8_grad's, Wt the transposed weights [experts, K, N], dW [experts, N, K]
-    with zeros for an expert without rows.  Rows of no expert are not written in dX."""
+    with zeros for an expert without rows.  Rows of no expert are zeros in dX."""
     _starts(starts, Wt.count)
     return _gradients(dY, X, Wt, starts, grad_dtype, stream)
 

@@ -386,7 +386,38 @@ __global__ void __launch_bounds__(256) k_fp8_dequantize(const Fp8View m, int64_t
   }
 }
 
+// Zeros into the rows of y [rows][row bytes, a multiple of 2] before the first group and behind the last: where starts do not
+// fall, those in between all have a group; where they do, into every row.  Two runs of 16-bit words, 8 of them a thread
+// at a time; where every row has a group (the usual call) a workgroup reads starts and leaves: 2 us between other launches.
+__global__ void __launch_bounds__(256) k_fp8_clear_rest(const int32_t* starts, const int groups, const int rows, uint16_t* y,
+                                                        const int64_t width) {
+  int falls = 0;
+  for (int g = threadIdx.x; g < groups; g += 256) falls |= starts[g] > starts[g + 1];
+  falls = __syncthreads_or(falls);
+  const auto bound = [&](int v) { return (int64_t)(v < 0 ? 0 : (v > rows ? rows : v)); };
+  const int64_t all = rows * width, head = falls ? all : bound(starts[0]) * width, tail = falls ? all : bound(starts[groups]) * width;
+  const auto clear = [&](int64_t from, int64_t to) {   // words [from, to)
+    const int64_t each = (int64_t)gridDim.x * 256 * 8;
+    for (int64_t i = from / 8 * 8 + 8 * ((int64_t)blockIdx.x * 256 + threadIdx.x); i < to; i += each) {
+      if (i >= from && i + 8 <= to) {
+        *reinterpret_cast<u32x4*>(y + i) = u32x4{0u, 0u, 0u, 0u};
+      } else {
+        for (int64_t k = i < from ? from : i; k < i + 8 && k < to; ++k) y[k] = 0;
+      }
+    }
+  };
+  clear(0, head);
+  clear(tail, all);
+}
+
 }  // namespace
+
+hipError_t launch_fp8_clear_rest(const int32_t* starts, int32_t groups, int64_t rows, int64_t width, void* y, hipStream_t s) {
+  const int64_t blocks = (rows * width + 2047) / 2048, most = 2 * device_cus();
+  hipLaunchKernelGGL(k_fp8_clear_rest, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, s, starts, (int)groups,
+                     (int)rows, static_cast<uint16_t*>(y), width);
+  return hipGetLastError();
+}
 
 hipError_t launch_fp8_quantize(const Fp8QuantArgs& a, int32_t dtype, hipStream_t s) {
   if (dtype == SPL_F32) return quantize<F32In>(a, s);

@@ -153,6 +153,8 @@ struct Fp8QuantArgs {
   Fp8View out, out_t;                           // codes NULL: not wanted
 };
 hipError_t launch_fp8_quantize(const Fp8QuantArgs& a, int32_t dtype, hipStream_t s);
+// Zeros into the rows of y [rows][width] (16-bit words, 16-byte aligned) that no group has; in all where starts fall.
+hipError_t launch_fp8_clear_rest(const int32_t* starts, int32_t groups, int64_t rows, int64_t width, void* y, hipStream_t s);
 hipError_t launch_fp8_dequantize(const Fp8View& m, int64_t cols, int64_t count, int32_t dtype, void* out, hipStream_t s);
 
 // How the products' rows are grouped.

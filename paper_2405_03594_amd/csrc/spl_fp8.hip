@@ -338,6 +338,8 @@ spl_status spl_linear_fp8_grad(const void* dY, int64_t dy_stride, const void* X,
     e = spl::launch_fp8_quantize(z, dtype, stream);
   }
   void* partial = base + g.partial;
+  if (e == hipSuccess && dX && starts)                  // before the product, which then writes the rows of experts
+    e = spl::launch_fp8_clear_rest(starts, (int32_t)experts, M, K, dX, stream);
   if (e == hipSuccess && dX) {
     Fp8GemmArgs a{};
     a.x = q, a.w = spl::fp8_view(*Wt), a.M = M, a.N = K, a.blocks = a.w.pitch / 128, a.dtype = dtype, a.y = dX;

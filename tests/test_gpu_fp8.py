@@ -489,3 +489,59 @@ def test_streams_and_graphs():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(got, eager[r])), r
+
+
+@pytest.mark.parametrize("starts", [[0, 90, 90, 150], [37, 90, 90, 300], [37, 64, 200, 263], [0, 0, 0, 0], [300, 300, 300, 300],
+                                    [-5, 3, 3, 299], [200, 50, 120, 120], [290, 300, 0, 10], [0, 290, 10, 300]])
+@pytest.mark.parametrize("N,K", [(40, 77), (130, 256)])
+def test_grouped_grad_rows_of_no_expert(starts, N, K):
+    """dX is defined everywhere: a row that no expert has did not reach the loss, so its gradient is zero, whatever stood
+    in the memory before (the largest allocations of the process are filled with NaN first, so that a result on them shows)."""
+    spl = _spl()
+    M, E = 300, len(starts) - 1
+    x, dy = _x((M, K), torch.bfloat16, 1), _x((M, N), torch.bfloat16, 2)
+    w = _x((E, N, K), torch.float32, 3)
+    at = torch.tensor(starts, dtype=torch.int32).cuda()
+    _, wt = spl.quantize_fp8_both(w.cuda(), 128)
+    x, dy = x.cuda(), dy.cuda()
+    owned = torch.zeros(M, dtype=torch.bool)
+    for a, b in zip(starts, starts[1:]):
+        owned[max(a, 0):max(b, 0)] = True
+    for _ in range(3):
+        hold = [torch.full((n,), float("nan"), dtype=torch.bfloat16, device="cuda") for n in (M * K, M * K, 2 * M * K)]
+        torch.cuda.synchronize()
+        del hold
+        dx, _ = spl.linear_fp8_grouped_grad(dy, x, wt, at)
+        assert (dx.cpu()[~owned] == 0).all()
+        assert torch.isfinite(dx).all()
+    if all(a <= b for a, b in zip(starts, starts[1:])):
+        for e, (a, b) in enumerate(zip(starts, starts[1:])):
+            a = max(a, 0)
+            if b > a:
+                hdy, hw = ref.round_trip(_np(dy[a:b])), ref.round_trip(_np(w[e]), 128)
+                _near(dx[a:b], hdy @ hw, _bound(hdy, hw.T, torch.bfloat16), f"dX of {e}")
+
+
+def test_grouped_grad_rows_of_no_expert_in_given_memory():
+    """The library's call on memory of the caller: dX on dY's own memory too, which has been read by then; nothing behind
+    dX is touched, at every alignment that a row's end can have."""
+    import ctypes
+
+    spl = _spl()
+    L = spl.lib()
+    for M, N, K, starts in ((70, 64, 64, [9, 9, 40, 61]), (33, 5, 5, [3, 10, 20, 30]), (129, 9, 9, [0, 1, 64, 128])):
+        E = len(starts) - 1
+        x, dy = _x((M, K), torch.bfloat16, 1).cuda(), _x((M, N), torch.bfloat16, 2).cuda()
+        _, wt = spl.quantize_fp8_both(_x((E, N, K), torch.float32, 3).cuda(), 128)
+        at = torch.tensor(starts, dtype=torch.int32).cuda()
+        want, _ = spl.linear_fp8_grouped_grad(dy, x, wt, at)
+        assert (want[:starts[0]] == 0).all() and (want[starts[-1]:] == 0).all()
+        ws = torch.empty(L.spl_linear_fp8_grad_workspace_bytes(M, N, K, E), dtype=torch.uint8, device="cuda")
+        stream = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+        store = torch.full((M * K + 64,), 5.0, dtype=torch.bfloat16, device="cuda")
+        shared = dy.clone()                            # N == K: dX in dY's memory
+        for dev, dx in ((dy, store[:M * K].view(M, K)), (shared, shared)):
+            st = L.spl_linear_fp8_grad(dev.data_ptr(), N, x.data_ptr(), K, 2, M, wt.view(), at.data_ptr(), 5, dx.data_ptr(), None,
+                                       ws.data_ptr(), stream)
+            assert st == 0 and torch.equal(dx, want)
+        assert (store[M * K:] == 5).all()
