@@ -845,8 +845,9 @@ spl_status spl_linear_fp8_grad(const void* dY, int64_t dy_stride, const void* X,
  * sum rounded on its own, with t = step:
  *   g = grad * *grad_scale             (no product without grad_scale)
  *   m = m beta1 + g (1 - beta1)        v = v beta2 + g g (1 - beta2)
- *   p = p (1 - lr decay) - lr / (1 - beta1^t) * (m / (sqrt(v) / sqrt(1 - beta2^t) + eps))
- * the factors of a tensor computed in 64 bits and rounded to fp32 once.
+ *   p = p (1 - lr decay) - (lr / (1 - beta1^t)) (m / (sqrt(v) (1 / sqrt(1 - beta2^t)) + eps))
+ * the quotient and the root too; the factors (beta1, 1 - beta1, beta2, 1 - beta2, 1 - lr decay, lr / (1 - beta1^t),
+ * 1 / sqrt(1 - beta2^t), eps) computed in 64 bits and rounded to fp32 once.  g g (1 - beta2) is (g g) (1 - beta2).
  *
  * A tensor: n elements of param (fp32, bf16, fp16), grad (the same, its own
  * type) and, with copy_dtype, of copy (fp16 or bf16), the new p rounded to it

@@ -4,12 +4,19 @@
 // a workgroup; a thread has 8 neighbouring elements at a time, so that 8-bit
 // states' blocks of 128 are 16 neighbouring lanes and their scales come from
 // four lane moves.  Everything is read and written once, which bounds it: 60.8 million elements, fp32 p, bf16
-// gradient and copy, 340 us (5.0 TB/s); 8-bit states 205 to 210 (4.6 to 4.7).  16 small tensors 4.4 us.
+// gradient and copy, 340 us (5.0 TB/s); 8-bit states 218 (4.5; 208 with the root that is not rounded to nearest, so there
+// the arithmetic counts too).  16 small tensors 4.4 us.
+#include <math.h>
 #include <string.h>
 
 #include <type_traits>
 
 #include "spl_fp8.h"
+
+// Every product and sum is rounded by itself, as the formula in spl.h has it: by default a product that is added is fused
+// with the sum, the compiler's choice which, and the update would differ between compilers.  (The intrinsics named after
+// roundings to nearest do not keep products and sums apart here, and the one of the root is the approximate instruction.)
+#pragma clang fp contract(off)
 
 namespace spl {
 namespace {
@@ -118,7 +125,7 @@ __device__ __forceinline__ double power(double x, int64_t t) {
 __device__ __forceinline__ float stochastic(float x, uint32_t rnd, bool keep) {
   const float a = fabsf(x);
   float r = __uint_as_float((__float_as_uint(a) + rnd) & 0xfff00000u);
-  if (a < 0x1p-6f) r = __fmul_rn(floorf(__fadd_rn(__fmul_rn(a, 512.f), __fmul_rn((float)rnd, 0x1p-20f))), 0x1p-9f);
+  if (a < 0x1p-6f) r = floorf(a * 512.f + (float)rnd * 0x1p-20f) * 0x1p-9f;
   if (keep && r < 0x1p-9f) r = 0x1p-9f;
   return copysignf(r, x);
 }
@@ -132,7 +139,7 @@ __device__ __forceinline__ void encode8(float (&x)[8], const uint32_t (&rnd)[8],
   const uint32_t byte = fp8_scale_byte(row16_max(m));
   const float f = fp8_inverse(byte);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = stochastic(__fmul_rn(x[j], f), rnd[j], keep && x[j] > 0.f);
+  for (int j = 0; j < 8; ++j) x[j] = stochastic(x[j] * f, rnd[j], keep && x[j] > 0.f);
   u32x2 q = {fp8_four(x[0], x[1], x[2], x[3]), fp8_four(x[4], x[5], x[6], x[7])};
   if (byte == 255) q = u32x2{0x7f7f7f7fu, 0x7f7f7f7fu};
   if (!mine) return;
@@ -143,10 +150,10 @@ __device__ __forceinline__ void decode8(const uint8_t* c, const uint8_t* s, int6
   const u32x2 q = mine ? *reinterpret_cast<const u32x2*>(c + i) : u32x2{0u, 0u};
   const uint32_t byte = mine ? s[i >> 7] : 0u;
   const float f = byte == 255 ? __uint_as_float(0x7fc00000u) : (byte == 0 ? 0x1p-127f : __uint_as_float(byte << 23));
-  x[0] = __fmul_rn(__builtin_amdgcn_cvt_f32_fp8((int)q.x, 0), f), x[1] = __fmul_rn(__builtin_amdgcn_cvt_f32_fp8((int)q.x, 1), f);
-  x[2] = __fmul_rn(__builtin_amdgcn_cvt_f32_fp8((int)q.x, 2), f), x[3] = __fmul_rn(__builtin_amdgcn_cvt_f32_fp8((int)q.x, 3), f);
-  x[4] = __fmul_rn(__builtin_amdgcn_cvt_f32_fp8((int)q.y, 0), f), x[5] = __fmul_rn(__builtin_amdgcn_cvt_f32_fp8((int)q.y, 1), f);
-  x[6] = __fmul_rn(__builtin_amdgcn_cvt_f32_fp8((int)q.y, 2), f), x[7] = __fmul_rn(__builtin_amdgcn_cvt_f32_fp8((int)q.y, 3), f);
+  x[0] = __builtin_amdgcn_cvt_f32_fp8((int)q.x, 0) * f, x[1] = __builtin_amdgcn_cvt_f32_fp8((int)q.x, 1) * f;
+  x[2] = __builtin_amdgcn_cvt_f32_fp8((int)q.x, 2) * f, x[3] = __builtin_amdgcn_cvt_f32_fp8((int)q.x, 3) * f;
+  x[4] = __builtin_amdgcn_cvt_f32_fp8((int)q.y, 0) * f, x[5] = __builtin_amdgcn_cvt_f32_fp8((int)q.y, 1) * f;
+  x[6] = __builtin_amdgcn_cvt_f32_fp8((int)q.y, 2) * f, x[7] = __builtin_amdgcn_cvt_f32_fp8((int)q.y, 3) * f;
 }
 
 template <class P, class G, bool k8>
@@ -176,7 +183,7 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const Chunk* chunks, const A
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         if (j >= have) m[j] = v[j] = 0.f;
-        v[j] = __fmul_rn(v[j], v[j]);
+        v[j] = v[j] * v[j];
       }
     } else {
       get8<F32P>(t.m, i, have, wide, m);
@@ -184,12 +191,11 @@ __global__ void __launch_bounds__(kThreads) k_adamw(const Chunk* chunks, const A
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float d = __fmul_rn(g[j], gs);
-      m[j] = __fadd_rn(__fmul_rn(m[j], b1), __fmul_rn(d, c1));
-      v[j] = __fadd_rn(__fmul_rn(v[j], b2), __fmul_rn(__fmul_rn(d, d), c2));
-      r[j] = __fsqrt_rn(v[j]);
-      const float u = __fdiv_rn(m[j], __fadd_rn(__fmul_rn(r[j], root), eps));
-      p[j] = __fsub_rn(__fmul_rn(p[j], keep), __fmul_rn(rate, u));
+      const float d = g[j] * gs;
+      m[j] = m[j] * b1 + d * c1;
+      v[j] = v[j] * b2 + d * d * c2;
+      r[j] = sqrtf(v[j]);                            // (to nearest, as the quotient: hipcc's default for both)
+      p[j] = p[j] * keep - rate * (m[j] / (r[j] * root + eps));
     }
     if (mine) {
       put8<P>(t.p, i, have, wide, p);
