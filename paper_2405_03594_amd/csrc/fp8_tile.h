@@ -79,6 +79,23 @@ __device__ __forceinline__ Fp8Part fp8_part(const Fp8GemmArgs& a, int size, int 
   return p;
 }
 
+// The blocks [b0, b1) that a wave of `waves` sums of [k0, k1): 1, 2 or a multiple of 4 of them, from a multiple of 4 (so many)
+// on, so that the scale bytes of those requested together are of one word; those from `first` on are of the sum.
+struct Fp8Run {
+  int b0, b1, first;
+};
+__host__ __device__ __forceinline__ Fp8Run fp8_run(int k0, int k1, int wave, int waves) {
+  const int start = k0 & ~3;
+  int per = (k1 - start + waves - 1) / waves;
+  per = per < 3 ? per : (per + 3) & ~3;
+  Fp8Run r;
+  r.b0 = start + wave * per, r.b1 = r.b0 + per < k1 ? r.b0 + per : k1;
+  r.first = r.b0 > k0 ? r.b0 : k0;
+  return r;
+}
+// The scale byte of a block, in the low bits, from the word of four blocks that it is in.
+__host__ __device__ __forceinline__ uint32_t fp8_scale_at(uint32_t word, int block) { return word >> (8 * (block & 3)); }
+
 __device__ __forceinline__ uint16_t fp8_half(float v, int32_t dtype) {
   return dtype == SPL_BF16 ? Bf16::from_f32(v) : F16::from_f32(v);
 }

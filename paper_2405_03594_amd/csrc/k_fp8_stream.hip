@@ -96,14 +96,10 @@ __global__ void __launch_bounds__(64 * kWaves, kEach) k_fp8_stream(const Fp8Gemm
       xh[j] = static_cast<const uint16_t*>(a.x16) + m * a.x16_stride;
     }
   }
-  // A wave's blocks: 1, 2 or a multiple of 4 of them, so that the scale bytes of those requested together are of one word.
   // Places before k0 and from k1 on take a block of the wave's again, with codes of zero for X: a NaN in it is in the sum anyway.
   static_assert(U == 4 || U == 2, "a word's blocks");
-  const int start = p.k0 & ~3;
-  int per = (p.k1 - start + kWaves - 1) / kWaves;
-  per = per < 3 ? per : (per + 3) & ~3;
-  const int b0 = start + wave * per, b1 = b0 + per < p.k1 ? b0 + per : p.k1;
-  const int first = b0 > p.k0 ? b0 : p.k0;
+  const Fp8Run run = fp8_run(p.k0, p.k1, wave, kWaves);
+  const int b0 = run.b0, b1 = run.b1, first = run.first;
   const auto block = [&](int b) { return b < first ? first : (b < b1 ? b : b1 - 1); };
   f32x4 acc[NR][MT];
 #pragma unroll
@@ -115,7 +111,7 @@ __global__ void __launch_bounds__(64 * kWaves, kEach) k_fp8_stream(const Fp8Gemm
     Part<T> x[U][MT];
     Part<Codes> w[U][NR];
     uint32_t sw[NR], sx[MT];
-    const int word = b & ~3, shift = 8 * (b & 3);
+    const int word = b & ~3;                     // (a place past the word is not of the sum)
     if constexpr (kCodes) {
 #pragma unroll
       for (int j = 0; j < MT; ++j) sx[j] = *reinterpret_cast<const uint32_t*>(xs[j] + word);
@@ -155,7 +151,7 @@ __global__ void __launch_bounds__(64 * kWaves, kEach) k_fp8_stream(const Fp8Gemm
 #pragma unroll
       for (int j = 0; j < MT; ++j) {
         if constexpr (kCodes)
-          x0[u][j] = x[u][j].q[0], x1[u][j] = x[u][j].q[1], sb[u][j] = sx[j] >> (shift + 8 * u);
+          x0[u][j] = x[u][j].q[0], x1[u][j] = x[u][j].q[1], sb[u][j] = fp8_scale_at(sx[j], b + u);
         else
           sb[u][j] = quantize<T>(x[u][j], x0[u][j], x1[u][j]);
         x0[u][j] &= live, x1[u][j] &= live, sb[u][j] &= live;
@@ -167,7 +163,7 @@ __global__ void __launch_bounds__(64 * kWaves, kEach) k_fp8_stream(const Fp8Gemm
       const uint32_t live = b + u >= p.k0 && b + u < b1 ? ~0u : 0u;
 #pragma unroll
       for (int i = 0; i < NR; ++i) {
-        const uint32_t sa = (sw[i] >> (shift + 8 * u)) & live;      // the matrix instruction takes the low byte
+        const uint32_t sa = fp8_scale_at(sw[i], b + u) & live;      // the matrix instruction takes the low byte
         if constexpr (kExact) {
           const Wide8 v = fp8_widen32(w[u][i].q[0], w[u][i].q[1], sa & 255u);
 #pragma unroll
