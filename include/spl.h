@@ -841,6 +841,20 @@ spl_status spl_linear_fp8_grad(const void* dY, int64_t dy_stride, const void* X,
                                int64_t M, const spl_fp8_matrix* Wt, const int32_t* starts, int32_t grad_dtype,
                                void* dX, void* dW, void* workspace, hipStream_t stream);
 
+/* Which kernel a product of these sizes takes, for tests and profiles; the choice goes by the sizes and the current
+ * device's compute units (256 where there is none).
+ *   form         0: spl_linear_fp8 (x_dtype 0) or spl_linear_fp8_rows (that x_dtype); 1: the same of `groups` experts;
+ *                2: spl_linear_fp8_grouped_weight_grad of dYt with M rows, Xt with N, `groups` experts and cols tokens.
+ * -1 for what the calls reject, else
+ *   1, 2, 3      streaming, codes of X: 16, 32, 32 rows of X by 16, 16, 32 of W a workgroup;
+ *   4, 5, 6      streaming, rows of X quantized on the way: 16, 16, 32 rows of X by 16, 32, 16 of W;
+ *                8 more than that where eight waves share a sum, not four;
+ *   16 to 19     tiles of 128 x 64, 128 x 128, 256 x 128, 256 x 256 (rows of W by rows of X);
+ *   20           tiles of 256 x 256, the rest of W in tiles of 256 x 128;  21: 128 x 256 (fp32 results);
+ *   22           128 x 64 with sums split over workgroups, and their join. */
+int32_t spl_linear_fp8_kernel(int32_t form, int64_t M, int64_t N, int64_t cols, int64_t groups, int32_t x_dtype,
+                              int32_t dtype);
+
 /* AdamW over many tensors in one launch.  Per element, in fp32, every product and
  * sum rounded on its own, with t = step:
  *   g = grad * *grad_scale             (no product without grad_scale)

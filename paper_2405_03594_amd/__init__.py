@@ -217,6 +217,7 @@ def lib() -> ctypes.CDLL:
         "spl_linear_fp8_grouped_weight_grad": (ctypes.c_int, [MQ, MQ, P, I64, I64, I32, P, P]),
         "spl_linear_fp8_grad_workspace_bytes": (I64, [I64, I64, I64, I64]),
         "spl_linear_fp8_grad": (ctypes.c_int, [P, I64, P, I64, I32, I64, MQ, P, I32, P, P, P, P]),
+        "spl_linear_fp8_kernel": (I32, [I32, I64, I64, I64, I64, I32, I32]),
         "spl_adamw_plan_chunks": (I64, [TP, I64, YP]),
         "spl_adamw_plan_bytes": (I64, [TP, I64, YP]),
         "spl_adamw_plan": (ctypes.c_int, [TP, I64, YP, P]),

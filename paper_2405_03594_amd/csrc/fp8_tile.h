@@ -148,6 +148,7 @@ inline double fp8_rows_each(const Fp8GemmArgs& a) {
   return a.mode == kFp8Rows ? 1.5 * (double)a.M / a.groups : (double)a.M;
 }
 
-hipError_t launch_fp8_stream(const Fp8GemmArgs& a, hipStream_t s);
+int32_t fp8_stream_kernel(const Fp8GemmArgs& a);
+hipError_t launch_fp8_stream(const Fp8GemmArgs& a, int32_t kernel, hipStream_t s);
 
 }  // namespace spl

@@ -401,32 +401,47 @@ int splits_of(int64_t M, int64_t N, int32_t blocks) {
   return splits;
 }
 
-template <class T>
-hipError_t by_size(const Fp8GemmArgs& a, hipStream_t s) {
+// The kind of tile; with kTileMixed, `columns` of 256 x 256 tiles.
+int32_t tile_kernel(const Fp8GemmArgs& a, int64_t& columns) {
   const int cus = device_cus();
   const double st = about_stages(a), t64 = about_tiles(a, 128, 64), t128 = about_tiles(a, 128, 128);
-  if constexpr (T::code == SPL_F32) {
+  if (a.dtype == SPL_F32) {
     const double large = kLarge32.rounds(about_tiles(a, 128, 256), st, cus), small = kSmall32.rounds(t128, st, cus),
                  narrow = kNarrow32.rounds(t64, st, cus);
-    if (narrow <= small && narrow <= large) return launch_tile<T, true, 4, 2, 2, 2, 3>(a, s);
-    return small <= large ? launch_tile<T, true, 4, 4, 2, 2, 2>(a, s) : launch_tile<T, true, 4, 4, 2, 4, 3>(a, s);
-  } else {
-    const double t256 = about_tiles(a, 256, 256);
-    const double large = kLarge.rounds(t256, st, cus), middle = kMiddle.rounds(about_tiles(a, 256, 128), st, cus),
-                 deep = kDeep.rounds(t128, st, cus), narrow = kNarrow.rounds(t64, st, cus);
-    double best = large < middle ? large : middle;
-    best = deep < best ? deep : best;
-    best = narrow < best ? narrow : best;
-    if (a.mode == kFp8Plain && t256 > cus) {           // whole rounds of large tiles, the rest of the columns in middle ones
-      const int64_t tm = (a.M + 255) / 256, tn = (a.N + 255) / 256;
-      const int64_t tnb = (int64_t)(t256 / cus) * cus / tm;
-      const double mixed = kLarge.rounds((double)(tnb * tm), st, cus) +
-                           kRest.rounds((double)(tn - tnb) * (double)((a.M + 127) / 128), st, cus);
-      if (tnb > 0 && tnb < tn && mixed < best) return launch_mixed<T>(a, tnb, s);
+    if (narrow <= small && narrow <= large) return kTile64;
+    return small <= large ? kTile128 : kTileWide;
+  }
+  const double t256 = about_tiles(a, 256, 256);
+  const double large = kLarge.rounds(t256, st, cus), middle = kMiddle.rounds(about_tiles(a, 256, 128), st, cus),
+               deep = kDeep.rounds(t128, st, cus), narrow = kNarrow.rounds(t64, st, cus);
+  double best = large < middle ? large : middle;
+  best = deep < best ? deep : best;
+  best = narrow < best ? narrow : best;
+  if (a.mode == kFp8Plain && t256 > cus) {             // whole rounds of large tiles, the rest of the columns in middle ones
+    const int64_t tm = (a.M + 255) / 256, tn = (a.N + 255) / 256;
+    const int64_t tnb = (int64_t)(t256 / cus) * cus / tm;
+    const double mixed = kLarge.rounds((double)(tnb * tm), st, cus) +
+                         kRest.rounds((double)(tn - tnb) * (double)((a.M + 127) / 128), st, cus);
+    if (tnb > 0 && tnb < tn && mixed < best) {
+      columns = tnb;
+      return kTileMixed;
     }
-    if (best == narrow) return launch_tile<T, false, 4, 2, 2, 2, 3>(a, s);
-    if (best == deep) return launch_tile<T, false, 4, 4, 2, 2, 4>(a, s);
-    return best == middle ? launch_tile<T, false, 4, 4, 4, 2, 3>(a, s) : launch_tile<T, false, 8, 8, 2, 2, 2>(a, s);
+  }
+  if (best == narrow) return kTile64;
+  if (best == deep) return kTile128;
+  return best == middle ? kTileMiddle : kTileLarge;
+}
+
+template <class T>
+hipError_t launch_kind(const Fp8GemmArgs& a, int32_t kind, int64_t columns, hipStream_t s) {
+  if constexpr (T::code == SPL_F32) {
+    if (kind == kTile64) return launch_tile<T, true, 4, 2, 2, 2, 3>(a, s);
+    return kind == kTile128 ? launch_tile<T, true, 4, 4, 2, 2, 2>(a, s) : launch_tile<T, true, 4, 4, 2, 4, 3>(a, s);
+  } else {
+    if (kind == kTileMixed) return launch_mixed<T>(a, columns, s);
+    if (kind == kTile64) return launch_tile<T, false, 4, 2, 2, 2, 3>(a, s);
+    if (kind == kTile128) return launch_tile<T, false, 4, 4, 2, 2, 4>(a, s);
+    return kind == kTileMiddle ? launch_tile<T, false, 4, 4, 4, 2, 3>(a, s) : launch_tile<T, false, 8, 8, 2, 2, 2>(a, s);
   }
 }
 
@@ -474,11 +489,22 @@ int64_t fp8_partial_bytes(int64_t M, int64_t N, int32_t blocks) {
   return splits > 1 ? 4 * M * N * splits : 0;
 }
 
+static int32_t kernel_of(const Fp8GemmArgs& a, int64_t& columns) {
+  if (a.x16 || streams(a)) return fp8_stream_kernel(a);
+  return a.mode == kFp8Plain && a.partial ? (int32_t)kTileSplit : tile_kernel(a, columns);
+}
+int32_t fp8_kernel(const Fp8GemmArgs& a) {
+  int64_t columns;
+  return kernel_of(a, columns);
+}
+
 hipError_t launch_fp8_gemm(const Fp8GemmArgs& given, hipStream_t s) {
   Fp8GemmArgs a = given;
   a.splits = 1;
-  if (a.x16 || streams(a)) return launch_fp8_stream(a, s);
-  if (a.mode == kFp8Plain && a.partial) {
+  int64_t columns = 0;
+  const int32_t kind = kernel_of(a, columns);
+  if (kind < kTile64) return launch_fp8_stream(a, kind, s);
+  if (kind == kTileSplit) {
     a.splits = splits_of(a.M, a.N, a.blocks);
     a.y = a.partial;
     hipError_t e = a.dtype == SPL_F32 ? launch_tile<F32Out, true, 4, 2, 2, 2, 3>(a, s) : launch_tile<F32Out, false, 4, 2, 2, 2, 3>(a, s);
@@ -494,8 +520,8 @@ hipError_t launch_fp8_gemm(const Fp8GemmArgs& given, hipStream_t s) {
       hipLaunchKernelGGL(k_fp8_join<F16>, grid, dim3(256), 0, s, from, a.splits, n, given.y);
     return hipGetLastError();
   }
-  if (a.dtype == SPL_F32) return by_size<F32Out>(a, s);
-  return a.dtype == SPL_BF16 ? by_size<Bf16>(a, s) : by_size<F16>(a, s);
+  if (a.dtype == SPL_F32) return launch_kind<F32Out>(a, kind, columns, s);
+  return a.dtype == SPL_BF16 ? launch_kind<Bf16>(a, kind, columns, s) : launch_kind<F16>(a, kind, columns, s);
 }
 
 }  // namespace spl

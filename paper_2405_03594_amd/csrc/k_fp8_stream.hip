@@ -205,33 +205,40 @@ hipError_t launch(const Fp8GemmArgs& a, int wide, hipStream_t s) {
     hipLaunchKernelGGL((k_fp8_stream<T, MT, NR, U, W, E, false>), grid, dim3(64 * W), 0, s, a, wide);
   return hipGetLastError();
 }
-// Four waves for up to 16 blocks of 128 columns, which would leave eight of them two or fewer each (us, 4 / 8 waves:
-// 5632 x 2048 6.0 / 8.2, 1111 x 1000 3.9 / 5.0, 4096 x 4096 7.6 / 6.5, 4096 x 11008 16.3 / 13.0).
 template <class T, int MT, int NR, int U, int E>
-hipError_t by_sum(const Fp8GemmArgs& a, int wide, hipStream_t s) {
-  if (a.blocks <= 16) return launch<T, MT, NR, U, 4, E>(a, wide, s);
-  return launch<T, MT, NR, U, 8, E>(a, wide, s);
+hipError_t by_sum(const Fp8GemmArgs& a, bool eight, int wide, hipStream_t s) {
+  return eight ? launch<T, MT, NR, U, 8, E>(a, wide, s) : launch<T, MT, NR, U, 4, E>(a, wide, s);
 }
-// Rows in 16 bits are quantized by each workgroup anew, which is most of its arithmetic: two blocks of 16 rows of W a
-// workgroup where there are plenty (us, two / one: 1 x 11008 x 4096, 344 workgroups of two, 15.5 / 14.5; 32 rows of 8
-// experts x 5632 x 2048, 1408 of them, 19.3 / 21.3).
 template <class T>
-hipError_t rows16(const Fp8GemmArgs& a, hipStream_t s) {
+hipError_t rows16(const Fp8GemmArgs& a, int32_t kernel, bool eight, hipStream_t s) {
   const int wide = (reinterpret_cast<uintptr_t>(a.x16) & 15) == 0 && a.x16_stride % 8 == 0;
-  const int64_t wgs = (a.N + 31) / 32 * (a.mode == kFp8Rows ? (a.M < a.groups ? a.M : a.groups) : 1);
-  if (fp8_rows_each(a) > 16) return by_sum<T, 2, 1, 2, 4>(a, wide, s);
-  if (wgs >= 4 * device_cus()) return by_sum<T, 1, 2, 2, 5>(a, wide, s);
-  return by_sum<T, 1, 1, 2, 6>(a, wide, s);
+  if (kernel == kRows32) return by_sum<T, 2, 1, 2, 4>(a, eight, wide, s);
+  if (kernel == kRows16x32) return by_sum<T, 1, 2, 2, 5>(a, eight, wide, s);
+  return by_sum<T, 1, 1, 2, 6>(a, eight, wide, s);
 }
 
 }  // namespace
 
-hipError_t launch_fp8_stream(const Fp8GemmArgs& a, hipStream_t s) {
-  if (a.x16) return a.x16_dtype == SPL_BF16 ? rows16<Bf16>(a, s) : rows16<F16>(a, s);
+// Four waves for up to 16 blocks of 128 columns, which would leave eight of them two or fewer each (us, 4 / 8 waves:
+// 5632 x 2048 6.0 / 8.2, 1111 x 1000 3.9 / 5.0, 4096 x 4096 7.6 / 6.5, 4096 x 11008 16.3 / 13.0).
+// Rows in 16 bits are quantized by each workgroup anew, which is most of its arithmetic: two blocks of 16 rows of W a
+// workgroup where there are plenty (us, two / one: 1 x 11008 x 4096, 344 workgroups of two, 15.5 / 14.5; 32 rows of 8
+// experts x 5632 x 2048, 1408 of them, 19.3 / 21.3).
+int32_t fp8_stream_kernel(const Fp8GemmArgs& a) {
+  const int32_t eight = a.blocks <= 16 ? 0 : kEightWaves;
   const double each = fp8_rows_each(a);
-  if (each <= 16) return by_sum<Codes, 1, 1, 4, 6>(a, 0, s);
-  if (each <= 32) return by_sum<Codes, 2, 1, 4, 4>(a, 0, s);
-  return by_sum<Codes, 2, 2, 4, 2>(a, 0, s);
+  if (!a.x16) return eight + (each <= 16 ? kStream16 : (each <= 32 ? kStream32 : kStream32x32));
+  const int64_t wgs = (a.N + 31) / 32 * (a.mode == kFp8Rows ? (a.M < a.groups ? a.M : a.groups) : 1);
+  return eight + (each > 16 ? kRows32 : (wgs >= 4 * device_cus() ? kRows16x32 : kRows16));
+}
+
+hipError_t launch_fp8_stream(const Fp8GemmArgs& a, int32_t kernel, hipStream_t s) {
+  const bool eight = kernel >= kEightWaves;
+  kernel -= eight ? kEightWaves : 0;
+  if (a.x16) return a.x16_dtype == SPL_BF16 ? rows16<Bf16>(a, kernel, eight, s) : rows16<F16>(a, kernel, eight, s);
+  if (kernel == kStream16) return by_sum<Codes, 1, 1, 4, 6>(a, eight, 0, s);
+  if (kernel == kStream32) return by_sum<Codes, 2, 1, 4, 4>(a, eight, 0, s);
+  return by_sum<Codes, 2, 2, 4, 2>(a, eight, 0, s);
 }
 
 }  // namespace spl

@@ -177,6 +177,12 @@ struct Fp8GemmArgs {
   void* partial;                                // fp8_partial_bytes, or NULL where that is 0
 };
 hipError_t launch_fp8_gemm(const Fp8GemmArgs& a, hipStream_t s);
+// The kernel that it launches, by the numbers of spl_linear_fp8_kernel.
+enum {
+  kStream16 = 1, kStream32 = 2, kStream32x32 = 3, kRows16 = 4, kRows16x32 = 5, kRows32 = 6, kEightWaves = 8,
+  kTile64 = 16, kTile128 = 17, kTileMiddle = 18, kTileLarge = 19, kTileMixed = 20, kTileWide = 21, kTileSplit = 22
+};
+int32_t fp8_kernel(const Fp8GemmArgs& a);
 // Scratch of a plain product of codes whose sum is split over workgroups: fp32 [splits][M][N]; 0: it is not.  The same for
 // every type of y.
 int64_t fp8_partial_bytes(int64_t M, int64_t N, int32_t blocks);

@@ -358,6 +358,26 @@ spl_status spl_linear_fp8_grad(const void* dY, int64_t dy_stride, const void* X,
   return launched(e);
 }
 
+int32_t spl_linear_fp8_kernel(int32_t form, int64_t M, int64_t N, int64_t cols, int64_t groups, int32_t x_dtype,
+                              int32_t dtype) {
+  if (form < 0 || form > 2 || M < 1 || !float_type(dtype) || (x_dtype != 0 && (!half_type(x_dtype) || form == 2))) return -1;
+  Fp8GemmArgs a{};
+  a.M = M, a.N = N, a.dtype = dtype;
+  if (form == 2) {
+    const int64_t want = spl_fp8_grouped_cols(cols, groups);
+    if (want < 0 || !sizes_ok(M, want, 1) || !sizes_ok(N, want, 1) || N > kMaxBytes / M / groups) return -1;
+    a.blocks = (int32_t)(want / 128), a.mode = spl::kFp8Sum, a.groups = (int32_t)groups, a.tokens = (int32_t)cols;
+    return spl::fp8_kernel(a);
+  }
+  const int64_t experts = form == 1 ? groups : 1;
+  if (!product_ok(M, N, cols, experts) || ((form == 1 || x_dtype) && M > kMaxCols)) return -1;
+  a.blocks = (int32_t)(spl::fp8_pitch(cols) / 128), a.mode = form == 1 ? spl::kFp8Rows : spl::kFp8Plain;
+  a.groups = (int32_t)experts;
+  if (x_dtype && spl::fp8_fused(M, N, cols, experts)) a.x16 = &a;      // (looked at, not read)
+  if (form == 0 && !a.x16 && spl::fp8_partial_bytes(M, N, a.blocks) > 0) a.partial = &a;
+  return spl::fp8_kernel(a);
+}
+
 static bool adamw_types(const spl_adamw_types* ty) {
   return ty && float_type(ty->param_dtype) && float_type(ty->grad_dtype) &&
          (ty->copy_dtype == 0 || half_type(ty->copy_dtype)) && (ty->state_bits == 32 || ty->state_bits == 8);
