@@ -128,3 +128,26 @@ def _check(spl, sizes, pd, gd, bits, shift, scale):
                                                (torch.bfloat16, torch.float32, 1, 0.37), (torch.float16, torch.float16, 3, 3.0)])
 def test_every_operation_is_rounded_by_itself(pd, gd, shift, scale, bits):
     _check(_spl(), SMALL, pd, gd, bits, shift, scale)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("pd,gd,shift,scale", [(torch.float32, torch.bfloat16, 0, 0.37), (torch.bfloat16, torch.float32, 1, None)])
+def test_many_elements(pd, gd, shift, scale, bits):
+    """Chunks of 8192: later turns of a chunk's loop, ends in each of them, scales of blocks in them, bits of far elements."""
+    spl = _spl()
+    assert sum(LARGE) > 2048 * 2048
+    _check(spl, LARGE, pd, gd, bits, shift, scale)
+
+
+def test_chunks_of_a_plan():
+    """Where the chunks change their length: 2048 x 2048 elements in all are still cut into 2048 each, one more into 8192."""
+    spl = _spl()
+    for n, chunks in ((2048 * 2048, 2048), (2048 * 2048 + 1, 513)):
+        t = [torch.zeros(n, device="cuda") for _ in range(4)]
+        t[1].fill_(1.0)
+        plan = spl.adamw_plan(*[[x] for x in t])
+        assert plan.chunks == chunks
+        spl.adamw_step(plan, LR, (B1, B2), EPS, step=1)
+        want = [torch.from_numpy(np.broadcast_to(x, n)) for x in
+                update(np.zeros(1, F), np.ones(1, F), np.zeros(1, F), np.zeros(1, F), 1, None, 0.01)[:3]]
+        assert all(torch.equal(t[i].cpu(), w) for i, w in ((0, want[0]), (2, want[1]), (3, want[2]))), n
