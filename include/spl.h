@@ -775,9 +775,12 @@ spl_status spl_dequantize_fp8(const spl_fp8_matrix* A, int32_t dtype, void* out,
 
 /* Y [M][N] = X W^T of two such matrices that share cols: X of M rows, W of N, of
  * either block.  fp32 sums, one rounding to dtype (fp16, bf16 or fp32).  For results of
- * 16 bits the sums are those of the 8-bit matrix instructions, which align the products
- * added at once and keep some 17 bits of them (1e-5 to 5e-5 of the sum, below the result's
- * rounding); for fp32 results the codes are widened to bf16, scale included, and summed
+ * 16 bits the sums are those of the 8-bit matrix instructions, which align the products of a
+ * block of 128 columns, added at once, to the largest of them and drop what is below 2^-16 of
+ * it: a sum is off by up to 2^-9 of the largest |x w| of each block, on random values of both
+ * signs by 1e-5 to 5e-5 of the root of the sum of their squares.  That is below the result's rounding unless
+ * the sum cancels: small products beside large ones of opposite signs may be lost.  For fp32
+ * results the codes are widened to bf16, scale included, and summed
  * exactly but for fp32's roundings, at half the rate: values past bf16's range are
  * infinities there, those below 2^-133 zeros.  With
  * W and X the transposes of dY and of X it is the weight's gradient, with X = dY

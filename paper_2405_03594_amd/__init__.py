@@ -1540,7 +1540,9 @@ def _fp8_rows(X, cols: int, name: str = "X"):
 def linear_fp8(X, W: Fp8Matrix, dtype: torch.dtype | None = None, out: torch.Tensor | None = None,
                stream=None) -> torch.Tensor:
     """Y [M, N] = X W^T in 8-bit floats (see spl_linear_fp8).  X: an Fp8Matrix, or fp16 / bf16 activations [M, K] that are
-    quantized on the way, a scale for 128 columns of a row.  Y: dtype, else that of out, else X's (bf16 for codes)."""
+    quantized on the way, a scale for 128 columns of a row.  Y: dtype, else that of out, else X's (bf16 for codes).  Sums
+    of 16-bit results are off by up to 2^-9 of each block's largest product, those of fp32 results by fp32's roundings only:
+    where large products cancel and what is left counts, ask for torch.float32."""
     L, w = lib(), W.view()
     if w.count != 1:
         raise ValueError("W is several matrices: linear_fp8_grouped")

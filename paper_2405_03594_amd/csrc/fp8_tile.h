@@ -16,11 +16,13 @@ __device__ __forceinline__ f32x4 fp8_mfma(u32x4 a0, u32x4 a1, u32x4 b0, u32x4 b1
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, (int)sa, 0, (int)sb);
 }
 
-// The matrix instructions of 8-bit floats align the products that they add at once to the largest of them and keep
-// some 17 bits: sums are 1e-5 to 5e-5 off, whatever their length (measured on values over 8 to 30 powers of two; on
-// Gaussian ones 1.3e-5).  That is a tenth of bf16's rounding and less than fp16's, so results of 16 bits
-// take them; for fp32 results the codes are widened to bf16, which holds them exactly, scale included, and
-// summed by its instructions, at half the rate (off by 1e-8 to 3e-7 on the same values).
+// The matrix instructions of 8-bit floats align the products that they add at once (a block's 128) to the largest of them
+// and keep some 17 bits of each: what 127 of them lose below 2^-16 of the largest is at most 2^-9 of it.  Measured on
+// values of both signs over 8 to 30 powers of two, sums of 128 to 2048 products are 1e-5 to 5e-5 of the root of the sum of the
+// products' squares off (1.3e-5 on Gaussian ones).  Where a sum is of that root's size this is 3 to 13 thousandths of
+// bf16's half step (2^-8) and 2 to 10 hundredths of fp16's (2^-11), so results of 16 bits take them; a sum that cancels
+// to less loses more of itself than its rounding.  For fp32 results the codes are widened to bf16, which holds them exactly,
+// scale included, and summed by its instructions, at half the rate (off by 1e-8 to 3e-7 on the same values).
 __device__ __forceinline__ uint32_t fp8_widen(uint32_t q, float scale, bool high) {
   return high ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q, scale, true))
               : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q, scale, false));

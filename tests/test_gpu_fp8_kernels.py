@@ -232,3 +232,24 @@ def test_split_sums_and_tiles_in_graphs():
             assert torch.equal(spl.linear_fp8(xs[0][2], ws[0]), eager[0][2])
             torch.cuda.synchronize()
             assert all(torch.equal(a, e[r]) for a, e in zip(out, eager)), r
+
+
+@pytest.mark.parametrize("M,N,K,k16,k32", [c for c in cases.CODES if c[3] in (1, 9, 3, 16, 17, 18, 19, 20, 22)][::2], ids=str)
+def test_sums_that_cancel(M, N, K, k16, k32):
+    """What the documents say of sums whose products cancel: those of fp32 results keep what is left, those of 16-bit
+    results are off by up to 2^-9 of each block's largest product.  In each whole block of 128 two products of 2^16 cancel
+    and the other 126 are 2^-2 each, 31.5 in all: exact in fp32 (the sums on the way are multiples of 2^-2 below 2^18)."""
+    spl = _spl()
+    K = K // 128 * 128
+    x, w = torch.full((M, K), 2.0 ** -2), torch.ones((N, K))
+    for k in range(0, K, 128):
+        x[:, k + 3], x[:, k + 77] = 256.0, -256.0
+        w[:, k + 3] = w[:, k + 77] = 256.0
+    q, qw = spl.quantize_fp8(x.cuda()), spl.quantize_fp8(w.cuda(), 128)
+    assert np.array_equal(_held(q), _np(x)) and np.array_equal(_held(qw), _np(w))      # codes hold the values
+    want = 31.5 * (K // 128)
+    assert (spl.linear_fp8(q, qw, dtype=torch.float32) == want).all()
+    for dtype in (torch.bfloat16, torch.float16):
+        y = _np(spl.linear_fp8(q, qw, dtype=dtype))
+        bound = 2.0 ** -9 * 2.0 ** 16 * (K // 128) * (1 + EPS[dtype]) + EPS[dtype] * want
+        assert (np.abs(y - want) <= bound).all(), (dtype, np.abs(y - want).max(), bound)
