@@ -763,7 +763,7 @@ int64_t spl_fp8_scales_bytes(int64_t rows, int64_t cols, int64_t count, int32_t 
  * What no entry of X falls to is left as it was: the bytes of scales past the
  * last block, with starts also rows of no group and columns past the last.
  * rows == 0 is a no-op.  rows and cols up to 2^22 each (SPL_ERR_UNSUPPORTED past
- * that). */
+ * that, and for more than 65535 blocks of 128 rows that groups may need). */
 int64_t spl_fp8_grouped_cols(int64_t rows, int64_t groups);
 spl_status spl_quantize_fp8(const void* X, int32_t dtype, int64_t rows, int64_t cols, int64_t row_stride, int64_t count,
                             const int32_t* starts, int64_t groups, const spl_fp8_matrix* out,
@@ -785,7 +785,7 @@ spl_status spl_dequantize_fp8(const spl_fp8_matrix* A, int32_t dtype, void* out,
  * infinities there, those below 2^-133 zeros.  With
  * W and X the transposes of dY and of X it is the weight's gradient, with X = dY
  * and W the transpose of the weight that of the activations.
- *   Y            [M][N], 16-byte aligned, overwritten.
+ *   Y            [M][N], 16-byte aligned, overwritten.  N < 2^28 (else SPL_ERR_UNSUPPORTED, here and below).
  *   workspace    spl_linear_fp8_workspace_bytes(M, N, cols) bytes (-1 for sizes
  *                that the call rejects, 0: NULL will do), 256-byte aligned,
  *                caller-owned, overwritten.
@@ -797,7 +797,7 @@ spl_status spl_linear_fp8(const spl_fp8_matrix* X, const spl_fp8_matrix* W, int3
 /* The same from activations X [M][cols] of x_dtype (fp16 or bf16), rows
  * row_stride elements apart, that are quantized on the way, block 1, as
  * spl_quantize_fp8 does: the result is that of the two calls but for the order of
- * the sums.  W as above, Y of dtype.
+ * the sums.  W as above, Y of dtype; M up to 2^22 (SPL_ERR_UNSUPPORTED past that, by expert too).
  *   workspace    spl_linear_fp8_rows_workspace_bytes(...) bytes, 256-byte aligned. */
 int64_t spl_linear_fp8_rows_workspace_bytes(int64_t M, int64_t N, int64_t cols);
 spl_status spl_linear_fp8_rows(const void* X, int32_t x_dtype, int64_t M, int64_t row_stride, const spl_fp8_matrix* W,

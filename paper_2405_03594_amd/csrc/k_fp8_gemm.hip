@@ -78,7 +78,7 @@ __device__ __forceinline__ void tile_body(const Fp8GemmArgs& a, int w, int tn, i
     bm = grp * 4 + in % h;
     bn = in / h;
   }
-  const Fp8Part p = fp8_part(a, BM, bm, blockIdx.z);
+  const Fp8Part p = fp8_part(a, BM, a.first_tile + bm, blockIdx.z);
   if (p.none) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int wn = wave % WN, wm = wave / WN, fr = lane & 15, fg = lane >> 4;
@@ -327,7 +327,7 @@ __global__ void __launch_bounds__(256, 1) k_fp8_mixed(const Fp8GemmArgs a, const
 }
 
 constexpr int tile_lds(int BN, int BM, int R) { return R * (BN + BM) * 128 + 4 * (BN + BM) * 4; }
-constexpr int64_t kMostTiles = (int64_t)1 << 22;
+constexpr int64_t kMostTiles = (int64_t)1 << 22;        // of a launch; more rows' take further ones
 
 template <class T, bool kExact, int FN, int FM, int WN, int WM, int R>
 hipError_t launch_tile(const Fp8GemmArgs& a, hipStream_t s) {
@@ -336,10 +336,14 @@ hipError_t launch_tile(const Fp8GemmArgs& a, hipStream_t s) {
   auto* kernel = k_fp8_tile<T, kExact, FN, FM, WN, WM, R>;
   const hipError_t e = allow_lds_once(done, kernel, LDS);
   if (e != hipSuccess) return e;
-  const int64_t tn = (a.N + BN - 1) / BN, tm = fp8_row_tiles(a, BM);
-  if (tn * tm >= kMostTiles) return hipErrorNotSupported;
-  const dim3 grid((unsigned)(tn * tm), 1u, a.mode == kFp8Sum ? (unsigned)a.groups : (unsigned)a.splits);
-  hipLaunchKernelGGL(kernel, grid, dim3(64 * WN * WM), LDS, s, a, (int)tn, (int)tm);
+  const int64_t tn = (a.N + BN - 1) / BN, all = fp8_row_tiles(a, BM);   // (N < 2^28: tn is half of kMostTiles at most)
+  Fp8GemmArgs part = a;
+  for (int64_t first = 0; first < all; first += kMostTiles / tn) {
+    const int64_t tm = all - first < kMostTiles / tn ? all - first : kMostTiles / tn;
+    const dim3 grid((unsigned)(tn * tm), 1u, a.mode == kFp8Sum ? (unsigned)a.groups : (unsigned)a.splits);
+    part.first_tile = (int32_t)first;
+    hipLaunchKernelGGL(kernel, grid, dim3(64 * WN * WM), LDS, s, part, (int)tn, (int)tm);
+  }
   return hipGetLastError();
 }
 
@@ -350,7 +354,6 @@ hipError_t launch_mixed(const Fp8GemmArgs& a, int64_t tnb, hipStream_t s) {
   const hipError_t e = allow_lds_once(done, k_fp8_mixed<T>, LDS);
   if (e != hipSuccess) return e;
   const int64_t tmb = fp8_row_tiles(a, 256), tm = fp8_row_tiles(a, 128), tn = (a.N + 255) / 256 - tnb;
-  if (tnb * tmb + tn * tm >= kMostTiles) return hipErrorNotSupported;
   hipLaunchKernelGGL(k_fp8_mixed<T>, dim3((unsigned)(tnb * tmb + tn * tm)), dim3(256), LDS, s, a, (int)tnb, (int)tmb,
                      (int)tn, (int)tm);
   return hipGetLastError();
@@ -422,7 +425,7 @@ int32_t tile_kernel(const Fp8GemmArgs& a, int64_t& columns) {
     const int64_t tnb = (int64_t)(t256 / cus) * cus / tm;
     const double mixed = kLarge.rounds((double)(tnb * tm), st, cus) +
                          kRest.rounds((double)(tn - tnb) * (double)((a.M + 127) / 128), st, cus);
-    if (tnb > 0 && tnb < tn && mixed < best) {
+    if (tnb > 0 && tnb < tn && mixed < best && 2 * tn * tm < kMostTiles) {   // (in one launch)
       columns = tnb;
       return kTileMixed;
     }

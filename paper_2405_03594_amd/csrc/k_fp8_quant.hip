@@ -365,8 +365,8 @@ hipError_t quantize(const Fp8QuantArgs& a, hipStream_t s) {
 
 // out = code * 2^e, one rounding: a thread an entry's group of 8.
 template <class T>
-__global__ void __launch_bounds__(256) k_fp8_dequantize(const Fp8View m, int64_t cols, int64_t groups, void* out) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+__global__ void __launch_bounds__(256) k_fp8_dequantize(const Fp8View m, int64_t cols, int64_t first, int64_t groups, void* out) {
+  const int64_t i = first + (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= groups) return;
   const int64_t per = (cols + 7) / 8, row = i / per, c = 8 * (i - row * per);
   const int64_t z = row / m.rows, r = row - z * m.rows;
@@ -425,15 +425,17 @@ hipError_t launch_fp8_quantize(const Fp8QuantArgs& a, int32_t dtype, hipStream_t
 }
 
 hipError_t launch_fp8_dequantize(const Fp8View& m, int64_t cols, int64_t count, int32_t dtype, void* out, hipStream_t s) {
-  const int64_t groups = count * m.rows * ((cols + 7) / 8), blocks = (groups + 255) / 256;
-  if (blocks > ((int64_t)1 << 24) - 1) return hipErrorNotSupported;
-  const dim3 grid((unsigned)blocks);
-  if (dtype == SPL_F32)
-    hipLaunchKernelGGL(k_fp8_dequantize<F32In>, grid, dim3(256), 0, s, m, cols, groups, out);
-  else if (dtype == SPL_BF16)
-    hipLaunchKernelGGL(k_fp8_dequantize<Bf16>, grid, dim3(256), 0, s, m, cols, groups, out);
-  else
-    hipLaunchKernelGGL(k_fp8_dequantize<F16>, grid, dim3(256), 0, s, m, cols, groups, out);
+  const int64_t groups = count * m.rows * ((cols + 7) / 8), most = ((int64_t)1 << 24) - 1;   // workgroups of a launch
+  for (int64_t first = 0; first < groups; first += 256 * most) {
+    const int64_t blocks = (groups - first + 255) / 256;
+    const dim3 grid((unsigned)(blocks < most ? blocks : most));
+    if (dtype == SPL_F32)
+      hipLaunchKernelGGL(k_fp8_dequantize<F32In>, grid, dim3(256), 0, s, m, cols, first, groups, out);
+    else if (dtype == SPL_BF16)
+      hipLaunchKernelGGL(k_fp8_dequantize<Bf16>, grid, dim3(256), 0, s, m, cols, first, groups, out);
+    else
+      hipLaunchKernelGGL(k_fp8_dequantize<F16>, grid, dim3(256), 0, s, m, cols, first, groups, out);
+  }
   return hipGetLastError();
 }
 

@@ -68,7 +68,7 @@ template <class T, int MT, int NR, int U, int kWaves, int kEach, bool kExact>
 __global__ void __launch_bounds__(64 * kWaves, kEach) k_fp8_stream(const Fp8GemmArgs a, const int wide) {
   constexpr bool kCodes = std::is_same<T, Codes>::value;
   __shared__ f32x4 sums[kWaves][NR * MT][64];
-  const Fp8Part p = fp8_part(a, 16 * MT, blockIdx.y, blockIdx.z);
+  const Fp8Part p = fp8_part(a, 16 * MT, a.first_tile + (int)blockIdx.y, blockIdx.z);
   if (p.none) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int fr = lane & 15, fg = lane >> 4;
@@ -197,12 +197,16 @@ __global__ void __launch_bounds__(64 * kWaves, kEach) k_fp8_stream(const Fp8Gemm
 template <class T, int MT, int NR, int U, int W, int E>
 hipError_t launch(const Fp8GemmArgs& a, int wide, hipStream_t s) {
   const int64_t tiles = fp8_row_tiles(a, 16 * MT);
-  if (tiles > 65535) return hipErrorNotSupported;
-  const dim3 grid((unsigned)((a.N + 16 * NR - 1) / (16 * NR)), (unsigned)tiles, a.mode == kFp8Sum ? (unsigned)a.groups : 1u);
-  if (a.dtype == SPL_F32)
-    hipLaunchKernelGGL((k_fp8_stream<T, MT, NR, U, W, E, true>), grid, dim3(64 * W), 0, s, a, wide);
-  else
-    hipLaunchKernelGGL((k_fp8_stream<T, MT, NR, U, W, E, false>), grid, dim3(64 * W), 0, s, a, wide);
+  Fp8GemmArgs part = a;
+  for (int64_t first = 0; first < tiles; first += 65535) {          // what a grid's second axis holds
+    const dim3 grid((unsigned)((a.N + 16 * NR - 1) / (16 * NR)), (unsigned)(tiles - first < 65535 ? tiles - first : 65535),
+                    a.mode == kFp8Sum ? (unsigned)a.groups : 1u);
+    part.first_tile = (int32_t)first;
+    if (a.dtype == SPL_F32)
+      hipLaunchKernelGGL((k_fp8_stream<T, MT, NR, U, W, E, true>), grid, dim3(64 * W), 0, s, part, wide);
+    else
+      hipLaunchKernelGGL((k_fp8_stream<T, MT, NR, U, W, E, false>), grid, dim3(64 * W), 0, s, part, wide);
+  }
   return hipGetLastError();
 }
 template <class T, int MT, int NR, int U, int E>

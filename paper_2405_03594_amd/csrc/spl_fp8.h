@@ -167,6 +167,7 @@ struct Fp8GemmArgs {
   int32_t dtype;                                // of y
   int32_t mode;
   int32_t splits;                               // of the sum (set by the launcher)
+  int32_t first_tile;                           // of rows, of this launch (set by the launcher)
   const int32_t* starts;
   int32_t groups;
   int32_t tokens;                               // kFp8Sum: the rows that starts counts

@@ -18,6 +18,7 @@ constexpr int64_t kMaxRows = (int64_t)1 << 31;
 constexpr int64_t kMaxCols = (int64_t)1 << 22;
 constexpr int64_t kMaxBytes = (int64_t)1 << 42;
 constexpr int64_t kMaxCount = 65535;
+constexpr int64_t kMaxN = (int64_t)1 << 28;             // rows of W: 2^32 threads of the streaming kernels
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 bool given(const void* p, uintptr_t a) { return p && aligned(p, a); }
@@ -90,7 +91,7 @@ spl_status rows_product(const void* X, int32_t x_dtype, int64_t M, int64_t row_s
   if (!apart(Y, bytes, *W) || !apart(Y, bytes, X, rows_bytes(M, row_stride, W->cols, x_dtype)) ||
       !apart(Y, bytes, workspace, need))
     return SPL_ERR_INVALID_ARG;
-  if (M > kMaxCols) return SPL_ERR_UNSUPPORTED;
+  if (M > kMaxCols || W->rows >= kMaxN) return SPL_ERR_UNSUPPORTED;
   (void)hipGetLastError();
   Fp8GemmArgs a{};
   a.w = spl::fp8_view(*W);
@@ -189,6 +190,7 @@ spl_status spl_linear_fp8(const spl_fp8_matrix* X, const spl_fp8_matrix* W, int3
     return SPL_ERR_INVALID_ARG;
   const int64_t bytes = X->rows * W->rows * type_bytes(dtype);
   if (!apart(Y, bytes, *X) || !apart(Y, bytes, *W)) return SPL_ERR_INVALID_ARG;
+  if (W->rows >= kMaxN) return SPL_ERR_UNSUPPORTED;
   Fp8GemmArgs a{};
   a.x = spl::fp8_view(*X), a.w = spl::fp8_view(*W);
   a.M = X->rows, a.N = W->rows, a.blocks = a.w.pitch / 128, a.dtype = dtype, a.y = Y, a.mode = spl::kFp8Plain;
@@ -220,7 +222,7 @@ spl_status spl_linear_fp8_grouped(const spl_fp8_matrix* X, const spl_fp8_matrix*
     return SPL_ERR_INVALID_ARG;
   const int64_t bytes = X->rows * W->rows * type_bytes(dtype);
   if (!apart(Y, bytes, *X) || !apart(Y, bytes, *W)) return SPL_ERR_INVALID_ARG;
-  if (X->rows > kMaxCols) return SPL_ERR_UNSUPPORTED;
+  if (X->rows > kMaxCols || W->rows >= kMaxN) return SPL_ERR_UNSUPPORTED;
   Fp8GemmArgs a{};
   a.x = spl::fp8_view(*X), a.w = spl::fp8_view(*W);
   a.M = X->rows, a.N = W->rows, a.blocks = a.w.pitch / 128, a.dtype = dtype, a.y = Y;
@@ -252,6 +254,7 @@ spl_status spl_linear_fp8_grouped_weight_grad(const spl_fp8_matrix* dYt, const s
     return SPL_ERR_INVALID_ARG;
   const int64_t bytes = experts * dYt->rows * Xt->rows * type_bytes(dtype);
   if (!apart(dW, bytes, *dYt) || !apart(dW, bytes, *Xt)) return SPL_ERR_INVALID_ARG;
+  if (Xt->rows >= kMaxN) return SPL_ERR_UNSUPPORTED;
   Fp8GemmArgs a{};
   a.x = spl::fp8_view(*dYt), a.w = spl::fp8_view(*Xt);
   a.M = dYt->rows, a.N = Xt->rows, a.blocks = a.w.pitch / 128, a.dtype = dtype, a.y = dW;
@@ -365,12 +368,12 @@ int32_t spl_linear_fp8_kernel(int32_t form, int64_t M, int64_t N, int64_t cols, 
   a.M = M, a.N = N, a.dtype = dtype;
   if (form == 2) {
     const int64_t want = spl_fp8_grouped_cols(cols, groups);
-    if (want < 0 || !sizes_ok(M, want, 1) || !sizes_ok(N, want, 1) || N > kMaxBytes / M / groups) return -1;
+    if (want < 0 || !sizes_ok(M, want, 1) || !sizes_ok(N, want, 1) || N >= kMaxN || N > kMaxBytes / M / groups) return -1;
     a.blocks = (int32_t)(want / 128), a.mode = spl::kFp8Sum, a.groups = (int32_t)groups, a.tokens = (int32_t)cols;
     return spl::fp8_kernel(a);
   }
   const int64_t experts = form == 1 ? groups : 1;
-  if (!product_ok(M, N, cols, experts) || ((form == 1 || x_dtype) && M > kMaxCols)) return -1;
+  if (!product_ok(M, N, cols, experts) || N >= kMaxN || ((form == 1 || x_dtype) && M > kMaxCols)) return -1;
   a.blocks = (int32_t)(spl::fp8_pitch(cols) / 128), a.mode = form == 1 ? spl::kFp8Rows : spl::kFp8Plain;
   a.groups = (int32_t)experts;
   if (x_dtype && spl::fp8_fused(M, N, cols, experts)) a.x16 = &a;      // (looked at, not read)

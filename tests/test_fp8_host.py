@@ -149,6 +149,19 @@ def test_refused_products(L):
     assert L.spl_linear_fp8_grouped_weight_grad(x, w, P(0x60000), 0, 100, F32, Y, None) == INVALID
 
 
+def test_products_past_the_grids(L):
+    """W of 2^28 rows, which the streaming kernels' grids do not hold; one row less is a size like others."""
+    huge = dict(rows=1 << 28, codes_bytes=1 << 36, scales_bytes=1 << 36, cols=128)
+    Y, x, starts, ws = P(0x7000000000000), _m(cols=128, rows=4, codes=P(0x6000000000000)), P(0x50000), P(0x5000000000000)
+    w = _m(codes=P(0x1000000000000), scales=P(0x2000000000000), **huge)
+    assert L.spl_linear_fp8(x, w, BF16, Y, ws, None) == UNSUPPORTED
+    assert L.spl_linear_fp8_rows(P(0x50000), BF16, 4, 128, w, BF16, Y, ws, None) == UNSUPPORTED
+    assert L.spl_linear_fp8_grouped(x, w, starts, BF16, Y, None) == UNSUPPORTED
+    assert L.spl_linear_fp8_grouped_weight_grad(x, w, starts, 1, 100, BF16, Y, None) == UNSUPPORTED
+    assert L.spl_linear_fp8_kernel(0, 4, 1 << 28, 128, 0, 0, BF16) == -1
+    assert L.spl_linear_fp8_kernel(0, 4, (1 << 28) - 1, 128, 0, 0, BF16) == 1
+
+
 def test_refused_shared_memory(L):
     """Results in the memory of what the same call reads or writes: refused before anything runs (64 x 256 codes at 0x10000
     are 0x4000 bytes, 64 x 4 scales at 0x20000 are 0x100)."""
