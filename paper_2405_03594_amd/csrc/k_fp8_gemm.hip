@@ -448,12 +448,15 @@ hipError_t launch_kind(const Fp8GemmArgs& a, int32_t kind, int64_t columns, hipS
   }
 }
 
-// Whether the streaming kernel is the one: up to 32 rows of a matrix, of a group 16 (us, streaming / tiles, 5632 x 2048, 8
-// experts: 32 rows 17.7 / 20.1, 64 22.9 / 22.1, 128 31.3 / 23.6); up to 64 where tiles of 128 x 64 would take longer
-// (us, streaming / tiles whose sums are not split, 64 rows: 4096 x 4096 11.1 / 16.3, 11008 x 4096 31.1 / 15.8).
+// Whether the streaming kernel is the one: up to 32 rows of a matrix; up to 64 where tiles of 128 x 64 would take longer
+// (us, streaming / tiles whose sums are not split, 64 rows: 4096 x 4096 11.1 / 16.3, 11008 x 4096 31.1 / 15.8); of groups by
+// the sum's length, as tiles end with a round whatever it is (us, streaming / tiles, (rows) experts x N x cols: (16) 8 x 4096 x 1024
+// and (64) 32 x 2048 x 1024 11.1 / 8.1 and 16.9 / 14.3, (100) 16 x 4096 x 1408 21.5 / 23.5, (32, 48, 64, 85) 8 x 5632 x 2048 17.6,
+// 21.8, 22.8, 25.5 / 20.3, 21.9, 22.1, 20.2, (100) 16 x 2048 x 2048 13.8 / 17.0, (600) 64 x 1408 x 2048 41.5 / 37.9, (160)
+// 16 x 1024 x 4096 20.1 / 20.4, (40) 4 x 4096 x 4096 20.6 / 21.0, (80) 8 x 1024 x 8192 23.3 / 36.0).
 bool streams(const Fp8GemmArgs& a) {
   const double each = fp8_rows_each(a);
-  if (a.mode == kFp8Rows) return each <= 16;
+  if (a.mode == kFp8Rows) return a.blocks > 8 && each <= (a.blocks > 16 ? 16 : 10);
   if (each <= 32) return true;
   if (each > 64 || a.mode != kFp8Plain || splits_of(a.M, a.N, a.blocks) > 1) return false;
   const double cus = device_cus(), wgs = (double)((a.N + 31) / 32) * 2 / cus;

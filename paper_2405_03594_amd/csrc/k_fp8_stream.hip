@@ -11,8 +11,8 @@
 // entries, the largest magnitude is found by two lane moves, and the codes are
 // those of k_fp8_quantize.
 //
-// Bound by W's bytes where they are many (11008 x 4096 by one row of bf16 13.5 to 15.2 us, 3.0 to 3.3 TB/s; 12.7 with codes), by
-// the launch and two trips to memory where they are few (1111 x 1000 3.9).
+// Bound by W's bytes where they are many (11008 x 4096 by one row 12.7 us with codes, 3.5 TB/s; 8192 x 8192 by one of bf16 17.7
+// with the launch that quantizes it, 3.8 TB/s), by the launch and two trips to memory where they are few (1111 x 1000 3.9).
 #include <type_traits>
 
 #include "fp8_tile.h"
@@ -226,14 +226,16 @@ hipError_t rows16(const Fp8GemmArgs& a, int32_t kernel, bool eight, hipStream_t 
 // Four waves for up to 16 blocks of 128 columns, which would leave eight of them two or fewer each (us, 4 / 8 waves:
 // 5632 x 2048 6.0 / 8.2, 1111 x 1000 3.9 / 5.0, 4096 x 4096 7.6 / 6.5, 4096 x 11008 16.3 / 13.0).
 // Rows in 16 bits are quantized by each workgroup anew, which is most of its arithmetic: two blocks of 16 rows of W a
-// workgroup where there are plenty (us, two / one: 1 x 11008 x 4096, 344 workgroups of two, 15.5 / 14.5; 32 rows of 8
-// experts x 5632 x 2048, 1408 of them, 19.3 / 21.3).
+// workgroup where that leaves each CU one, of long sums four, which then end more evenly (us, two / one: 1 x 4096 x 4096, 128
+// workgroups of two, 8.8 / 7.8; 16 x 8192 x 2048, 256 of them, 7.9 / 9.1; 1 x 11008 x 2048 9.2 / 9.7; 1 x 32000 x 1000 10.9 /
+// 12.7; 1 x 11008 x 4096 15.8 / 14.7; of experts, 16 rows of 8 x 1024 x 1024, 256 of them, 5.0 / 5.6, 32 rows of 8 x 5632 x 2048
+// 19.0 / 21.8, 64 rows of 32 x 2048 x 1024 11.2 / 13.9, 24 rows of 8 x 4096 x 4096 23.6 / 26.8).
 int32_t fp8_stream_kernel(const Fp8GemmArgs& a) {
   const int32_t eight = a.blocks <= 16 ? 0 : kEightWaves;
   const double each = fp8_rows_each(a);
   if (!a.x16) return eight + (each <= 16 ? kStream16 : (each <= 32 ? kStream32 : kStream32x32));
   const int64_t wgs = (a.N + 31) / 32 * (a.mode == kFp8Rows ? (a.M < a.groups ? a.M : a.groups) : 1);
-  return eight + (each > 16 ? kRows32 : (wgs >= 4 * device_cus() ? kRows16x32 : kRows16));
+  return eight + (each > 16 ? kRows32 : (wgs >= (a.blocks <= 16 ? 1 : 4) * device_cus() ? kRows16x32 : kRows16));
 }
 
 hipError_t launch_fp8_stream(const Fp8GemmArgs& a, int32_t kernel, hipStream_t s) {

@@ -187,12 +187,21 @@ int32_t fp8_kernel(const Fp8GemmArgs& a);
 // Scratch of a plain product of codes whose sum is split over workgroups: fp32 [splits][M][N]; 0: it is not.  The same for
 // every type of y.
 int64_t fp8_partial_bytes(int64_t M, int64_t N, int32_t blocks);
-// Whether the kernel for few rows quantizes rows of 16 bits itself, which every workgroup of 16 or 32 rows of W does anew:
-// up to 16 rows of a matrix, up to 32 of a small one (us, fused / two launches: 24 x 1111 x 1000 6.3 / 9.3, 24 x 4096 x 4096 12.6 / 12.2,
-// 24 x 11008 x 4096 28 / 24, 16 x 11008 x 4096 20 / 19 and a launch's host time).
+// Whether the kernel for few rows quantizes rows of 16 bits itself, which every workgroup of 16 or 32 rows of W does anew,
+// or a launch before it does.  us in a graph, weights from memory, fused / two launches (a call of its own costs the host 7.8 /
+// 12.3 us, which is why what is near is fused).  A matrix: by one row 4096 x 4096 7.8 / 8.9, 8192 x 2048 7.4 / 8.3, 11008 x 4096
+// 14.7 / 13.9 (13.5 / 13.7 with weights in the cache), 9000 x 6000 19.8 / 18.2, 8192 x 8192 19.2 / 17.6, 32000 x 4096 33 / 29; by
+// 16 rows 8192 x 2048 7.7 / 9.9, 4096 x 4096 9.7 / 10.0, 1024 x 8192 14.2 / 13.1, 11008 x 4096 20.6 / 19.5; by 24 1111 x 1000 6.3 /
+// 7.6, 2048 x 2048 8.0 / 7.5, 4096 x 4096 12.4 / 11.3; by 32 1111 x 1000 6.5 / 8.0, 4096 x 2048 8.9 / 8.5, 4096 x 4096 14.3 / 12.1.
+// Experts, (rows) experts x N x cols: (64) 8 x 4096 x 1024 9.9 / 10.9, (600) 64 x 1024 x 1024 18.1 / 21.3, (160) 16 x 2048 x 2048
+// 19.3 / 21.9, (64) 8 x 5632 x 2048 23.8 / 24.6 and (85) 27.1 / 22.8, (600) 64 x 1408 x 2048 42.7 / 41.0; of longer sums (64) 16 x
+// 1024 x 4096 19.3 / 19.1 and (128) 24.0 / 20.8, (24) 4 x 4096 x 4096 18.0 / 17.4, (40) 8 x 1024 x 8192 22.0 / 19.9.
 inline bool fp8_fused(int64_t M, int64_t N, int64_t cols, int64_t experts) {
-  if (experts > 1) return 3 * M <= 32 * experts;
-  return M <= 16 || (M <= 32 && N * cols <= (int64_t)1 << 24);
+  if (experts > 1) {                            // up to so many rows each, where groups are one and a half times the mean
+    const int64_t most = cols > 2048 ? 6 : (N * cols <= ((int64_t)1 << 26) / experts ? 16 : 12);
+    return 3 * M <= 2 * most * experts;
+  }
+  return M <= 32 && N * cols <= (int64_t)3 << 24 && M * N * cols <= (int64_t)1 << 28;
 }
 
 struct AdamwHyper {

@@ -37,6 +37,7 @@ def test_cases_reach_their_kernels(kernel):
         for t, k16, k32 in ((0, c16, c32), (F16, r16, r32), (BF16, r16, r32)):
             for d, want in ((F16, k16), (BF16, k16), (F32, k32)):
                 check((len(starts) - 1, M, N, K, t, d), kernel(1, M, N, K, len(starts) - 1, t, d), want)
+            half.add(k16), full.add(k32)
     for starts, M, N, T, k16, k32 in cases.SUMS:
         for d, want in ((F16, k16), (BF16, k16), (F32, k32)):
             check((len(starts) - 1, M, N, T, d), kernel(2, M, N, T, len(starts) - 1, 0, d), want)
@@ -63,3 +64,27 @@ def test_workspace_goes_with_the_kernel(kernel):
         assert (need(M, N, K) > 0) == (k16 == 22) == (k32 == 22), (M, N, K)
         if k16 == 22:
             assert need(M, N, K) >= 2 * 4 * M * N and need(M, N, K) % 256 == 0
+
+
+def test_choices_at_measured_sizes(kernel):
+    """At the sizes that the choices' comments give two times for, the choice is the faster side, or the one launch where
+    the two are near."""
+    one, two = ((4, 5, 6, 12, 13, 14), (1, 2, 9, 10, 16, 17, 18, 19))
+    for M, N, K, fused in ((1, 4096, 4096, True), (1, 8192, 2048, True), (1, 11008, 4096, True), (1, 9000, 6000, False),
+                           (1, 8192, 8192, False), (1, 32000, 4096, False), (16, 8192, 2048, True), (16, 4096, 4096, True),
+                           (16, 11008, 4096, False), (24, 1111, 1000, True), (24, 4096, 4096, False), (32, 1111, 1000, True),
+                           (32, 4096, 4096, False)):
+        assert kernel(0, M, N, K, 0, BF16, BF16) in (one if fused else two), (M, N, K)
+    for M, E, N, K, fused in ((64, 8, 4096, 1024, True), (600, 64, 1024, 1024, True), (160, 16, 2048, 2048, True),
+                              (64, 8, 5632, 2048, True), (85, 8, 5632, 2048, False), (600, 64, 1408, 2048, False),
+                              (128, 16, 1024, 4096, False), (24, 4, 4096, 4096, False), (40, 8, 1024, 8192, False)):
+        assert kernel(1, M, N, K, E, BF16, BF16) in (one if fused else two), (M, E, N, K)
+    for M, E, N, K, streams in ((16, 8, 4096, 1024, False), (64, 32, 2048, 1024, False), (100, 16, 4096, 1408, True),
+                                (32, 8, 5632, 2048, True), (64, 8, 5632, 2048, False), (85, 8, 5632, 2048, False),
+                                (100, 16, 2048, 2048, True), (600, 64, 1408, 2048, False), (160, 16, 1024, 4096, True),
+                                (40, 4, 4096, 4096, True), (80, 8, 1024, 8192, True)):
+        assert (kernel(1, M, N, K, E, 0, BF16) in (1, 9)) == streams, (M, E, N, K)
+    for M, N, K, E, wide in ((1, 4096, 4096, 0, False), (16, 8192, 2048, 0, True), (1, 11008, 2048, 0, True), (1, 32000, 1000, 0, True),
+                             (1, 11008, 4096, 0, False), (16, 1024, 1024, 8, True), (32, 5632, 2048, 8, True),
+                             (24, 4096, 4096, 8, True)):
+        assert (kernel(1 if E else 0, M, N, K, E, BF16, BF16) in (5, 13)) == wide, (M, N, K, E)
