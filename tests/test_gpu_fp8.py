@@ -545,3 +545,52 @@ def test_grouped_grad_rows_of_no_expert_in_given_memory():
                                        ws.data_ptr(), stream)
             assert st == 0 and torch.equal(dx, want)
         assert (store[M * K:] == 5).all()
+
+
+def test_expert_training_run():
+    """The set by expert as a program uses it: rows sorted by an assignment that changes from step to step (some experts
+    without rows, padding rows of none behind the last), forward, both gradients, one AdamW step over all experts with 32-bit
+    states and a 16-bit copy, and the weights quantized again."""
+    spl = _spl()
+    g = torch.Generator().manual_seed(6)
+    E, N, K, M, pad = 6, 150, 260, 400, 17
+    master = (torch.randn(E, N, K, generator=g) * 0.05).cuda()
+    grad, m, v = torch.empty_like(master), torch.zeros_like(master), torch.zeros_like(master)
+    copy = master.to(torch.bfloat16)
+    plan = spl.adamw_plan([master], [grad], [m], [v], weight_decay=0.0, copies=[copy])
+    for t in range(1, 4):
+        expert = torch.randint(0, E, (M,), generator=g)
+        expert[expert == t] = 0                        # one expert without rows
+        order = torch.argsort(expert, stable=True)
+        starts = torch.zeros(E + 1, dtype=torch.int32)
+        starts[1:] = torch.cumsum(torch.bincount(expert, minlength=E), 0)
+        x = torch.zeros((M + pad, K), dtype=torch.bfloat16)
+        x[:M] = torch.randn(M, K, generator=g).to(torch.bfloat16)[order]
+        dy = torch.full((M + pad, N), float("nan"), dtype=torch.bfloat16)      # what stands in the padding is nobody's
+        dy[:M] = (torch.randn(M, N, generator=g) * 0.01).to(torch.bfloat16)
+        x, dy, at = x.cuda(), dy.cuda(), starts.cuda()
+        w, wt = spl.quantize_fp8_both(master, 128)
+        y = torch.zeros((M + pad, N), dtype=torch.bfloat16, device="cuda")
+        spl.linear_fp8_grouped(x, w, at, out=y)
+        dx, dw = spl.linear_fp8_grouped_grad(dy, x, wt, at)
+        grad.copy_(dw)
+        before = master.clone()
+        spl.adamw_step(plan, 1e-3, step=t)
+        assert (y[M:] == 0).all() and (dx[M:] == 0).all()
+        for e in range(E):
+            a, b = int(starts[e]), int(starts[e + 1])
+            if a == b:
+                assert (dw[e] == 0).all()
+                continue
+            hw = ref.round_trip(_np(before[e]), 128)
+            hx, hdy = ref.round_trip(_np(x[a:b])), ref.round_trip(_np(dy[a:b]))
+            _near(y[a:b], hx @ hw.T, _bound(hx, hw, torch.bfloat16), f"Y of {e}")
+            _near(dx[a:b], hdy @ hw, _bound(hdy, hw.T, torch.bfloat16), f"dX of {e}")
+            p, q = ref.round_trip(_np(dy[a:b]).T), ref.round_trip(_np(x[a:b]).T)
+            _near(dw[e], p @ q.T, _bound(p, q, torch.float32), f"dW of {e}")
+        if t == 1:                                     # the first step is lr against the gradient's sign, none without one
+            moved = (master - before).cpu()
+            some = grad.abs().cpu() > 1e-5
+            assert (moved[grad.cpu() == 0] == 0).all() and (moved[some] * torch.sign(grad.cpu()[some]) < 0).all()
+            assert (moved.abs() <= 1e-3 * 1.01 + 1e-6).all()
+        assert torch.equal(copy, master.to(torch.bfloat16))
