@@ -874,7 +874,7 @@ int32_t spl_linear_fp8_kernel(int32_t form, int64_t M, int64_t N, int64_t cols, 
  * 128) bytes, of which those past n are not used.  An 8-bit state is rounded to one of the two
  * codes next to it, up where 20 random bits, which are a hash of (seed, step,
  * the tensor's place in the plan, the element), reach the distance, so that
- * small changes count on average; r > 0 does not become 0.  A block that gets an
+ * small changes count on average; r > 0 is not rounded to 0 (its square may be, below 2^-75).  A block that gets an
  * infinity or a NaN is NaN from then on.
  *
  * A plan lists the tensors: spl_adamw_plan writes spl_adamw_plan_bytes bytes of

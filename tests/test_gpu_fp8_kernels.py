@@ -253,3 +253,15 @@ def test_sums_that_cancel(M, N, K, k16, k32):
         y = _np(spl.linear_fp8(q, qw, dtype=dtype))
         bound = 2.0 ** -9 * 2.0 ** 16 * (K // 128) * (1 + EPS[dtype]) + EPS[dtype] * want
         assert (np.abs(y - want) <= bound).all(), (dtype, np.abs(y - want).max(), bound)
+
+
+@pytest.mark.parametrize("case", [c for c in cases.CODES if c[3] in (1, 10, 3, 16, 17, 18, 19, 20, 22)][1::2], ids=_id)
+def test_both_operands_in_wide_blocks(case):
+    """X with a scale for 128 x 128 entries too, and a matrix times its own transpose."""
+    spl = _spl()
+    M, N, K, k16, k32 = case
+    q, qw = spl.quantize_fp8(_random((M, K), 1).cuda(), 128), spl.quantize_fp8(_random((N, K), 2).cuda(), 128)
+    h, hw = _held(q), _held(qw)
+    for dtype in FLOATS:
+        _check(spl.linear_fp8(q, qw, dtype=dtype), h, hw, f"{dtype}")
+    _check(spl.linear_fp8(qw, qw, dtype=torch.float32), hw, hw, "W W^T")
