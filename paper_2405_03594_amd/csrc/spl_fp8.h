@@ -191,17 +191,23 @@ int64_t fp8_partial_bytes(int64_t M, int64_t N, int32_t blocks);
 // or a launch before it does.  us in a graph, weights from memory, fused / two launches (a call of its own costs the host 7.8 /
 // 12.3 us, which is why what is near is fused).  A matrix: by one row 4096 x 4096 7.8 / 8.9, 8192 x 2048 7.4 / 8.3, 11008 x 4096
 // 14.7 / 13.9 (13.5 / 13.7 with weights in the cache), 9000 x 6000 19.8 / 18.2, 8192 x 8192 19.2 / 17.6, 32000 x 4096 33 / 29; by
-// 16 rows 8192 x 2048 7.7 / 9.9, 4096 x 4096 9.7 / 10.0, 1024 x 8192 14.2 / 13.1, 11008 x 4096 20.6 / 19.5; by 24 1111 x 1000 6.3 /
-// 7.6, 2048 x 2048 8.0 / 7.5, 4096 x 4096 12.4 / 11.3; by 32 1111 x 1000 6.5 / 8.0, 4096 x 2048 8.9 / 8.5, 4096 x 4096 14.3 / 12.1.
+// 16 rows 8192 x 2048 7.7 / 9.9, 4096 x 4096 9.7 / 10.0, 1024 x 8192 14.2 / 13.1, 11008 x 4096 20.6 / 19.5; 512 x 11008
+// 17.5 / 15.0; by 24 1111 x 1000 6.3 / 7.6, 2048 x 2048 8.0 / 7.5, 1024 x 4096 11.2 / 10.1, 4096 x 4096 12.4 / 11.3; by 32 1111 x
+// 1000 6.5 / 8.0, 4096 x 2048 8.9 / 8.5, 4096 x 4096 14.3 / 12.1.
 // Experts, (rows) experts x N x cols: (64) 8 x 4096 x 1024 9.9 / 10.9, (600) 64 x 1024 x 1024 18.1 / 21.3, (160) 16 x 2048 x 2048
 // 19.3 / 21.9, (64) 8 x 5632 x 2048 23.8 / 24.6 and (85) 27.1 / 22.8, (600) 64 x 1408 x 2048 42.7 / 41.0; of longer sums (64) 16 x
 // 1024 x 4096 19.3 / 19.1 and (128) 24.0 / 20.8, (24) 4 x 4096 x 4096 18.0 / 17.4, (40) 8 x 1024 x 8192 22.0 / 19.9.
+// Where cols are no multiple of 8, rows one after another are not aligned, and entries are loaded one by one: 1 x 1111 x 1001 6.8 /
+// 6.5, 8 x 8192 x 1004 8.8 / 9.0, 1 x 4096 x 2100 13.3 / 7.6, 8 x 4096 x 4100 32.8 / 10.3; (6) 8 x 2048 x 1003 8.9 / 9.8 and (32)
+// 13.3 / 10.4, (32) 8 x 5632 x 2050 53 / 24.
 inline bool fp8_fused(int64_t M, int64_t N, int64_t cols, int64_t experts) {
+  const bool whole = cols % 8 == 0;
+  if (!whole && cols > 1024) return false;
   if (experts > 1) {                            // up to so many rows each, where groups are one and a half times the mean
-    const int64_t most = cols > 2048 ? 6 : (N * cols <= ((int64_t)1 << 26) / experts ? 16 : 12);
+    const int64_t most = !whole ? 3 : (cols > 2048 ? 6 : (N * cols <= ((int64_t)1 << 26) / experts ? 16 : 12));
     return 3 * M <= 2 * most * experts;
   }
-  return M <= 32 && N * cols <= (int64_t)3 << 24 && M * N * cols <= (int64_t)1 << 28;
+  return M <= 32 && M * cols <= (int64_t)1 << 16 && N * cols <= (int64_t)3 << 24 && M * N * cols <= (int64_t)1 << 28;
 }
 
 struct AdamwHyper {

@@ -72,12 +72,14 @@ def test_choices_at_measured_sizes(kernel):
     one, two = ((4, 5, 6, 12, 13, 14), (1, 2, 9, 10, 16, 17, 18, 19))
     for M, N, K, fused in ((1, 4096, 4096, True), (1, 8192, 2048, True), (1, 11008, 4096, True), (1, 9000, 6000, False),
                            (1, 8192, 8192, False), (1, 32000, 4096, False), (16, 8192, 2048, True), (16, 4096, 4096, True),
-                           (16, 11008, 4096, False), (24, 1111, 1000, True), (24, 4096, 4096, False), (32, 1111, 1000, True),
-                           (32, 4096, 4096, False)):
+                           (16, 11008, 4096, False), (8, 1024, 8192, True), (16, 1024, 8192, False), (24, 1111, 1000, True), (24, 4096, 4096, False), (32, 1111, 1000, True),
+                           (32, 4096, 4096, False), (16, 512, 11008, False), (24, 1024, 4096, False), (1, 1111, 1001, True), (8, 8192, 1004, True),
+                           (1, 4096, 2100, False), (8, 4096, 4100, False)):
         assert kernel(0, M, N, K, 0, BF16, BF16) in (one if fused else two), (M, N, K)
     for M, E, N, K, fused in ((64, 8, 4096, 1024, True), (600, 64, 1024, 1024, True), (160, 16, 2048, 2048, True),
                               (64, 8, 5632, 2048, True), (85, 8, 5632, 2048, False), (600, 64, 1408, 2048, False),
-                              (128, 16, 1024, 4096, False), (24, 4, 4096, 4096, False), (40, 8, 1024, 8192, False)):
+                              (128, 16, 1024, 4096, False), (24, 4, 4096, 4096, False), (40, 8, 1024, 8192, False), (6, 8, 2048, 1003, True),
+                              (32, 8, 2048, 1003, False), (32, 8, 5632, 2050, False)):
         assert kernel(1, M, N, K, E, BF16, BF16) in (one if fused else two), (M, E, N, K)
     for M, E, N, K, streams in ((16, 8, 4096, 1024, False), (64, 32, 2048, 1024, False), (100, 16, 4096, 1408, True),
                                 (32, 8, 5632, 2048, True), (64, 8, 5632, 2048, False), (85, 8, 5632, 2048, False),

@@ -148,6 +148,6 @@ def test_chunks_of_a_plan():
         plan = spl.adamw_plan(*[[x] for x in t])
         assert plan.chunks == chunks
         spl.adamw_step(plan, LR, (B1, B2), EPS, step=1)
-        want = [torch.from_numpy(np.broadcast_to(x, n)) for x in
+        want = [torch.from_numpy(np.broadcast_to(x, n).copy()) for x in
                 update(np.zeros(1, F), np.ones(1, F), np.zeros(1, F), np.zeros(1, F), 1, None, 0.01)[:3]]
         assert all(torch.equal(t[i].cpu(), w) for i, w in ((0, want[0]), (2, want[1]), (3, want[2]))), n
